@@ -348,6 +348,107 @@ seer_status seer_gather_response(const void* x_packed, seer_dtype dt, const int3
                                  int d, int T_cap, void* x_resp, int32_t* cu_resp_out, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Paged key/value cache with grouped heads: for servers that admit prompts,
+ * draft or refine a few rows per step and keep the accepted ones, over caches
+ * whose lengths change.  The paper has no counterpart; the contiguous cache
+ * above is laid out once per truncated batch.
+ * A pool of pages holds one layer's keys and values: page p owns rows
+ * [p * page_size, (p + 1) * page_size) of kv, each row K | V of n_kv_heads heads
+ * in the call's dtype; row t of request b is row t % page_size of page
+ * table[b * max_pages + t / page_size].  One table serves every layer's pool.
+ * Query head h reads key/value head h / (n_heads / n_kv_heads).
+ * What the device finds inconsistent (lengths outside the buffers, pages outside
+ * the pool, too few free pages) is recorded (seer_check_device) and that
+ * request's or row's part left out; no access leaves the buffers named.
+ * ------------------------------------------------------------------------- */
+#define SEER_MAX_DRAFT 64          /* new rows of a request that a tree can hold */
+#define SEER_MAX_REQUESTS 16384    /* requests of a call */
+
+typedef struct {
+  void* kv;               /* device [n_pages * page_size, 2 * n_kv_heads * head_dim] */
+  const int32_t* table;   /* device [B, max_pages] */
+  int n_pages;
+  int page_size;          /* a power of two from 8 to 1024; n_pages * page_size < 2^31 */
+  int max_pages;          /* pages of the longest request that the table holds */
+  int n_kv_heads;
+  int head_dim;           /* <= 128, a multiple of 16 (fp32: of 8) */
+} seer_pages;
+
+/* Pages, slots and positions of a step's new rows, from the requests' lengths.
+ * Request b has cached_len[b] rows in the cache and adds new_len[b]; its new rows
+ * are packed, rows cu_new_out[b] .. cu_new_out[b+1] - 1.  It owns the first
+ * ceil(cached_len / page_size) entries of its table row; the entries up to
+ * ceil((cached_len + new_len) / page_size) are taken from the free list, requests in
+ * order, from free_pages[*free_head] on, and written to the table.
+ *   kv_len_out[b]   = cached_len[b] + new_len[b]      (device int32 [B])
+ *   slot_out[r]     = the pool row of new row r, -1 where it has none
+ *   position_out[r] = cached_len[b] + i of the request's i-th new row, or, with
+ *                     parent, cached_len[b] + its depth
+ *   mask_out[r]     = bit j set where new row j of the request is the row itself or
+ *                     an ancestor (without parent: j <= i); may be NULL
+ *   *free_head_out  = *free_head + the pages taken (not the same address)
+ * parent          device int32 [T_cap] or NULL: new row i's parent among the
+ *                 request's new rows, -1 for a child of the last cached row; a
+ *                 parent comes before its children
+ * T_cap           rows of slot_out, position_out, mask_out and parent; rows past
+ *                 cu_new_out[B] are untouched
+ * With parent or mask_out a request has at most SEER_MAX_DRAFT new rows.  Table
+ * entries of taken pages beyond the free list become -1.  Every output depends on
+ * the inputs alone, so a call may be repeated. */
+seer_status seer_page_tables(const int32_t* cached_len, const int32_t* new_len, int B, int page_size, int n_pages,
+                             const int32_t* free_pages, int n_free, const int32_t* free_head, int32_t* table,
+                             int max_pages, int T_cap, const int32_t* parent, int32_t* cu_new_out, int32_t* kv_len_out,
+                             int32_t* slot_out, int32_t* position_out, uint64_t* mask_out, int32_t* free_head_out,
+                             void* stream);
+
+/* Stores the K | V part of packed rows q | k | v (n_heads query heads, then
+ * pages->n_kv_heads key and as many value heads; ld_qkv values per row) at their
+ * slots, the keys turned by their position as in seer_rope (theta 0: as they are).
+ * rotated, when not NULL, receives the turned q | k of every row (ld_rotated values
+ * per row); it may be qkv itself with its ld.  Rows: M_dev (device int32, may be
+ * NULL) overrides T_cap.  slot -1: nothing is stored for the row; two rows of a call
+ * with one slot leave either there.  position: device int32 [T_cap], NULL when
+ * theta is 0.  Angles are exact to fp32 at any position; one rounding per value. */
+seer_status seer_kv_append(const void* qkv, int ld_qkv, seer_dtype dt, int n_heads, int T_cap, const int32_t* M_dev,
+                           const int32_t* slot, const int32_t* position, float theta, void* rotated, int ld_rotated,
+                           const seer_pages* pages, void* stream);
+
+/* Keeps the accepted rows of each request's draft: row cached_len[b] + k of request
+ * b becomes its row cached_len[b] + accepted[b * max_draft + k], k < n_accepted[b]
+ * (accepted ascends strictly, as the rows of a path from the root do), and
+ * len_out[b] = cached_len[b] + n_accepted[b] is its next cached_len.  A request with
+ * a list that does not ascend, leaves the draft or meets a page outside the pool
+ * keeps nothing and is recorded.  One call per layer's pool. */
+seer_status seer_kv_accept(seer_dtype dt, const int32_t* cached_len, const int32_t* accepted, const int32_t* n_accepted,
+                           int B, int max_draft, const seer_pages* pages, int32_t* len_out, void* stream);
+
+/* Causal attention over whole packed prompts with grouped heads: per sequence,
+ * row i attends to rows 0 .. i, scores divided by sqrt(head_dim).  q, k, v and o are
+ * rows of n_heads or n_kv_heads heads, ld_* values apart (column blocks of one
+ * packed buffer, or buffers of their own), 16-byte aligned.  cu_seqlens device
+ * int32 [B+1], read on the device; rows past cu_seqlens[B] are untouched.  head_dim:
+ * 64 or 128 for 16-bit types, a multiple of 4 up to 128 for fp32.  o must not
+ * overlap the inputs.  A key that a row does not see never reaches its result, not
+ * even an infinite or NaN one.  No workspace. */
+seer_status seer_attention_causal(const void* q, int ld_q, const void* k, int ld_k, const void* v, int ld_v, void* o,
+                                  int ld_o, seer_dtype dt, const int32_t* cu_seqlens, int B, int T_cap, int n_heads,
+                                  int n_kv_heads, int head_dim, void* stream);
+
+/* Attention of each request's new rows over its pages (their own keys stored there
+ * before, seer_kv_append): new row i sees the kv_len[b] - n cached rows, n =
+ * cu_new[b+1] - cu_new[b], and the new rows j with bit j of mask[row] set (mask
+ * NULL: j <= i).  n <= max_draft <= SEER_MAX_DRAFT; n = 1 decodes single tokens.  A
+ * row that sees no key is 0.  A page outside the pool reads as zeros and is
+ * recorded.  head_dim, scaling and hidden keys as above.
+ * ws: seer_attention_tree_workspace_size() bytes; calls that share one must not
+ * overlap on the GPU; nothing in it needs to start at zero. */
+seer_status seer_attention_tree(const void* q, int ld_q, void* o, int ld_o, seer_dtype dt, const int32_t* cu_new,
+                                const int32_t* kv_len, const uint64_t* mask, int B, int T_cap, int n_heads,
+                                int max_draft, const seer_pages* pages, void* ws, size_t ws_bytes, void* stream);
+seer_status seer_attention_tree_workspace_size(seer_dtype dt, int B, int n_heads, int n_kv_heads, int head_dim,
+                                               int max_draft, size_t* bytes);
+
+/* ---------------------------------------------------------------------------
  * Diagnostics.
  * ------------------------------------------------------------------------- */
 /* Thread-local message describing the last failure of this thread. */

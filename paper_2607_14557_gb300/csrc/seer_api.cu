@@ -2,7 +2,6 @@
 // TMA descriptor encoding, workspace layout and kernel sequencing; all
 // arithmetic runs in the kernels of tc_gemm.cu, tc_attn.cu, simt.cu and
 // aux_kernels.cu.
-#include <cudaTypedefs.h>
 #include <nvtx3/nvToolsExt.h>
 
 #include <algorithm>
@@ -17,7 +16,7 @@
 #include <thread>
 #include <vector>
 
-#include "../../include/seer.h"
+#include "api.h"
 #include "common.cuh"
 #include "kernels.h"
 
@@ -33,6 +32,15 @@ namespace {
 
 thread_local std::string g_msg;
 
+__device__ int g_dev_err;
+
+std::mutex g_dev_mu;
+DeviceInfo g_dev[64];
+
+}  // namespace
+
+namespace seer {
+
 seer_status fail(seer_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -46,28 +54,6 @@ seer_status fail(seer_status st, const char* fmt, ...) {
 seer_status cuda_fail(cudaError_t e, const char* where) {
   return fail(SEER_ERR_CUDA, "%s: %s (%s)", where, cudaGetErrorName(e), cudaGetErrorString(e));
 }
-
-#define SEER_CUDA(call, where)                          \
-  do {                                                  \
-    cudaError_t e_ = (call);                            \
-    if (e_ != cudaSuccess) return cuda_fail(e_, where); \
-  } while (0)
-
-#define SEER_TRY(expr)                 \
-  do {                                 \
-    seer_status s_ = (expr);           \
-    if (s_ != SEER_OK) return s_;      \
-  } while (0)
-
-__device__ int g_dev_err;
-
-struct DeviceInfo {
-  int* err = nullptr;
-  int num_sms = 0;
-};
-
-std::mutex g_dev_mu;
-DeviceInfo g_dev[64];
 
 seer_status device_info(DeviceInfo** out) {
   int dev = 0;
@@ -85,20 +71,17 @@ seer_status device_info(DeviceInfo** out) {
   return SEER_OK;
 }
 
-bool valid_dt(seer_dtype dt) { return dt == SEER_F32 || dt == SEER_BF16 || dt == SEER_F16; }
-bool is16(seer_dtype dt) { return dt == SEER_BF16 || dt == SEER_F16; }
-size_t esize(seer_dtype dt) { return dt == SEER_F32 ? 4 : 2; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+}  // namespace seer
+
+namespace {
 
 // ------------------------------------------------------------ TMA descriptors
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 std::once_flag g_encode_once;
 
-// Row-major [rows, cols] 16-bit matrix with leading dimension ld elements, in
-// boxes of box_cols columns x box_rows rows: 128-byte swizzle for operand
-// tiles (64 columns = 128 bytes), none for the GEMM epilogue's store chunks.
-seer_status make_map16(CUtensorMap* m, const void* base, seer_dtype dt, uint64_t rows, uint64_t cols, uint64_t ld,
-                       uint32_t box_rows, uint32_t box_cols = 64, bool swizzle128 = true) {
+}  // namespace
+
+PFN_cuTensorMapEncodeTiled_v12000 seer::tensor_map_encoder() {
   std::call_once(g_encode_once, [] {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -106,13 +89,24 @@ seer_status make_map16(CUtensorMap* m, const void* base, seer_dtype dt, uint64_t
         q == cudaDriverEntryPointSuccess)
       g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
   });
-  if (g_encode == nullptr) return fail(SEER_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  return g_encode;
+}
+
+namespace {
+
+// Row-major [rows, cols] 16-bit matrix with leading dimension ld elements, in
+// boxes of box_cols columns x box_rows rows: 128-byte swizzle for operand
+// tiles (64 columns = 128 bytes), none for the GEMM epilogue's store chunks.
+seer_status make_map16(CUtensorMap* m, const void* base, seer_dtype dt, uint64_t rows, uint64_t cols, uint64_t ld,
+                       uint32_t box_rows, uint32_t box_cols = 64, bool swizzle128 = true) {
+  const PFN_cuTensorMapEncodeTiled_v12000 encode = tensor_map_encoder();
+  if (encode == nullptr) return fail(SEER_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   cuuint64_t dims[2] = {cols, rows > 0 ? rows : 1};
   cuuint64_t strides[1] = {ld * 2};
   cuuint32_t box[2] = {box_cols, box_rows};
   cuuint32_t estr[2] = {1, 1};
   const CUtensorMapDataType ty = dt == SEER_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  CUresult r = g_encode(m, ty, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  CUresult r = encode(m, ty, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                         swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(SEER_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
@@ -146,34 +140,30 @@ const char* const kPhaseNames[SEER_N_PHASES] = {"seer:detect_gemm", "seer:snr_sc
                                                  "seer:qkv",         "seer:attention", "seer:o_proj", "seer:norm2",
                                                  "seer:gate_up",     "seer:down",      "seer:kv_cache"};
 
-// Marks one kernel launch: an NVTX range on the host timeline (a no-op unless
-// a tool such as nsys or ncu --nvtx is attached), and, when profiling is on,
-// a pair of CUDA events on the launch's stream.
-class Phase {
- public:
-  Phase(int ph, cudaStream_t st) : ph_(ph), st_(st) {
-    nvtxRangePushA(kPhaseNames[ph]);
-    std::lock_guard<std::mutex> lk(g_prof.mu);
-    if (!g_prof.on || ((g_prof.mask >> ph) & 1u) == 0) return;
-    a_ = g_prof.get();
-    b_ = g_prof.get();
-    if (a_ && b_) cudaEventRecord(a_, st_);
-  }
-  ~Phase() {
-    nvtxRangePop();
-    if (!a_ || !b_) return;
-    cudaEventRecord(b_, st_);
-    std::lock_guard<std::mutex> lk(g_prof.mu);
-    g_prof.pending[ph_].push_back({a_, b_});
-  }
+}  // namespace
 
- private:
-  int ph_;
-  cudaStream_t st_;
-  cudaEvent_t a_ = nullptr, b_ = nullptr;
-};
+namespace seer {
 
-enum { PH_DETECT = 0, PH_SCAN, PH_PACK, PH_NORM1, PH_QKV, PH_ATTN, PH_OPROJ, PH_NORM2, PH_GATEUP, PH_DOWN, PH_KV };
+Phase::Phase(int ph, cudaStream_t st) : ph_(ph), st_(st) {
+  nvtxRangePushA(kPhaseNames[ph]);
+  std::lock_guard<std::mutex> lk(g_prof.mu);
+  if (!g_prof.on || ((g_prof.mask >> ph) & 1u) == 0) return;
+  a_ = g_prof.get();
+  b_ = g_prof.get();
+  if (a_ && b_) cudaEventRecord(a_, st_);
+}
+
+Phase::~Phase() {
+  nvtxRangePop();
+  if (!a_ || !b_) return;
+  cudaEventRecord(b_, st_);
+  std::lock_guard<std::mutex> lk(g_prof.mu);
+  g_prof.pending[ph_].push_back({a_, b_});
+}
+
+}  // namespace seer
+
+namespace {
 
 // ------------------------------------------------------------ workspace
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }

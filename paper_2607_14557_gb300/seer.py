@@ -22,6 +22,7 @@ SEER_F32, SEER_BF16, SEER_F16 = 0, 1, 2
 PATH_STATIC, PATH_VARLEN, PATH_EAGER = 0, 1, 2
 MAX_GROUPS = 32
 CTRL_WORDS = 8 + 4 * MAX_GROUPS
+MAX_DRAFT, MAX_REQUESTS = 64, 16384
 N_PHASES = 11
 PHASES = ("detect_gemm", "snr_scan", "pack", "norm1", "qkv", "attention", "o_proj", "norm2", "gate_up", "down",
           "kv_cache")
@@ -51,6 +52,12 @@ class seer_layer_weights(ctypes.Structure):
     _fields_ = [("w_qkv", ctypes.c_void_p), ("w_o", ctypes.c_void_p), ("w_gate", ctypes.c_void_p),
                 ("w_up", ctypes.c_void_p), ("w_down", ctypes.c_void_p), ("g_attn", ctypes.c_void_p),
                 ("g_mlp", ctypes.c_void_p)]
+
+
+class seer_pages(ctypes.Structure):
+    _fields_ = [("kv", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n_pages", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("max_pages", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int)]
 
 
 _lib = None
@@ -89,6 +96,13 @@ def lib() -> ctypes.CDLL:
             "seer_convert": [vp, i32, vp, i32, sz, vp],
             "seer_attention": [vp, vp, i32, vp, vp, i32, i32, i32, i32, vp, sz, vp],
             "seer_attention_noalloc": [vp, vp, i32, vp, vp, i32, i32, i32, i32, vp],
+            "seer_page_tables": [vp, vp, i32, i32, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp],
+            "seer_kv_append": [vp, i32, i32, i32, i32, vp, vp, vp, ctypes.c_float, vp, i32, ctypes.POINTER(seer_pages), vp],
+            "seer_kv_accept": [i32, vp, vp, vp, i32, i32, ctypes.POINTER(seer_pages), vp, vp],
+            "seer_attention_causal": [vp, i32, vp, i32, vp, i32, vp, i32, i32, vp, i32, i32, i32, i32, i32, vp],
+            "seer_attention_tree": [vp, i32, vp, i32, i32, vp, vp, vp, i32, i32, i32, i32, ctypes.POINTER(seer_pages), vp,
+                                    sz, vp],
+            "seer_attention_tree_workspace_size": [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
             "seer_check_device": [ctypes.POINTER(ctypes.c_int)],
             "seer_selftest_wait_timeout": [i32, vp],
             "seer_profile_enable": [i32],
@@ -259,6 +273,79 @@ def seer_attention(qkv, o, dt, cu_seqlens, kv_len, B, T_capacity, n_heads, head_
 def seer_attention_noalloc(qkv, o, dt, cu_seqlens, kv_len, B, T_capacity, n_heads, head_dim, stream=None):
     _check(lib().seer_attention_noalloc(_p(qkv), _p(o), _dt(dt), _p(cu_seqlens), _p(kv_len), B, T_capacity, n_heads,
                                         head_dim, _stream(stream)))
+
+
+# ----------------------------------------------------------------- paged K/V cache
+def _dev(t, device, dtype=None):
+    """Address of a tensor (None, a raw address) that is on `device` and, when a
+    dtype is named, a contiguous array of it."""
+    if not isinstance(t, torch.Tensor):
+        return t
+    if not t.is_cuda or t.get_device() != device:
+        raise ValueError(f"a tensor on {t.device} is not on the current device cuda:{device}")
+    if dtype is not None and (t.dtype != dtype or not t.is_contiguous()):
+        raise ValueError(f"expected a contiguous {dtype} tensor, got {t.dtype} with strides {tuple(t.stride())}")
+    return t.data_ptr()
+
+
+def make_pages(kv, table, n_pages, page_size, max_pages, n_kv_heads, head_dim) -> seer_pages:
+    """The struct keeps addresses only: kv and table must outlive it."""
+    if isinstance(kv, torch.Tensor) and (not kv.is_contiguous() or
+                                         kv.numel() < n_pages * page_size * 2 * n_kv_heads * head_dim):
+        raise ValueError("kv must be contiguous and hold n_pages * page_size rows of 2 * n_kv_heads * head_dim values")
+    if isinstance(table, torch.Tensor) and (table.dtype != torch.int32 or not table.is_contiguous()):
+        raise ValueError("table must be a contiguous int32 tensor")
+    return seer_pages(_p(kv), _p(table), n_pages, page_size, max_pages, n_kv_heads, head_dim)
+
+
+def seer_page_tables(cached_len, new_len, B, page_size, n_pages, free_pages, n_free, free_head, table, max_pages, T_cap,
+                     parent, cu_new_out, kv_len_out, slot_out, position_out, mask_out, free_head_out, stream=None):
+    """mask_out: an int64 tensor (bit j of the 64 is new row j)."""
+    dev, i32 = torch.cuda.current_device(), torch.int32
+    _check(lib().seer_page_tables(_dev(cached_len, dev, i32), _dev(new_len, dev, i32), B, page_size, n_pages,
+                                  _dev(free_pages, dev, i32), n_free, _dev(free_head, dev, i32), _dev(table, dev, i32),
+                                  max_pages, T_cap, _dev(parent, dev, i32), _dev(cu_new_out, dev, i32),
+                                  _dev(kv_len_out, dev, i32), _dev(slot_out, dev, i32), _dev(position_out, dev, i32),
+                                  _dev(mask_out, dev, torch.int64), _dev(free_head_out, dev, i32), _stream(stream)))
+
+
+def seer_kv_append(qkv, ld_qkv, dt, n_heads, T_cap, M_dev, slot, position, theta, rotated, ld_rotated, pages,
+                   stream=None):
+    dev, i32 = torch.cuda.current_device(), torch.int32
+    _check(lib().seer_kv_append(_dev(qkv, dev), ld_qkv, _dt(dt), n_heads, T_cap, _dev(M_dev, dev, i32),
+                                _dev(slot, dev, i32), _dev(position, dev, i32), theta, _dev(rotated, dev), ld_rotated,
+                                ctypes.byref(pages), _stream(stream)))
+
+
+def seer_kv_accept(dt, cached_len, accepted, n_accepted, B, max_draft, pages, len_out, stream=None):
+    dev, i32 = torch.cuda.current_device(), torch.int32
+    _check(lib().seer_kv_accept(_dt(dt), _dev(cached_len, dev, i32), _dev(accepted, dev, i32),
+                                _dev(n_accepted, dev, i32), B, max_draft, ctypes.byref(pages), _dev(len_out, dev, i32),
+                                _stream(stream)))
+
+
+def seer_attention_causal(q, ld_q, k, ld_k, v, ld_v, o, ld_o, dt, cu_seqlens, B, T_cap, n_heads, n_kv_heads, head_dim,
+                          stream=None):
+    dev = torch.cuda.current_device()
+    _check(lib().seer_attention_causal(_dev(q, dev), ld_q, _dev(k, dev), ld_k, _dev(v, dev), ld_v, _dev(o, dev), ld_o,
+                                       _dt(dt), _dev(cu_seqlens, dev, torch.int32), B, T_cap, n_heads, n_kv_heads,
+                                       head_dim, _stream(stream)))
+
+
+def seer_attention_tree(q, ld_q, o, ld_o, dt, cu_new, kv_len, mask, B, T_cap, n_heads, max_draft, pages, ws, ws_bytes,
+                        stream=None):
+    """mask: an int64 tensor as from seer_page_tables, or None (causal)."""
+    dev, i32 = torch.cuda.current_device(), torch.int32
+    _check(lib().seer_attention_tree(_dev(q, dev), ld_q, _dev(o, dev), ld_o, _dt(dt), _dev(cu_new, dev, i32),
+                                     _dev(kv_len, dev, i32), _dev(mask, dev, torch.int64), B, T_cap, n_heads, max_draft,
+                                     ctypes.byref(pages), _dev(ws, dev), ws_bytes, _stream(stream)))
+
+
+def seer_attention_tree_workspace_size(dt, B, n_heads, n_kv_heads, head_dim, max_draft) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().seer_attention_tree_workspace_size(_dt(dt), B, n_heads, n_kv_heads, head_dim, max_draft,
+                                                    ctypes.byref(out)))
+    return out.value
 
 
 def seer_check_device() -> int:
