@@ -2,6 +2,7 @@
 // grouped-head attention kernels that use them.  Not part of the public ABI.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -96,6 +97,11 @@ struct GqaParams {
   int splits;             // CUDA-core kernel: shares of a request's keys
   int* err;
 };
+// 16-bit causal attention on the tensor cores.  mQ: q as [T_cap][n_heads][head_dim] in boxes
+// of floor(128 / g) x g x 64, g = n_heads / n_kv; mK, mV: [T_cap][n_kv][head_dim] in
+// boxes of 128 x 1 x 64; all with the 128-byte swizzle.
+cudaError_t launch_tc_causal(const CUtensorMap& mQ, const CUtensorMap& mK, const CUtensorMap& mV, const GqaParams& p,
+                             bool f16, int num_sms, cudaStream_t st);
 cudaError_t launch_gqa_simt(int type, bool paged, const GqaParams& p, int num_sms, cudaStream_t st);
 // Shares of the keys, and bytes of partial results, of a paged call on the CUDA-core kernel.
 int gqa_simt_splits(int B, int n_heads, int n_kv, int max_new, int num_sms);

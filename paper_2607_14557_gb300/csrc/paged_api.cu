@@ -74,6 +74,23 @@ seer_status check_heads(const char* what, int n_heads, int n_kv, int head_dim, s
   return SEER_OK;
 }
 
+// Tensor map of 16-bit heads: rows (ld apart) x heads (dh apart) x dh columns, in boxes of
+// box_rows x box_heads x 64 with the 128-byte swizzle.
+seer_status map_heads(CUtensorMap* m, const void* base, seer_dtype dt, long rows, long ld, int heads, int dh, int box_rows,
+                      int box_heads) {
+  const PFN_cuTensorMapEncodeTiled_v12000 encode = tensor_map_encoder();
+  if (encode == nullptr) return fail(SEER_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dh), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(dh) * 2, static_cast<cuuint64_t>(ld) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_heads), static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t step[3] = {1, 1, 1};
+  const CUresult r = encode(m, dt == SEER_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                            const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(SEER_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+  return SEER_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -223,7 +240,18 @@ seer_status seer_attention_causal(const void* q, int ld_q, const void* k, int ld
   p.head_dim = head_dim;
   p.splits = 1;
   p.err = di->err;
+  if (T_cap == 0) return SEER_OK;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (is16(dt)) {
+    const int g = n_heads / n_kv_heads;
+    CUtensorMap mq, mk, mv;
+    SEER_TRY(map_heads(&mq, q, dt, T_cap, ld_q, n_heads, head_dim, 128 / g, g));
+    SEER_TRY(map_heads(&mk, k, dt, T_cap, ld_k, n_kv_heads, head_dim, 128, 1));
+    SEER_TRY(map_heads(&mv, v, dt, T_cap, ld_v, n_kv_heads, head_dim, 128, 1));
+    Phase ph(PH_ATTN, st);
+    SEER_CUDA(launch_tc_causal(mq, mk, mv, p, dt == SEER_F16, di->num_sms, st), "causal attention launch");
+    return SEER_OK;
+  }
   Phase ph(PH_ATTN, st);
   SEER_CUDA(launch_gqa_simt(dt, false, p, di->num_sms, st), "causal attention launch");
   return SEER_OK;

@@ -56,7 +56,9 @@ def attend(q, k, v, seen, dt):
     The bound counts: the stored result's rounding (u |o|); the probabilities rounded to
     dt before the product with v (u each, in numerator and sum: 2 u A, A = sum w |v|);
     fp32 scores (a chain of dh products: dh 2^-24 sum |q k|), exponent and exponential
-    (2^-22 |s| + 2^-21), each twice again; fp32 sums over the keys (n 2^-24, twice)."""
+    (2^-22 |s| + 2^-21), each twice again; fp32 sums over the keys (n 2^-24, twice).
+    f16 probabilities below its normal range are off by at most 2^-25 each, of a sum that
+    is at least 1: in numerator and sum, 2^-25 (sum |v| + n |o|) over the seen keys."""
     q, k, v = (t.astype(np.float64) for t in (q, k, v))
     m, n = q.shape[0], k.shape[0]
     dh = q.shape[1]
@@ -73,7 +75,8 @@ def attend(q, k, v, seen, dt):
     u = U[dt]
     rel = 2 * (u if dt != "f32" else 0) + 2 * (dh * 2.0 ** -24 * size + 2.0 ** -22 * size + 2.0 ** -21) + 2 * n * 2.0 ** -24
     o = w @ v0
-    return o, u * np.abs(o) + rel * (w @ np.abs(v0)) + 2.0 ** -25 * (dt == "f16")
+    small = 2.0 ** -25 * (dt == "f16")
+    return o, u * np.abs(o) + rel * (w @ np.abs(v0)) + small * (1 + seen @ np.abs(v0) + seen.sum(-1, keepdims=True) * np.abs(o))
 
 
 def causal(q, k, v, cu, dt):
