@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libseer.so")
 SOURCES = ["seer_api.cu", "tc_gemm.cu", "tc_attn.cu", "simt.cu", "aux_kernels.cu", "seer_noalloc.cu", "paged_api.cu",
-           "paged.cu", "gqa_simt.cu", "tc_causal.cu"]
+           "paged.cu", "gqa_simt.cu", "tc_causal.cu", "tc_tree.cu"]
 HEADERS = ["common.cuh", "kernels.h", "attn_schedule.cuh", "api.h", "paged.h", "attn_math.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

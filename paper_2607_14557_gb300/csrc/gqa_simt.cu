@@ -339,8 +339,6 @@ cudaError_t launch_gqa_simt(int type, bool paged, const GqaParams& p, int num_sm
   if (p.T_cap <= 0) return cudaSuccess;
   switch (type) {
     case kF32: return launch_type<kF32>(paged, p, st);
-    case kBF16: return launch_type<kBF16>(paged, p, st);
-    case kF16: return launch_type<kF16>(paged, p, st);
     default: return cudaErrorInvalidValue;
   }
 }

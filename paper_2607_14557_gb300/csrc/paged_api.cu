@@ -266,7 +266,8 @@ seer_status seer_attention_tree_workspace_size(seer_dtype dt, int B, int n_heads
   if (!bytes) return fail(SEER_ERR_INVALID_ARG, "tree attention: bytes is null");
   DeviceInfo* di;
   SEER_TRY(device_info(&di));
-  *bytes = gqa_simt_part_bytes(B, n_heads, n_kv_heads, head_dim, max_draft, di->num_sms);
+  *bytes = is16(dt) ? tc_tree_part_bytes(n_heads, n_kv_heads, head_dim, max_draft, di->num_sms)
+                    : gqa_simt_part_bytes(B, n_heads, n_kv_heads, head_dim, max_draft, di->num_sms);
   return SEER_OK;
 }
 
@@ -314,9 +315,20 @@ seer_status seer_attention_tree(const void* q, int ld_q, void* o, int ld_o, seer
   p.page_shift = pg.page_shift;
   p.max_pages = pg.max_pages;
   p.part = static_cast<float*>(ws);
-  p.splits = gqa_simt_splits(B, n_heads, pg.n_kv, max_draft, di->num_sms);
   p.err = di->err;
+  if (T_cap == 0) return SEER_OK;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (is16(dt)) {
+    const int g = n_heads / pg.n_kv, page = 1 << pg.page_shift;
+    CUtensorMap mq, mkv;
+    SEER_TRY(map_heads(&mq, q, dt, T_cap, ld_q, n_heads, pg.head_dim, tc_tree_box_tokens(n_heads, pg.n_kv, max_draft), g));
+    SEER_TRY(map_heads(&mkv, pg.kv, dt, static_cast<long>(pg.n_pages) << pg.page_shift, p.ld_k, 2 * pg.n_kv, pg.head_dim,
+                       page < 128 ? page : 128, 1));
+    Phase ph(PH_ATTN, st);
+    SEER_CUDA(launch_tc_tree(mq, mkv, p, dt == SEER_F16, di->num_sms, st), "tree attention launch");
+    return SEER_OK;
+  }
+  p.splits = gqa_simt_splits(B, n_heads, pg.n_kv, max_draft, di->num_sms);
   Phase ph(PH_ATTN, st);
   SEER_CUDA(launch_gqa_simt(dt, true, p, di->num_sms, st), "tree attention launch");
   return SEER_OK;

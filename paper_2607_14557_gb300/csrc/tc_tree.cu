@@ -1,0 +1,786 @@
+// Attention of a few new rows per request over a paged key/value cache on tcgen05 for
+// sm_103a (head_dim 64 or 128; q, the cache, P and the output all f16, or all bf16).
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = 2^(s_ij - m_i),  s_ij = q_i k_j log2(e) / sqrt(dh)
+// over the cached rows and the new rows whose bit is set in the row's mask.
+//
+// Bound by HBM: a key/value row is read once for the g = n_heads / n_kv query heads that
+// share it and for all of a request's new rows, which together are the rows of one 128-row
+// tile (128 / g tokens, row = token * g + head; more tokens: more tiles).  The MMAs of a
+// mostly empty tile cost no more than its K and V take to arrive.
+//
+// A unit is (request, key/value head, row tile); its work the 128-key tiles of its cache.
+// All units' key tiles form one line, cut into equal runs, one per CTA, so lengths may
+// differ as they like and one long request fills the GPU.  A CTA takes its run as pieces of
+// units; a piece that is not a whole unit leaves its unnormalised sums, maximum and weight
+// in the workspace, and tree_merge_kernel joins a unit's pieces in order of their keys.
+// Where the runs start follows from the lengths by a prefix sum that every CTA makes.
+//
+// Two CTAs per SM (192 threads, 256 columns of tensor memory), so one's loads and MMAs run
+// beside the other's softmax:
+//   warp 0     producer: decodes the pieces, publishes them in a shared ring, and loads Q,
+//              then K_j and V_j; a box per page, a lane per box
+//   warp 1     MMA issuer: S = Q K_j^T, then O += P V_j with P written over S
+//   warps 2-5  softmax, a thread per row; warps without a row of the tile only pass on
+// Hidden keys and non-finite values are treated as in tc_causal.cu: scores dropped, value
+// rows past the request's end cleared, and a unit whose masked tile holds a non-finite
+// value recomputed row by row.
+#include <math.h>
+
+#include "attn_math.cuh"
+#include "common.cuh"
+#include "paged.h"
+
+namespace seer {
+namespace {
+
+constexpr int BQ = 128;                     // rows of a tile
+constexpr int BKV = 128;                    // keys of a tile
+constexpr int THREADS = 192;
+constexpr int PANEL = 16384;
+constexpr int BAR_BYTES = 512;
+constexpr uint32_t TMEM_COLS = 256;
+constexpr uint32_t TM_O = 128;              // S at column 0, O at 128
+constexpr float RESCALE_THRESHOLD = 8.0f;   // log2 units
+constexpr int U_SLOTS = 4;
+constexpr int U_READERS = 1 + 4;            // issuer, softmax warps
+
+template <int DH>
+struct Layout {
+  static constexpr int TILE = 128 * DH * 2;
+  static constexpr int STAGES = 128 / DH;   // K ring and V ring: 64 KB of keys and values in flight per CTA
+  static constexpr int OFF_K = TILE;
+  static constexpr int OFF_V = OFF_K + STAGES * TILE;
+  static constexpr int OFF_BAR = OFF_V + STAGES * TILE;
+  static constexpr int BYTES = OFF_BAR + BAR_BYTES + 1024;
+};
+static_assert(2 * (Layout<128>::BYTES + 1024) <= 227 * 1024, "two CTAs per SM");
+
+// A piece: keys [tile0 * 128, tile1 * 128) of a unit.  n < 0: no more pieces.
+struct Piece {
+  int q0, tok0, n, kv;                      // request's first row, the tile's first token, its new rows, its keys
+  int b, kvh, tile0, tile1;
+  int part;                                 // slot of its partial result, or -1: a whole unit
+};
+static_assert(sizeof(Piece) == 36, "ring entries");
+
+struct Request {
+  int q0, n, kv;
+  bool good;
+};
+__device__ __forceinline__ Request read_request(const GqaParams& p, int b) {
+  Request r{0, 0, 0, true};
+  if (b >= p.B) return r;
+  r.q0 = p.cu[b];
+  r.n = p.cu[b + 1] - r.q0;
+  r.kv = p.kv_len[b];
+  r.good = r.q0 >= 0 && r.n >= 0 && r.n <= p.T_cap - r.q0 && r.n <= p.max_new && r.kv >= r.n &&
+           r.kv <= (static_cast<long long>(p.max_pages) << p.page_shift);
+  if (!r.good) r.n = r.kv = 0;
+  return r;
+}
+__device__ __forceinline__ int key_tiles(int kv) { return static_cast<int>((kv + static_cast<unsigned>(BKV) - 1) / BKV); }
+// Key tiles of all units of a request.
+__device__ __forceinline__ long long line_length(const GqaParams& p, const Request& r, int tpt) {
+  return static_cast<long long>(p.n_kv) * ((r.n + tpt - 1) / tpt) * key_tiles(r.kv);
+}
+
+// Run c of n over a line of `total`: [cut(c), cut(c + 1)), and the run that holds x.
+__device__ __forceinline__ long long cut(long long total, int c, int n) { return total * c / n; }
+__device__ __forceinline__ int run_of(long long total, long long x, int n) {
+  return static_cast<int>(((x + 1) * n - 1) / total);
+}
+
+// Units that begin in a run and do not end there (at most one per run).
+struct Join {
+  int q0, tok0, n, kvh;                     // n = 0: none
+  int first, last;                          // runs: its pieces are slot 2 first + 1, then 2 c of the later ones
+  int pad[2];
+};
+
+__device__ __forceinline__ Piece read_piece(uint64_t* u_full, uint64_t* u_empty, const Piece* ring, int i,
+                                            volatile int* abort, int* err, int lane) {
+  const int s = i % U_SLOTS;
+  const bool ok = warp_wait(&u_full[s], (i / U_SLOTS) & 1, abort, err);
+  Piece w = ring[s];
+  if (!ok) w.n = -1;
+  __syncwarp();
+  if (lane == 0 && ok) mbar_arrive(&u_empty[s]);
+  return w;
+}
+
+// Bits of the keys that new row `tok` sees among the request's new rows.
+__device__ __forceinline__ uint64_t visible(const GqaParams& p, const Piece& u, int tok) {
+  const uint64_t all = u.n >= 64 ? ~0ull : (1ull << u.n) - 1;
+  const uint64_t bits = p.mask ? p.mask[u.q0 + tok] : (tok >= 63 ? ~0ull : (2ull << tok) - 1);
+  return bits & all;
+}
+
+// Where a row's result goes: the output, divided by its weight, or its partial slot.
+template <bool F16, int DH>
+struct RowOut {
+  uint16_t* o = nullptr;
+  float* part = nullptr;
+  float* stats = nullptr;                   // (max, weight)
+};
+template <bool F16, int DH>
+__device__ __forceinline__ RowOut<F16, DH> row_out(const GqaParams& p, const Piece& u, int tok, int head, int r, int rows) {
+  RowOut<F16, DH> w;
+  if (u.part < 0) {
+    w.o = static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.q0 + tok) * p.ld_o + head * DH;
+  } else {
+    float* slot = p.part + static_cast<size_t>(u.part) * rows * (DH + 4);   // rows x DH sums, (max, weight) each, 16-byte multiples
+    w.part = slot + r * DH;
+    w.stats = slot + rows * DH + 2 * r;
+  }
+  return w;
+}
+// 8 columns from c on, scaled by inv (output only).
+template <bool F16, int DH>
+__device__ __forceinline__ uint32_t store8(const RowOut<F16, DH>& w, int c, const float (&v)[8], float inv) {
+  if (w.o == nullptr) {
+    *reinterpret_cast<float4*>(w.part + c) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(w.part + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    return 0;
+  }
+  uint32_t q[4], bad = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    q[e] = pack2(v[2 * e] * inv, v[2 * e + 1] * inv, F16);
+    bad |= nonfinite_term(q[e], F16);
+  }
+  *reinterpret_cast<uint4*>(w.o + c) = make_uint4(q[0], q[1], q[2], q[3]);
+  return bad;
+}
+
+// One row of a piece from global memory, key by key: only for pieces that met a
+// non-finite value in a masked tile.
+template <bool F16, int DH>
+__device__ __noinline__ uint32_t recompute_row(const GqaParams& p, const Piece* piece, int tok, int head, int r, int rows) {
+  const Piece u = *piece;
+  const uint16_t* q = static_cast<const uint16_t*>(p.q) + static_cast<size_t>(u.q0 + tok) * p.ld_q + head * DH;
+  const uint64_t bits = visible(p, u, tok);
+  const int ctx = u.kv - u.n, begin = u.tile0 * BKV, end = min(u.kv, u.tile1 * BKV);
+  const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(DH));
+  // pool row of key j; -1: hidden, -2: on a page outside the pool (zeros)
+  const auto row_of = [&](int j) -> long long {
+    if (j >= ctx && !((bits >> (j - ctx)) & 1)) return -1;
+    const int page = p.table[static_cast<size_t>(u.b) * p.max_pages + (j >> p.page_shift)];
+    return page < 0 || page >= p.n_pages ? -2 : (static_cast<long long>(page) << p.page_shift) + (j & ((1 << p.page_shift) - 1));
+  };
+  const auto score = [&](long long row) {
+    if (row < 0) return 0.f;
+    const uint32_t* a = reinterpret_cast<const uint32_t*>(q);
+    const uint32_t* b = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.k) + row * p.ld_k + u.kvh * DH);
+    float s = 0.f;
+    for (int d = 0; d < DH / 2; ++d) s += lo16(a[d], F16) * lo16(b[d], F16) + hi16(a[d], F16) * hi16(b[d], F16);
+    return s * scale_log2;
+  };
+  float m = -INFINITY;
+  for (int j = begin; j < end; ++j) {
+    const long long row = row_of(j);
+    if (row != -1) m = fmaxf(m, score(row));
+  }
+  const float base = m == -INFINITY ? 0.f : m;
+  const RowOut<F16, DH> out = row_out<F16, DH>(p, u, tok, head, r, rows);
+  uint32_t bad = 0;
+  float l = 0.f;
+  for (int c = 0; c < DH; c += 8) {
+    float acc[8] = {};
+    l = 0.f;
+    for (int j = begin; j < end; ++j) {
+      const long long row = row_of(j);
+      if (row == -1) continue;
+      const float w = ex2(score(row) - base);
+      l += w;
+      if (row < 0) continue;
+      const uint32_t* b = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.v) + row * p.ld_v + u.kvh * DH + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[2 * e] = fmaf(w, lo16(b[e], F16), acc[2 * e]);
+        acc[2 * e + 1] = fmaf(w, hi16(b[e], F16), acc[2 * e + 1]);
+      }
+    }
+    bad |= store8<F16, DH>(out, c, acc, l == 0.f ? 0.f : 1.f / l);
+  }
+  if (out.stats) *reinterpret_cast<float2*>(out.stats) = make_float2(m, l);
+  return bad;
+}
+
+template <bool F16, int DH>
+__global__ void __launch_bounds__(THREADS, 2)
+    tc_tree_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mKV, const GqaParams p,
+                   const int q_box, const int min_tiles, Join* __restrict__ joins) {
+  pdl_enter();
+  using Lay = Layout<DH>;
+  constexpr int TILE = Lay::TILE, PANELS = DH / 64, STAGES = Lay::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Lay::OFF_BAR);
+  uint64_t* q_full = bars + 0;
+  uint64_t* q_empty = bars + 1;
+  uint64_t* s_full = bars + 2;
+  uint64_t* p_full = bars + 3;
+  uint64_t* p_full2 = bars + 4;
+  uint64_t* o_done = bars + 5;
+  uint64_t* o_free = bars + 6;
+  uint64_t* k_full = bars + 7;               // [STAGES]
+  uint64_t* k_empty = k_full + STAGES;
+  uint64_t* v_full = k_empty + STAGES;
+  uint64_t* v_empty = v_full + STAGES;
+  uint64_t* u_full = v_empty + STAGES;       // [U_SLOTS]
+  uint64_t* u_empty = u_full + U_SLOTS;      // [U_SLOTS]
+  Piece* ring = reinterpret_cast<Piece*>(u_empty + U_SLOTS);     // [U_SLOTS]
+  volatile int* odd = reinterpret_cast<volatile int*>(ring + U_SLOTS);   // [4], as in tc_causal.cu
+  uint32_t* tmem_slot = const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(odd + 4));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  static_assert(8 * (7 + 4 * 2 + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 <= BAR_BYTES, "barrier block");
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int G = p.n_heads / p.n_kv, TPT = BQ / G;
+  const int part_rows = min(TPT, p.max_new) * G;          // rows of a partial slot
+
+  // ---- the line of key tiles: its length and the request where this CTA's run begins
+  __shared__ long long warp_sum[THREADS / 32];
+  __shared__ long long start_off;
+  __shared__ int start_b;
+  const int chunk = (p.B + THREADS - 1) / THREADS;
+  const int b_lo = min(p.B, static_cast<int>(threadIdx.x) * chunk), b_hi = min(p.B, b_lo + chunk);
+  long long mine = 0;
+  for (int b = b_lo; b < b_hi; ++b) {
+    const Request r = read_request(p, b);
+    if (!r.good && blockIdx.x == 0) record_error(p.err, kErrLayout);
+    mine += line_length(p, r, TPT);
+  }
+  long long inc = mine;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, inc, off);
+    if (lane >= off) inc += v;
+  }
+  if (lane == 31) warp_sum[warp] = inc;
+  __syncthreads();
+  long long before = inc - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    before += w < warp ? warp_sum[w] : 0;
+    total += warp_sum[w];
+  }
+  const long long want = (total + min_tiles - 1) / min_tiles;
+  const int runs = want < gridDim.x ? static_cast<int>(want) : static_cast<int>(gridDim.x), c = blockIdx.x;
+  if (c >= runs) {
+    if (threadIdx.x == 0) joins[c] = Join{};
+    return;                                               // the whole CTA
+  }
+  const long long run0 = cut(total, c, runs), run1 = cut(total, c + 1, runs);
+  if (mine > 0 && run0 >= before && run0 < before + mine) {
+    long long at = before;
+    for (int b = b_lo; b < b_hi; ++b) {
+      const long long n = line_length(p, read_request(p, b), TPT);
+      if (run0 < at + n) {
+        start_b = b;
+        start_off = run0 - at;
+        break;
+      }
+      at += n;
+    }
+  }
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
+    mbar_init(s_full, 1);
+    mbar_init(p_full, 4);
+    mbar_init(p_full2, 4);
+    mbar_init(o_done, 1);
+    mbar_init(o_free, 4);
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(&k_full[i], 1);
+      mbar_init(&k_empty[i], 1);
+      mbar_init(&v_full[i], 1);
+      mbar_init(&v_empty[i], 1);
+    }
+    for (int i = 0; i < U_SLOTS; ++i) {
+      mbar_init(&u_full[i], 1);
+      mbar_init(&u_empty[i], U_READERS);
+      odd[i] = 0;
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0) {
+    // -------------------------------------------------- producer
+    const bool leader = elect_one();
+    if (leader) {
+      tma_prefetch_desc(&mQ);
+      tma_prefetch_desc(&mKV);
+    }
+    __syncwarp();
+    const int box_rows = min(BKV, 1 << p.page_shift), boxes = BKV / box_rows;
+    const int out_of_pool = p.n_pages << p.page_shift;    // a row that the tensor map fills with zeros
+    int q_issued = 0, k_issued = 0, v_issued = 0;
+    bool ok = true;
+    int b = start_b;
+    long long off = start_off, at = run0;
+    int window = b;                                       // requests window .. window + 31 in the lanes' registers
+    Request mine_r = read_request(p, window + lane);
+    Join join{};
+    // pool row of this lane's box of key tile j
+    const auto box_row = [&](int bb, int kv, int j) {
+      const int key = j * BKV + lane * box_rows;
+      if (lane >= boxes || key >= kv) return -1;
+      const int page = p.table[static_cast<size_t>(bb) * p.max_pages + (key >> p.page_shift)];
+      if (page < 0 || page >= p.n_pages) {
+        record_error(p.err, kErrLayout);
+        return out_of_pool;
+      }
+      return (page << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+    };
+    for (int i = 0; ok; ++i) {
+      Piece u{};
+      u.n = -1;
+      Request r{};
+      if (at < run1) {
+        long long len;
+        for (;;) {                                        // requests without keys are passed over
+          if (b - window >= 32) {
+            window = b;
+            mine_r = read_request(p, window + lane);
+          }
+          r.q0 = __shfl_sync(0xffffffffu, mine_r.q0, b - window);
+          r.n = __shfl_sync(0xffffffffu, mine_r.n, b - window);
+          r.kv = __shfl_sync(0xffffffffu, mine_r.kv, b - window);
+          len = line_length(p, r, TPT);
+          if (off < len || b + 1 >= p.B) break;
+          off -= len;
+          ++b;
+        }
+        if (off >= len) at = run1;                        // the lengths changed under the call
+      }
+      if (at < run1) {
+        const int tiles = key_tiles(r.kv), row_tiles = (r.n + TPT - 1) / TPT;
+        const int unit = static_cast<int>(off / tiles);
+        u.q0 = r.q0;
+        u.n = r.n;
+        u.kv = r.kv;
+        u.b = b;
+        u.kvh = unit / row_tiles;
+        u.tok0 = (unit - u.kvh * row_tiles) * TPT;
+        u.tile0 = static_cast<int>(off - static_cast<long long>(unit) * tiles);
+        u.tile1 = static_cast<int>(min(static_cast<long long>(tiles), u.tile0 + (run1 - at)));
+        u.part = u.tile0 > 0 ? 2 * c : (u.tile1 < tiles ? 2 * c + 1 : -1);
+        if (u.tile0 == 0 && u.tile1 < tiles)
+          join = Join{u.q0, u.tok0, u.n, u.kvh, c, run_of(total, at + tiles - 1, runs), {0, 0}};
+        off += u.tile1 - u.tile0;
+        at += u.tile1 - u.tile0;
+      }
+      const int s = i % U_SLOTS;
+      if (i >= U_SLOTS && !warp_wait(&u_empty[s], (i / U_SLOTS - 1) & 1, abort_flag, p.err)) break;
+      if (lane == 0) {
+        ring[s] = u;
+        mbar_arrive(&u_full[s]);
+      }
+      __syncwarp();
+      if (u.n < 0) break;
+      int next_row = box_row(u.b, u.kv, u.tile0);         // the page of a tile is looked up a tile ahead
+      if (i > 0 && !warp_wait(q_empty, (i - 1) & 1, abort_flag, p.err)) break;
+      if (leader) {
+        mbar_arrive_expect_tx(q_full, PANELS * q_box * G * 128);
+        for (int x = 0; x < PANELS; ++x)
+          tma_load_3d(smem + x * PANEL, &mQ, q_full, 64 * x, u.kvh * G, u.q0 + u.tok0);
+      }
+      __syncwarp();
+      ++q_issued;
+      for (int j = u.tile0; j < u.tile1; ++j) {
+        const int row = next_row;
+        if (j + 1 < u.tile1) next_row = box_row(u.b, u.kv, j + 1);
+        const int bytes = __popc(__ballot_sync(0xffffffffu, row >= 0)) * box_rows * 128 * PANELS;
+        const int ks = k_issued % STAGES, ku = k_issued / STAGES;
+        if (ku > 0 && !warp_wait(&k_empty[ks], (ku - 1) & 1, abort_flag, p.err)) { ok = false; break; }
+        if (leader) mbar_arrive_expect_tx(&k_full[ks], bytes);
+        __syncwarp();
+        if (row >= 0)
+          for (int x = 0; x < PANELS; ++x)
+            tma_load_3d(smem + Lay::OFF_K + ks * TILE + x * PANEL + lane * box_rows * 128, &mKV, &k_full[ks], 64 * x, u.kvh, row);
+        __syncwarp();
+        ++k_issued;
+        const int vs = v_issued % STAGES, vu = v_issued / STAGES;
+        if (vu > 0 && !warp_wait(&v_empty[vs], (vu - 1) & 1, abort_flag, p.err)) { ok = false; break; }
+        if (leader) mbar_arrive_expect_tx(&v_full[vs], bytes);
+        __syncwarp();
+        if (row >= 0)
+          for (int x = 0; x < PANELS; ++x)
+            tma_load_3d(smem + Lay::OFF_V + vs * TILE + x * PANEL + lane * box_rows * 128, &mKV, &v_full[vs], 64 * x, p.n_kv + u.kvh, row);
+        __syncwarp();
+        ++v_issued;
+      }
+    }
+    if (lane == 0) joins[c] = join;
+    if (*abort_flag && leader) {
+      // let copies still in flight land before the CTA's shared memory is released
+      if (q_issued > 0) mbar_wait_drain(q_full, (q_issued - 1) & 1, 200000000ull);
+      for (int j = k_issued > STAGES ? k_issued - STAGES : 0; j < k_issued; ++j)
+        mbar_wait_drain(&k_full[j % STAGES], (j / STAGES) & 1, 200000000ull);
+      for (int j = v_issued > STAGES ? v_issued - STAGES : 0; j < v_issued; ++j)
+        mbar_wait_drain(&v_full[j % STAGES], (j / STAGES) & 1, 200000000ull);
+    }
+  } else if (warp == 1) {
+    // -------------------------------------------------- MMA issuer
+    const bool leader = elect_one();
+    constexpr uint32_t idesc_qk = make_idesc(BQ, BKV, 0, F16);
+    constexpr uint32_t idesc_pv = make_idesc(BQ, DH, 1, F16);
+    const uint64_t dq = make_sdesc_sw128(smem_u32(smem), 16, 1024);
+    const uint64_t dk0 = make_sdesc_sw128(smem_u32(smem + Lay::OFF_K), 16, 1024);
+    const uint64_t dv0 = make_sdesc_sw128(smem_u32(smem + Lay::OFF_V), PANEL, 1024);
+    const uint32_t dS = tmem, dO = tmem + TM_O;
+    unsigned kc = 0, vc = 0, pc = 0;                      // K, V and P tiles consumed
+    auto qk = [&](bool last) {
+      if (leader) {
+        const unsigned st = kc % STAGES;
+        const uint64_t dk = dk0 + static_cast<uint64_t>(st * (TILE >> 4));
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k) {
+          const uint64_t o = static_cast<uint64_t>(((k >> 2) * PANEL + (k & 3) * 32) >> 4);
+          tc_mma_f16(dS, dq + o, dk + o, idesc_qk, k > 0 ? 1u : 0u);
+        }
+        tc_commit(s_full);
+        tc_commit(&k_empty[st]);
+        if (last) tc_commit(q_empty);
+      }
+      __syncwarp();
+      ++kc;
+    };
+    auto pv = [&](bool fresh, int half) {
+      if (leader) {
+        const unsigned st = vc % STAGES;
+        const uint64_t dv = dv0 + static_cast<uint64_t>(st * (TILE >> 4));
+#pragma unroll
+        for (int kk = 0; kk < BKV / 32; ++kk) {
+          const int k = half * (BKV / 32) + kk;
+          tc_mma_f16_tmem_a(dO, dS + 8 * k, dv + static_cast<uint64_t>(k * 128), idesc_pv, (!fresh || k > 0) ? 1u : 0u);
+        }
+        if (half == 1) tc_commit(&v_empty[st]);
+      }
+      __syncwarp();
+    };
+    bool ok = true;
+    for (int i = 0; ok; ++i) {
+      const Piece u = read_piece(u_full, u_empty, ring, i, abort_flag, p.err, lane);
+      if (u.n < 0) break;
+      const int tiles = u.tile1 - u.tile0;
+      if (!warp_wait(q_full, i & 1, abort_flag, p.err) ||
+          !warp_wait(&k_full[kc % STAGES], (kc / STAGES) & 1u, abort_flag, p.err))
+        break;
+      tc_fence_after();
+      qk(tiles == 1);
+      for (int j = 0; j < tiles; ++j) {
+        if ((j == 0 && i > 0 && !warp_wait(o_free, (i - 1) & 1u, abort_flag, p.err)) ||   // the piece before is read out
+            !warp_wait(&v_full[vc % STAGES], (vc / STAGES) & 1u, abort_flag, p.err) ||
+            !warp_wait(p_full, pc & 1u, abort_flag, p.err)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        pv(j == 0, 0);
+        if (!warp_wait(p_full2, pc & 1u, abort_flag, p.err)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        pv(j == 0, 1);
+        ++vc;
+        ++pc;
+        if (j + 1 < tiles) {
+          if (!warp_wait(&k_full[kc % STAGES], (kc / STAGES) & 1u, abort_flag, p.err)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          qk(j + 2 == tiles);
+        } else {
+          if (leader) tc_commit(o_done);
+          __syncwarp();
+        }
+      }
+    }
+  } else {
+    // -------------------------------------------------- softmax warps 2..5
+    const int r = (warp & 3) * 32 + lane;                 // row of the tile == TMEM lane
+    const int rt = r / G, rh = r - rt * G;
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + lane_off, tO = tmem + lane_off + TM_O;
+    const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(DH));
+    int cs = 0, cv = 0;                                   // S tiles seen; V tiles of the pieces before
+    uint32_t nonfinite = 0;
+    bool ok = true;
+    for (int i = 0; ok; ++i) {
+      const Piece u = read_piece(u_full, u_empty, ring, i, abort_flag, p.err, lane);
+      if (u.n < 0) break;
+      const int ntok = min(TPT, u.n - u.tok0), tok = u.tok0 + rt, ctx = u.kv - u.n;
+      const bool valid_row = rt < ntok;
+      const bool busy = (warp & 3) * 32 < ntok * G;       // the warp holds rows of the tile
+      const uint64_t bits = valid_row ? visible(p, u, tok) : 0;
+      float m_ref = -INFINITY, l = 0.f;
+      for (int j = u.tile0; ok && j < u.tile1; ++j) {
+        if (!__all_sync(0xffffffffu, mbar_wait(s_full, cs & 1, abort_flag, p.err))) { ok = false; break; }
+        ++cs;
+        tc_fence_after();
+        const bool masked = (j + 1) * static_cast<long long>(BKV) > ctx;
+        float s[BKV];
+        float alpha = 1.f, neg = 0.f;
+        bool any_need = false;
+        if (busy) {
+          {
+            uint32_t ra[BKV / 32][32];
+#pragma unroll
+            for (int cc = 0; cc < BKV / 32; ++cc) tmem_ld32(tS + 32 * cc, ra[cc]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int cc = 0; cc < BKV / 32; ++cc)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) s[32 * cc + e] = __uint_as_float(ra[cc][e]);
+          }
+          if (masked) {
+            // new row 0 is key `sh` of the tile: keys before it are seen, then the row's bits
+            const int sh = ctx - j * BKV;
+            const auto word = [&](int at) -> uint32_t {   // keys at .. at + 31
+              const int x = at - sh;                      // index of key `at` among the new rows
+              if (x >= 64) return 0u;
+              if (x >= 0) return static_cast<uint32_t>(bits >> x);
+              if (x <= -32) return ~0u;
+              return (static_cast<uint32_t>(bits) << -x) | ((1u << -x) - 1);
+            };
+#pragma unroll
+            for (int w = 0; w < BKV / 32; ++w) {
+              const uint32_t see = word(32 * w);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) s[32 * w + e] = (see >> e) & 1u ? s[32 * w + e] : -INFINITY;
+            }
+          }
+          float mx[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mx[e] = fmaxf(s[e], s[e + 8]);
+#pragma unroll
+          for (int cc = 16; cc < BKV; cc += 16)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mx[e] = max3(mx[e], s[cc + e], s[cc + 8 + e]);
+#pragma unroll
+          for (int w = 4; w >= 1; w >>= 1)
+#pragma unroll
+            for (int e = 0; e < w; ++e) mx[e] = fmaxf(mx[e], mx[e + w]);
+          const float m_new = fmaxf(m_ref, mx[0] * scale_log2);
+          const bool need = j == u.tile0 || m_new > m_ref + RESCALE_THRESHOLD;
+          any_need = __any_sync(0xffffffffu, need);
+          if (need) {
+            alpha = m_ref == -INFINITY ? 0.f : ex2(m_ref - m_new);
+            m_ref = m_new;
+          }
+          neg = m_ref == -INFINITY ? 0.f : -m_ref;        // nothing seen so far: every term is 0
+        }
+        float rs[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          if (busy) {
+#pragma unroll
+            for (int cc = 2 * hf; cc < 2 * hf + 2; ++cc) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                float x0, x1;
+                ffma2(s[32 * cc + 2 * e], s[32 * cc + 2 * e + 1], scale_log2, scale_log2, neg, neg, x0, x1);
+                pk[e] = pack2(ex2(x0), ex2(x1), F16);
+                rs[(2 * e) & 3] = add_lo16<F16>(pk[e], rs[(2 * e) & 3]);
+                rs[(2 * e + 1) & 3] = add_hi16<F16>(pk[e], rs[(2 * e + 1) & 3]);
+              }
+              tmem_st16(tS + 16 * cc, pk);
+            }
+          }
+          if (hf == 0) {
+            if (busy && j > u.tile0 && any_need) {
+#pragma unroll 1
+              for (int cc = 0; cc < DH / 32; ++cc) {
+                uint32_t rr[32];
+                tmem_ld32(tO + 32 * cc, rr);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) rr[e] = __float_as_uint(__uint_as_float(rr[e]) * alpha);
+                tmem_st32(tO + 32 * cc, rr);
+              }
+            }
+            if (masked) {
+              const int vsi = cv + j - u.tile0, vst = vsi % STAGES;
+              if (!__all_sync(0xffffffffu, mbar_wait(&v_full[vst], (vsi / STAGES) & 1, abort_flag, p.err))) {
+                ok = false;
+                break;
+              }
+              const int valid = u.kv - j * BKV;
+              uint4* v = reinterpret_cast<uint4*>(smem + Lay::OFF_V + vst * TILE);
+              uint32_t bad = 0;
+#pragma unroll 4
+              for (int x = r; x < TILE / 16; x += 128) {
+                if (((x >> 3) & 127) < valid) {
+                  const uint4 w = v[x];
+                  bad |= nonfinite_term(w.x, F16) | nonfinite_term(w.y, F16) | nonfinite_term(w.z, F16) |
+                         nonfinite_term(w.w, F16);
+                } else {
+                  v[x] = make_uint4(0, 0, 0, 0);
+                }
+              }
+              if (bad & 0x80008000u) odd[i & 3] = i + 1;
+              fence_proxy_async_smem();
+            }
+          }
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(hf == 0 ? p_full : p_full2);
+        }
+        if (!ok) break;
+        l = l * alpha + ((rs[0] + rs[1]) + (rs[2] + rs[3]));
+      }
+      if (!ok) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(o_done, i & 1, abort_flag, p.err))) break;
+      tc_fence_after();
+      const int head = u.kvh * G + rh;
+      if (odd[i & 3] == i + 1) {
+        if (valid_row) {
+          const Piece copy = u;
+          nonfinite |= recompute_row<F16, DH>(p, &copy, tok, head, r, part_rows);
+        }
+        __syncwarp();
+      } else if (busy) {
+        const float inv_l = l == 0.f ? 0.f : 1.f / l;
+        RowOut<F16, DH> out;
+        if (valid_row) out = row_out<F16, DH>(p, u, tok, head, r, part_rows);
+#pragma unroll 1
+        for (int cc = 0; cc < DH / 32; ++cc) {
+          uint32_t rr[32];
+          tmem_ld32(tO + 32 * cc, rr);
+          tmem_ld_wait();
+          if (valid_row) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float v[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(rr[8 * e + k]);
+              nonfinite |= store8<F16, DH>(out, 32 * cc + 8 * e, v, inv_l);
+            }
+          }
+        }
+        if (valid_row && out.stats) *reinterpret_cast<float2*>(out.stats) = make_float2(m_ref, l);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(o_free);
+      cv += u.tile1 - u.tile0;
+    }
+    report_range(nonfinite, p.err);
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+// Joins the pieces of the unit that begins in run blockIdx.x and ends in a later one: a warp per
+// row, its pieces' sums weighted by 2^(max - largest max), in order of their keys.
+constexpr int MERGE_WARPS = 8;
+
+template <bool F16, int DH>
+__global__ void __launch_bounds__(32 * MERGE_WARPS) tree_merge_kernel(const GqaParams p, const Join* __restrict__ joins) {
+  pdl_enter();
+  const Join u = joins[blockIdx.x];
+  if (u.n == 0) return;
+  const int G = p.n_heads / p.n_kv, TPT = BQ / G, part_rows = min(TPT, p.max_new) * G;
+  const int rows = min(TPT, u.n - u.tok0) * G, lane = threadIdx.x & 31;
+  constexpr int COLS = DH / 32;                           // columns of a lane
+  const size_t stride = static_cast<size_t>(part_rows) * (DH + 4);
+  uint32_t nonfinite = 0;
+  for (int r = blockIdx.y * MERGE_WARPS + (threadIdx.x >> 5); r < rows; r += gridDim.y * MERGE_WARPS) {
+    float top = -INFINITY;
+    for (int c = u.first + lane; c <= u.last; c += 32)
+      top = fmaxf(top, p.part[(2 * c + (c == u.first)) * stride + part_rows * DH + 2 * r]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, acc[COLS] = {};
+#pragma unroll 4
+    for (int c = u.first; c <= u.last; ++c) {
+      const float* slot = p.part + (2 * c + (c == u.first)) * stride;
+      const float2 ml = *reinterpret_cast<const float2*>(slot + part_rows * DH + 2 * r);
+      const float w = ml.y == 0.f ? 0.f : ex2(ml.x - base);
+      sum += ml.y * w;
+      float v[COLS];
+      if (COLS == 4) {
+        const float4 f = *reinterpret_cast<const float4*>(slot + r * DH + 4 * lane);
+        v[0] = f.x, v[1] = f.y, v[2 % COLS] = f.z, v[3 % COLS] = f.w;
+      } else {
+        const float2 f = *reinterpret_cast<const float2*>(slot + r * DH + 2 * lane);
+        v[0] = f.x, v[1] = f.y;
+      }
+      if (w != 0.f)                                       // a piece without a seen key adds nothing
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) acc[e] = fmaf(w, v[e], acc[e]);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t* o = static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.q0 + u.tok0 + r / G) * p.ld_o + (u.kvh * G + r % G) * DH;
+#pragma unroll
+    for (int e = 0; e < COLS / 2; ++e) {
+      const uint32_t w = pack2(acc[2 * e] * inv, acc[2 * e + 1] * inv, F16);
+      nonfinite |= nonfinite_term(w, F16);
+      reinterpret_cast<uint32_t*>(o)[COLS / 2 * lane + e] = w;
+    }
+  }
+  report_range(nonfinite, p.err);
+}
+
+constexpr int CTAS_PER_SM = 2;
+constexpr int MIN_TILES = 2;                // key tiles of a run at least
+
+template <bool F16, int DH>
+cudaError_t launch_typed(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, int grid, int q_box, Join* joins,
+                         cudaStream_t st) {
+  static bool attr_set[64] = {};
+  cudaError_t e = set_smem_limit_once(tc_tree_kernel<F16, DH>, Layout<DH>::BYTES, attr_set);
+  if (e != cudaSuccess) return e;
+  e = launch_kernel(tc_tree_kernel<F16, DH>, dim3(grid), dim3(THREADS), Layout<DH>::BYTES, st, mQ, mKV, p, q_box, MIN_TILES, joins);
+  if (e != cudaSuccess) return e;
+  const int rows = q_box * (p.n_heads / p.n_kv);
+  return launch_kernel(tree_merge_kernel<F16, DH>, dim3(grid, (rows + 4 * MERGE_WARPS - 1) / (4 * MERGE_WARPS)), dim3(32 * MERGE_WARPS),
+                       0, st, p, static_cast<const Join*>(joins));
+}
+
+int tile_tokens(int n_heads, int n_kv, int max_new) {
+  const int tpt = BQ / (n_heads / n_kv);
+  return tpt < max_new ? tpt : max_new;
+}
+size_t part_floats(int n_heads, int n_kv, int head_dim, int max_new, int num_sms) {
+  return static_cast<size_t>(2 * CTAS_PER_SM) * num_sms * tile_tokens(n_heads, n_kv, max_new) * (n_heads / n_kv) * (head_dim + 4);
+}
+
+}  // namespace
+
+int tc_tree_box_tokens(int n_heads, int n_kv, int max_new) { return tile_tokens(n_heads, n_kv, max_new); }
+
+size_t tc_tree_part_bytes(int n_heads, int n_kv, int head_dim, int max_new, int num_sms) {
+  return ((part_floats(n_heads, n_kv, head_dim, max_new, num_sms) * 4 + 255) & ~size_t(255)) +
+         static_cast<size_t>(CTAS_PER_SM) * num_sms * sizeof(Join);
+}
+
+cudaError_t launch_tc_tree(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, bool f16, int num_sms, cudaStream_t st) {
+  const int q_box = tile_tokens(p.n_heads, p.n_kv, p.max_new), grid = CTAS_PER_SM * num_sms;
+  Join* joins = reinterpret_cast<Join*>(reinterpret_cast<uint8_t*>(p.part) +
+                                        ((part_floats(p.n_heads, p.n_kv, p.head_dim, p.max_new, num_sms) * 4 + 255) & ~size_t(255)));
+  if (p.head_dim == 128) return f16 ? launch_typed<true, 128>(mQ, mKV, p, grid, q_box, joins, st) : launch_typed<false, 128>(mQ, mKV, p, grid, q_box, joins, st);
+  return f16 ? launch_typed<true, 64>(mQ, mKV, p, grid, q_box, joins, st) : launch_typed<false, 64>(mQ, mKV, p, grid, q_box, joins, st);
+}
+
+}  // namespace seer
