@@ -44,16 +44,27 @@ constexpr float RESCALE_THRESHOLD = 8.0f;   // log2 units
 constexpr int U_SLOTS = 4;
 constexpr int U_READERS = 1 + 4;            // issuer, softmax warps
 
-template <int DH>
-struct Layout {
+// Shared memory of a CTA: QB buffers of QROWS rows of Q, then one ring of SLOTS key and
+// value tiles in turn.  The MMA reads 128 rows from a Q buffer; those past QROWS are other
+// bytes of this memory, in rows of S that nobody looks at.  Few rows leave room for a third
+// slot and a second Q buffer, so that loads go on across a tile's softmax and from piece to
+// piece.
+template <int DH_, int SLOTS_, int QB_, int QROWS_>
+struct Config {
+  static constexpr int DH = DH_, SLOTS = SLOTS_, QB = QB_, QROWS = QROWS_;
   static constexpr int TILE = 128 * DH * 2;
-  static constexpr int STAGES = 128 / DH;   // K ring and V ring: 64 KB of keys and values in flight per CTA
-  static constexpr int OFF_K = TILE;
-  static constexpr int OFF_V = OFF_K + STAGES * TILE;
-  static constexpr int OFF_BAR = OFF_V + STAGES * TILE;
+  static constexpr int Q_PANEL = QROWS * 128, Q_BYTES = DH / 64 * Q_PANEL;
+  static constexpr int OFF_RING = QB * Q_BYTES;
+  static constexpr int OFF_BAR = OFF_RING + SLOTS * TILE;
   static constexpr int BYTES = OFF_BAR + BAR_BYTES + 1024;
+  static_assert(Q_PANEL % 1024 == 0, "the 128-byte swizzle repeats every 8 rows");
+  static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two CTAs per SM");
+  static_assert(Q_BYTES * QB + SLOTS * TILE >= (QB - 1) * Q_BYTES + (DH / 64 - 1) * Q_PANEL + PANEL, "128 rows from any Q panel");
 };
-static_assert(2 * (Layout<128>::BYTES + 1024) <= 227 * 1024, "two CTAs per SM");
+using Wide64 = Config<64, 4, 2, 128>;
+using Few128 = Config<128, 3, 2, 24>;
+using Some128 = Config<128, 3, 1, 48>;
+using Wide128 = Config<128, 2, 1, 128>;
 
 // A piece: keys [tile0 * 128, tile1 * 128) of a unit.  n < 0: no more pieces.
 struct Piece {
@@ -62,6 +73,11 @@ struct Piece {
   int part;                                 // slot of its partial result, or -1: a whole unit
 };
 static_assert(sizeof(Piece) == 36, "ring entries");
+
+// Places of a unit on the line besides its key tiles: what a piece costs beyond them (Q,
+// the first and last round, its result), about one tile's time, two where it stores many
+// rows (us: a tile 2.9 and a piece 3.1 for 4 rows, 3.4 and 7.8 for 64 .. 128).
+__device__ __forceinline__ int unit_extra(int part_rows) { return part_rows <= 32 ? 1 : 2; }
 
 struct Request {
   int q0, n, kv;
@@ -79,9 +95,13 @@ __device__ __forceinline__ Request read_request(const GqaParams& p, int b) {
   return r;
 }
 __device__ __forceinline__ int key_tiles(int kv) { return static_cast<int>((kv + static_cast<unsigned>(BKV) - 1) / BKV); }
-// Key tiles of all units of a request.
-__device__ __forceinline__ long long line_length(const GqaParams& p, const Request& r, int tpt) {
-  return static_cast<long long>(p.n_kv) * ((r.n + tpt - 1) / tpt) * key_tiles(r.kv);
+// Places of all units of a request.
+__device__ __forceinline__ long long line_length(const GqaParams& p, const Request& r, int tpt, int extra) {
+  return r.n == 0 ? 0 : static_cast<long long>(p.n_kv) * ((r.n + tpt - 1) / tpt) * (key_tiles(r.kv) + extra);
+}
+// a / b for a >= 0, b > 0, by a 32-bit division where that is enough.
+__device__ __forceinline__ int quotient(long long a, int b) {
+  return static_cast<int>((a >> 32) == 0 ? static_cast<unsigned>(a) / static_cast<unsigned>(b) : a / b);
 }
 
 // Run c of n over a line of `total`: [cut(c), cut(c + 1)), and the run that holds x.
@@ -97,15 +117,16 @@ struct Join {
   int pad[2];
 };
 
-__device__ __forceinline__ Piece read_piece(uint64_t* u_full, uint64_t* u_empty, const Piece* ring, int i,
-                                            volatile int* abort, int* err, int lane) {
+// This CTA's i-th piece, or null when there are no more; by a whole warp, which gives the
+// entry back with release_piece() when it has done with it.
+__device__ __forceinline__ const Piece* read_piece(uint64_t* u_full, const Piece* ring, int i, volatile int* abort, int* err) {
   const int s = i % U_SLOTS;
-  const bool ok = warp_wait(&u_full[s], (i / U_SLOTS) & 1, abort, err);
-  Piece w = ring[s];
-  if (!ok) w.n = -1;
+  if (!warp_wait(&u_full[s], (i / U_SLOTS) & 1, abort, err) || ring[s].n < 0) return nullptr;
+  return ring + s;
+}
+__device__ __forceinline__ void release_piece(uint64_t* u_empty, int i, int lane) {
   __syncwarp();
-  if (lane == 0 && ok) mbar_arrive(&u_empty[s]);
-  return w;
+  if (lane == 0) mbar_arrive(&u_empty[i % U_SLOTS]);
 }
 
 // Bits of the keys that new row `tok` sees among the request's new rows.
@@ -206,50 +227,76 @@ __device__ __noinline__ uint32_t recompute_row(const GqaParams& p, const Piece* 
   return bad;
 }
 
-template <bool F16, int DH>
+template <bool F16, typename Cfg>
 __global__ void __launch_bounds__(THREADS, 2)
     tc_tree_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mKV, const GqaParams p,
-                   const int q_box, const int min_tiles, Join* __restrict__ joins) {
-  pdl_enter();
-  using Lay = Layout<DH>;
-  constexpr int TILE = Lay::TILE, PANELS = DH / 64, STAGES = Lay::STAGES;
+                   const int q_box, const int min_places, Join* __restrict__ joins) {
+  constexpr int DH = Cfg::DH, TILE = Cfg::TILE, PANELS = DH / 64, SLOTS = Cfg::SLOTS, QB = Cfg::QB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Lay::OFF_BAR);
-  uint64_t* q_full = bars + 0;
-  uint64_t* q_empty = bars + 1;
-  uint64_t* s_full = bars + 2;
-  uint64_t* p_full = bars + 3;
-  uint64_t* p_full2 = bars + 4;
-  uint64_t* o_done = bars + 5;
-  uint64_t* o_free = bars + 6;
-  uint64_t* k_full = bars + 7;               // [STAGES]
-  uint64_t* k_empty = k_full + STAGES;
-  uint64_t* v_full = k_empty + STAGES;
-  uint64_t* v_empty = v_full + STAGES;
-  uint64_t* u_full = v_empty + STAGES;       // [U_SLOTS]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Cfg::OFF_BAR);
+  uint64_t* s_full = bars + 0;
+  uint64_t* p_full = bars + 1;
+  uint64_t* p_full2 = bars + 2;
+  uint64_t* o_done = bars + 3;
+  uint64_t* o_free = bars + 4;
+  uint64_t* q_full = bars + 5;               // [QB]
+  uint64_t* q_empty = q_full + QB;           // [QB]
+  uint64_t* r_full = q_empty + QB;           // [SLOTS] tile 2 g (K) or 2 g + 1 (V) of this CTA's g-th key tile
+  uint64_t* r_empty = r_full + SLOTS;
+  uint64_t* u_full = r_empty + SLOTS;        // [U_SLOTS]
   uint64_t* u_empty = u_full + U_SLOTS;      // [U_SLOTS]
   Piece* ring = reinterpret_cast<Piece*>(u_empty + U_SLOTS);     // [U_SLOTS]
   volatile int* odd = reinterpret_cast<volatile int*>(ring + U_SLOTS);   // [4], as in tc_causal.cu
   uint32_t* tmem_slot = const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(odd + 4));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert(8 * (7 + 4 * 2 + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 <= BAR_BYTES, "barrier block");
+  static_assert(8 * (5 + 2 * QB + 2 * SLOTS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 <= BAR_BYTES, "barrier block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = p.n_heads / p.n_kv, TPT = BQ / G;
   const int part_rows = min(TPT, p.max_new) * G;          // rows of a partial slot
+  const int extra = unit_extra(part_rows);
+
+  // barriers and tensor memory, before the kernels ahead are waited for
+  if (threadIdx.x == 0) {
+    mbar_init(s_full, 1);
+    mbar_init(p_full, 4);
+    mbar_init(p_full2, 4);
+    mbar_init(o_done, 1);
+    mbar_init(o_free, 4);
+    for (int i = 0; i < QB; ++i) {
+      mbar_init(&q_full[i], 1);
+      mbar_init(&q_empty[i], 1);
+    }
+    for (int i = 0; i < SLOTS; ++i) {
+      mbar_init(&r_full[i], 1);
+      mbar_init(&r_empty[i], 1);
+    }
+    for (int i = 0; i < U_SLOTS; ++i) {
+      mbar_init(&u_full[i], 1);
+      mbar_init(&u_empty[i], U_READERS);
+      odd[i] = 0;
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&mQ);
+    tma_prefetch_desc(&mKV);
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
+  pdl_enter();
 
   // ---- the line of key tiles: its length and the request where this CTA's run begins
   __shared__ long long warp_sum[THREADS / 32];
   __shared__ long long start_off;
   __shared__ int start_b;
+  __shared__ Request start_r;
   const int chunk = (p.B + THREADS - 1) / THREADS;
   const int b_lo = min(p.B, static_cast<int>(threadIdx.x) * chunk), b_hi = min(p.B, b_lo + chunk);
   long long mine = 0;
   for (int b = b_lo; b < b_hi; ++b) {
     const Request r = read_request(p, b);
     if (!r.good && blockIdx.x == 0) record_error(p.err, kErrLayout);
-    mine += line_length(p, r, TPT);
+    mine += line_length(p, r, TPT, extra);
   }
   long long inc = mine;
 #pragma unroll
@@ -265,70 +312,44 @@ __global__ void __launch_bounds__(THREADS, 2)
     before += w < warp ? warp_sum[w] : 0;
     total += warp_sum[w];
   }
-  const long long want = (total + min_tiles - 1) / min_tiles;
-  const int runs = want < gridDim.x ? static_cast<int>(want) : static_cast<int>(gridDim.x), c = blockIdx.x;
-  if (c >= runs) {
-    if (threadIdx.x == 0) joins[c] = Join{};
-    return;                                               // the whole CTA
-  }
-  const long long run0 = cut(total, c, runs), run1 = cut(total, c + 1, runs);
-  if (mine > 0 && run0 >= before && run0 < before + mine) {
+  const int grid = gridDim.x, c = blockIdx.x;
+  const int runs = total < static_cast<long long>(grid) * min_places ? quotient(total + min_places - 1, min_places) : grid;
+  const bool idle = c >= runs;                            // the whole CTA
+  const long long run0 = idle ? 0 : cut(total, c, runs), run1 = idle ? 0 : cut(total, c + 1, runs);
+  if (!idle && mine > 0 && run0 >= before && run0 < before + mine) {
     long long at = before;
     for (int b = b_lo; b < b_hi; ++b) {
-      const long long n = line_length(p, read_request(p, b), TPT);
+      const Request r = read_request(p, b);
+      const long long n = line_length(p, r, TPT, extra);
       if (run0 < at + n) {
         start_b = b;
         start_off = run0 - at;
+        start_r = r;
         break;
       }
       at += n;
     }
   }
-
-  if (threadIdx.x == 0) {
-    mbar_init(q_full, 1);
-    mbar_init(q_empty, 1);
-    mbar_init(s_full, 1);
-    mbar_init(p_full, 4);
-    mbar_init(p_full2, 4);
-    mbar_init(o_done, 1);
-    mbar_init(o_free, 4);
-    for (int i = 0; i < STAGES; ++i) {
-      mbar_init(&k_full[i], 1);
-      mbar_init(&k_empty[i], 1);
-      mbar_init(&v_full[i], 1);
-      mbar_init(&v_empty[i], 1);
-    }
-    for (int i = 0; i < U_SLOTS; ++i) {
-      mbar_init(&u_full[i], 1);
-      mbar_init(&u_empty[i], U_READERS);
-      odd[i] = 0;
-    }
-    *abort_flag = 0;
-    fence_barrier_init();
-  }
-  if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  if (warp == 0) {
+  if (idle) {
+    if (threadIdx.x == 0) joins[c] = Join{};
+  } else if (warp == 0) {
     // -------------------------------------------------- producer
     const bool leader = elect_one();
-    if (leader) {
-      tma_prefetch_desc(&mQ);
-      tma_prefetch_desc(&mKV);
-    }
-    __syncwarp();
     const int box_rows = min(BKV, 1 << p.page_shift), boxes = BKV / box_rows;
     const int out_of_pool = p.n_pages << p.page_shift;    // a row that the tensor map fills with zeros
-    int q_issued = 0, k_issued = 0, v_issued = 0;
+    unsigned loaded = 0;                                  // ring tiles issued
+    int pieces = 0;
     bool ok = true;
     int b = start_b;
     long long off = start_off, at = run0;
-    int window = b;                                       // requests window .. window + 31 in the lanes' registers
-    Request mine_r = read_request(p, window + lane);
+    Request r = start_r;                                  // request b
+    int window = b - 32;                                  // requests window .. window + 31 in the lanes' registers
+    Request ahead{};
     Join join{};
     // pool row of this lane's box of key tile j
     const auto box_row = [&](int bb, int kv, int j) {
@@ -341,44 +362,60 @@ __global__ void __launch_bounds__(THREADS, 2)
       }
       return (page << p.page_shift) + (key & ((1 << p.page_shift) - 1));
     };
+    // a ring tile of this lane's box, columns of head `head` of the row's 2 n_kv
+    const auto load = [&](int row, int head, int bytes) {
+      const unsigned s = loaded % SLOTS, use = loaded / SLOTS;
+      if (use > 0 && !warp_wait(&r_empty[s], (use - 1) & 1, abort_flag, p.err)) return false;
+      if (leader) mbar_arrive_expect_tx(&r_full[s], bytes);
+      __syncwarp();
+      if (row >= 0)
+        for (int x = 0; x < PANELS; ++x)
+          tma_load_3d(smem + Cfg::OFF_RING + s * TILE + x * PANEL + lane * box_rows * 128, &mKV, &r_full[s], 64 * x, head, row);
+      __syncwarp();
+      ++loaded;
+      return true;
+    };
     for (int i = 0; ok; ++i) {
       Piece u{};
       u.n = -1;
-      Request r{};
-      if (at < run1) {
-        long long len;
-        for (;;) {                                        // requests without keys are passed over
+      while (at < run1) {                                 // the next stretch that holds key tiles
+        const long long len = line_length(p, r, TPT, extra);
+        if (off >= len) {                                 // on to the next request
+          off -= len;
+          if (++b >= p.B) {                               // the lengths changed under the call
+            at = run1;
+            break;
+          }
           if (b - window >= 32) {
             window = b;
-            mine_r = read_request(p, window + lane);
+            ahead = read_request(p, window + lane);
           }
-          r.q0 = __shfl_sync(0xffffffffu, mine_r.q0, b - window);
-          r.n = __shfl_sync(0xffffffffu, mine_r.n, b - window);
-          r.kv = __shfl_sync(0xffffffffu, mine_r.kv, b - window);
-          len = line_length(p, r, TPT);
-          if (off < len || b + 1 >= p.B) break;
-          off -= len;
-          ++b;
+          r.q0 = __shfl_sync(0xffffffffu, ahead.q0, b - window);
+          r.n = __shfl_sync(0xffffffffu, ahead.n, b - window);
+          r.kv = __shfl_sync(0xffffffffu, ahead.kv, b - window);
+          continue;
         }
-        if (off >= len) at = run1;                        // the lengths changed under the call
-      }
-      if (at < run1) {
-        const int tiles = key_tiles(r.kv), row_tiles = (r.n + TPT - 1) / TPT;
-        const int unit = static_cast<int>(off / tiles);
+        const int tiles = key_tiles(r.kv), places = tiles + extra, row_tiles = (r.n + TPT - 1) / TPT;
+        const int unit = quotient(off, places);
+        const int first = static_cast<int>(off - static_cast<long long>(unit) * places);
+        const int last = static_cast<int>(min(static_cast<long long>(places), first + (run1 - at)));
+        off += last - first;
+        at += last - first;
+        u.tile0 = max(first - extra, 0);
+        u.tile1 = last - extra;
+        if (u.tile1 <= u.tile0) continue;                 // only places without a tile
         u.q0 = r.q0;
         u.n = r.n;
         u.kv = r.kv;
         u.b = b;
         u.kvh = unit / row_tiles;
         u.tok0 = (unit - u.kvh * row_tiles) * TPT;
-        u.tile0 = static_cast<int>(off - static_cast<long long>(unit) * tiles);
-        u.tile1 = static_cast<int>(min(static_cast<long long>(tiles), u.tile0 + (run1 - at)));
         u.part = u.tile0 > 0 ? 2 * c : (u.tile1 < tiles ? 2 * c + 1 : -1);
         if (u.tile0 == 0 && u.tile1 < tiles)
-          join = Join{u.q0, u.tok0, u.n, u.kvh, c, run_of(total, at + tiles - 1, runs), {0, 0}};
-        off += u.tile1 - u.tile0;
-        at += u.tile1 - u.tile0;
+          join = Join{u.q0, u.tok0, u.n, u.kvh, c, run_of(total, at + (places - last) - 1, runs), {0, 0}};
+        break;
       }
+      if (u.tile1 <= u.tile0) u.n = -1;
       const int s = i % U_SLOTS;
       if (i >= U_SLOTS && !warp_wait(&u_empty[s], (i / U_SLOTS - 1) & 1, abort_flag, p.err)) break;
       if (lane == 0) {
@@ -388,120 +425,104 @@ __global__ void __launch_bounds__(THREADS, 2)
       __syncwarp();
       if (u.n < 0) break;
       int next_row = box_row(u.b, u.kv, u.tile0);         // the page of a tile is looked up a tile ahead
-      if (i > 0 && !warp_wait(q_empty, (i - 1) & 1, abort_flag, p.err)) break;
+      const int qs = i % QB;
+      if (i >= QB && !warp_wait(&q_empty[qs], (i / QB - 1) & 1, abort_flag, p.err)) break;
       if (leader) {
-        mbar_arrive_expect_tx(q_full, PANELS * q_box * G * 128);
+        mbar_arrive_expect_tx(&q_full[qs], PANELS * q_box * G * 128);
         for (int x = 0; x < PANELS; ++x)
-          tma_load_3d(smem + x * PANEL, &mQ, q_full, 64 * x, u.kvh * G, u.q0 + u.tok0);
+          tma_load_3d(smem + qs * Cfg::Q_BYTES + x * Cfg::Q_PANEL, &mQ, &q_full[qs], 64 * x, u.kvh * G, u.q0 + u.tok0);
       }
       __syncwarp();
-      ++q_issued;
+      ++pieces;
       for (int j = u.tile0; j < u.tile1; ++j) {
         const int row = next_row;
         if (j + 1 < u.tile1) next_row = box_row(u.b, u.kv, j + 1);
         const int bytes = __popc(__ballot_sync(0xffffffffu, row >= 0)) * box_rows * 128 * PANELS;
-        const int ks = k_issued % STAGES, ku = k_issued / STAGES;
-        if (ku > 0 && !warp_wait(&k_empty[ks], (ku - 1) & 1, abort_flag, p.err)) { ok = false; break; }
-        if (leader) mbar_arrive_expect_tx(&k_full[ks], bytes);
-        __syncwarp();
-        if (row >= 0)
-          for (int x = 0; x < PANELS; ++x)
-            tma_load_3d(smem + Lay::OFF_K + ks * TILE + x * PANEL + lane * box_rows * 128, &mKV, &k_full[ks], 64 * x, u.kvh, row);
-        __syncwarp();
-        ++k_issued;
-        const int vs = v_issued % STAGES, vu = v_issued / STAGES;
-        if (vu > 0 && !warp_wait(&v_empty[vs], (vu - 1) & 1, abort_flag, p.err)) { ok = false; break; }
-        if (leader) mbar_arrive_expect_tx(&v_full[vs], bytes);
-        __syncwarp();
-        if (row >= 0)
-          for (int x = 0; x < PANELS; ++x)
-            tma_load_3d(smem + Lay::OFF_V + vs * TILE + x * PANEL + lane * box_rows * 128, &mKV, &v_full[vs], 64 * x, p.n_kv + u.kvh, row);
-        __syncwarp();
-        ++v_issued;
+        if (!load(row, u.kvh, bytes) || !load(row, p.n_kv + u.kvh, bytes)) {
+          ok = false;
+          break;
+        }
       }
     }
     if (lane == 0) joins[c] = join;
     if (*abort_flag && leader) {
       // let copies still in flight land before the CTA's shared memory is released
-      if (q_issued > 0) mbar_wait_drain(q_full, (q_issued - 1) & 1, 200000000ull);
-      for (int j = k_issued > STAGES ? k_issued - STAGES : 0; j < k_issued; ++j)
-        mbar_wait_drain(&k_full[j % STAGES], (j / STAGES) & 1, 200000000ull);
-      for (int j = v_issued > STAGES ? v_issued - STAGES : 0; j < v_issued; ++j)
-        mbar_wait_drain(&v_full[j % STAGES], (j / STAGES) & 1, 200000000ull);
+      for (int j = max(pieces - QB, 0); j < pieces; ++j) mbar_wait_drain(&q_full[j % QB], (j / QB) & 1, 200000000ull);
+      for (unsigned j = loaded > SLOTS ? loaded - SLOTS : 0; j < loaded; ++j)
+        mbar_wait_drain(&r_full[j % SLOTS], (j / SLOTS) & 1, 200000000ull);
     }
   } else if (warp == 1) {
     // -------------------------------------------------- MMA issuer
     const bool leader = elect_one();
     constexpr uint32_t idesc_qk = make_idesc(BQ, BKV, 0, F16);
     constexpr uint32_t idesc_pv = make_idesc(BQ, DH, 1, F16);
-    const uint64_t dq = make_sdesc_sw128(smem_u32(smem), 16, 1024);
-    const uint64_t dk0 = make_sdesc_sw128(smem_u32(smem + Lay::OFF_K), 16, 1024);
-    const uint64_t dv0 = make_sdesc_sw128(smem_u32(smem + Lay::OFF_V), PANEL, 1024);
+    const uint64_t dq0 = make_sdesc_sw128(smem_u32(smem), 16, 1024);
+    const uint64_t dk0 = make_sdesc_sw128(smem_u32(smem + Cfg::OFF_RING), 16, 1024);
+    const uint64_t dv0 = make_sdesc_sw128(smem_u32(smem + Cfg::OFF_RING), PANEL, 1024);
     const uint32_t dS = tmem, dO = tmem + TM_O;
-    unsigned kc = 0, vc = 0, pc = 0;                      // K, V and P tiles consumed
-    auto qk = [&](bool last) {
+    unsigned g = 0;                                       // key tiles begun
+    auto full = [&](unsigned x) { return warp_wait(&r_full[x % SLOTS], (x / SLOTS) & 1u, abort_flag, p.err); };
+    auto qk = [&](int qs, bool last) {
       if (leader) {
-        const unsigned st = kc % STAGES;
+        const unsigned st = 2 * g % SLOTS;
         const uint64_t dk = dk0 + static_cast<uint64_t>(st * (TILE >> 4));
+        const uint64_t dq = dq0 + static_cast<uint64_t>(qs * (Cfg::Q_BYTES >> 4));
 #pragma unroll
         for (int k = 0; k < DH / 16; ++k) {
-          const uint64_t o = static_cast<uint64_t>(((k >> 2) * PANEL + (k & 3) * 32) >> 4);
-          tc_mma_f16(dS, dq + o, dk + o, idesc_qk, k > 0 ? 1u : 0u);
+          const uint64_t oq = static_cast<uint64_t>(((k >> 2) * Cfg::Q_PANEL + (k & 3) * 32) >> 4);
+          const uint64_t ok = static_cast<uint64_t>(((k >> 2) * PANEL + (k & 3) * 32) >> 4);
+          tc_mma_f16(dS, dq + oq, dk + ok, idesc_qk, k > 0 ? 1u : 0u);
         }
         tc_commit(s_full);
-        tc_commit(&k_empty[st]);
-        if (last) tc_commit(q_empty);
+        tc_commit(&r_empty[st]);
+        if (last) tc_commit(&q_empty[qs]);
       }
       __syncwarp();
-      ++kc;
+      ++g;
     };
-    auto pv = [&](bool fresh, int half) {
+    auto pv = [&](unsigned x, bool fresh, int half) {
       if (leader) {
-        const unsigned st = vc % STAGES;
-        const uint64_t dv = dv0 + static_cast<uint64_t>(st * (TILE >> 4));
+        const uint64_t dv = dv0 + static_cast<uint64_t>(x % SLOTS * (TILE >> 4));
 #pragma unroll
         for (int kk = 0; kk < BKV / 32; ++kk) {
           const int k = half * (BKV / 32) + kk;
           tc_mma_f16_tmem_a(dO, dS + 8 * k, dv + static_cast<uint64_t>(k * 128), idesc_pv, (!fresh || k > 0) ? 1u : 0u);
         }
-        if (half == 1) tc_commit(&v_empty[st]);
+        if (half == 1) tc_commit(&r_empty[x % SLOTS]);
       }
       __syncwarp();
     };
     bool ok = true;
     for (int i = 0; ok; ++i) {
-      const Piece u = read_piece(u_full, u_empty, ring, i, abort_flag, p.err, lane);
-      if (u.n < 0) break;
-      const int tiles = u.tile1 - u.tile0;
-      if (!warp_wait(q_full, i & 1, abort_flag, p.err) ||
-          !warp_wait(&k_full[kc % STAGES], (kc / STAGES) & 1u, abort_flag, p.err))
-        break;
+      const Piece* u = read_piece(u_full, ring, i, abort_flag, p.err);
+      if (u == nullptr) break;
+      const int tiles = u->tile1 - u->tile0, qs = i % QB;
+      release_piece(u_empty, i, lane);
+      if (!warp_wait(&q_full[qs], (i / QB) & 1, abort_flag, p.err) || !full(2 * g)) break;
       tc_fence_after();
-      qk(tiles == 1);
+      qk(qs, tiles == 1);
       for (int j = 0; j < tiles; ++j) {
+        const unsigned v = 2 * g - 1, pc = (g - 1) & 1u;  // V of the tile whose scores were issued last
         if ((j == 0 && i > 0 && !warp_wait(o_free, (i - 1) & 1u, abort_flag, p.err)) ||   // the piece before is read out
-            !warp_wait(&v_full[vc % STAGES], (vc / STAGES) & 1u, abort_flag, p.err) ||
-            !warp_wait(p_full, pc & 1u, abort_flag, p.err)) {
+            !full(v) || !warp_wait(p_full, pc, abort_flag, p.err)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        pv(j == 0, 0);
-        if (!warp_wait(p_full2, pc & 1u, abort_flag, p.err)) {
+        pv(v, j == 0, 0);
+        if (!warp_wait(p_full2, pc, abort_flag, p.err)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        pv(j == 0, 1);
-        ++vc;
-        ++pc;
+        pv(v, j == 0, 1);
         if (j + 1 < tiles) {
-          if (!warp_wait(&k_full[kc % STAGES], (kc / STAGES) & 1u, abort_flag, p.err)) {
+          if (!full(2 * g)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          qk(j + 2 == tiles);
+          qk(qs, j + 2 == tiles);
         } else {
           if (leader) tc_commit(o_done);
           __syncwarp();
@@ -511,26 +532,25 @@ __global__ void __launch_bounds__(THREADS, 2)
   } else {
     // -------------------------------------------------- softmax warps 2..5
     const int r = (warp & 3) * 32 + lane;                 // row of the tile == TMEM lane
-    const int rt = r / G, rh = r - rt * G;
+    const int rt = r / G;
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + lane_off, tO = tmem + lane_off + TM_O;
     const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(DH));
-    int cs = 0, cv = 0;                                   // S tiles seen; V tiles of the pieces before
+    unsigned g = 0;                                       // key tiles seen
     uint32_t nonfinite = 0;
     bool ok = true;
     for (int i = 0; ok; ++i) {
-      const Piece u = read_piece(u_full, u_empty, ring, i, abort_flag, p.err, lane);
-      if (u.n < 0) break;
-      const int ntok = min(TPT, u.n - u.tok0), tok = u.tok0 + rt, ctx = u.kv - u.n;
+      const Piece* u = read_piece(u_full, ring, i, abort_flag, p.err);
+      if (u == nullptr) break;
+      const int ntok = min(TPT, u->n - u->tok0), tile0 = u->tile0, tile1 = u->tile1;
       const bool valid_row = rt < ntok;
       const bool busy = (warp & 3) * 32 < ntok * G;       // the warp holds rows of the tile
-      const uint64_t bits = valid_row ? visible(p, u, tok) : 0;
+      const int first_masked = (u->kv - u->n) / BKV;      // tiles from here on hold new rows' keys
       float m_ref = -INFINITY, l = 0.f;
-      for (int j = u.tile0; ok && j < u.tile1; ++j) {
-        if (!__all_sync(0xffffffffu, mbar_wait(s_full, cs & 1, abort_flag, p.err))) { ok = false; break; }
-        ++cs;
+      for (int j = tile0; ok && j < tile1; ++j, ++g) {
+        if (!__all_sync(0xffffffffu, mbar_wait(s_full, g & 1u, abort_flag, p.err))) { ok = false; break; }
         tc_fence_after();
-        const bool masked = (j + 1) * static_cast<long long>(BKV) > ctx;
+        const bool masked = j >= first_masked;
         float s[BKV];
         float alpha = 1.f, neg = 0.f;
         bool any_need = false;
@@ -547,7 +567,8 @@ __global__ void __launch_bounds__(THREADS, 2)
           }
           if (masked) {
             // new row 0 is key `sh` of the tile: keys before it are seen, then the row's bits
-            const int sh = ctx - j * BKV;
+            const uint64_t bits = valid_row ? visible(p, *u, u->tok0 + rt) : 0;
+            const int sh = u->kv - u->n - j * BKV;
             const auto word = [&](int at) -> uint32_t {   // keys at .. at + 31
               const int x = at - sh;                      // index of key `at` among the new rows
               if (x >= 64) return 0u;
@@ -574,7 +595,7 @@ __global__ void __launch_bounds__(THREADS, 2)
 #pragma unroll
             for (int e = 0; e < w; ++e) mx[e] = fmaxf(mx[e], mx[e + w]);
           const float m_new = fmaxf(m_ref, mx[0] * scale_log2);
-          const bool need = j == u.tile0 || m_new > m_ref + RESCALE_THRESHOLD;
+          const bool need = j == tile0 || m_new > m_ref + RESCALE_THRESHOLD;
           any_need = __any_sync(0xffffffffu, need);
           if (need) {
             alpha = m_ref == -INFINITY ? 0.f : ex2(m_ref - m_new);
@@ -601,7 +622,7 @@ __global__ void __launch_bounds__(THREADS, 2)
             }
           }
           if (hf == 0) {
-            if (busy && j > u.tile0 && any_need) {
+            if (busy && j > tile0 && any_need) {
 #pragma unroll 1
               for (int cc = 0; cc < DH / 32; ++cc) {
                 uint32_t rr[32];
@@ -613,13 +634,13 @@ __global__ void __launch_bounds__(THREADS, 2)
               }
             }
             if (masked) {
-              const int vsi = cv + j - u.tile0, vst = vsi % STAGES;
-              if (!__all_sync(0xffffffffu, mbar_wait(&v_full[vst], (vsi / STAGES) & 1, abort_flag, p.err))) {
+              const unsigned vx = 2 * g + 1;
+              if (!__all_sync(0xffffffffu, mbar_wait(&r_full[vx % SLOTS], (vx / SLOTS) & 1u, abort_flag, p.err))) {
                 ok = false;
                 break;
               }
-              const int valid = u.kv - j * BKV;
-              uint4* v = reinterpret_cast<uint4*>(smem + Lay::OFF_V + vst * TILE);
+              const int valid = u->kv - j * BKV;
+              uint4* v = reinterpret_cast<uint4*>(smem + Cfg::OFF_RING + vx % SLOTS * TILE);
               uint32_t bad = 0;
 #pragma unroll 4
               for (int x = r; x < TILE / 16; x += 128) {
@@ -646,17 +667,14 @@ __global__ void __launch_bounds__(THREADS, 2)
       if (!ok) break;
       if (!__all_sync(0xffffffffu, mbar_wait(o_done, i & 1, abort_flag, p.err))) break;
       tc_fence_after();
-      const int head = u.kvh * G + rh;
+      const int tok = u->tok0 + rt, head = u->kvh * G + r - rt * G;
       if (odd[i & 3] == i + 1) {
-        if (valid_row) {
-          const Piece copy = u;
-          nonfinite |= recompute_row<F16, DH>(p, &copy, tok, head, r, part_rows);
-        }
+        if (valid_row) nonfinite |= recompute_row<F16, DH>(p, u, tok, head, r, part_rows);
         __syncwarp();
       } else if (busy) {
         const float inv_l = l == 0.f ? 0.f : 1.f / l;
         RowOut<F16, DH> out;
-        if (valid_row) out = row_out<F16, DH>(p, u, tok, head, r, part_rows);
+        if (valid_row) out = row_out<F16, DH>(p, *u, tok, head, r, part_rows);
 #pragma unroll 1
         for (int cc = 0; cc < DH / 32; ++cc) {
           uint32_t rr[32];
@@ -675,9 +693,8 @@ __global__ void __launch_bounds__(THREADS, 2)
         if (valid_row && out.stats) *reinterpret_cast<float2*>(out.stats) = make_float2(m_ref, l);
       }
       tc_fence_before();
-      __syncwarp();
+      release_piece(u_empty, i, lane);
       if (lane == 0) mbar_arrive(o_free);
-      cv += u.tile1 - u.tile0;
     }
     report_range(nonfinite, p.err);
   }
@@ -743,19 +760,28 @@ __global__ void __launch_bounds__(32 * MERGE_WARPS) tree_merge_kernel(const GqaP
 }
 
 constexpr int CTAS_PER_SM = 2;
-constexpr int MIN_TILES = 2;                // key tiles of a run at least
+constexpr int MIN_PLACES = 3;               // places of a run at least
 
-template <bool F16, int DH>
+template <bool F16, typename Cfg>
 cudaError_t launch_typed(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, int grid, int q_box, Join* joins,
                          cudaStream_t st) {
   static bool attr_set[64] = {};
-  cudaError_t e = set_smem_limit_once(tc_tree_kernel<F16, DH>, Layout<DH>::BYTES, attr_set);
+  cudaError_t e = set_smem_limit_once(tc_tree_kernel<F16, Cfg>, Cfg::BYTES, attr_set);
   if (e != cudaSuccess) return e;
-  e = launch_kernel(tc_tree_kernel<F16, DH>, dim3(grid), dim3(THREADS), Layout<DH>::BYTES, st, mQ, mKV, p, q_box, MIN_TILES, joins);
+  e = launch_kernel(tc_tree_kernel<F16, Cfg>, dim3(grid), dim3(THREADS), Cfg::BYTES, st, mQ, mKV, p, q_box, MIN_PLACES, joins);
   if (e != cudaSuccess) return e;
   const int rows = q_box * (p.n_heads / p.n_kv);
-  return launch_kernel(tree_merge_kernel<F16, DH>, dim3(grid, (rows + 4 * MERGE_WARPS - 1) / (4 * MERGE_WARPS)), dim3(32 * MERGE_WARPS),
-                       0, st, p, static_cast<const Join*>(joins));
+  return launch_kernel(tree_merge_kernel<F16, Cfg::DH>, dim3(grid, (rows + 4 * MERGE_WARPS - 1) / (4 * MERGE_WARPS)),
+                       dim3(32 * MERGE_WARPS), 0, st, p, static_cast<const Join*>(joins));
+}
+template <bool F16>
+cudaError_t launch_rows(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, int grid, int q_box, Join* joins,
+                        cudaStream_t st) {
+  const int rows = q_box * (p.n_heads / p.n_kv);
+  if (p.head_dim == 64) return launch_typed<F16, Wide64>(mQ, mKV, p, grid, q_box, joins, st);
+  if (rows <= Few128::QROWS) return launch_typed<F16, Few128>(mQ, mKV, p, grid, q_box, joins, st);
+  if (rows <= Some128::QROWS) return launch_typed<F16, Some128>(mQ, mKV, p, grid, q_box, joins, st);
+  return launch_typed<F16, Wide128>(mQ, mKV, p, grid, q_box, joins, st);
 }
 
 int tile_tokens(int n_heads, int n_kv, int max_new) {
@@ -779,8 +805,7 @@ cudaError_t launch_tc_tree(const CUtensorMap& mQ, const CUtensorMap& mKV, const 
   const int q_box = tile_tokens(p.n_heads, p.n_kv, p.max_new), grid = CTAS_PER_SM * num_sms;
   Join* joins = reinterpret_cast<Join*>(reinterpret_cast<uint8_t*>(p.part) +
                                         ((part_floats(p.n_heads, p.n_kv, p.head_dim, p.max_new, num_sms) * 4 + 255) & ~size_t(255)));
-  if (p.head_dim == 128) return f16 ? launch_typed<true, 128>(mQ, mKV, p, grid, q_box, joins, st) : launch_typed<false, 128>(mQ, mKV, p, grid, q_box, joins, st);
-  return f16 ? launch_typed<true, 64>(mQ, mKV, p, grid, q_box, joins, st) : launch_typed<false, 64>(mQ, mKV, p, grid, q_box, joins, st);
+  return f16 ? launch_rows<true>(mQ, mKV, p, grid, q_box, joins, st) : launch_rows<false>(mQ, mKV, p, grid, q_box, joins, st);
 }
 
 }  // namespace seer
