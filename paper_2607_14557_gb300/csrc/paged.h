@@ -104,8 +104,9 @@ cudaError_t launch_tc_causal(const CUtensorMap& mQ, const CUtensorMap& mK, const
                              bool f16, int num_sms, cudaStream_t st);
 // 16-bit attention of new rows over the pages on the tensor cores.  mQ: as above with boxes of
 // tc_tree_box_tokens() rows; mKV: the pool as [rows][2 * n_kv][head_dim] in boxes of
-// min(128, page size) x 1 x 64.  p.part: tc_tree_part_bytes().
+// tc_tree_box_keys() x 1 x 64.  p.part: tc_tree_part_bytes().
 int tc_tree_box_tokens(int n_heads, int n_kv, int max_new);
+int tc_tree_box_keys(int n_heads, int n_kv, int head_dim, int max_new, int page_size);
 size_t tc_tree_part_bytes(int n_heads, int n_kv, int head_dim, int max_new, int num_sms);
 cudaError_t launch_tc_tree(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, bool f16, int num_sms,
                            cudaStream_t st);

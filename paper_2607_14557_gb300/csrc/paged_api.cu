@@ -323,7 +323,7 @@ seer_status seer_attention_tree(const void* q, int ld_q, void* o, int ld_o, seer
     CUtensorMap mq, mkv;
     SEER_TRY(map_heads(&mq, q, dt, T_cap, ld_q, n_heads, pg.head_dim, tc_tree_box_tokens(n_heads, pg.n_kv, max_draft), g));
     SEER_TRY(map_heads(&mkv, pg.kv, dt, static_cast<long>(pg.n_pages) << pg.page_shift, p.ld_k, 2 * pg.n_kv, pg.head_dim,
-                       page < 128 ? page : 128, 1));
+                       tc_tree_box_keys(n_heads, pg.n_kv, pg.head_dim, max_draft, page), 1));
     Phase ph(PH_ATTN, st);
     SEER_CUDA(launch_tc_tree(mq, mkv, p, dt == SEER_F16, di->num_sms, st), "tree attention launch");
     return SEER_OK;

@@ -137,7 +137,6 @@ template <bool F16, int DH>
 __global__ void __launch_bounds__(THREADS, 1)
     tc_causal_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mK,
                      const __grid_constant__ CUtensorMap mV, const GqaParams p) {
-  pdl_enter();
   using Lay = Layout<DH>;
   constexpr int TILE = Lay::TILE, PANELS = DH / 64;
   extern __shared__ uint8_t smem_raw[];
@@ -168,7 +167,11 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int lane = threadIdx.x & 31;
   const int G = p.n_heads / p.n_kv, TPT = BQ / G;
 
+  // barriers and tensor memory, before the kernels ahead are waited for
   if (threadIdx.x == 0) {
+    tma_prefetch_desc(&mQ);
+    tma_prefetch_desc(&mK);
+    tma_prefetch_desc(&mV);
     mbar_init(q_full, 1);
     mbar_init(q_empty, NT);
     for (int i = 0; i < STAGES; ++i) {
@@ -194,6 +197,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
+  pdl_enter();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -259,12 +263,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (warp == 0) {
     // -------------------------------------------------- TMA producer
     const bool leader = elect_one();
-    if (leader) {
-      tma_prefetch_desc(&mQ);
-      tma_prefetch_desc(&mK);
-      tma_prefetch_desc(&mV);
-    }
-    __syncwarp();
     int q_issued = 0, k_issued = 0, v_issued = 0;
     bool ok = true;
     for (int i = 0; ok; ++i) {
@@ -563,26 +561,30 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (valid_row) nonfinite |= recompute_row<F16, DH>(p, u.seq0, tok, head, u.kvh);
         __syncwarp();
       } else {
-        uint16_t* orow = static_cast<uint16_t*>(p.o) + (valid_row ? static_cast<size_t>(u.seq0 + tok) * p.ld_o + head * DH : 0);
+        RowStore store;
+        store.set(p.o, static_cast<long long>(u.seq0 + tok) * p.ld_o + head * DH, valid_row, lane);
+        uint32_t top = 0;
 #pragma unroll 1
         for (int cc = 0; cc < DH / 32; ++cc) {
           uint32_t rr[32];
           tmem_ld32(tO + 32 * cc, rr);
           tmem_ld_wait();
-          if (valid_row) {
-            uint4* dst = reinterpret_cast<uint4*>(orow + 32 * cc);
+          uint4 v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t q[4];
+          for (int e = 0; e < 4; ++e) {
+            uint32_t q[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                q[k] = pack2(__uint_as_float(rr[8 * e + 2 * k]) * inv_l, __uint_as_float(rr[8 * e + 2 * k + 1]) * inv_l, F16);
-                nonfinite |= nonfinite_term(q[k], F16);
-              }
-              dst[e] = make_uint4(q[0], q[1], q[2], q[3]);
+            for (int k = 0; k < 4; ++k) {
+              float x0, x1;
+              ffma2(__uint_as_float(rr[8 * e + 2 * k]), __uint_as_float(rr[8 * e + 2 * k + 1]), inv_l, inv_l, 0.f, 0.f, x0, x1);
+              q[k] = pack2(x0, x1, F16);
+              top = max_abs2<F16>(top, q[k]);
             }
+            v[e] = make_uint4(q[0], q[1], q[2], q[3]);
           }
+          store.put(v, 32 * cc, lane);
         }
+        if (valid_row) nonfinite |= nonfinite_term(top, F16);
       }
       tc_fence_before();
       __syncwarp();

@@ -48,23 +48,29 @@ constexpr int U_READERS = 1 + 4;            // issuer, softmax warps
 // value tiles in turn.  The MMA reads 128 rows from a Q buffer; those past QROWS are other
 // bytes of this memory, in rows of S that nobody looks at.  Few rows leave room for a third
 // slot and a second Q buffer, so that loads go on across a tile's softmax and from piece to
-// piece.
+// piece.  Where Q fills 32 KB the ring is one key slot and three halves of value tiles (64
+// keys; SLOTS = 0): half of the next V is under way before this V is used up.
 template <int DH_, int SLOTS_, int QB_, int QROWS_>
 struct Config {
   static constexpr int DH = DH_, SLOTS = SLOTS_, QB = QB_, QROWS = QROWS_;
+  static constexpr bool HALVES = SLOTS == 0;
+  static constexpr int BARS = HALVES ? 4 : SLOTS;         // K, then the halves; or the slots
   static constexpr int TILE = 128 * DH * 2;
+  static constexpr int V_PANEL = HALVES ? PANEL / 2 : PANEL;   // 64 columns of a V tile or half
   static constexpr int Q_PANEL = QROWS * 128, Q_BYTES = DH / 64 * Q_PANEL;
   static constexpr int OFF_RING = QB * Q_BYTES;
-  static constexpr int OFF_BAR = OFF_RING + SLOTS * TILE;
-  static constexpr int BYTES = OFF_BAR + BAR_BYTES + 1024;
+  static constexpr int RING = HALVES ? TILE + 3 * TILE / 2 : SLOTS * TILE;
+  static constexpr int OFF_BAR = OFF_RING + RING;
+  static constexpr int BOX = HALVES ? 64 : 128;           // most rows of a box of the pool
+  static constexpr int BYTES = OFF_BAR + BAR_BYTES;
   static_assert(Q_PANEL % 1024 == 0, "the 128-byte swizzle repeats every 8 rows");
   static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two CTAs per SM");
-  static_assert(Q_BYTES * QB + SLOTS * TILE >= (QB - 1) * Q_BYTES + (DH / 64 - 1) * Q_PANEL + PANEL, "128 rows from any Q panel");
+  static_assert(Q_BYTES * QB + RING >= (QB - 1) * Q_BYTES + (DH / 64 - 1) * Q_PANEL + PANEL, "128 rows from any Q panel");
 };
 using Wide64 = Config<64, 4, 2, 128>;
 using Few128 = Config<128, 3, 2, 24>;
 using Some128 = Config<128, 3, 1, 48>;
-using Wide128 = Config<128, 2, 1, 128>;
+using Wide128 = Config<128, 0, 1, 128>;
 
 // A piece: keys [tile0 * 128, tile1 * 128) of a unit.  n < 0: no more pieces.
 struct Piece {
@@ -137,11 +143,15 @@ __device__ __forceinline__ uint64_t visible(const GqaParams& p, const Piece& u, 
 }
 
 // Where a row's result goes: the output, divided by its weight, or its partial slot.
+// A slot holds the sums as [column / 4][row] float4, so that a warp stores 512 bytes in one
+// piece (a row's 512 bytes one after the other took 2 us for 128 rows), then each row's
+// (max, weight).
 template <bool F16, int DH>
 struct RowOut {
   uint16_t* o = nullptr;
-  float* part = nullptr;
-  float* stats = nullptr;                   // (max, weight)
+  float4* part = nullptr;                   // the row's first float4; the next is `rows` on
+  float2* stats = nullptr;
+  int rows = 0;
 };
 template <bool F16, int DH>
 __device__ __forceinline__ RowOut<F16, DH> row_out(const GqaParams& p, const Piece& u, int tok, int head, int r, int rows) {
@@ -149,9 +159,10 @@ __device__ __forceinline__ RowOut<F16, DH> row_out(const GqaParams& p, const Pie
   if (u.part < 0) {
     w.o = static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.q0 + tok) * p.ld_o + head * DH;
   } else {
-    float* slot = p.part + static_cast<size_t>(u.part) * rows * (DH + 4);   // rows x DH sums, (max, weight) each, 16-byte multiples
-    w.part = slot + r * DH;
-    w.stats = slot + rows * DH + 2 * r;
+    float* slot = p.part + static_cast<size_t>(u.part) * rows * (DH + 4);
+    w.part = reinterpret_cast<float4*>(slot) + r;
+    w.stats = reinterpret_cast<float2*>(slot + rows * DH) + r;
+    w.rows = rows;
   }
   return w;
 }
@@ -159,8 +170,8 @@ __device__ __forceinline__ RowOut<F16, DH> row_out(const GqaParams& p, const Pie
 template <bool F16, int DH>
 __device__ __forceinline__ uint32_t store8(const RowOut<F16, DH>& w, int c, const float (&v)[8], float inv) {
   if (w.o == nullptr) {
-    *reinterpret_cast<float4*>(w.part + c) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4*>(w.part + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    w.part[(c / 4) * w.rows] = make_float4(v[0], v[1], v[2], v[3]);
+    w.part[(c / 4 + 1) * w.rows] = make_float4(v[4], v[5], v[6], v[7]);
     return 0;
   }
   uint32_t q[4], bad = 0;
@@ -223,17 +234,22 @@ __device__ __noinline__ uint32_t recompute_row(const GqaParams& p, const Piece* 
     }
     bad |= store8<F16, DH>(out, c, acc, l == 0.f ? 0.f : 1.f / l);
   }
-  if (out.stats) *reinterpret_cast<float2*>(out.stats) = make_float2(m, l);
+  if (out.stats) *out.stats = make_float2(m, l);
   return bad;
 }
 
 template <bool F16, typename Cfg>
 __global__ void __launch_bounds__(THREADS, 2)
     tc_tree_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mKV, const GqaParams p,
-                   const int q_box, const int min_places, Join* __restrict__ joins) {
-  constexpr int DH = Cfg::DH, TILE = Cfg::TILE, PANELS = DH / 64, SLOTS = Cfg::SLOTS, QB = Cfg::QB;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+                   const int q_box, Join* __restrict__ joins) {
+  constexpr int DH = Cfg::DH, TILE = Cfg::TILE, PANELS = DH / 64, QB = Cfg::QB;
+  constexpr int SLOTS = Cfg::HALVES ? 1 : Cfg::SLOTS;
+  extern __shared__ __align__(1024) uint8_t smem[];       // all of the CTA's shared memory, so it starts aligned
+  if ((smem_u32(smem) & 1023u) != 0) {
+    pdl_enter();
+    if (threadIdx.x == 0) record_error(p.err, kErrLayout);
+    return;
+  }
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Cfg::OFF_BAR);
   uint64_t* s_full = bars + 0;
   uint64_t* p_full = bars + 1;
@@ -242,20 +258,48 @@ __global__ void __launch_bounds__(THREADS, 2)
   uint64_t* o_free = bars + 4;
   uint64_t* q_full = bars + 5;               // [QB]
   uint64_t* q_empty = q_full + QB;           // [QB]
-  uint64_t* r_full = q_empty + QB;           // [SLOTS] tile 2 g (K) or 2 g + 1 (V) of this CTA's g-th key tile
-  uint64_t* r_empty = r_full + SLOTS;
-  uint64_t* u_full = r_empty + SLOTS;        // [U_SLOTS]
+  uint64_t* r_full = q_empty + QB;           // [BARS] ring
+  uint64_t* r_empty = r_full + Cfg::BARS;
+  uint64_t* u_full = r_empty + Cfg::BARS;    // [U_SLOTS]
   uint64_t* u_empty = u_full + U_SLOTS;      // [U_SLOTS]
   Piece* ring = reinterpret_cast<Piece*>(u_empty + U_SLOTS);     // [U_SLOTS]
   volatile int* odd = reinterpret_cast<volatile int*>(ring + U_SLOTS);   // [4], as in tc_causal.cu
   uint32_t* tmem_slot = const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(odd + 4));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert(8 * (5 + 2 * QB + 2 * SLOTS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 <= BAR_BYTES, "barrier block");
+  struct Start {                             // where this CTA's run begins
+    long long warp_sum[THREADS / 32];
+    long long off;
+    Request r;
+    int b;
+  };
+  constexpr int START_AT = (8 * (5 + 2 * QB + 2 * Cfg::BARS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 + 7) & ~7;
+  static_assert(START_AT + sizeof(Start) <= BAR_BYTES, "barrier block");
+  Start& start = *reinterpret_cast<Start*>(smem + Cfg::OFF_BAR + START_AT);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = p.n_heads / p.n_kv, TPT = BQ / G;
   const int part_rows = min(TPT, p.max_new) * G;          // rows of a partial slot
   const int extra = unit_extra(part_rows);
+
+  // Places of the ring.  Of this CTA's g-th key tile, K is ring tile 2 g and V 2 g + 1 (slot
+  // x % SLOTS, used x / SLOTS times before); in halves, K is always slot 0 and half h of V is
+  // half slot (2 g + h) % 3.
+  struct Place {
+    int bar, off;
+    unsigned use;
+  };
+  const auto k_place = [](unsigned g) {
+    if (Cfg::HALVES) return Place{0, Cfg::OFF_RING, g};
+    return Place{static_cast<int>(2 * g % SLOTS), Cfg::OFF_RING + static_cast<int>(2 * g % SLOTS) * TILE, 2 * g / SLOTS};
+  };
+  const auto v_place = [](unsigned g, int h) {            // half h; of whole tiles, where half h begins
+    if (Cfg::HALVES) {
+      const unsigned x = 2 * g + h;
+      return Place{1 + static_cast<int>(x % 3), Cfg::OFF_RING + TILE + static_cast<int>(x % 3) * (TILE / 2), x / 3};
+    }
+    const unsigned x = 2 * g + 1;
+    return Place{static_cast<int>(x % SLOTS), Cfg::OFF_RING + static_cast<int>(x % SLOTS) * TILE + h * 8192, x / SLOTS};
+  };
 
   // barriers and tensor memory, before the kernels ahead are waited for
   if (threadIdx.x == 0) {
@@ -268,7 +312,7 @@ __global__ void __launch_bounds__(THREADS, 2)
       mbar_init(&q_full[i], 1);
       mbar_init(&q_empty[i], 1);
     }
-    for (int i = 0; i < SLOTS; ++i) {
+    for (int i = 0; i < Cfg::BARS; ++i) {
       mbar_init(&r_full[i], 1);
       mbar_init(&r_empty[i], 1);
     }
@@ -286,10 +330,6 @@ __global__ void __launch_bounds__(THREADS, 2)
   pdl_enter();
 
   // ---- the line of key tiles: its length and the request where this CTA's run begins
-  __shared__ long long warp_sum[THREADS / 32];
-  __shared__ long long start_off;
-  __shared__ int start_b;
-  __shared__ Request start_r;
   const int chunk = (p.B + THREADS - 1) / THREADS;
   const int b_lo = min(p.B, static_cast<int>(threadIdx.x) * chunk), b_hi = min(p.B, b_lo + chunk);
   long long mine = 0;
@@ -304,16 +344,17 @@ __global__ void __launch_bounds__(THREADS, 2)
     const long long v = __shfl_up_sync(0xffffffffu, inc, off);
     if (lane >= off) inc += v;
   }
-  if (lane == 31) warp_sum[warp] = inc;
+  if (lane == 31) start.warp_sum[warp] = inc;
   __syncthreads();
   long long before = inc - mine, total = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
-    before += w < warp ? warp_sum[w] : 0;
-    total += warp_sum[w];
+    before += w < warp ? start.warp_sum[w] : 0;
+    total += start.warp_sum[w];
   }
   const int grid = gridDim.x, c = blockIdx.x;
-  const int runs = total < static_cast<long long>(grid) * min_places ? quotient(total + min_places - 1, min_places) : grid;
+  const int least = extra + 1;                            // places of a run
+  const int runs = total < static_cast<long long>(grid) * least ? quotient(total + least - 1, least) : grid;
   const bool idle = c >= runs;                            // the whole CTA
   const long long run0 = idle ? 0 : cut(total, c, runs), run1 = idle ? 0 : cut(total, c + 1, runs);
   if (!idle && mine > 0 && run0 >= before && run0 < before + mine) {
@@ -322,9 +363,9 @@ __global__ void __launch_bounds__(THREADS, 2)
       const Request r = read_request(p, b);
       const long long n = line_length(p, r, TPT, extra);
       if (run0 < at + n) {
-        start_b = b;
-        start_off = run0 - at;
-        start_r = r;
+        start.b = b;
+        start.off = run0 - at;
+        start.r = r;
         break;
       }
       at += n;
@@ -340,14 +381,14 @@ __global__ void __launch_bounds__(THREADS, 2)
   } else if (warp == 0) {
     // -------------------------------------------------- producer
     const bool leader = elect_one();
-    const int box_rows = min(BKV, 1 << p.page_shift), boxes = BKV / box_rows;
+    const int box_rows = min(Cfg::BOX, 1 << p.page_shift), boxes = BKV / box_rows;
     const int out_of_pool = p.n_pages << p.page_shift;    // a row that the tensor map fills with zeros
-    unsigned loaded = 0;                                  // ring tiles issued
+    unsigned g = 0;                                       // key tiles loaded
     int pieces = 0;
     bool ok = true;
-    int b = start_b;
-    long long off = start_off, at = run0;
-    Request r = start_r;                                  // request b
+    int b = start.b;
+    long long off = start.off, at = run0;
+    Request r = start.r;                                  // request b
     int window = b - 32;                                  // requests window .. window + 31 in the lanes' registers
     Request ahead{};
     Join join{};
@@ -362,17 +403,18 @@ __global__ void __launch_bounds__(THREADS, 2)
       }
       return (page << p.page_shift) + (key & ((1 << p.page_shift) - 1));
     };
-    // a ring tile of this lane's box, columns of head `head` of the row's 2 n_kv
-    const auto load = [&](int row, int head, int bytes) {
-      const unsigned s = loaded % SLOTS, use = loaded / SLOTS;
-      if (use > 0 && !warp_wait(&r_empty[s], (use - 1) & 1, abort_flag, p.err)) return false;
-      if (leader) mbar_arrive_expect_tx(&r_full[s], bytes);
+    // Lanes `mine` load their box (row >= 0), columns of head `head` of the row's 2 n_kv, to
+    // `place`, whose first row is key `key0` of the tile.
+    const auto load = [&](const Place& at_place, int row, bool mine_box, int key0, int head, int panel) {
+      const bool go = mine_box && row >= 0;
+      const int bytes = __popc(__ballot_sync(0xffffffffu, go)) * box_rows * 128 * PANELS;
+      if (at_place.use > 0 && !warp_wait(&r_empty[at_place.bar], (at_place.use - 1) & 1, abort_flag, p.err)) return false;
+      if (leader) mbar_arrive_expect_tx(&r_full[at_place.bar], bytes);
       __syncwarp();
-      if (row >= 0)
+      if (go)
         for (int x = 0; x < PANELS; ++x)
-          tma_load_3d(smem + Cfg::OFF_RING + s * TILE + x * PANEL + lane * box_rows * 128, &mKV, &r_full[s], 64 * x, head, row);
+          tma_load_3d(smem + at_place.off + x * panel + (lane * box_rows - key0) * 128, &mKV, &r_full[at_place.bar], 64 * x, head, row);
       __syncwarp();
-      ++loaded;
       return true;
     };
     for (int i = 0; ok; ++i) {
@@ -437,19 +479,26 @@ __global__ void __launch_bounds__(THREADS, 2)
       for (int j = u.tile0; j < u.tile1; ++j) {
         const int row = next_row;
         if (j + 1 < u.tile1) next_row = box_row(u.b, u.kv, j + 1);
-        const int bytes = __popc(__ballot_sync(0xffffffffu, row >= 0)) * box_rows * 128 * PANELS;
-        if (!load(row, u.kvh, bytes) || !load(row, p.n_kv + u.kvh, bytes)) {
-          ok = false;
-          break;
+        ok = load(k_place(g), row, true, 0, u.kvh, PANEL);
+        if (Cfg::HALVES) {
+          const bool high = lane * box_rows >= BKV / 2;
+          ok = ok && load(v_place(g, 0), row, !high, 0, p.n_kv + u.kvh, Cfg::V_PANEL) &&
+               load(v_place(g, 1), row, high, BKV / 2, p.n_kv + u.kvh, Cfg::V_PANEL);
+        } else {
+          ok = ok && load(v_place(g, 0), row, true, 0, p.n_kv + u.kvh, Cfg::V_PANEL);
         }
+        if (!ok) break;
+        ++g;
       }
     }
     if (lane == 0) joins[c] = join;
     if (*abort_flag && leader) {
       // let copies still in flight land before the CTA's shared memory is released
       for (int j = max(pieces - QB, 0); j < pieces; ++j) mbar_wait_drain(&q_full[j % QB], (j / QB) & 1, 200000000ull);
-      for (unsigned j = loaded > SLOTS ? loaded - SLOTS : 0; j < loaded; ++j)
-        mbar_wait_drain(&r_full[j % SLOTS], (j / SLOTS) & 1, 200000000ull);
+      for (unsigned j = g > 2 ? g - 3 : 0; j <= g; ++j) { // (waits on tiles that were not issued run out)
+        mbar_wait_drain(&r_full[k_place(j).bar], k_place(j).use & 1, 20000000ull);
+        for (int h = 0; h < 2; ++h) mbar_wait_drain(&r_full[v_place(j, h).bar], v_place(j, h).use & 1, 20000000ull);
+      }
     }
   } else if (warp == 1) {
     // -------------------------------------------------- MMA issuer
@@ -457,15 +506,15 @@ __global__ void __launch_bounds__(THREADS, 2)
     constexpr uint32_t idesc_qk = make_idesc(BQ, BKV, 0, F16);
     constexpr uint32_t idesc_pv = make_idesc(BQ, DH, 1, F16);
     const uint64_t dq0 = make_sdesc_sw128(smem_u32(smem), 16, 1024);
-    const uint64_t dk0 = make_sdesc_sw128(smem_u32(smem + Cfg::OFF_RING), 16, 1024);
-    const uint64_t dv0 = make_sdesc_sw128(smem_u32(smem + Cfg::OFF_RING), PANEL, 1024);
+    const uint64_t dk0 = make_sdesc_sw128(smem_u32(smem), 16, 1024);
+    const uint64_t dv0 = make_sdesc_sw128(smem_u32(smem), Cfg::V_PANEL, 1024);
     const uint32_t dS = tmem, dO = tmem + TM_O;
     unsigned g = 0;                                       // key tiles begun
-    auto full = [&](unsigned x) { return warp_wait(&r_full[x % SLOTS], (x / SLOTS) & 1u, abort_flag, p.err); };
+    auto full = [&](const Place& x) { return warp_wait(&r_full[x.bar], x.use & 1u, abort_flag, p.err); };
     auto qk = [&](int qs, bool last) {
       if (leader) {
-        const unsigned st = 2 * g % SLOTS;
-        const uint64_t dk = dk0 + static_cast<uint64_t>(st * (TILE >> 4));
+        const Place at = k_place(g);
+        const uint64_t dk = dk0 + static_cast<uint64_t>(at.off >> 4);
         const uint64_t dq = dq0 + static_cast<uint64_t>(qs * (Cfg::Q_BYTES >> 4));
 #pragma unroll
         for (int k = 0; k < DH / 16; ++k) {
@@ -474,21 +523,20 @@ __global__ void __launch_bounds__(THREADS, 2)
           tc_mma_f16(dS, dq + oq, dk + ok, idesc_qk, k > 0 ? 1u : 0u);
         }
         tc_commit(s_full);
-        tc_commit(&r_empty[st]);
+        tc_commit(&r_empty[at.bar]);
         if (last) tc_commit(&q_empty[qs]);
       }
       __syncwarp();
       ++g;
     };
-    auto pv = [&](unsigned x, bool fresh, int half) {
+    auto pv = [&](const Place& at, bool fresh, int half) {   // half of the tile's 128 keys
       if (leader) {
-        const uint64_t dv = dv0 + static_cast<uint64_t>(x % SLOTS * (TILE >> 4));
+        const uint64_t dv = dv0 + static_cast<uint64_t>(at.off >> 4);
 #pragma unroll
-        for (int kk = 0; kk < BKV / 32; ++kk) {
-          const int k = half * (BKV / 32) + kk;
-          tc_mma_f16_tmem_a(dO, dS + 8 * k, dv + static_cast<uint64_t>(k * 128), idesc_pv, (!fresh || k > 0) ? 1u : 0u);
-        }
-        if (half == 1) tc_commit(&r_empty[x % SLOTS]);
+        for (int kk = 0; kk < BKV / 32; ++kk)
+          tc_mma_f16_tmem_a(dO, dS + 8 * (half * (BKV / 32) + kk), dv + static_cast<uint64_t>(kk * 128), idesc_pv,
+                            (!fresh || half > 0 || kk > 0) ? 1u : 0u);
+        if (half == 1 || Cfg::HALVES) tc_commit(&r_empty[at.bar]);
       }
       __syncwarp();
     };
@@ -498,26 +546,27 @@ __global__ void __launch_bounds__(THREADS, 2)
       if (u == nullptr) break;
       const int tiles = u->tile1 - u->tile0, qs = i % QB;
       release_piece(u_empty, i, lane);
-      if (!warp_wait(&q_full[qs], (i / QB) & 1, abort_flag, p.err) || !full(2 * g)) break;
+      if (!warp_wait(&q_full[qs], (i / QB) & 1, abort_flag, p.err) || !full(k_place(g))) break;
       tc_fence_after();
       qk(qs, tiles == 1);
       for (int j = 0; j < tiles; ++j) {
-        const unsigned v = 2 * g - 1, pc = (g - 1) & 1u;  // V of the tile whose scores were issued last
+        const unsigned pc = (g - 1) & 1u;                 // the tile whose scores were issued last
+        const Place v0 = v_place(g - 1, 0), v1 = v_place(g - 1, 1);
         if ((j == 0 && i > 0 && !warp_wait(o_free, (i - 1) & 1u, abort_flag, p.err)) ||   // the piece before is read out
-            !full(v) || !warp_wait(p_full, pc, abort_flag, p.err)) {
+            !full(v0) || !warp_wait(p_full, pc, abort_flag, p.err)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        pv(v, j == 0, 0);
-        if (!warp_wait(p_full2, pc, abort_flag, p.err)) {
+        pv(v0, j == 0, 0);
+        if ((Cfg::HALVES && !full(v1)) || !warp_wait(p_full2, pc, abort_flag, p.err)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        pv(v, j == 0, 1);
+        pv(v1, j == 0, 1);
         if (j + 1 < tiles) {
-          if (!full(2 * g)) {
+          if (!full(k_place(g))) {
             ok = false;
             break;
           }
@@ -634,24 +683,29 @@ __global__ void __launch_bounds__(THREADS, 2)
               }
             }
             if (masked) {
-              const unsigned vx = 2 * g + 1;
-              if (!__all_sync(0xffffffffu, mbar_wait(&r_full[vx % SLOTS], (vx / SLOTS) & 1u, abort_flag, p.err))) {
-                ok = false;
-                break;
-              }
               const int valid = u->kv - j * BKV;
-              uint4* v = reinterpret_cast<uint4*>(smem + Cfg::OFF_RING + vx % SLOTS * TILE);
               uint32_t bad = 0;
+#pragma unroll 1
+              for (int h = 0; h < (Cfg::HALVES ? 2 : 1); ++h) {
+                const Place at = v_place(g, h);
+                if (!__all_sync(0xffffffffu, mbar_wait(&r_full[at.bar], at.use & 1u, abort_flag, p.err))) {
+                  ok = false;
+                  break;
+                }
+                uint4* v = reinterpret_cast<uint4*>(smem + at.off);
+                constexpr int KEYS = Cfg::HALVES ? 64 : 128;
 #pragma unroll 4
-              for (int x = r; x < TILE / 16; x += 128) {
-                if (((x >> 3) & 127) < valid) {
-                  const uint4 w = v[x];
-                  bad |= nonfinite_term(w.x, F16) | nonfinite_term(w.y, F16) | nonfinite_term(w.z, F16) |
-                         nonfinite_term(w.w, F16);
-                } else {
-                  v[x] = make_uint4(0, 0, 0, 0);
+                for (int x = r; x < KEYS * DH / 8; x += 128) {   // 16 bytes: 8 to a key of a panel
+                  if (((x >> 3) & (KEYS - 1)) + h * KEYS < valid) {
+                    const uint4 w = v[x];
+                    bad |= nonfinite_term(w.x, F16) | nonfinite_term(w.y, F16) | nonfinite_term(w.z, F16) |
+                           nonfinite_term(w.w, F16);
+                  } else {
+                    v[x] = make_uint4(0, 0, 0, 0);
+                  }
                 }
               }
+              if (!ok) break;
               if (bad & 0x80008000u) odd[i & 3] = i + 1;
               fence_proxy_async_smem();
             }
@@ -690,7 +744,7 @@ __global__ void __launch_bounds__(THREADS, 2)
             }
           }
         }
-        if (valid_row && out.stats) *reinterpret_cast<float2*>(out.stats) = make_float2(m_ref, l);
+        if (valid_row && out.stats) *out.stats = make_float2(m_ref, l);
       }
       tc_fence_before();
       release_piece(u_empty, i, lane);
@@ -707,60 +761,59 @@ __global__ void __launch_bounds__(THREADS, 2)
   }
 }
 
-// Joins the pieces of the unit that begins in run blockIdx.x and ends in a later one: a warp per
-// row, its pieces' sums weighted by 2^(max - largest max), in order of their keys.
-constexpr int MERGE_WARPS = 8;
+// Joins the pieces of the unit that begins in run blockIdx.x and ends in a later one, in order
+// of their keys: sums and weights relative to a running maximum, so that a piece's numbers
+// are read once and several pieces' reads are under way.  A thread takes 8 columns of one of
+// 32 rows of the tile; fewer rows sit side by side.
+constexpr int MERGE_THREADS = 512;
 
 template <bool F16, int DH>
-__global__ void __launch_bounds__(32 * MERGE_WARPS) tree_merge_kernel(const GqaParams p, const Join* __restrict__ joins) {
+__global__ void __launch_bounds__(MERGE_THREADS) tree_merge_kernel(const GqaParams p, const Join* __restrict__ joins) {
+  const int G = p.n_heads / p.n_kv, TPT = BQ / G, part_rows = min(TPT, p.max_new) * G;
   pdl_enter();
   const Join u = joins[blockIdx.x];
-  if (u.n == 0) return;
-  const int G = p.n_heads / p.n_kv, TPT = BQ / G, part_rows = min(TPT, p.max_new) * G;
-  const int rows = min(TPT, u.n - u.tok0) * G, lane = threadIdx.x & 31;
-  constexpr int COLS = DH / 32;                           // columns of a lane
-  const size_t stride = static_cast<size_t>(part_rows) * (DH + 4);
+  const int rows = min(TPT, u.n - u.tok0) * G, row0 = blockIdx.y * 32;
+  if (u.n == 0 || row0 >= rows) return;
+  const int side = rows - row0 > 16 ? 32 : (rows - row0 > 8 ? 16 : (rows - row0 > 4 ? 8 : 4));
+  const int r = row0 + (threadIdx.x & (side - 1));
   uint32_t nonfinite = 0;
-  for (int r = blockIdx.y * MERGE_WARPS + (threadIdx.x >> 5); r < rows; r += gridDim.y * MERGE_WARPS) {
-    float top = -INFINITY;
-    for (int c = u.first + lane; c <= u.last; c += 32)
-      top = fmaxf(top, p.part[(2 * c + (c == u.first)) * stride + part_rows * DH + 2 * r]);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, acc[COLS] = {};
+  if (r < rows) {
+    const size_t stride = static_cast<size_t>(part_rows) * (DH + 4);
+    const float* slot0 = p.part + (2 * u.first + 1) * stride;          // the unit's first piece
+    const float* slots = p.part + 2 * (u.first + 1) * stride;          // the next ones, 2 slots apart
+    const int more = u.last - u.first;
+    const size_t orow = static_cast<size_t>(u.q0 + u.tok0 + r / G) * p.ld_o + (u.kvh * G + r % G) * DH;
+    for (int col = threadIdx.x / side * 8; col < DH; col += MERGE_THREADS / side * 8) {
+      float m = -INFINITY, sum = 0.f, acc[8] = {};
 #pragma unroll 4
-    for (int c = u.first; c <= u.last; ++c) {
-      const float* slot = p.part + (2 * c + (c == u.first)) * stride;
-      const float2 ml = *reinterpret_cast<const float2*>(slot + part_rows * DH + 2 * r);
-      const float w = ml.y == 0.f ? 0.f : ex2(ml.x - base);
-      sum += ml.y * w;
-      float v[COLS];
-      if (COLS == 4) {
-        const float4 f = *reinterpret_cast<const float4*>(slot + r * DH + 4 * lane);
-        v[0] = f.x, v[1] = f.y, v[2 % COLS] = f.z, v[3 % COLS] = f.w;
-      } else {
-        const float2 f = *reinterpret_cast<const float2*>(slot + r * DH + 2 * lane);
-        v[0] = f.x, v[1] = f.y;
+      for (int c = 0; c <= more; ++c) {
+        const float* slot = c == 0 ? slot0 : slots + 2 * (c - 1) * stride;
+        const float2 ml = reinterpret_cast<const float2*>(slot + part_rows * DH)[r];
+        const float4* v = reinterpret_cast<const float4*>(slot) + col / 4 * part_rows + r;
+        const float4 a = v[0], b = v[part_rows];
+        if (ml.y == 0.f) continue;                        // a piece without a seen key adds nothing
+        const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.f : top;
+        const float old = ex2(m - base), w = ex2(ml.x - base);
+        m = top;
+        sum = fmaf(sum, old, ml.y * w);
+        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = fmaf(acc[e], old, w * f[e]);
       }
-      if (w != 0.f)                                       // a piece without a seen key adds nothing
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      uint32_t q[4];
 #pragma unroll
-        for (int e = 0; e < COLS; ++e) acc[e] = fmaf(w, v[e], acc[e]);
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    uint16_t* o = static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.q0 + u.tok0 + r / G) * p.ld_o + (u.kvh * G + r % G) * DH;
-#pragma unroll
-    for (int e = 0; e < COLS / 2; ++e) {
-      const uint32_t w = pack2(acc[2 * e] * inv, acc[2 * e + 1] * inv, F16);
-      nonfinite |= nonfinite_term(w, F16);
-      reinterpret_cast<uint32_t*>(o)[COLS / 2 * lane + e] = w;
+      for (int e = 0; e < 4; ++e) {
+        q[e] = pack2(acc[2 * e] * inv, acc[2 * e + 1] * inv, F16);
+        nonfinite |= nonfinite_term(q[e], F16);
+      }
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + orow + col) = make_uint4(q[0], q[1], q[2], q[3]);
     }
   }
   report_range(nonfinite, p.err);
 }
 
 constexpr int CTAS_PER_SM = 2;
-constexpr int MIN_PLACES = 3;               // places of a run at least
 
 template <bool F16, typename Cfg>
 cudaError_t launch_typed(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, int grid, int q_box, Join* joins,
@@ -768,11 +821,11 @@ cudaError_t launch_typed(const CUtensorMap& mQ, const CUtensorMap& mKV, const Gq
   static bool attr_set[64] = {};
   cudaError_t e = set_smem_limit_once(tc_tree_kernel<F16, Cfg>, Cfg::BYTES, attr_set);
   if (e != cudaSuccess) return e;
-  e = launch_kernel(tc_tree_kernel<F16, Cfg>, dim3(grid), dim3(THREADS), Cfg::BYTES, st, mQ, mKV, p, q_box, MIN_PLACES, joins);
+  e = launch_kernel(tc_tree_kernel<F16, Cfg>, dim3(grid), dim3(THREADS), Cfg::BYTES, st, mQ, mKV, p, q_box, joins);
   if (e != cudaSuccess) return e;
   const int rows = q_box * (p.n_heads / p.n_kv);
-  return launch_kernel(tree_merge_kernel<F16, Cfg::DH>, dim3(grid, (rows + 4 * MERGE_WARPS - 1) / (4 * MERGE_WARPS)),
-                       dim3(32 * MERGE_WARPS), 0, st, p, static_cast<const Join*>(joins));
+  return launch_kernel(tree_merge_kernel<F16, Cfg::DH>, dim3(grid, (rows + 31) / 32), dim3(MERGE_THREADS), 0, st, p,
+                       static_cast<const Join*>(joins));
 }
 template <bool F16>
 cudaError_t launch_rows(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, int grid, int q_box, Join* joins,
@@ -795,6 +848,11 @@ size_t part_floats(int n_heads, int n_kv, int head_dim, int max_new, int num_sms
 }  // namespace
 
 int tc_tree_box_tokens(int n_heads, int n_kv, int max_new) { return tile_tokens(n_heads, n_kv, max_new); }
+int tc_tree_box_keys(int n_heads, int n_kv, int head_dim, int max_new, int page_size) {
+  const int rows = tile_tokens(n_heads, n_kv, max_new) * (n_heads / n_kv);
+  const int most = head_dim == 128 && rows > Some128::QROWS ? Wide128::BOX : Few128::BOX;
+  return page_size < most ? page_size : most;
+}
 
 size_t tc_tree_part_bytes(int n_heads, int n_kv, int head_dim, int max_new, int num_sms) {
   return ((part_floats(n_heads, n_kv, head_dim, max_new, num_sms) * 4 + 255) & ~size_t(255)) +
