@@ -3,6 +3,7 @@
 Translation units compile in parallel into ``_build/`` and link into
 ``paper_2607_14557_gb300/libseer.so``.  The library links the shared CUDA
 runtime so it shares one runtime instance with PyTorch in the same process.
+``binding.cpp`` becomes the extension module ``_seer_binding`` beside it.
 """
 from __future__ import annotations
 
@@ -10,12 +11,14 @@ import concurrent.futures
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libseer.so")
+BINDING = os.path.join(PKG, "_seer_binding.so")
 SOURCES = ["seer_api.cu", "tc_gemm.cu", "tc_attn.cu", "simt.cu", "aux_kernels.cu", "seer_noalloc.cu", "paged_api.cu",
            "paged.cu", "gqa_simt.cu", "tc_causal.cu", "tc_tree.cu"]
 HEADERS = ["common.cuh", "kernels.h", "attn_schedule.cuh", "api.h", "paged.h", "attn_math.cuh"]
@@ -34,10 +37,10 @@ def _cuda_lib_dir(nv: str) -> str:
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(BINDING):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.join(ROOT, "include", "seer.h"), __file__]
+    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
+    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["binding.cpp"]] + [os.path.join(ROOT, "include", "seer.h"), __file__]
     return any(os.path.getmtime(p) > t for p in deps if os.path.exists(p))
 
 
@@ -62,8 +65,10 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
             print(r.stdout + r.stderr)
         return obj
 
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        binding = ex.submit(_compile_binding, nv)
         objs = list(ex.map(compile_one, SOURCES))
+        binding_obj = binding.result()
     tmp = LIB + ".tmp"
     libdir = _cuda_lib_dir(nv)
     cmd = [nv, *ARCH, "-shared", "-cudart", "shared", "-o", tmp, *objs, "-Xlinker", f"-rpath,{libdir}"]
@@ -71,7 +76,36 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    _link_binding(binding_obj)
     return LIB
+
+
+def _run(cmd, what):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what} failed:\n{r.stdout}\n{r.stderr}")
+
+
+def _compile_binding(nv: str) -> str:
+    import torch
+
+    inc = os.path.join(os.path.dirname(torch.__file__), "include")
+    obj = os.path.join(BUILD, "binding.o")
+    _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          "-I", inc, "-I", os.path.join(inc, "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
+          "-I", os.path.join(os.path.dirname(_cuda_lib_dir(nv)), "include"), "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj],
+         "compiling binding.cpp")
+    return obj
+
+
+def _link_binding(obj: str) -> None:
+    import torch
+
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = BINDING + ".tmp"
+    _run([os.environ.get("CXX", "g++"), "-shared", "-o", tmp, obj, "-L", PKG, "-l:libseer.so", "-L", lib, "-ltorch_python", "-lc10_cuda",
+          "-lc10", f"-Wl,-rpath,$ORIGIN:{lib}"], "linking the binding")
+    os.replace(tmp, BINDING)
 
 
 if __name__ == "__main__":

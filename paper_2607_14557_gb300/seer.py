@@ -276,16 +276,18 @@ def seer_attention_noalloc(qkv, o, dt, cu_seqlens, kv_len, B, T_capacity, n_head
 
 
 # ----------------------------------------------------------------- paged K/V cache
-def _dev(t, device, dtype=None):
-    """Address of a tensor (None, a raw address) that is on `device` and, when a
-    dtype is named, a contiguous array of it."""
-    if not isinstance(t, torch.Tensor):
-        return t
-    if not t.is_cuda or t.get_device() != device:
-        raise ValueError(f"a tensor on {t.device} is not on the current device cuda:{device}")
-    if dtype is not None and (t.dtype != dtype or not t.is_contiguous()):
-        raise ValueError(f"expected a contiguous {dtype} tensor, got {t.dtype} with strides {tuple(t.stride())}")
-    return t.data_ptr()
+# These go through the extension module _seer_binding: tensors have to be on the current
+# device, index arrays contiguous and of the type that the C entry reads (ValueError).
+_native_module = None
+
+
+def _native():
+    global _native_module
+    if _native_module is None:
+        lib()                                   # raises when nothing has been built
+        from . import _seer_binding
+        _native_module = _seer_binding
+    return _native_module
 
 
 def make_pages(kv, table, n_pages, page_size, max_pages, n_kv_heads, head_dim) -> seer_pages:
@@ -301,44 +303,32 @@ def make_pages(kv, table, n_pages, page_size, max_pages, n_kv_heads, head_dim) -
 def seer_page_tables(cached_len, new_len, B, page_size, n_pages, free_pages, n_free, free_head, table, max_pages, T_cap,
                      parent, cu_new_out, kv_len_out, slot_out, position_out, mask_out, free_head_out, stream=None):
     """mask_out: an int64 tensor (bit j of the 64 is new row j)."""
-    dev, i32 = torch.cuda.current_device(), torch.int32
-    _check(lib().seer_page_tables(_dev(cached_len, dev, i32), _dev(new_len, dev, i32), B, page_size, n_pages,
-                                  _dev(free_pages, dev, i32), n_free, _dev(free_head, dev, i32), _dev(table, dev, i32),
-                                  max_pages, T_cap, _dev(parent, dev, i32), _dev(cu_new_out, dev, i32),
-                                  _dev(kv_len_out, dev, i32), _dev(slot_out, dev, i32), _dev(position_out, dev, i32),
-                                  _dev(mask_out, dev, torch.int64), _dev(free_head_out, dev, i32), _stream(stream)))
+    _check(_native().seer_page_tables(cached_len, new_len, B, page_size, n_pages, free_pages, n_free, free_head, table,
+                                      max_pages, T_cap, parent, cu_new_out, kv_len_out, slot_out, position_out, mask_out,
+                                      free_head_out, stream))
 
 
 def seer_kv_append(qkv, ld_qkv, dt, n_heads, T_cap, M_dev, slot, position, theta, rotated, ld_rotated, pages,
                    stream=None):
-    dev, i32 = torch.cuda.current_device(), torch.int32
-    _check(lib().seer_kv_append(_dev(qkv, dev), ld_qkv, _dt(dt), n_heads, T_cap, _dev(M_dev, dev, i32),
-                                _dev(slot, dev, i32), _dev(position, dev, i32), theta, _dev(rotated, dev), ld_rotated,
-                                ctypes.byref(pages), _stream(stream)))
+    _check(_native().seer_kv_append(qkv, ld_qkv, _dt(dt), n_heads, T_cap, M_dev, slot, position, theta, rotated,
+                                    ld_rotated, pages, stream))
 
 
 def seer_kv_accept(dt, cached_len, accepted, n_accepted, B, max_draft, pages, len_out, stream=None):
-    dev, i32 = torch.cuda.current_device(), torch.int32
-    _check(lib().seer_kv_accept(_dt(dt), _dev(cached_len, dev, i32), _dev(accepted, dev, i32),
-                                _dev(n_accepted, dev, i32), B, max_draft, ctypes.byref(pages), _dev(len_out, dev, i32),
-                                _stream(stream)))
+    _check(_native().seer_kv_accept(_dt(dt), cached_len, accepted, n_accepted, B, max_draft, pages, len_out, stream))
 
 
 def seer_attention_causal(q, ld_q, k, ld_k, v, ld_v, o, ld_o, dt, cu_seqlens, B, T_cap, n_heads, n_kv_heads, head_dim,
                           stream=None):
-    dev = torch.cuda.current_device()
-    _check(lib().seer_attention_causal(_dev(q, dev), ld_q, _dev(k, dev), ld_k, _dev(v, dev), ld_v, _dev(o, dev), ld_o,
-                                       _dt(dt), _dev(cu_seqlens, dev, torch.int32), B, T_cap, n_heads, n_kv_heads,
-                                       head_dim, _stream(stream)))
+    _check(_native().seer_attention_causal(q, ld_q, k, ld_k, v, ld_v, o, ld_o, _dt(dt), cu_seqlens, B, T_cap, n_heads,
+                                           n_kv_heads, head_dim, stream))
 
 
 def seer_attention_tree(q, ld_q, o, ld_o, dt, cu_new, kv_len, mask, B, T_cap, n_heads, max_draft, pages, ws, ws_bytes,
                         stream=None):
     """mask: an int64 tensor as from seer_page_tables, or None (causal)."""
-    dev, i32 = torch.cuda.current_device(), torch.int32
-    _check(lib().seer_attention_tree(_dev(q, dev), ld_q, _dev(o, dev), ld_o, _dt(dt), _dev(cu_new, dev, i32),
-                                     _dev(kv_len, dev, i32), _dev(mask, dev, torch.int64), B, T_cap, n_heads, max_draft,
-                                     ctypes.byref(pages), _dev(ws, dev), ws_bytes, _stream(stream)))
+    _check(_native().seer_attention_tree(q, ld_q, o, ld_o, _dt(dt), cu_new, kv_len, mask, B, T_cap, n_heads, max_draft,
+                                         pages, ws, ws_bytes, stream))
 
 
 def seer_attention_tree_workspace_size(dt, B, n_heads, n_kv_heads, head_dim, max_draft) -> int:

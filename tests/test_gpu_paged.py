@@ -682,5 +682,5 @@ def test_binding_refuses_tensors_elsewhere():
     g = x.to(cuda())
     with pytest.raises(ValueError, match="current device"):
         S.seer_attention_causal(x, 512, g, 512, g, 512, g.clone(), 512, "bf16", i32([0, 4]), 1, 4, 2, 1, 128)
-    with pytest.raises(ValueError, match="int32"):
+    with pytest.raises(ValueError, match="Int"):
         S.seer_attention_causal(g, 512, g[:, 256:], 512, g[:, 384:], 512, g.clone(), 512, "bf16", i32([0, 4]).long(), 1, 4, 2, 1, 128)
