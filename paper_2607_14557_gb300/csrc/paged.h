@@ -94,7 +94,7 @@ struct GqaParams {
   const int* table;       // paged
   int n_pages, page_shift, max_pages;
   float* part;            // paged: partial results, see gqa_part_floats
-  int splits;             // CUDA-core kernel: shares of a request's keys
+  int splits;             // CUDA-core kernel, paged: shares of a request's keys
   int* err;
 };
 // 16-bit causal attention on the tensor cores.  mQ: q as [T_cap][n_heads][head_dim] in boxes
@@ -111,7 +111,7 @@ size_t tc_tree_part_bytes(int n_heads, int n_kv, int head_dim, int max_new, int 
 cudaError_t launch_tc_tree(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, bool f16, int num_sms,
                            cudaStream_t st);
 // CUDA-core kernels (fp32).
-cudaError_t launch_gqa_simt(int type, bool paged, const GqaParams& p, int num_sms, cudaStream_t st);
+cudaError_t launch_gqa_simt(bool paged, const GqaParams& p, int num_sms, cudaStream_t st);
 // Shares of the keys, and bytes of partial results, of a paged call on the CUDA-core kernel.
 int gqa_simt_splits(int B, int n_heads, int n_kv, int max_new, int num_sms);
 size_t gqa_simt_part_bytes(int B, int n_heads, int n_kv, int head_dim, int max_new, int num_sms);

@@ -238,7 +238,6 @@ seer_status seer_attention_causal(const void* q, int ld_q, const void* k, int ld
   p.n_heads = n_heads;
   p.n_kv = n_kv_heads;
   p.head_dim = head_dim;
-  p.splits = 1;
   p.err = di->err;
   if (T_cap == 0) return SEER_OK;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -253,7 +252,7 @@ seer_status seer_attention_causal(const void* q, int ld_q, const void* k, int ld
     return SEER_OK;
   }
   Phase ph(PH_ATTN, st);
-  SEER_CUDA(launch_gqa_simt(dt, false, p, di->num_sms, st), "causal attention launch");
+  SEER_CUDA(launch_gqa_simt(false, p, di->num_sms, st), "causal attention launch");
   return SEER_OK;
 }
 
@@ -330,7 +329,7 @@ seer_status seer_attention_tree(const void* q, int ld_q, void* o, int ld_o, seer
   }
   p.splits = gqa_simt_splits(B, n_heads, pg.n_kv, max_draft, di->num_sms);
   Phase ph(PH_ATTN, st);
-  SEER_CUDA(launch_gqa_simt(dt, true, p, di->num_sms, st), "tree attention launch");
+  SEER_CUDA(launch_gqa_simt(true, p, di->num_sms, st), "tree attention launch");
   return SEER_OK;
 }
 
