@@ -219,12 +219,16 @@ constexpr int kAppendRows = 4;
 // position * rate modulo 1 in 64-bit integers (rate = theta^(-2i/dh) / 2 pi, from the host in
 // fp64), which is exact however far the position; its fraction then goes to sincospif.
 // One pass: q, k and v are read once, q | k written to `rotated`, k | v to the cache row.
-// Bound by HBM; a block takes up to four rows so that their sines are one a thread.
+// Bound by HBM.  A block takes up to four rows, so that their sines are one a thread, and a
+// thread UNROLL of their items (16 bytes of a head's lower half and the 16 of its upper half),
+// loads ahead of the stores.  Sines and cosines lie in groups of four, the groups of
+// neighbouring lanes side by side (pair by pair they met 8 times in a bank).
 template <int T, bool ROTATE>
 __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const KvAppendArgs a, const __grid_constant__ TurnRates rates) {
   pdl_enter();
   using V = Vec16<T>;
-  __shared__ float2 turn[kAppendRows][64];
+  constexpr int QUADS = V::N / 4, UNROLL = 3, es = 16 / V::N;
+  __shared__ float4 cosines[kAppendRows][QUADS][64 / V::N], sines[kAppendRows][QUADS][64 / V::N];
   __shared__ int slots[kAppendRows];
   const int dh = a.pages.head_dim, half = dh / 2, n_kv = a.pages.n_kv;
   int M = a.M_dev ? *a.M_dev : a.T_cap;
@@ -233,21 +237,21 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const KvAppen
     M = M < 0 ? 0 : a.T_cap;
   }
   const int pool_rows = a.pages.n_pages << a.pages.page_shift;
-  const int per_head = half / V::N;               // vector pairs of a head
-  const int pairs = (a.n_heads + n_kv) * per_head;
-  const int v_vecs = n_kv * dh / V::N;
-  const int items = pairs + v_vecs;
-  constexpr int es = 16 / V::N;
-  const long kv_row = 2l * n_kv * dh * es;
+  const int per_head = half / V::N;               // items of a head
+  const int items = (a.n_heads + 2 * n_kv) * per_head;
+  const long kv_row = 2l * n_kv * dh * es, high = static_cast<long>(half) * es;
   const int G = a.rows_per_block;
   for (int row0 = blockIdx.x * G; row0 < M; row0 += gridDim.x * G) {
     const int rows = min(G, M - row0);
     __syncthreads();                              // the rows before are done with the tables
     if (ROTATE)
       for (int j = threadIdx.x; j < rows * half; j += kAppendThreads) {
-        const int r = j / half, i = j - r * half;
+        const int r = j / half, i = j - r * half, c = i / V::N, e = i % V::N;
         const uint64_t part = static_cast<uint64_t>(static_cast<int64_t>(a.position[row0 + r])) * rates.rate[i];
-        sincospif(static_cast<float>(static_cast<int64_t>(part)) * 0x1p-63f, &turn[r][i].y, &turn[r][i].x);
+        float sn, cs;
+        sincospif(static_cast<float>(static_cast<int64_t>(part)) * 0x1p-63f, &sn, &cs);
+        reinterpret_cast<float*>(&cosines[r][e / 4][c])[e % 4] = cs;
+        reinterpret_cast<float*>(&sines[r][e / 4][c])[e % 4] = sn;
       }
     if (threadIdx.x < rows) {
       int s = a.slot[row0 + threadIdx.x];
@@ -258,45 +262,59 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const KvAppen
       slots[threadIdx.x] = s;
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < rows * items; j += kAppendThreads) {
-      const int r = j / items, it = j - r * items, s = slots[r];
-      const uint8_t* src = a.qkv + static_cast<size_t>(row0 + r) * a.ld;
-      uint8_t* rot = a.rotated ? a.rotated + static_cast<size_t>(row0 + r) * a.ld_rot : nullptr;
-      uint8_t* dst = s < 0 ? nullptr : static_cast<uint8_t*>(a.pages.kv) + static_cast<size_t>(s) * kv_row;
-      if (it >= pairs) {                          // v as it is
-        const long at = static_cast<long>(it - pairs) * 16;
-        if (dst)
-          *reinterpret_cast<uint4*>(dst + kv_row / 2 + at) =
-              *reinterpret_cast<const uint4*>(src + static_cast<long>(a.n_heads + n_kv) * dh * es + at);
-        continue;
-      }
-      const int head = it / per_head, c = it - head * per_head;
-      const long at = (static_cast<long>(head) * dh + c * V::N) * es, high = static_cast<long>(half) * es;
-      const bool key = head >= a.n_heads;
-      if (!rot && !(key && dst)) continue;
-      uint4 lo = *reinterpret_cast<const uint4*>(src + at), hi = *reinterpret_cast<const uint4*>(src + at + high);
-      if (ROTATE) {
-        float x[V::N], y[V::N];
-        V::unpack(lo, x);
-        V::unpack(hi, y);
+    for (int j0 = threadIdx.x; j0 < rows * items; j0 += UNROLL * kAppendThreads) {
+      uint4 lo[UNROLL], hi[UNROLL];
+      int row[UNROLL], head[UNROLL], chunk[UNROLL];
 #pragma unroll
-        for (int e = 0; e < V::N; ++e) {
-          const float2 t = turn[r][c * V::N + e];
-          const float u = fmaf(x[e], t.x, -y[e] * t.y), w = fmaf(y[e], t.x, x[e] * t.y);
-          x[e] = u;
-          y[e] = w;
+      for (int u = 0; u < UNROLL; ++u) {
+        const int j = j0 + u * kAppendThreads;
+        row[u] = j / items;
+        const int it = j - row[u] * items;
+        head[u] = it / per_head;
+        chunk[u] = it - head[u] * per_head;
+        const bool wanted = row[u] < rows && ((a.rotated && head[u] < a.n_heads + n_kv) || (head[u] >= a.n_heads && slots[row[u]] >= 0));
+        if (!wanted) {
+          row[u] = -1;
+          continue;
         }
-        lo = V::pack(x);
-        hi = V::pack(y);
+        const uint8_t* src = a.qkv + static_cast<size_t>(row0 + row[u]) * a.ld + static_cast<long>(head[u]) * dh * es + chunk[u] * 16;
+        lo[u] = *reinterpret_cast<const uint4*>(src);
+        hi[u] = *reinterpret_cast<const uint4*>(src + high);
       }
-      if (rot) {
-        *reinterpret_cast<uint4*>(rot + at) = lo;
-        *reinterpret_cast<uint4*>(rot + at + high) = hi;
-      }
-      if (key && dst) {
-        const long kat = at - static_cast<long>(a.n_heads) * dh * es;
-        *reinterpret_cast<uint4*>(dst + kat) = lo;
-        *reinterpret_cast<uint4*>(dst + kat + high) = hi;
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        if (row[u] < 0) continue;
+        const bool turned = head[u] < a.n_heads + n_kv;
+        if (ROTATE && turned) {
+          float x[V::N], y[V::N];
+          V::unpack(lo[u], x);
+          V::unpack(hi[u], y);
+#pragma unroll
+          for (int g = 0; g < QUADS; ++g) {
+            const float4 c4 = cosines[row[u]][g][chunk[u]], s4 = sines[row[u]][g][chunk[u]];
+            const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p = x[4 * g + e], w = y[4 * g + e];
+              x[4 * g + e] = fmaf(p, cs[e], -w * sn[e]);
+              y[4 * g + e] = fmaf(w, cs[e], p * sn[e]);
+            }
+          }
+          lo[u] = V::pack(x);
+          hi[u] = V::pack(y);
+        }
+        const long at = static_cast<long>(head[u]) * dh * es + chunk[u] * 16;
+        if (turned && a.rotated) {
+          uint8_t* rot = a.rotated + static_cast<size_t>(row0 + row[u]) * a.ld_rot + at;
+          *reinterpret_cast<uint4*>(rot) = lo[u];
+          *reinterpret_cast<uint4*>(rot + high) = hi[u];
+        }
+        if (head[u] >= a.n_heads && slots[row[u]] >= 0) {   // k | v follow q as they do in the cache row
+          uint8_t* dst = static_cast<uint8_t*>(a.pages.kv) + static_cast<size_t>(slots[row[u]]) * kv_row + at -
+                         static_cast<long>(a.n_heads) * dh * es;
+          *reinterpret_cast<uint4*>(dst) = lo[u];
+          *reinterpret_cast<uint4*>(dst + high) = hi[u];
+        }
       }
     }
   }
