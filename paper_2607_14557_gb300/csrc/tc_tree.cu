@@ -111,7 +111,10 @@ __device__ __forceinline__ int quotient(long long a, int b) {
 }
 
 // Run c of n over a line of `total`: [cut(c), cut(c + 1)), and the run that holds x.
-__device__ __forceinline__ long long cut(long long total, int c, int n) { return total * c / n; }
+__device__ __forceinline__ long long cut(long long total, int c, int n) {
+  const long long x = total * c;
+  return (x >> 32) == 0 ? static_cast<unsigned>(x) / static_cast<unsigned>(n) : x / n;
+}
 __device__ __forceinline__ int run_of(long long total, long long x, int n) {
   return static_cast<int>(((x + 1) * n - 1) / total);
 }
@@ -392,6 +395,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     int window = b - 32;                                  // requests window .. window + 31 in the lanes' registers
     Request ahead{};
     Join join{};
+    long long join_end = 0;                               // last place of its unit
     // pool row of this lane's box of key tile j
     const auto box_row = [&](int bb, int kv, int j) {
       const int key = j * BKV + lane * box_rows;
@@ -454,10 +458,14 @@ __global__ void __launch_bounds__(THREADS, 2)
         u.tok0 = (unit - u.kvh * row_tiles) * TPT;
         u.part = u.tile0 > 0 ? 2 * c : (u.tile1 < tiles ? 2 * c + 1 : -1);
         if (u.tile0 == 0 && u.tile1 < tiles)
-          join = Join{u.q0, u.tok0, u.n, u.kvh, c, run_of(total, at + (places - last) - 1, runs), {0, 0}};
+        {
+          join = Join{u.q0, u.tok0, u.n, u.kvh, c, 0, {0, 0}};
+          join_end = at + (places - last) - 1;
+        }
         break;
       }
       if (u.tile1 <= u.tile0) u.n = -1;
+      int next_row = u.n < 0 ? -1 : box_row(u.b, u.kv, u.tile0);   // the page of a tile is looked up a tile ahead
       const int s = i % U_SLOTS;
       if (i >= U_SLOTS && !warp_wait(&u_empty[s], (i / U_SLOTS - 1) & 1, abort_flag, p.err)) break;
       if (lane == 0) {
@@ -466,7 +474,6 @@ __global__ void __launch_bounds__(THREADS, 2)
       }
       __syncwarp();
       if (u.n < 0) break;
-      int next_row = box_row(u.b, u.kv, u.tile0);         // the page of a tile is looked up a tile ahead
       const int qs = i % QB;
       if (i >= QB && !warp_wait(&q_empty[qs], (i / QB - 1) & 1, abort_flag, p.err)) break;
       if (leader) {
@@ -491,6 +498,7 @@ __global__ void __launch_bounds__(THREADS, 2)
         ++g;
       }
     }
+    if (join.n > 0) join.last = run_of(total, join_end, runs);
     if (lane == 0) joins[c] = join;
     if (*abort_flag && leader) {
       // let copies still in flight land before the CTA's shared memory is released
@@ -764,51 +772,73 @@ __global__ void __launch_bounds__(THREADS, 2)
 // Joins the pieces of the unit that begins in run blockIdx.x and ends in a later one, in order
 // of their keys: sums and weights relative to a running maximum, so that a piece's numbers
 // are read once and several pieces' reads are under way.  A thread takes 8 columns of one of
-// 32 rows of the tile; fewer rows sit side by side.
+// 32 rows of the tile; fewer rows leave threads to share the pieces among (one token over
+// 12000 keys has 38 of them: 39 us with one thread a row and column group), whose results
+// then meet in shared memory.
 constexpr int MERGE_THREADS = 512;
 
 template <bool F16, int DH>
 __global__ void __launch_bounds__(MERGE_THREADS) tree_merge_kernel(const GqaParams p, const Join* __restrict__ joins) {
+  constexpr int CHUNKS = DH / 8;
+  __shared__ float shares[MERGE_THREADS][11];             // max, weight, sums
   const int G = p.n_heads / p.n_kv, TPT = BQ / G, part_rows = min(TPT, p.max_new) * G;
   pdl_enter();
   const Join u = joins[blockIdx.x];
   const int rows = min(TPT, u.n - u.tok0) * G, row0 = blockIdx.y * 32;
   if (u.n == 0 || row0 >= rows) return;
-  const int side = rows - row0 > 16 ? 32 : (rows - row0 > 8 ? 16 : (rows - row0 > 4 ? 8 : 4));
-  const int r = row0 + (threadIdx.x & (side - 1));
-  uint32_t nonfinite = 0;
-  if (r < rows) {
-    const size_t stride = static_cast<size_t>(part_rows) * (DH + 4);
-    const float* slot0 = p.part + (2 * u.first + 1) * stride;          // the unit's first piece
-    const float* slots = p.part + 2 * (u.first + 1) * stride;          // the next ones, 2 slots apart
-    const int more = u.last - u.first;
-    const size_t orow = static_cast<size_t>(u.q0 + u.tok0 + r / G) * p.ld_o + (u.kvh * G + r % G) * DH;
-    for (int col = threadIdx.x / side * 8; col < DH; col += MERGE_THREADS / side * 8) {
-      float m = -INFINITY, sum = 0.f, acc[8] = {};
+  const int left = rows - row0, side = left > 16 ? 32 : (left > 8 ? 16 : (left > 4 ? 8 : (left > 2 ? 4 : 2)));
+  const int pieces = u.last - u.first + 1, most = MERGE_THREADS / (side * CHUNKS), subs = pieces < most ? pieces : most;
+  const int r = row0 + static_cast<int>(threadIdx.x) % side, col = static_cast<int>(threadIdx.x) / side % CHUNKS * 8;
+  const int sub = threadIdx.x / (side * CHUNKS);
+  const bool mine = r < rows && sub < subs;
+  const size_t stride = static_cast<size_t>(part_rows) * (DH + 4);
+  float m = -INFINITY, sum = 0.f, acc[8] = {};
+  const auto add = [&](float m1, float sum1, const float (&f)[8]) {
+    if (sum1 == 0.f) return;                              // a share without a seen key adds nothing
+    const float top = fmaxf(m, m1), base = top == -INFINITY ? 0.f : top;
+    const float old = ex2(m - base), w = ex2(m1 - base);
+    m = top;
+    sum = fmaf(sum, old, sum1 * w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = fmaf(acc[e], old, w * f[e]);
+  };
+  if (mine) {
+    const int c1 = pieces * (sub + 1) / subs;
 #pragma unroll 4
-      for (int c = 0; c <= more; ++c) {
-        const float* slot = c == 0 ? slot0 : slots + 2 * (c - 1) * stride;
-        const float2 ml = reinterpret_cast<const float2*>(slot + part_rows * DH)[r];
-        const float4* v = reinterpret_cast<const float4*>(slot) + col / 4 * part_rows + r;
-        const float4 a = v[0], b = v[part_rows];
-        if (ml.y == 0.f) continue;                        // a piece without a seen key adds nothing
-        const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.f : top;
-        const float old = ex2(m - base), w = ex2(ml.x - base);
-        m = top;
-        sum = fmaf(sum, old, ml.y * w);
-        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = fmaf(acc[e], old, w * f[e]);
-      }
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      uint32_t q[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        q[e] = pack2(acc[2 * e] * inv, acc[2 * e + 1] * inv, F16);
-        nonfinite |= nonfinite_term(q[e], F16);
-      }
-      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + orow + col) = make_uint4(q[0], q[1], q[2], q[3]);
+    for (int c = pieces * sub / subs; c < c1; ++c) {      // the unit's first piece is in its run's second slot
+      const float* slot = p.part + (2 * (u.first + c) + (c == 0 ? 1 : 0)) * stride;
+      const float2 ml = reinterpret_cast<const float2*>(slot + part_rows * DH)[r];
+      const float4* v = reinterpret_cast<const float4*>(slot) + col / 4 * part_rows + r;
+      const float4 a = v[0], b = v[part_rows];
+      const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      add(ml.x, ml.y, f);
     }
+  }
+  if (subs > 1) {
+    float* mine_at = shares[threadIdx.x];
+    mine_at[0] = m;
+    mine_at[1] = sum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mine_at[2 + e] = acc[e];
+    __syncthreads();
+    if (sub == 0)
+      for (int k = 1; k < subs; ++k) {
+        const float* s = shares[threadIdx.x + k * side * CHUNKS];
+        const float f[8] = {s[2], s[3], s[4], s[5], s[6], s[7], s[8], s[9]};
+        add(s[0], s[1], f);
+      }
+  }
+  uint32_t nonfinite = 0;
+  if (mine && sub == 0) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint32_t q[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      q[e] = pack2(acc[2 * e] * inv, acc[2 * e + 1] * inv, F16);
+      nonfinite |= nonfinite_term(q[e], F16);
+    }
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.q0 + u.tok0 + r / G) * p.ld_o + (u.kvh * G + r % G) * DH + col) =
+        make_uint4(q[0], q[1], q[2], q[3]);
   }
   report_range(nonfinite, p.err);
 }
