@@ -44,33 +44,32 @@ constexpr float RESCALE_THRESHOLD = 8.0f;   // log2 units
 constexpr int U_SLOTS = 4;
 constexpr int U_READERS = 1 + 4;            // issuer, softmax warps
 
-// Shared memory of a CTA: QB buffers of QROWS rows of Q, then one ring of SLOTS key and
-// value tiles in turn.  The MMA reads 128 rows from a Q buffer; those past QROWS are other
-// bytes of this memory, in rows of S that nobody looks at.  Few rows leave room for a third
-// slot and a second Q buffer, so that loads go on across a tile's softmax and from piece to
-// piece.  Where Q fills 32 KB the ring is one key slot and three halves of value tiles (64
-// keys; SLOTS = 0): half of the next V is under way before this V is used up.
-template <int DH_, int SLOTS_, int QB_, int QROWS_>
+// Shared memory of a CTA: QROWS rows of Q, then one ring of SLOTS key and value tiles in turn.
+// The MMA reads 128 rows from Q; those past QROWS are other bytes of this memory, in rows of S
+// that nobody looks at.  Few rows leave room for a third slot, so that loads go on across a
+// tile's softmax (a second Q buffer on top gained nothing).  Where Q fills 32 KB the ring is
+// one key slot and three halves of value tiles (64 keys; SLOTS = 0): half of the next V is
+// under way before this V is used up.
+template <int DH_, int SLOTS_, int QROWS_>
 struct Config {
-  static constexpr int DH = DH_, SLOTS = SLOTS_, QB = QB_, QROWS = QROWS_;
+  static constexpr int DH = DH_, SLOTS = SLOTS_, QROWS = QROWS_;
   static constexpr bool HALVES = SLOTS == 0;
   static constexpr int BARS = HALVES ? 4 : SLOTS;         // K, then the halves; or the slots
   static constexpr int TILE = 128 * DH * 2;
   static constexpr int V_PANEL = HALVES ? PANEL / 2 : PANEL;   // 64 columns of a V tile or half
   static constexpr int Q_PANEL = QROWS * 128, Q_BYTES = DH / 64 * Q_PANEL;
-  static constexpr int OFF_RING = QB * Q_BYTES;
+  static constexpr int OFF_RING = Q_BYTES;
   static constexpr int RING = HALVES ? TILE + 3 * TILE / 2 : SLOTS * TILE;
   static constexpr int OFF_BAR = OFF_RING + RING;
   static constexpr int BOX = HALVES ? 64 : 128;           // most rows of a box of the pool
   static constexpr int BYTES = OFF_BAR + BAR_BYTES;
   static_assert(Q_PANEL % 1024 == 0, "the 128-byte swizzle repeats every 8 rows");
   static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two CTAs per SM");
-  static_assert(Q_BYTES * QB + RING >= (QB - 1) * Q_BYTES + (DH / 64 - 1) * Q_PANEL + PANEL, "128 rows from any Q panel");
+  static_assert(Q_BYTES + RING >= (DH / 64 - 1) * Q_PANEL + PANEL, "128 rows from any Q panel");
 };
-using Wide64 = Config<64, 4, 2, 128>;
-using Few128 = Config<128, 3, 2, 24>;
-using Some128 = Config<128, 3, 1, 48>;
-using Wide128 = Config<128, 0, 1, 128>;
+using Dims64 = Config<64, 5, 128>;
+using Few128 = Config<128, 3, 48>;
+using Wide128 = Config<128, 0, 128>;
 
 // A piece: keys [tile0 * 128, tile1 * 128) of a unit.  n < 0: no more pieces.
 struct Piece {
@@ -80,10 +79,11 @@ struct Piece {
 };
 static_assert(sizeof(Piece) == 36, "ring entries");
 
-// Places of a unit on the line besides its key tiles: what a piece costs beyond them (Q,
-// the first and last round, its result), about one tile's time, two where it stores many
-// rows (us: a tile 2.9 and a piece 3.1 for 4 rows, 3.4 and 7.8 for 64 .. 128).
-__device__ __forceinline__ int unit_extra(int part_rows) { return part_rows <= 32 ? 1 : 2; }
+// Places of a unit on the line besides its key tiles: what a piece costs beyond them (Q, the
+// first and last round, its result, the join), in key tiles.  Measured, us, at 1 / 2 / 3 places
+// of few rows: 64 single tokens 103 / 98 / 98, 12 requests' 32-row drafts 42 / 40 / 40, heads of
+// 64 71 / 67 / 69; at 2 / 4 / 6 / 8 of many rows: 12 trees 66 / 59 / 59 / 62.
+__device__ __forceinline__ int unit_extra(int part_rows) { return part_rows <= 32 ? 2 : 5; }
 
 struct Request {
   int q0, n, kv;
@@ -245,7 +245,7 @@ template <bool F16, typename Cfg>
 __global__ void __launch_bounds__(THREADS, 2)
     tc_tree_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mKV, const GqaParams p,
                    const int q_box, Join* __restrict__ joins) {
-  constexpr int DH = Cfg::DH, TILE = Cfg::TILE, PANELS = DH / 64, QB = Cfg::QB;
+  constexpr int DH = Cfg::DH, TILE = Cfg::TILE, PANELS = DH / 64;
   constexpr int SLOTS = Cfg::HALVES ? 1 : Cfg::SLOTS;
   extern __shared__ __align__(1024) uint8_t smem[];       // all of the CTA's shared memory, so it starts aligned
   if ((smem_u32(smem) & 1023u) != 0) {
@@ -259,9 +259,9 @@ __global__ void __launch_bounds__(THREADS, 2)
   uint64_t* p_full2 = bars + 2;
   uint64_t* o_done = bars + 3;
   uint64_t* o_free = bars + 4;
-  uint64_t* q_full = bars + 5;               // [QB]
-  uint64_t* q_empty = q_full + QB;           // [QB]
-  uint64_t* r_full = q_empty + QB;           // [BARS] ring
+  uint64_t* q_full = bars + 5;
+  uint64_t* q_empty = bars + 6;
+  uint64_t* r_full = bars + 7;               // [BARS] ring
   uint64_t* r_empty = r_full + Cfg::BARS;
   uint64_t* u_full = r_empty + Cfg::BARS;    // [U_SLOTS]
   uint64_t* u_empty = u_full + U_SLOTS;      // [U_SLOTS]
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     Request r;
     int b;
   };
-  constexpr int START_AT = (8 * (5 + 2 * QB + 2 * Cfg::BARS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 + 7) & ~7;
+  constexpr int START_AT = (8 * (7 + 2 * Cfg::BARS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 + 7) & ~7;
   static_assert(START_AT + sizeof(Start) <= BAR_BYTES, "barrier block");
   Start& start = *reinterpret_cast<Start*>(smem + Cfg::OFF_BAR + START_AT);
 
@@ -311,10 +311,8 @@ __global__ void __launch_bounds__(THREADS, 2)
     mbar_init(p_full2, 4);
     mbar_init(o_done, 1);
     mbar_init(o_free, 4);
-    for (int i = 0; i < QB; ++i) {
-      mbar_init(&q_full[i], 1);
-      mbar_init(&q_empty[i], 1);
-    }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
     for (int i = 0; i < Cfg::BARS; ++i) {
       mbar_init(&r_full[i], 1);
       mbar_init(&r_empty[i], 1);
@@ -356,8 +354,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     total += start.warp_sum[w];
   }
   const int grid = gridDim.x, c = blockIdx.x;
-  const int least = extra + 1;                            // places of a run
-  const int runs = total < static_cast<long long>(grid) * least ? quotient(total + least - 1, least) : grid;
+  const int runs = total < grid ? static_cast<int>(total) : grid;
   const bool idle = c >= runs;                            // the whole CTA
   const long long run0 = idle ? 0 : cut(total, c, runs), run1 = idle ? 0 : cut(total, c + 1, runs);
   if (!idle && mine > 0 && run0 >= before && run0 < before + mine) {
@@ -474,12 +471,11 @@ __global__ void __launch_bounds__(THREADS, 2)
       }
       __syncwarp();
       if (u.n < 0) break;
-      const int qs = i % QB;
-      if (i >= QB && !warp_wait(&q_empty[qs], (i / QB - 1) & 1, abort_flag, p.err)) break;
+      if (i > 0 && !warp_wait(q_empty, (i - 1) & 1, abort_flag, p.err)) break;
       if (leader) {
-        mbar_arrive_expect_tx(&q_full[qs], PANELS * q_box * G * 128);
+        mbar_arrive_expect_tx(q_full, PANELS * q_box * G * 128);
         for (int x = 0; x < PANELS; ++x)
-          tma_load_3d(smem + qs * Cfg::Q_BYTES + x * Cfg::Q_PANEL, &mQ, &q_full[qs], 64 * x, u.kvh * G, u.q0 + u.tok0);
+          tma_load_3d(smem + x * Cfg::Q_PANEL, &mQ, q_full, 64 * x, u.kvh * G, u.q0 + u.tok0);
       }
       __syncwarp();
       ++pieces;
@@ -502,7 +498,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     if (lane == 0) joins[c] = join;
     if (*abort_flag && leader) {
       // let copies still in flight land before the CTA's shared memory is released
-      for (int j = max(pieces - QB, 0); j < pieces; ++j) mbar_wait_drain(&q_full[j % QB], (j / QB) & 1, 200000000ull);
+      if (pieces > 0) mbar_wait_drain(q_full, (pieces - 1) & 1, 20000000ull);
       for (unsigned j = g > 2 ? g - 3 : 0; j <= g; ++j) { // (waits on tiles that were not issued run out)
         mbar_wait_drain(&r_full[k_place(j).bar], k_place(j).use & 1, 20000000ull);
         for (int h = 0; h < 2; ++h) mbar_wait_drain(&r_full[v_place(j, h).bar], v_place(j, h).use & 1, 20000000ull);
@@ -513,17 +509,16 @@ __global__ void __launch_bounds__(THREADS, 2)
     const bool leader = elect_one();
     constexpr uint32_t idesc_qk = make_idesc(BQ, BKV, 0, F16);
     constexpr uint32_t idesc_pv = make_idesc(BQ, DH, 1, F16);
-    const uint64_t dq0 = make_sdesc_sw128(smem_u32(smem), 16, 1024);
+    const uint64_t dq = make_sdesc_sw128(smem_u32(smem), 16, 1024);
     const uint64_t dk0 = make_sdesc_sw128(smem_u32(smem), 16, 1024);
     const uint64_t dv0 = make_sdesc_sw128(smem_u32(smem), Cfg::V_PANEL, 1024);
     const uint32_t dS = tmem, dO = tmem + TM_O;
     unsigned g = 0;                                       // key tiles begun
     auto full = [&](const Place& x) { return warp_wait(&r_full[x.bar], x.use & 1u, abort_flag, p.err); };
-    auto qk = [&](int qs, bool last) {
+    auto qk = [&](bool last) {
       if (leader) {
         const Place at = k_place(g);
         const uint64_t dk = dk0 + static_cast<uint64_t>(at.off >> 4);
-        const uint64_t dq = dq0 + static_cast<uint64_t>(qs * (Cfg::Q_BYTES >> 4));
 #pragma unroll
         for (int k = 0; k < DH / 16; ++k) {
           const uint64_t oq = static_cast<uint64_t>(((k >> 2) * Cfg::Q_PANEL + (k & 3) * 32) >> 4);
@@ -532,7 +527,7 @@ __global__ void __launch_bounds__(THREADS, 2)
         }
         tc_commit(s_full);
         tc_commit(&r_empty[at.bar]);
-        if (last) tc_commit(&q_empty[qs]);
+        if (last) tc_commit(q_empty);
       }
       __syncwarp();
       ++g;
@@ -552,11 +547,11 @@ __global__ void __launch_bounds__(THREADS, 2)
     for (int i = 0; ok; ++i) {
       const Piece* u = read_piece(u_full, ring, i, abort_flag, p.err);
       if (u == nullptr) break;
-      const int tiles = u->tile1 - u->tile0, qs = i % QB;
+      const int tiles = u->tile1 - u->tile0;
       release_piece(u_empty, i, lane);
-      if (!warp_wait(&q_full[qs], (i / QB) & 1, abort_flag, p.err) || !full(k_place(g))) break;
+      if (!warp_wait(q_full, i & 1, abort_flag, p.err) || !full(k_place(g))) break;
       tc_fence_after();
-      qk(qs, tiles == 1);
+      qk(tiles == 1);
       for (int j = 0; j < tiles; ++j) {
         const unsigned pc = (g - 1) & 1u;                 // the tile whose scores were issued last
         const Place v0 = v_place(g - 1, 0), v1 = v_place(g - 1, 1);
@@ -579,7 +574,7 @@ __global__ void __launch_bounds__(THREADS, 2)
             break;
           }
           tc_fence_after();
-          qk(qs, j + 2 == tiles);
+          qk(j + 2 == tiles);
         } else {
           if (leader) tc_commit(o_done);
           __syncwarp();
@@ -861,9 +856,8 @@ template <bool F16>
 cudaError_t launch_rows(const CUtensorMap& mQ, const CUtensorMap& mKV, const GqaParams& p, int grid, int q_box, Join* joins,
                         cudaStream_t st) {
   const int rows = q_box * (p.n_heads / p.n_kv);
-  if (p.head_dim == 64) return launch_typed<F16, Wide64>(mQ, mKV, p, grid, q_box, joins, st);
+  if (p.head_dim == 64) return launch_typed<F16, Dims64>(mQ, mKV, p, grid, q_box, joins, st);
   if (rows <= Few128::QROWS) return launch_typed<F16, Few128>(mQ, mKV, p, grid, q_box, joins, st);
-  if (rows <= Some128::QROWS) return launch_typed<F16, Some128>(mQ, mKV, p, grid, q_box, joins, st);
   return launch_typed<F16, Wide128>(mQ, mKV, p, grid, q_box, joins, st);
 }
 
@@ -880,7 +874,7 @@ size_t part_floats(int n_heads, int n_kv, int head_dim, int max_new, int num_sms
 int tc_tree_box_tokens(int n_heads, int n_kv, int max_new) { return tile_tokens(n_heads, n_kv, max_new); }
 int tc_tree_box_keys(int n_heads, int n_kv, int head_dim, int max_new, int page_size) {
   const int rows = tile_tokens(n_heads, n_kv, max_new) * (n_heads / n_kv);
-  const int most = head_dim == 128 && rows > Some128::QROWS ? Wide128::BOX : Few128::BOX;
+  const int most = head_dim == 128 && rows > Few128::QROWS ? Wide128::BOX : Few128::BOX;
   return page_size < most ? page_size : most;
 }
 
