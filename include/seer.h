@@ -368,7 +368,7 @@ typedef struct {
   void* kv;               /* device [n_pages * page_size, 2 * n_kv_heads * head_dim] */
   const int32_t* table;   /* device [B, max_pages] */
   int n_pages;
-  int page_size;          /* a power of two from 8 to 1024; n_pages * page_size < 2^31 */
+  int page_size;          /* a power of two from 8 to 1024; n_pages * page_size < 2^31 - 1024 */
   int max_pages;          /* pages of the longest request that the table holds */
   int n_kv_heads;
   int head_dim;           /* <= 128, a multiple of 16 (fp32: of 8) */

@@ -13,6 +13,9 @@ static_assert(SEER_MAX_DRAFT == kMaxDraft && SEER_MAX_REQUESTS == kPageTableMaxB
 
 namespace {
 
+// Row numbers are 32-bit; a page past the pool's end is one too.
+constexpr long long kMaxPoolRows = 0x7fffffffll - 1024;
+
 int log2_exact(int v) {
   int s = 0;
   while ((1 << s) < v) ++s;
@@ -38,8 +41,8 @@ seer_status check_pages(const char* what, const seer_pages* g, seer_dtype dt, Pa
   if (g->n_pages <= 0 || g->max_pages <= 0 || g->n_kv_heads <= 0 || g->head_dim <= 0)
     return fail(SEER_ERR_INVALID_ARG, "%s: page counts, heads and head_dim must be positive", what);
   SEER_TRY(check_page_size(what, g->page_size));
-  if (static_cast<long long>(g->n_pages) * g->page_size > 0x7fffffffll)
-    return fail(SEER_ERR_UNSUPPORTED, "%s: the pool has more than 2^31 - 1 rows", what);
+  if (static_cast<long long>(g->n_pages) * g->page_size > kMaxPoolRows)
+    return fail(SEER_ERR_UNSUPPORTED, "%s: the pool has more than %lld rows", what, kMaxPoolRows);
   const int step = dt == SEER_F32 ? 8 : 16;
   if (g->head_dim > 128 || g->head_dim % step != 0)
     return fail(SEER_ERR_UNSUPPORTED, "%s: head_dim must be a multiple of %d and at most 128 (got %d)", what, step, g->head_dim);
@@ -108,8 +111,8 @@ seer_status seer_page_tables(const int32_t* cached_len, const int32_t* new_len, 
     return fail(SEER_ERR_INVALID_ARG, "page tables: bad sizes");
   if (n_free > 0 && !free_pages) return fail(SEER_ERR_INVALID_ARG, "page tables: free_pages is null");
   if (T_cap > 0 && (!slot_out || !position_out)) return fail(SEER_ERR_INVALID_ARG, "page tables: null row output");
-  if (static_cast<long long>(n_pages) * page_size > 0x7fffffffll)
-    return fail(SEER_ERR_UNSUPPORTED, "page tables: the pool has more than 2^31 - 1 rows");
+  if (static_cast<long long>(n_pages) * page_size > kMaxPoolRows)
+    return fail(SEER_ERR_UNSUPPORTED, "page tables: the pool has more than %lld rows", kMaxPoolRows);
   if (free_head == free_head_out || cached_len == kv_len_out || new_len == kv_len_out || new_len == cu_new_out ||
       cached_len == cu_new_out)
     return fail(SEER_ERR_INVALID_ARG, "page tables: an output is also an input");

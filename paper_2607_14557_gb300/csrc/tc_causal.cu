@@ -228,6 +228,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     };
     int g = most;                             // units of group g: [base, base + count)
     long base = 0, count = 0;
+    int b0 = 0, passed = 0;                   // sequences b0 .. hold the next unit; so many before them reach g
     for (int i = 0;; ++i) {
       const long u = (i & 1) ? (i + 1l) * grid - 1 - blockIdx.x : static_cast<long>(i) * grid + blockIdx.x;
       const int s = i % U_SLOTS;
@@ -238,18 +239,19 @@ __global__ void __launch_bounds__(THREADS, 1)
           base += count;
           --g;
           int n = 0;
-          for (int b0 = 0; b0 < p.B; b0 += 32) n += __popc(reach(b0, g));
+          for (int x = 0; x < p.B; x += 32) n += __popc(reach(x, g));
           count = static_cast<long>(n) * H;
+          b0 = passed = 0;
         }
-        const int k = static_cast<int>(u - base);
-        int nth = k / H, b = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
+        const int k = static_cast<int>(u - base), nth = k / H;
+        int b = 0;
+        for (; b0 < p.B; b0 += 32) {          // a group's units come in order, so this goes on where it stopped
           const uint32_t m = reach(b0, g);
-          if (nth < __popc(m)) {
-            b = b0 + __fns(m, 0, nth + 1);
+          if (nth - passed < __popc(m)) {
+            b = b0 + __fns(m, 0, nth - passed + 1);
             break;
           }
-          nth -= __popc(m);
+          passed += __popc(m);
         }
         w = make_int4(p.cu[b], p.cu[b + 1] - p.cu[b], g * span, k % H);
       }

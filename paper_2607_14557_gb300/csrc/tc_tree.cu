@@ -766,16 +766,17 @@ __global__ void __launch_bounds__(THREADS, 2)
 
 // Joins the pieces of the unit that begins in run blockIdx.x and ends in a later one, in order
 // of their keys: sums and weights relative to a running maximum, so that a piece's numbers
-// are read once and several pieces' reads are under way.  A thread takes 8 columns of one of
-// 32 rows of the tile; fewer rows leave threads to share the pieces among (one token over
+// are read once and several pieces' reads are under way.  A thread takes 16 columns of one of
+// 32 rows of the tile (8 columns: twice the threads, 12 trees 60 us instead of 58); fewer rows leave threads to share the pieces among (one token over
 // 12000 keys has 38 of them: 39 us with one thread a row and column group), whose results
 // then meet in shared memory.
-constexpr int MERGE_THREADS = 512;
+constexpr int MERGE_THREADS = 256, MERGE_COLS = 16;
 
 template <bool F16, int DH>
 __global__ void __launch_bounds__(MERGE_THREADS) tree_merge_kernel(const GqaParams p, const Join* __restrict__ joins) {
-  constexpr int CHUNKS = DH / 8;
-  __shared__ float shares[MERGE_THREADS][11];             // max, weight, sums
+  constexpr int CHUNKS = DH / MERGE_COLS;
+  static_assert(32 * CHUNKS <= MERGE_THREADS, "a thread for every row and column group");
+  __shared__ float shares[MERGE_THREADS][MERGE_COLS + 3]; // max, weight, sums
   const int G = p.n_heads / p.n_kv, TPT = BQ / G, part_rows = min(TPT, p.max_new) * G;
   pdl_enter();
   const Join u = joins[blockIdx.x];
@@ -783,19 +784,19 @@ __global__ void __launch_bounds__(MERGE_THREADS) tree_merge_kernel(const GqaPara
   if (u.n == 0 || row0 >= rows) return;
   const int left = rows - row0, side = left > 16 ? 32 : (left > 8 ? 16 : (left > 4 ? 8 : (left > 2 ? 4 : 2)));
   const int pieces = u.last - u.first + 1, most = MERGE_THREADS / (side * CHUNKS), subs = pieces < most ? pieces : most;
-  const int r = row0 + static_cast<int>(threadIdx.x) % side, col = static_cast<int>(threadIdx.x) / side % CHUNKS * 8;
+  const int r = row0 + static_cast<int>(threadIdx.x) % side, col = static_cast<int>(threadIdx.x) / side % CHUNKS * MERGE_COLS;
   const int sub = threadIdx.x / (side * CHUNKS);
   const bool mine = r < rows && sub < subs;
   const size_t stride = static_cast<size_t>(part_rows) * (DH + 4);
-  float m = -INFINITY, sum = 0.f, acc[8] = {};
-  const auto add = [&](float m1, float sum1, const float (&f)[8]) {
+  float m = -INFINITY, sum = 0.f, acc[MERGE_COLS] = {};
+  const auto add = [&](float m1, float sum1, const float (&f)[MERGE_COLS]) {
     if (sum1 == 0.f) return;                              // a share without a seen key adds nothing
     const float top = fmaxf(m, m1), base = top == -INFINITY ? 0.f : top;
     const float old = ex2(m - base), w = ex2(m1 - base);
     m = top;
     sum = fmaf(sum, old, sum1 * w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = fmaf(acc[e], old, w * f[e]);
+    for (int e = 0; e < MERGE_COLS; ++e) acc[e] = fmaf(acc[e], old, w * f[e]);
   };
   if (mine) {
     const int c1 = pieces * (sub + 1) / subs;
@@ -804,8 +805,15 @@ __global__ void __launch_bounds__(MERGE_THREADS) tree_merge_kernel(const GqaPara
       const float* slot = p.part + (2 * (u.first + c) + (c == 0 ? 1 : 0)) * stride;
       const float2 ml = reinterpret_cast<const float2*>(slot + part_rows * DH)[r];
       const float4* v = reinterpret_cast<const float4*>(slot) + col / 4 * part_rows + r;
-      const float4 a = v[0], b = v[part_rows];
-      const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      float f[MERGE_COLS];
+#pragma unroll
+      for (int e = 0; e < MERGE_COLS / 4; ++e) {
+        const float4 a = v[e * part_rows];
+        f[4 * e] = a.x;
+        f[4 * e + 1] = a.y;
+        f[4 * e + 2] = a.z;
+        f[4 * e + 3] = a.w;
+      }
       add(ml.x, ml.y, f);
     }
   }
@@ -814,26 +822,31 @@ __global__ void __launch_bounds__(MERGE_THREADS) tree_merge_kernel(const GqaPara
     mine_at[0] = m;
     mine_at[1] = sum;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) mine_at[2 + e] = acc[e];
+    for (int e = 0; e < MERGE_COLS; ++e) mine_at[2 + e] = acc[e];
     __syncthreads();
     if (sub == 0)
       for (int k = 1; k < subs; ++k) {
         const float* s = shares[threadIdx.x + k * side * CHUNKS];
-        const float f[8] = {s[2], s[3], s[4], s[5], s[6], s[7], s[8], s[9]};
+        float f[MERGE_COLS];
+#pragma unroll
+        for (int e = 0; e < MERGE_COLS; ++e) f[e] = s[2 + e];
         add(s[0], s[1], f);
       }
   }
   uint32_t nonfinite = 0;
   if (mine && sub == 0) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    uint32_t q[4];
+    uint16_t* o = static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.q0 + u.tok0 + r / G) * p.ld_o + (u.kvh * G + r % G) * DH + col;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      q[e] = pack2(acc[2 * e] * inv, acc[2 * e + 1] * inv, F16);
-      nonfinite |= nonfinite_term(q[e], F16);
+    for (int h = 0; h < MERGE_COLS / 8; ++h) {
+      uint32_t q[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        q[e] = pack2(acc[8 * h + 2 * e] * inv, acc[8 * h + 2 * e + 1] * inv, F16);
+        nonfinite |= nonfinite_term(q[e], F16);
+      }
+      reinterpret_cast<uint4*>(o)[h] = make_uint4(q[0], q[1], q[2], q[3]);
     }
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.q0 + u.tok0 + r / G) * p.ld_o + (u.kvh * G + r % G) * DH + col) =
-        make_uint4(q[0], q[1], q[2], q[3]);
   }
   report_range(nonfinite, p.err);
 }

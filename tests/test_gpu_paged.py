@@ -518,6 +518,117 @@ def test_tree_records_lengths_that_do_not_fit():
         S.seer_attention_tree(q, 512, torch.empty_like(q), 512, "bf16", i32([0, 2, 4]), i32([60, 64]), None, 2, 6, 4, 3, pool.struct, None, 0)
 
 
+def test_tree_ignores_mask_bits_beyond_the_draft():
+    rng = np.random.default_rng(21)
+    for dt, dh in (("bf16", 128), ("f32", 64)):
+        new, kv_len, cu = [3, 9], [130, 70], [0, 3, 12]
+        pool = Pool(rng, kv_len, 16, 2, dh, dt)
+        q = rnd(rng, (12, 4 * dh), dt)
+        mask = words_of(rng, new, "tree")
+        wide = [w | (((1 << 64) - 1) ^ ((1 << (3 if r < 3 else 9)) - 1)) for r, w in enumerate(mask)]
+        a, b = run_tree(pool, q, cu, kv_len, 4, dt, mask), run_tree(pool, q, cu, kv_len, 4, dt, wide)
+        assert torch.equal(a, b)
+    assert S.seer_check_device() == 0
+
+
+def test_pool_past_32_bit_offsets():
+    """Pages behind the 4 GB and the 2^32-value mark of a pool."""
+    rng = np.random.default_rng(22)
+    dt, hq, hk, dh, page = "bf16", 8, 4, 128, 64
+    n_pages = (1 << 33) // (page * 2 * hk * dh * 2) * 2 + 40          # 16 GB
+    kv = torch.empty((n_pages * page, 2 * hk * dh), dtype=TDT[dt], device=cuda())
+    ids = [n_pages - 1, 3, n_pages - 9, n_pages // 2, n_pages - 20, 0]
+    table = i32([ids])
+    pages = S.make_pages(kv, table, n_pages, page, len(ids), hk, dh)
+    kv_len, T = 6 * 64 - 5, 20
+    small = rnd(rng, (len(ids) * page, 2 * hk * dh), dt)
+    for i, p in enumerate(ids):
+        kv[p * page:(p + 1) * page] = small[i * page:(i + 1) * page]
+    x = rnd(rng, (T, (hq + 2 * hk) * dh), dt)
+    slot = [ids[t // page] * page + t % page for t in range(kv_len - T, kv_len)]
+    S.seer_kv_append(x, x.stride(0), dt, hq, T, None, i32(slot), None, 0.0, None, 0, pages)
+    small[kv_len - T:kv_len] = x[:, hq * dh:]
+    for i, p in enumerate(ids):
+        assert torch.equal(kv[p * page:(p + 1) * page], small[i * page:(i + 1) * page]), i
+    size = S.seer_attention_tree_workspace_size(dt, 1, hq, hk, dh, T)
+    ws = torch.empty(size, dtype=torch.uint8, device=cuda())
+    o = torch.zeros((T, hq * dh), dtype=TDT[dt], device=cuda())
+    S.seer_attention_tree(x, x.stride(0), o, o.stride(0), dt, i32([0, T]), i32([kv_len]), None, 1, T, hq, T, pages, ws, size)
+    ref, bound = R.tree(host(x)[:, :hq * dh].reshape(T, hq, dh), host(small).reshape(-1, 2, hk, dh), [list(range(6))], page, [0, T],
+                        [kv_len], None, dt)
+    close(host(o).reshape(ref.shape), ref, bound)
+    out = i32([0])
+    S.seer_kv_accept(dt, i32([kv_len - T]), i32([[1, 5, 19] + [0] * 17]), i32([3]), 1, 20, pages, out)
+    for k, a in enumerate((1, 5, 19)):
+        assert torch.equal(kv[slot[k]], x[a, hq * dh:])
+    assert S.seer_check_device() == 0 and out.tolist() == [kv_len - T + 3]
+
+
+def test_causal_rows_past_32_bit_offsets():
+    rng = np.random.default_rng(23)
+    dt, hq, hk, dh, cap = "bf16", 4, 2, 128, 2_200_000
+    w = (hq + 2 * hk) * dh                                            # 2.2e6 x 1024 values: past 2^31
+    x = torch.empty((cap, w), dtype=TDT[dt], device=cuda())
+    x[-300:] = rnd(rng, (300, w), dt)
+    cu = [cap - 300, cap - 140, cap]
+    o = torch.full((cap, hq * dh), 5.0, dtype=TDT[dt], device=cuda())
+    run_causal(x, np.array(cu), hq, hk, dh, dt, o=o)
+    ref, bound = causal_ref(x[-300:], np.array([0, 160, 300]), hq, hk, dh, dt)
+    close(host(o[-300:]).reshape(ref.shape), ref, bound)
+    assert (o[:-300] == 5.0).all()
+    assert S.seer_check_device() == 0
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_causal_many_short_prompts(dt):
+    rng = np.random.default_rng(24)
+    lens = [int(v) for v in rng.integers(0, 5, 3000)]
+    x, cu = causal_case(rng, lens, 4, 2, 64, dt)
+    ref, bound = causal_ref(x, cu, 4, 2, 64, dt)
+    close(host(run_causal(x, cu, 4, 2, 64, dt)).reshape(ref.shape), ref, bound)
+    assert S.seer_check_device() == 0
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_tree_many_requests(dt):
+    rng = np.random.default_rng(25)
+    B = 1500
+    new = [int(v) for v in rng.integers(0, 3, B)]
+    kv_len = [int(v) + n for v, n in zip(rng.integers(0, 70, B), new)]
+    pool = Pool(rng, kv_len, 8, 1, 64, dt)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(int)
+    q = rnd(rng, (cu[-1], 3 * 64), dt)
+    ref, bound = tree_ref(pool, q, cu, kv_len, 3, dt)
+    close(host(run_tree(pool, q, cu, kv_len, 3, dt)).reshape(ref.shape), ref, bound)
+    assert S.seer_check_device() == 0
+
+
+def test_streams_given_and_launch_overlap_off():
+    rng = np.random.default_rng(26)
+    dt, hq, hk, dh = "f16", 4, 2, 128
+    x, cu = causal_case(rng, [200, 90], hq, hk, dh, dt)
+    pool = Pool(rng, [300, 64], 16, hk, dh, dt)
+    q = rnd(rng, (7, hq * dh), dt)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    want = run_causal(x, cu, hq, hk, dh, dt), run_tree(pool, q, [0, 3, 7], [300, 64], hq, dt)
+    torch.cuda.synchronize()
+    outs = []
+    before = S.seer_set_launch_overlap(False)
+    try:
+        for s in (side, side.cuda_stream, None):
+            a = torch.full_like(want[0], 5.0)
+            b = torch.full_like(want[1], 5.0)
+            torch.cuda.synchronize()
+            outs.append((run_causal(x, cu, hq, hk, dh, dt, o=a, stream=s), run_tree(pool, q, [0, 3, 7], [300, 64], hq, dt, o=b, stream=s)))
+            torch.cuda.synchronize()
+    finally:
+        S.seer_set_launch_overlap(before)
+    for a, b in outs:
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+    assert S.seer_check_device() == 0
+
+
 # ------------------------------------------------------------------ together
 def test_prompt_draft_accept_steps():
     """Prompts, then rounds of drafting a tree, attending, and keeping a path of it: every
