@@ -1,8 +1,8 @@
 // fp32 attention of grouped heads on the CUDA cores (the tensor cores have no fp32-input
 // mode): causal over packed prompts, and new rows over a paged cache.
 //   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(q_i k_j / sqrt(dh) - max),  over the keys j that row i sees
-// A block has 32 of the n * g (token, head of the group) rows that share a key/value head,
-// 128 threads with 4 rows x 4 keys each; keys in tiles of 64 with an online softmax (expf),
+// A block has 32 (few blocks: 16) of the n * g (token, head of the group) rows that share a
+// key/value head, 128 threads with 4 (2) rows x 4 keys each; keys in tiles of 64 with an online softmax (expf),
 // K, V and Q in shared memory by cp.async, the next K under way during a tile's PV and the
 // next V during the next scores.  Lanes as in the fp32 kernels of simt.cu.
 // Few blocks would leave the longest row's tiles in a chain (5 prompts of 1 .. 300 rows, 34 us
@@ -17,14 +17,14 @@
 namespace seer {
 namespace {
 
-constexpr int BQ = 32, TY = 8, NTH = 16 * TY;
+constexpr int TY = 8, NTH = 16 * TY;
 constexpr int KT = 64;                        // keys per tile
 constexpr int PS = KT + 16;                   // floats per row of probabilities
 constexpr int MAX_PARTS = 8;                  // blocks of a cluster
 // Staged rows hold 64 or 128 dims, zeros past head_dim, so that every address is a constant
 // away from a thread's own; an odd number of 16-byte words meets no bank twice.
 __host__ __device__ constexpr int row_ld(int dims) { return dims + 4; }
-__host__ __device__ constexpr int smem_floats(int dims) { return (BQ + 2 * KT) * row_ld(dims) + BQ * PS + 2 * BQ; }
+__host__ __device__ constexpr int smem_floats(int rows, int dims) { return (rows + 2 * KT) * row_ld(dims) + rows * PS + 2 * rows; }
 
 __device__ __forceinline__ void copy16(float* dst, const float* src, bool valid) {   // zeros where !valid
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(valid ? 16 : 0) : "memory");
@@ -74,13 +74,14 @@ __device__ __forceinline__ Span read_span(const GqaParams& p, int b) {
 }
 
 // CLUSTER: the blocks of a cluster share a tile's keys.
-template <bool PAGED, bool CLUSTER, int HALVES>
+template <bool PAGED, bool CLUSTER, int BQ, int HALVES>
 __global__ void __launch_bounds__(NTH) gqa_simt_kernel(const GqaParams p) {
   constexpr int TM = BQ / TY, DIMS = 64 * HALVES, ld = row_ld(DIMS);
   pdl_enter();
   const int dh = p.head_dim, G = p.n_heads / p.n_kv;
   const int parts = p.splits, split = CLUSTER ? static_cast<int>(cluster_ctarank()) : (PAGED ? static_cast<int>(blockIdx.x) % parts : 0);
-  const int unit = blockIdx.x / parts;
+  // causal: a sequence's last rows, which see the most keys, first
+  const int unit = PAGED ? blockIdx.x / parts : (gridDim.x - 1 - blockIdx.x) / parts;
   int b, kvh, R0;
   if (PAGED) {
     const int tiles = (p.max_new * G + BQ - 1) / BQ;
@@ -392,33 +393,44 @@ __global__ void __launch_bounds__(256) gqa_merge_kernel(const GqaParams p) {
         make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
 }
 
-long causal_units(const GqaParams& p) { return (static_cast<long>(p.T_cap) * (p.n_heads / p.n_kv) / BQ + p.B) * p.n_kv; }
-long paged_units(int B, int n_heads, int n_kv, int max_new) {
-  return static_cast<long>(B) * n_kv * ((static_cast<long>(max_new) * (n_heads / n_kv) + BQ - 1) / BQ);
+long causal_units(const GqaParams& p, int rows) { return (static_cast<long>(p.T_cap) * (p.n_heads / p.n_kv) / rows + p.B) * p.n_kv; }
+long paged_units(int B, int n_heads, int n_kv, int max_new, int rows) {
+  return static_cast<long>(B) * n_kv * ((static_cast<long>(max_new) * (n_heads / n_kv) + rows - 1) / rows);
 }
+// Rows of a block: 32, or 16 where blocks of 32 would leave SMs idle.  us at 32 / 16: prompts of
+// 1 .. 300 rows, 4 heads of 64 (96 blocks) 16.1 / 13.9; eight drafts of 8 rows over 300 .. 3000
+// (16) 37 / 31; one prompt of 2000, 4 heads of 128 (251) 167 / 204; eight of 300, 8 heads of 64
+// (664) 43.9 / 44.4.
+int block_rows(long units_of_32, int num_sms) { return units_of_32 <= num_sms ? 16 : 32; }
 
-template <bool PAGED, bool CLUSTER, int HALVES>
+template <bool PAGED, bool CLUSTER, int BQ, int HALVES>
 cudaError_t launch_typed(const GqaParams& p, cudaStream_t st) {
-  const long blocks = (PAGED ? paged_units(p.B, p.n_heads, p.n_kv, p.max_new) : causal_units(p)) * p.splits;
+  const long blocks = (PAGED ? paged_units(p.B, p.n_heads, p.n_kv, p.max_new, BQ) : causal_units(p, BQ)) * p.splits;
   if (blocks > 0x7fffffffL) return cudaErrorInvalidValue;
+  constexpr int smem = 4 * smem_floats(BQ, 64 * HALVES);
   static bool attr_set[64] = {};
-  cudaError_t e = set_smem_limit_once(gqa_simt_kernel<PAGED, CLUSTER, HALVES>, 4 * smem_floats(64 * HALVES), attr_set);
+  cudaError_t e = set_smem_limit_once(gqa_simt_kernel<PAGED, CLUSTER, BQ, HALVES>, smem, attr_set);
   if (e != cudaSuccess) return e;
-  e = launch_kernel_overlap(launch_overlap_enabled(), CLUSTER ? p.splits : 1, gqa_simt_kernel<PAGED, CLUSTER, HALVES>,
-                            dim3(static_cast<unsigned>(blocks)), dim3(NTH), 4 * smem_floats(64 * HALVES), st, p);
+  e = launch_kernel_overlap(launch_overlap_enabled(), CLUSTER ? p.splits : 1, gqa_simt_kernel<PAGED, CLUSTER, BQ, HALVES>,
+                            dim3(static_cast<unsigned>(blocks)), dim3(NTH), smem, st, p);
   if (e != cudaSuccess || !PAGED || p.splits == 1) return e;
   const long warps = static_cast<long>(p.B) * p.max_new * p.n_heads;
   return launch_kernel(gqa_merge_kernel, dim3(static_cast<unsigned>((warps + 7) / 8)), dim3(256), 0, st, p);
 }
-template <bool PAGED, bool CLUSTER>
+template <bool PAGED, bool CLUSTER, int BQ>
 cudaError_t launch_halves(const GqaParams& p, cudaStream_t st) {
-  return p.head_dim <= 64 ? launch_typed<PAGED, CLUSTER, 1>(p, st) : launch_typed<PAGED, CLUSTER, 2>(p, st);
+  return p.head_dim <= 64 ? launch_typed<PAGED, CLUSTER, BQ, 1>(p, st) : launch_typed<PAGED, CLUSTER, BQ, 2>(p, st);
+}
+template <bool PAGED, bool CLUSTER>
+cudaError_t launch_rows(const GqaParams& p, int rows, cudaStream_t st) {
+  return rows == 16 ? launch_halves<PAGED, CLUSTER, 16>(p, st) : launch_halves<PAGED, CLUSTER, 32>(p, st);
 }
 
 }  // namespace
 
 int gqa_simt_splits(int B, int n_heads, int n_kv, int max_new, int num_sms) {
-  const long units = paged_units(B, n_heads, n_kv, max_new);
+  const int rows = block_rows(paged_units(B, n_heads, n_kv, max_new, 32), num_sms);
+  const long units = paged_units(B, n_heads, n_kv, max_new, rows);
   const long s = (4l * num_sms + units - 1) / units;
   return static_cast<int>(s < 1 ? 1 : (s > 32 ? 32 : s));
 }
@@ -431,13 +443,15 @@ size_t gqa_simt_part_bytes(int B, int n_heads, int n_kv, int head_dim, int max_n
 cudaError_t launch_gqa_simt(bool paged, const GqaParams& args, int num_sms, cudaStream_t st) {
   GqaParams p = args;
   if (p.T_cap <= 0) return cudaSuccess;
-  if (paged) return launch_halves<true, false>(p, st);
+  if (paged)
+    return launch_rows<true, false>(p, block_rows(paged_units(p.B, p.n_heads, p.n_kv, p.max_new, 32), num_sms), st);
+  const int rows = block_rows(causal_units(p, 32), num_sms);
   // causal: blocks that share a tile's keys, as many as the SMs hold at once, where
   // prompts have the tiles to share on average
-  const long units = causal_units(p);
+  const long units = causal_units(p, rows);
   p.splits = 1;
   while (p.splits < MAX_PARTS && units * p.splits * 2 <= 4l * num_sms && p.T_cap / p.B >= KT * p.splits) p.splits *= 2;
-  return p.splits > 1 ? launch_halves<false, true>(p, st) : launch_halves<false, false>(p, st);
+  return p.splits > 1 ? launch_rows<false, true>(p, rows, st) : launch_rows<false, false>(p, rows, st);
 }
 
 }  // namespace seer
