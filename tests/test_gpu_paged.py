@@ -589,6 +589,17 @@ def test_causal_many_short_prompts(dt):
     assert S.seer_check_device() == 0
 
 
+@pytest.mark.parametrize("hq,hk,dh", [(32, 8, 128), (8, 8, 64), (16, 2, 128)])
+def test_causal_many_units_per_sm(hq, hk, dh):
+    """Dozens of short units in a row on every SM, after a few long ones."""
+    rng = np.random.default_rng(27)
+    lens = [700] + [int(v) for v in rng.integers(1, 200, 150)] + [400]
+    x, cu = causal_case(rng, lens, hq, hk, dh, "bf16")
+    ref, bound = causal_ref(x, cu, hq, hk, dh, "bf16")
+    close(host(run_causal(x, cu, hq, hk, dh, "bf16")).reshape(ref.shape), ref, bound)
+    assert S.seer_check_device() == 0
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_tree_many_requests(dt):
     rng = np.random.default_rng(25)
