@@ -11,7 +11,7 @@ namespace {
 // Bound by latency (launch, two dependent loads, the scan): 8 B + 4 bytes a page + 8 to
 // 20 bytes a row is little.  Every block repeats the scan of the whole batch, so that
 // rows need no second launch; rows then spread over the grid and find their request by
-// bisection in shared memory.
+// bisection in shared memory.  8 requests of one row 2.6 us, 256 prompts (93k rows) 4.9.
 constexpr int kTableThreads = 256;
 
 // Exclusive prefix of v over the block's threads, and the block's total; two values at once.
@@ -222,7 +222,8 @@ constexpr int kAppendRows = 4;
 // Bound by HBM.  A block takes up to four rows, so that their sines are one a thread, and a
 // thread UNROLL of their items (16 bytes of a head's lower half and the 16 of its upper half),
 // loads ahead of the stores.  Sines and cosines lie in groups of four, the groups of
-// neighbouring lanes side by side (pair by pair they met 8 times in a bank).
+// neighbouring lanes side by side (pair by pair they met 8 times in a bank).  17.9k rows of
+// 32 + 8 + 8 heads of 128, 479 MB, 73 us (6.5 TB/s; one item a thread at a time 88); 64 rows 2.9.
 template <int T, bool ROTATE>
 __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const KvAppendArgs a, const __grid_constant__ TurnRates rates) {
   pdl_enter();
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const KvAppen
 // Cache row cached + k of a request becomes its row cached + accepted[k], in ascending k.
 // accepted ascends strictly, so accepted[k] >= k and a row is read before a later k could
 // overwrite it; a thread moves the same 16 bytes of every row in that order, eight rows'
-// loads ahead of their stores.  Latency: a few rows a request.
+// loads ahead of their stores.  Latency: a few rows a request (128 requests 2.3 us).
 constexpr int kAcceptThreads = 128;
 
 __global__ void __launch_bounds__(kAcceptThreads) kv_accept_kernel(const KvAcceptArgs a) {

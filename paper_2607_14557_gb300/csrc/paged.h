@@ -79,6 +79,8 @@ struct KvAcceptArgs {
 constexpr int kMaxDraft = 64;
 cudaError_t launch_kv_accept(const KvAcceptArgs& a, cudaStream_t st);
 
+// Keys of a request at most, so that a tile past them still has a 32-bit number.
+constexpr int kMaxKeys = 0x7fffffff - 1024;
 // Attention of grouped heads: query head h reads key/value head h / (n_heads / n_kv).
 struct GqaParams {
   const void* q;          // [T_cap, ld_q]

@@ -446,7 +446,7 @@ def test_tree_rows_that_see_all_or_nothing(dt, dh, kind):
 
 
 @pytest.mark.parametrize("dt,dh", [("bf16", 128), ("f32", 64)])
-@pytest.mark.parametrize("hq,hk,B", [(32, 8, 3), (64, 1, 2), (16, 16, 1), (9, 3, 40)])
+@pytest.mark.parametrize("hq,hk,B", [(32, 8, 3), (64, 1, 2), (128, 1, 2), (16, 16, 1), (9, 3, 40)])
 def test_tree_many_heads_and_requests(dt, dh, hq, hk, B):
     rng = np.random.default_rng(B)
     ctx = [int(v) for v in rng.integers(0, 900, B)]
@@ -508,7 +508,7 @@ def test_tree_records_lengths_that_do_not_fit():
     pool = Pool(rng, [64, 64], 16, 2, 128, "bf16")
     q = rnd(rng, (6, 4 * 128), "bf16")
     for cu, kv_len in (([0, 2, 4], [65, 64]), ([0, 2, 4], [1, 64]), ([0, 2, 7], [60, 64]), ([-1, 2, 4], [60, 64]), ([0, 4, 6], [60, 64]),
-                       ([0, 2, 4], [-5, 64]), ([0, 2, 1], [60, 64]), ([0, 2, 4], [2 ** 31 - 1, 64])):
+                       ([0, 2, 4], [-5, 64]), ([0, 2, 1], [60, 64]), ([0, 2, 4], [2 ** 31 - 1, 64]), ([0, 2, 4], [-2 ** 31, 64])):
         o = run_tree(pool, q, cu, kv_len, 4, "bf16", draft=3)
         assert S.seer_check_device() == 2, (cu, kv_len)
         if cu[2] == 4 and kv_len != [60, 64]:               # the other request's rows are there
