@@ -359,7 +359,8 @@ seer_status seer_gather_response(const void* x_packed, seer_dtype dt, const int3
  * Query head h reads key/value head h / (n_heads / n_kv_heads).
  * What the device finds inconsistent (lengths outside the buffers, pages outside
  * the pool, too few free pages) is recorded (seer_check_device) and that
- * request's or row's part left out; no access leaves the buffers named.
+ * request's or row's part left out; no access leaves the buffers named.  T_cap is at
+ * most 2^30; masks are 8-byte aligned.
  * ------------------------------------------------------------------------- */
 #define SEER_MAX_DRAFT 64          /* new rows of a request that a tree can hold */
 #define SEER_MAX_REQUESTS 16384    /* requests of a call */
@@ -379,7 +380,8 @@ typedef struct {
  * are packed, rows cu_new_out[b] .. cu_new_out[b+1] - 1.  It owns the first
  * ceil(cached_len / page_size) entries of its table row; the entries up to
  * ceil((cached_len + new_len) / page_size) are taken from the free list, requests in
- * order, from free_pages[*free_head] on, and written to the table.
+ * order, from free_pages[*free_head] on, and written to the table.  A request holds
+ * at most max_pages * page_size rows, and at most 2^31 - 1025.
  *   kv_len_out[b]   = cached_len[b] + new_len[b]      (device int32 [B])
  *   slot_out[r]     = the pool row of new row r, -1 where it has none
  *   position_out[r] = cached_len[b] + i of the request's i-th new row, or, with
@@ -393,8 +395,8 @@ typedef struct {
  * T_cap           rows of slot_out, position_out, mask_out and parent; rows past
  *                 cu_new_out[B] are untouched
  * With parent or mask_out a request has at most SEER_MAX_DRAFT new rows.  Table
- * entries of taken pages beyond the free list become -1.  Every output depends on
- * the inputs alone, so a call may be repeated. */
+ * entries of taken pages beyond the free list become -1.  No output is an input.
+ * Every output depends on the inputs alone, so a call may be repeated. */
 seer_status seer_page_tables(const int32_t* cached_len, const int32_t* new_len, int B, int page_size, int n_pages,
                              const int32_t* free_pages, int n_free, const int32_t* free_head, int32_t* table,
                              int max_pages, int T_cap, const int32_t* parent, int32_t* cu_new_out, int32_t* kv_len_out,
@@ -406,9 +408,10 @@ seer_status seer_page_tables(const int32_t* cached_len, const int32_t* new_len, 
  * slots, the keys turned by their position as in seer_rope (theta 0: as they are).
  * rotated, when not NULL, receives the turned q | k of every row (ld_rotated values
  * per row); it may be qkv itself with its ld.  Rows: M_dev (device int32, may be
- * NULL) overrides T_cap.  slot -1: nothing is stored for the row; two rows of a call
- * with one slot leave either there.  position: device int32 [T_cap], NULL when
- * theta is 0.  Angles are exact to fp32 at any position; one rounding per value. */
+ * NULL) overrides T_cap.  slot -1: nothing is stored for the row; slots of a call
+ * are distinct (two rows with one leave pieces of either there).  position: device
+ * int32 [T_cap], NULL when theta is 0; theta is 0 or at least 1.  Angles are exact to
+ * fp32 at any position; one rounding per value. */
 seer_status seer_kv_append(const void* qkv, int ld_qkv, seer_dtype dt, int n_heads, int T_cap, const int32_t* M_dev,
                            const int32_t* slot, const int32_t* position, float theta, void* rotated, int ld_rotated,
                            const seer_pages* pages, void* stream);

@@ -15,6 +15,10 @@ namespace {
 
 // Row numbers are 32-bit; a page past the pool's end is one too.
 constexpr long long kMaxPoolRows = 0x7fffffffll - 1024;
+// Row loops step by a grid's worth of rows in 32 bits.
+constexpr int kMaxRows = 1 << 30;
+// Key tiles of a tree call at most, by its capacities: places on its line times runs stay in 64 bits.
+constexpr double kMaxTreeTiles = 1125899906842624.0;   // 2^50
 
 int log2_exact(int v) {
   int s = 0;
@@ -31,6 +35,12 @@ seer_status check_page_size(const char* what, int page_size) {
 seer_status check_requests(const char* what, int B) {
   if (B <= 0) return fail(SEER_ERR_INVALID_ARG, "%s: B must be positive", what);
   if (B > SEER_MAX_REQUESTS) return fail(SEER_ERR_UNSUPPORTED, "%s: at most %d requests", what, SEER_MAX_REQUESTS);
+  return SEER_OK;
+}
+
+seer_status check_capacity(const char* what, int T_cap) {
+  if (T_cap < 0) return fail(SEER_ERR_INVALID_ARG, "%s: bad sizes", what);
+  if (T_cap > kMaxRows) return fail(SEER_ERR_UNSUPPORTED, "%s: at most %d rows", what, kMaxRows);
   return SEER_OK;
 }
 
@@ -107,15 +117,19 @@ seer_status seer_page_tables(const int32_t* cached_len, const int32_t* new_len, 
   SEER_TRY(check_page_size("page tables", page_size));
   if (!cached_len || !new_len || !free_head || !table || !cu_new_out || !kv_len_out || !free_head_out)
     return fail(SEER_ERR_INVALID_ARG, "page tables: null pointer");
-  if (n_pages <= 0 || max_pages <= 0 || n_free < 0 || T_cap < 0)
-    return fail(SEER_ERR_INVALID_ARG, "page tables: bad sizes");
+  if (n_pages <= 0 || max_pages <= 0 || n_free < 0) return fail(SEER_ERR_INVALID_ARG, "page tables: bad sizes");
+  SEER_TRY(check_capacity("page tables", T_cap));
   if (n_free > 0 && !free_pages) return fail(SEER_ERR_INVALID_ARG, "page tables: free_pages is null");
   if (T_cap > 0 && (!slot_out || !position_out)) return fail(SEER_ERR_INVALID_ARG, "page tables: null row output");
   if (static_cast<long long>(n_pages) * page_size > kMaxPoolRows)
     return fail(SEER_ERR_UNSUPPORTED, "page tables: the pool has more than %lld rows", kMaxPoolRows);
-  if (free_head == free_head_out || cached_len == kv_len_out || new_len == kv_len_out || new_len == cu_new_out ||
-      cached_len == cu_new_out)
-    return fail(SEER_ERR_INVALID_ARG, "page tables: an output is also an input");
+  if (reinterpret_cast<uintptr_t>(mask_out) % 8 != 0) return fail(SEER_ERR_UNSUPPORTED, "page tables: mask_out must be 8-byte aligned");
+  // every block reads the inputs, so no block's outputs may replace them
+  const void* const in[] = {cached_len, new_len, free_head, free_pages, parent};
+  const void* const out[] = {cu_new_out, kv_len_out, free_head_out, table, slot_out, position_out, mask_out};
+  for (const void* i : in)
+    for (const void* o : out)
+      if (i != nullptr && i == o) return fail(SEER_ERR_INVALID_ARG, "page tables: an output is also an input");
   DeviceInfo* di;
   SEER_TRY(device_info(&di));
   PageTableArgs a{};
@@ -149,7 +163,8 @@ seer_status seer_kv_append(const void* qkv, int ld_qkv, seer_dtype dt, int n_hea
                            const seer_pages* pages, void* stream) {
   KvAppendArgs a{};
   SEER_TRY(check_pages("append", pages, dt, &a.pages));
-  if (n_heads < 0 || T_cap < 0) return fail(SEER_ERR_INVALID_ARG, "append: bad sizes");
+  if (n_heads < 0) return fail(SEER_ERR_INVALID_ARG, "append: bad sizes");
+  SEER_TRY(check_capacity("append", T_cap));
   const int dh = pages->head_dim;
   const long long q = static_cast<long long>(n_heads) * dh, k = static_cast<long long>(pages->n_kv_heads) * dh;
   if (q > (1 << 20)) return fail(SEER_ERR_UNSUPPORTED, "append: rows of more than 2^20 query values");
@@ -157,7 +172,8 @@ seer_status seer_kv_append(const void* qkv, int ld_qkv, seer_dtype dt, int n_hea
   if (rotated) SEER_TRY(check_rows("append", "rotated", rotated, ld_rotated, q + k, dt));
   if (rotated == qkv && ld_rotated != ld_qkv) return fail(SEER_ERR_INVALID_ARG, "append: in place, rotated has qkv's ld");
   if (!slot) return fail(SEER_ERR_INVALID_ARG, "append: slot is null");
-  if (!(theta >= 0.f) || !std::isfinite(theta)) return fail(SEER_ERR_INVALID_ARG, "append: theta must be 0 (off) or a finite positive base");
+  if (!(theta == 0.f || theta >= 1.f) || !std::isfinite(theta))
+    return fail(SEER_ERR_INVALID_ARG, "append: theta must be 0 (off) or a finite base from 1 on");
   if (theta > 0.f && !position) return fail(SEER_ERR_INVALID_ARG, "append: rotation needs positions");
   DeviceInfo* di;
   SEER_TRY(device_info(&di));
@@ -175,9 +191,9 @@ seer_status seer_kv_append(const void* qkv, int ld_qkv, seer_dtype dt, int n_hea
   TurnRates rates{};
   if (theta > 0.f)
     for (int i = 0; i < dh / 2; ++i) {
-      // turns per position; bases below 1 turn faster than once a row, and whole turns drop out
+      // turns per position, less than 1 / 6
       const double turns = std::exp2(-2.0 * i / dh * std::log2(static_cast<double>(theta))) / 6.283185307179586476925;
-      rates.rate[i] = static_cast<uint64_t>((turns - std::floor(turns)) * 18446744073709551616.0);
+      rates.rate[i] = static_cast<uint64_t>(turns * 18446744073709551616.0);
     }
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   Phase ph(PH_KV, st);
@@ -216,7 +232,7 @@ seer_status seer_attention_causal(const void* q, int ld_q, const void* k, int ld
                                   int n_kv_heads, int head_dim, void* stream) {
   SEER_TRY(check_requests("causal attention", B));
   SEER_TRY(check_heads("causal attention", n_heads, n_kv_heads, head_dim, dt));
-  if (T_cap < 0) return fail(SEER_ERR_INVALID_ARG, "causal attention: bad sizes");
+  SEER_TRY(check_capacity("causal attention", T_cap));
   if (!cu_seqlens) return fail(SEER_ERR_INVALID_ARG, "causal attention: cu_seqlens is null");
   const long long qc = static_cast<long long>(n_heads) * head_dim, kc = static_cast<long long>(n_kv_heads) * head_dim;
   SEER_TRY(check_rows("causal attention", "q", q, ld_q, qc, dt));
@@ -280,10 +296,13 @@ seer_status seer_attention_tree(const void* q, int ld_q, void* o, int ld_o, seer
   SEER_TRY(check_requests("tree attention", B));
   SEER_TRY(check_pages("tree attention", pages, dt, &pg));
   SEER_TRY(check_heads("tree attention", n_heads, pages->n_kv_heads, pages->head_dim, dt));
-  if (T_cap < 0) return fail(SEER_ERR_INVALID_ARG, "tree attention: bad sizes");
+  SEER_TRY(check_capacity("tree attention", T_cap));
   if (max_draft < 1 || max_draft > SEER_MAX_DRAFT)
     return fail(SEER_ERR_INVALID_ARG, "tree attention: max_draft must be in [1, %d]", SEER_MAX_DRAFT);
   if (!cu_new || !kv_len) return fail(SEER_ERR_INVALID_ARG, "tree attention: null pointer");
+  if (reinterpret_cast<uintptr_t>(mask) % 8 != 0) return fail(SEER_ERR_UNSUPPORTED, "tree attention: mask must be 8-byte aligned");
+  if (static_cast<double>(B) * pages->n_kv_heads * max_draft * (static_cast<double>(pages->max_pages) * pages->page_size / 128 + 8) > kMaxTreeTiles)
+    return fail(SEER_ERR_UNSUPPORTED, "tree attention: more key tiles than 2^50 fit the tables");
   const long long qc = static_cast<long long>(n_heads) * pages->head_dim;
   SEER_TRY(check_rows("tree attention", "q", q, ld_q, qc, dt));
   SEER_TRY(check_rows("tree attention", "o", o, ld_o, qc, dt));

@@ -297,6 +297,8 @@ def make_pages(kv, table, n_pages, page_size, max_pages, n_kv_heads, head_dim) -
         raise ValueError("kv must be contiguous and hold n_pages * page_size rows of 2 * n_kv_heads * head_dim values")
     if isinstance(table, torch.Tensor) and (table.dtype != torch.int32 or not table.is_contiguous()):
         raise ValueError("table must be a contiguous int32 tensor")
+    if isinstance(kv, torch.Tensor) and isinstance(table, torch.Tensor) and kv.device != table.device:
+        raise ValueError("kv and table are on different devices")
     return seer_pages(_p(kv), _p(table), n_pages, page_size, max_pages, n_kv_heads, head_dim)
 
 

@@ -44,6 +44,15 @@ def test_page_tables_refuse(L, kw, status):
     assert tables(L, **kw) == status and b"page tables" in L.seer_last_error()
 
 
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=(1 << 30) + 1), UNSUPPORTED), (dict(mask=64 * P + 4), UNSUPPORTED), (dict(slot=16 * P), INVALID), (dict(pos=16 * P), INVALID),
+    (dict(mask=16 * P), INVALID), (dict(table=8 * P), INVALID), (dict(slot=9 * P), INVALID)])
+def test_page_tables_refuse_sizes_and_shared_buffers(L, kw, status):
+    a = dict(free=8 * P, head=9 * P, table=10 * P, slot=11 * P, pos=12 * P, parent=16 * P)
+    a.update(kw)
+    assert tables(L, **a) == status and b"page tables" in L.seer_last_error()
+
+
 def append(L, pg=None, **kw):
     a = dict(qkv=P, ld=4 * 64 + 4 * 64, dt=1, heads=4, T=8, M=None, slot=P, pos=P, theta=1e4, rot=2 * P, ld_rot=6 * 64)
     a.update(kw)
@@ -67,6 +76,11 @@ def test_append_refuses_pools(L, pg, status):
     (dict(theta=-1.0), INVALID), (dict(theta=math.nan), INVALID), (dict(theta=math.inf), INVALID), (dict(T=-1), INVALID),
     (dict(heads=-1), INVALID), (dict(dt=3), INVALID)])
 def test_append_refuses(L, kw, status):
+    assert append(L, **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [(dict(T=(1 << 30) + 1), UNSUPPORTED), (dict(theta=0.5), INVALID), (dict(theta=1e-40), INVALID)])
+def test_append_refuses_rows_and_bases(L, kw, status):
     assert append(L, **kw) == status
 
 
@@ -104,6 +118,18 @@ def test_tree_refuses(L, kw, status):
     a = dict(q=P, ld_q=256, o=2 * P, ld_o=256, dt=1, cu=P, kv=P, mask=None, B=2, T=8, hq=4, draft=4)
     a.update(kw)
     assert L.seer_attention_tree(*a.values(), ctypes.byref(pages()), P, 1 << 30, None) == status
+
+
+def test_attention_refuses_row_counts_past_30_bits(L):
+    assert causal(L, T=(1 << 30) + 1) == UNSUPPORTED
+    assert L.seer_attention_tree(P, 256, 2 * P, 256, 1, P, P, None, 2, (1 << 30) + 1, 4, 4, ctypes.byref(pages()), P, 1 << 30, None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("mask,pg", [(P + 4, {}), (None, dict(n_kv_heads=1 << 14, max_pages=(1 << 31) - 1, page_size=1024))])
+def test_tree_refuses_odd_masks_and_endless_tables(L, mask, pg):
+    hk = pg.get("n_kv_heads", 2)
+    st = L.seer_attention_tree(P, hk * 64, 2 * P, hk * 64, 1, P, P, mask, 16384 if pg else 2, 8, hk, 4, ctypes.byref(pages(**pg)), P, 1 << 30, None)
+    assert st == UNSUPPORTED and (b"aligned" if mask else b"2^50") in L.seer_last_error()
 
 
 @pytest.mark.parametrize("args,status", [((1, 0, 4, 2, 64, 8), INVALID), ((1, 2, 5, 2, 64, 8), INVALID), ((1, 2, 4, 2, 80, 8), UNSUPPORTED),
