@@ -10,6 +10,7 @@
 #include <stdexcept>
 #include <string>
 #include <tuple>
+#include <type_traits>
 
 #include "../../include/seer.h"
 
@@ -47,7 +48,7 @@ struct Arg {                                // integers
   static T get(PyObject* o, int) {
     const long long v = PyLong_AsLongLong(o);
     if (v == -1 && PyErr_Occurred()) throw PythonError();
-    if (static_cast<long long>(static_cast<T>(v)) != v) throw Refused("an integer argument is out of range");
+    if (static_cast<long long>(static_cast<T>(v)) != v || (v < 0 && std::is_unsigned_v<T>)) throw Refused("an integer argument is out of range");
     return static_cast<T>(v);
   }
 };

@@ -267,12 +267,12 @@ __global__ void __launch_bounds__(NTH) gqa_simt_kernel(const GqaParams p) {
       }
     };
     if (odd) {                                // a key that a row does not see adds nothing, whatever its value
-      for (int k = 0; k < valid; ++k)
+      for (int k = 0; k < valid; ++k) {       // (a seen one adds even with a weight of 0)
+        const int a = k0 + k - sp.ctx;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          const float w = Ps[(ty + TY * i) * PS + k];
-          if (w != 0.f) add(i, w, Vs + k * ld);
-        }
+        for (int i = 0; i < TM; ++i)
+          if (a < 0 || (chain ? a <= tok[i] : ((bits[i] >> a) & 1) != 0)) add(i, Ps[(ty + TY * i) * PS + k], Vs + k * ld);
+      }
     } else {
       const int keys = min(KT, (valid + 3) & ~3);   // past the valid keys P is 0 and V zero-filled
 #pragma unroll 2
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(NTH) gqa_simt_kernel(const GqaParams p) {
           const uint32_t ml = cluster_addr(Ms + 2 * r, k);
           const float weight = ld_cluster(ml + 4), w = weight == 0.f ? 0.f : expf(ld_cluster(ml) - base);
           total += weight * w;
-          if (w != 0.f) {                     // a share without a seen key adds nothing
+          if (weight != 0.f) {                // a share without a seen key adds nothing
             const float4 v = ld_cluster4(cluster_addr(Vs + r * ld + c, k));
             acc = make_float4(fmaf(w, v.x, acc.x), fmaf(w, v.y, acc.y), fmaf(w, v.z, acc.z), fmaf(w, v.w, acc.w));
           }

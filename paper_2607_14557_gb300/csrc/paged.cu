@@ -59,7 +59,7 @@ __device__ __forceinline__ Request read_request(const PageTableArgs& a, int b, b
     c = max(c, 0);
     n = max(n, 0);
   }
-  const long long room = static_cast<long long>(a.max_pages) << a.page_shift;
+  const long long room = min(static_cast<long long>(a.max_pages) << a.page_shift, static_cast<long long>(kMaxKeys));
   const long long total = static_cast<long long>(c) + n;
   if (total > room && report) record_error(a.err, kErrCapacity);
   if (n > kMaxDraft && (a.parent || a.mask) && report) record_error(a.err, kErrLayout);
@@ -143,13 +143,15 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(const PageTa
     const int i = row - cu[lo];
     const long long at = static_cast<long long>(r.cached) + i;
     const long long page_index = at >> a.page_shift;
-    int page = -1;                 // a row past the table has no slot
+    int page = -1;                 // a row past the request's room has no slot
     // entries that were there are read from the table, new ones from the free list: other
     // blocks may not have written them yet
-    if (page_index < r.old_pages)
-      page = checked_page(a, a.table[static_cast<size_t>(lo) * a.max_pages + page_index], kErrLayout, true);
-    else if (page_index < r.pages)
-      page = free_page(a, first[lo] + page_index - r.old_pages, false);
+    if (at < r.kv_len) {
+      if (page_index < r.old_pages)
+        page = checked_page(a, a.table[static_cast<size_t>(lo) * a.max_pages + page_index], kErrLayout, true);
+      else
+        page = free_page(a, first[lo] + page_index - r.old_pages, false);
+    }
     a.slot[row] = page < 0 ? -1 : page * page_rows + static_cast<int>(at & (page_rows - 1));
     int depth = i;
     uint64_t bits = 0;

@@ -146,6 +146,19 @@ def test_page_tables_record_what_does_not_fit(what, code):
         assert t["mask"].tolist()[:70] == [0] * 70 and t["mask"].tolist()[70:] == [1 << i for i in range(9)]
 
 
+def test_page_tables_requests_of_nearly_2_31_rows():
+    table = torch.zeros((1, 1 << 22), dtype=torch.int32, device=cuda())
+    top = 2 ** 31 - 1025
+    for c, n, code, kv, slot in [(top - 2, 2, 0, top, [1021, 1022]), (top - 1, 2, 5, top, [1022, -1]), (2 ** 31 - 1, 1, 5, top, [-1]),
+                                 (2 ** 31 - 1, 2 ** 31 - 1, 5, top, [-1])]:
+        out = [i32([-7] * 2), i32([-7]), i32([-7] * 2), i32([-7] * 2), i32([-7])]
+        S.seer_page_tables(i32([c]), i32([n]), 1, 1024, 5, i32([3, 4]), 2, i32([0]), table, 1 << 22, min(n, 2), None, out[0], out[1], out[2],
+                           out[3], None, out[4])
+        got = S.seer_check_device()
+        assert got == code or (code and got == 1)            # (more rows than slot_out holds is recorded too)
+        assert out[1].tolist() == [kv] and out[4].tolist() == [0] and out[2].tolist()[:len(slot)] == slot
+
+
 # ------------------------------------------------------------------ append
 class Pool:
     """A pool of pages, a table of random pages for requests of kv rows each."""
@@ -216,6 +229,18 @@ def test_append_records_slots_outside_the_pool_and_bad_row_counts():
     assert torch.equal(pool.kv[1], x[0, 128:]) and torch.equal(pool.kv[2], x[1, 128:])
     S.seer_kv_append(x, 384, "bf16", 2, 0, None, i32([1]), None, 0.0, None, 0, pool.struct)
     assert S.seer_check_device() == 0
+
+
+def test_append_rows_with_one_slot_leave_pieces_of_either():
+    rng = np.random.default_rng(1)
+    pool = Pool(rng, [40], 16, 2, 64, "bf16")
+    x = rnd(rng, (8, 6 * 64), "bf16")
+    before = pool.kv.clone()
+    S.seer_kv_append(x, 384, "bf16", 2, 8, None, i32([5] * 8), None, 0.0, None, 0, pool.struct)
+    got, rows = pool.kv[5].reshape(-1, 8), x[:, 128:].reshape(8, -1, 8)
+    assert (got == rows).all(-1).any(0).all()
+    before[5] = pool.kv[5]
+    assert torch.equal(before, pool.kv) and S.seer_check_device() == 0
 
 
 # ------------------------------------------------------------------ accept
@@ -342,6 +367,26 @@ def test_causal_infinite_values_reach_their_column_alone(dt, dh):
     keep = np.ones(ref.shape, bool)
     keep[150:, :, 5] = False
     close(got[keep], ref[keep], bound[keep])
+    S.seer_check_device()
+
+
+@pytest.mark.parametrize("dt,dh", [("bf16", 128), ("f16", 64), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("n", [300, 1400])
+def test_causal_a_seen_nan_counts_whatever_its_weight(dt, dh, n):
+    """Rows 3 and 257 score 0 where the keys from 130 on score dh * 25 / sqrt(dh) >= 200: e^-200 is 0 in 32 bits."""
+    x = torch.zeros((n, 3 * dh), dtype=TDT[dt], device=cuda())
+    x[:, :dh] = 5.0
+    x[130:, dh:2 * dh] = 5.0
+    x[257, dh:2 * dh] = 0.0
+    x[:, 2 * dh:] = 1.0
+    x[3, 2 * dh] = math.nan
+    x[257, 2 * dh + 1] = math.nan
+    o = host(run_causal(x, [0, n], 1, 1, dh, dt))
+    want = np.ones((n, dh))
+    want[3:, 0] = math.nan
+    want[257:, 1] = math.nan
+    assert np.array_equal(np.isnan(o), np.isnan(want))
+    close(np.nan_to_num(o, nan=1.0), np.ones((n, dh)), 2.0 ** -7)
     S.seer_check_device()
 
 
@@ -804,5 +849,8 @@ def test_binding_refuses_tensors_elsewhere():
     g = x.to(cuda())
     with pytest.raises(ValueError, match="current device"):
         S.seer_attention_causal(x, 512, g, 512, g, 512, g.clone(), 512, "bf16", i32([0, 4]), 1, 4, 2, 1, 128)
+    pool = Pool(np.random.default_rng(0), [40], 16, 2, 128, "bf16")
+    with pytest.raises(ValueError, match="range"):          # a workspace of -1 bytes is not a large one
+        S.seer_attention_tree(g, 512, g.clone(), 512, "bf16", i32([0, 4]), i32([40]), None, 1, 4, 4, 4, pool.struct, g, -1)
     with pytest.raises(ValueError, match="Int"):
         S.seer_attention_causal(g, 512, g[:, 256:], 512, g[:, 384:], 512, g.clone(), 512, "bf16", i32([0, 4]).long(), 1, 4, 2, 1, 128)
