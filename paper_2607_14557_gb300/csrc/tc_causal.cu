@@ -29,8 +29,9 @@
 // P is exponentiated in fp32 and rounded to the 16-bit type that the PV MMA reads; the row
 // sums add the rounded values, so numerator and normaliser carry the same rounding.
 // A key that a row does not see has P = 0, which an infinite or NaN value row would still
-// turn into NaN in the MMA.  So value rows past the unit's last token are cleared, and a
-// masked tile with a non-finite value sends the unit's rows to recompute_row().
+// turn into NaN in the MMA.  So value rows past the unit's last token are cleared, and the
+// rows of a unit with a non-finite value in a masked tile are left to recompute_units() after
+// the last unit, when no wait with a time limit is pending.
 #include <math.h>
 
 #include "attn_math.cuh"
@@ -65,8 +66,8 @@ struct Layout {
 };
 // up to 199680 bytes leave 60 KB of the SM to L1
 static_assert(Layout<128>::BYTES <= 199680, "L1 carve-out");
-// barriers, the unit ring, the odd-value marks, the TMEM base and the abort flag
-static_assert(8 * (2 + 4 * STAGES + 6 * NT + 2 * U_SLOTS) + 16 * U_SLOTS + 16 * NT + 8 <= BAR_BYTES, "barrier block");
+// barriers, the unit ring, the odd-value marks, the TMEM base and two flags
+static_assert(8 * (2 + 4 * STAGES + 6 * NT + 2 * U_SLOTS) + 16 * U_SLOTS + 16 * NT + 12 <= BAR_BYTES, "barrier block");
 
 // seq0 < 0: no more units.
 struct Unit {
@@ -94,47 +95,108 @@ __device__ __forceinline__ Unit read_unit(uint64_t* u_full, uint64_t* u_empty, c
   return Unit{w.x, w.y, w.z, w.w};
 }
 
-// One row from global memory, key by key and 16 columns at a time: only for rows whose
-// unit met a non-finite value in a masked tile.
+// This CTA's units, by a whole warp: units in order of descending token group, the sequences that
+// reach a group counted once on the way.
+struct UnitWalk {
+  int span, H, lane;
+  int mine;                                 // units per head of sequence `lane`: the first 32 stay in registers
+  long total;
+  int g;                                    // units of group g: [base, base + count)
+  long base = 0, count = 0;
+  int b0 = 0, passed = 0;                   // sequences b0 .. hold the next unit; so many before them reach g
+
+  // Units of sequence b per head; 0 where it leaves the buffers.
+  __device__ __forceinline__ int groups_of(const GqaParams& p, int b, bool report) const {
+    if (b >= p.B) return 0;
+    const int c0 = p.cu[b], n = p.cu[b + 1] - c0;
+    const bool good = c0 >= 0 && n >= 0 && n <= p.T_cap - c0;
+    if (!good && report) record_error(p.err, kErrLayout);
+    return good ? (n + span - 1) / span : 0;
+  }
+  // Which of sequences x .. x + 31 have a group g.
+  __device__ __forceinline__ uint32_t reach(const GqaParams& p, int x) const {
+    const int n = x == 0 ? mine : groups_of(p, x + lane, false);
+    return __ballot_sync(0xffffffffu, n > g);
+  }
+  __device__ __forceinline__ UnitWalk(const GqaParams& p, int tpt, int lane_, bool report) : span(NT * tpt), H(p.n_kv), lane(lane_) {
+    mine = groups_of(p, lane, report);
+    int most = mine, sum = mine;
+    for (int b = lane + 32; b < p.B; b += 32) {
+      const int n = groups_of(p, b, report);
+      most = max(most, n);
+      sum += n;
+    }
+    g = __reduce_max_sync(0xffffffffu, most);
+    total = static_cast<long>(__reduce_add_sync(0xffffffffu, sum)) * H;
+  }
+  // The CTA's i-th unit, i ascending; seq0 < 0 past its last.
+  __device__ __forceinline__ int4 unit(const GqaParams& p, int i) {
+    const int grid = gridDim.x;
+    const long u = (i & 1) ? (i + 1l) * grid - 1 - blockIdx.x : static_cast<long>(i) * grid + blockIdx.x;
+    if (u >= total) return make_int4(-1, 0, 0, 0);
+    while (u >= base + count) {
+      base += count;
+      --g;
+      int n = 0;
+      for (int x = 0; x < p.B; x += 32) n += __popc(reach(p, x));
+      count = static_cast<long>(n) * H;
+      b0 = passed = 0;
+    }
+    const int k = static_cast<int>(u - base), nth = k / H;
+    int b = 0;
+    for (; b0 < p.B; b0 += 32) {            // a group's units come in order, so this goes on where it stopped
+      const uint32_t m = reach(p, b0);
+      if (nth - passed < __popc(m)) {
+        b = b0 + __fns(m, 0, nth - passed + 1);
+        break;
+      }
+      passed += __popc(m);
+    }
+    return make_int4(p.cu[b], p.cu[b + 1] - p.cu[b], g * span, k % H);
+  }
+};
+
+// The rows that a non-finite value in a masked tile may have reached, from global memory by
+// every warp of the CTA.  Its units are looked over once more, so that none need be remembered.
 template <bool F16, int DH>
-__device__ __noinline__ uint32_t recompute_row(const GqaParams& p, int seq0, int tok, int head, int kvh) {
-  const uint16_t* q = static_cast<const uint16_t*>(p.q) + static_cast<size_t>(seq0 + tok) * p.ld_q + head * DH;
-  const uint16_t* k = static_cast<const uint16_t*>(p.k) + static_cast<size_t>(seq0) * p.ld_k + kvh * DH;
-  const uint16_t* v = static_cast<const uint16_t*>(p.v) + static_cast<size_t>(seq0) * p.ld_v + kvh * DH;
-  uint16_t* o = static_cast<uint16_t*>(p.o) + static_cast<size_t>(seq0 + tok) * p.ld_o + head * DH;
-  const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(DH));
-  const auto score = [&](int j) {
-    const uint32_t* a = reinterpret_cast<const uint32_t*>(q);
-    const uint32_t* b = reinterpret_cast<const uint32_t*>(k + static_cast<size_t>(j) * p.ld_k);
-    float s = 0.f;
-    for (int d = 0; d < DH / 2; ++d) s += lo16(a[d], F16) * lo16(b[d], F16) + hi16(a[d], F16) * hi16(b[d], F16);
-    return s * scale_log2;
-  };
-  float m = -INFINITY;
-  for (int j = 0; j <= tok; ++j) m = fmaxf(m, score(j));
-  const float base = m == -INFINITY ? 0.f : m;
-  uint32_t bad = 0;
-  for (int c = 0; c < DH; c += 16) {
-    float acc[16] = {}, l = 0.f;
-    for (int j = 0; j <= tok; ++j) {
-      const float w = ex2(score(j) - base);
-      const uint32_t* b = reinterpret_cast<const uint32_t*>(v + static_cast<size_t>(j) * p.ld_v + c);
-      l += w;
+__device__ __noinline__ void recompute_units(const GqaParams& p) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int G = p.n_heads / p.n_kv, TPT = BQ / G;
+  UnitWalk walk(p, TPT, lane, false);
+  uint32_t nonfinite = 0;
+  for (int i = 0;; ++i) {
+    const int4 w = walk.unit(p, i);
+    if (w.x < 0) break;
+    const Unit u{w.x, w.y, w.z, w.w};
+    const Span d = span_of(u, TPT);
+    const uint16_t* k = static_cast<const uint16_t*>(p.k) + static_cast<size_t>(u.seq0) * p.ld_k + u.kvh * DH;
+    const uint16_t* v = static_cast<const uint16_t*>(p.v) + static_cast<size_t>(u.seq0) * p.ld_v + u.kvh * DH;
+    for (int t = 0; t < d.nt; ++t) {
+      const int first = u.tok0 + t * TPT, tokens = min(TPT, u.L - first);
+      const int masked = (first + 1) / BKV * BKV;          // first key of the masked key tiles
+      uint32_t bad = 0;
+      for (int x = threadIdx.x; x < (d.kend - masked) * (DH / 8); x += THREADS) {
+        const uint4 a = reinterpret_cast<const uint4*>(v + static_cast<size_t>(masked + x / (DH / 8)) * p.ld_v)[x % (DH / 8)];
+        bad |= nonfinite_term(a.x, F16) | nonfinite_term(a.y, F16) | nonfinite_term(a.z, F16) | nonfinite_term(a.w, F16);
+      }
+      if (!__syncthreads_or((bad & 0x80008000u) != 0)) continue;
+      for (int r = warp; r < tokens * G; r += THREADS / 32) {
+        const int tok = first + r / G, head = u.kvh * G + r % G;
+        const uint16_t* q = static_cast<const uint16_t*>(p.q) + static_cast<size_t>(u.seq0 + tok) * p.ld_q + head * DH;
+        const auto at = [&](int j) { return KeyAt{k + static_cast<size_t>(j) * p.ld_k, v + static_cast<size_t>(j) * p.ld_v, true}; };
+        const RowSums<DH> sums = attend_row<F16, DH>(q, 0, tok + 1, at, lane);
+        const float inv = sums.l == 0.f ? 0.f : 1.f / sums.l;
+        uint32_t* o = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.seq0 + tok) * p.ld_o + head * DH);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        acc[2 * e] = fmaf(w, lo16(b[e], F16), acc[2 * e]);
-        acc[2 * e + 1] = fmaf(w, hi16(b[e], F16), acc[2 * e + 1]);
+        for (int e = 0; e < DH / 64; ++e) {
+          const uint32_t x = pack2(sums.acc[2 * e] * inv, sums.acc[2 * e + 1] * inv, F16);
+          nonfinite |= nonfinite_term(x, F16);
+          o[lane * (DH / 64) + e] = x;
+        }
       }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t w = pack2(acc[2 * e] * inv, acc[2 * e + 1] * inv, F16);
-      bad |= nonfinite_term(w, F16);
-      reinterpret_cast<uint32_t*>(o + c)[e] = w;
-    }
   }
-  return bad;
+  report_range(nonfinite, p.err);
 }
 
 template <bool F16, int DH>
@@ -166,6 +228,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   volatile int* odd = reinterpret_cast<volatile int*>(ring + U_SLOTS);
   uint32_t* tmem_slot = const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(odd + 4 * NT));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* any_odd = abort_flag + 1;    // some unit's rows are left to recompute_units()
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -197,7 +260,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&u_empty[i], U_READERS);
     }
     for (int i = 0; i < 4 * NT; ++i) odd[i] = 0;
-    *abort_flag = 0;
+    *abort_flag = *any_odd = 0;
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
@@ -209,56 +272,11 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (warp == 3) {
     // -------------------------------------------------- scheduler
-    const int span = NT * TPT, H = p.n_kv, grid = gridDim.x;
-    const auto groups_of = [&](int b) {       // units of sequence b per head; 0 where it leaves the buffers
-      if (b >= p.B) return 0;
-      const int c0 = p.cu[b], n = p.cu[b + 1] - c0;
-      const bool good = c0 >= 0 && n >= 0 && n <= p.T_cap - c0;
-      if (!good && blockIdx.x == 0) record_error(p.err, kErrLayout);
-      return good ? (n + span - 1) / span : 0;
-    };
-    const int mine = groups_of(lane);         // the first 32 sequences' stay in registers
-    int most = mine, sum = mine;
-    for (int b = lane + 32; b < p.B; b += 32) {
-      const int n = groups_of(b);
-      most = max(most, n);
-      sum += n;
-    }
-    most = __reduce_max_sync(0xffffffffu, most);
-    const long total = static_cast<long>(__reduce_add_sync(0xffffffffu, sum)) * H;
-    const auto reach = [&](int b0, int g) {   // which of sequences b0 .. b0 + 31 have a group g
-      const int n = b0 == 0 ? mine : groups_of(b0 + lane);
-      return __ballot_sync(0xffffffffu, n > g);
-    };
-    int g = most;                             // units of group g: [base, base + count)
-    long base = 0, count = 0;
-    int b0 = 0, passed = 0;                   // sequences b0 .. hold the next unit; so many before them reach g
+    UnitWalk walk(p, TPT, lane, blockIdx.x == 0);
     for (int i = 0;; ++i) {
-      const long u = (i & 1) ? (i + 1l) * grid - 1 - blockIdx.x : static_cast<long>(i) * grid + blockIdx.x;
       const int s = i % U_SLOTS;
       if (i >= U_SLOTS && !warp_wait(&u_empty[s], (i / U_SLOTS - 1) & 1, abort_flag, p.err)) break;
-      int4 w = make_int4(-1, 0, 0, 0);
-      if (u < total) {
-        while (u >= base + count) {
-          base += count;
-          --g;
-          int n = 0;
-          for (int x = 0; x < p.B; x += 32) n += __popc(reach(x, g));
-          count = static_cast<long>(n) * H;
-          b0 = passed = 0;
-        }
-        const int k = static_cast<int>(u - base), nth = k / H;
-        int b = 0;
-        for (; b0 < p.B; b0 += 32) {          // a group's units come in order, so this goes on where it stopped
-          const uint32_t m = reach(b0, g);
-          if (nth - passed < __popc(m)) {
-            b = b0 + __fns(m, 0, nth - passed + 1);
-            break;
-          }
-          passed += __popc(m);
-        }
-        w = make_int4(p.cu[b], p.cu[b + 1] - p.cu[b], g * span, k % H);
-      }
+      const int4 w = walk.unit(p, i);
       if (lane == 0) {
         ring[s] = w;
         mbar_arrive(&u_full[s]);
@@ -564,8 +582,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const bool valid_row = rt < TPT && tok < u.L;
       const int head = u.kvh * G + rh;
       if (odd[4 * t + (i & 3)] == i + 1) {
-        if (valid_row) nonfinite |= recompute_row<F16, DH>(p, u.seq0, tok, head, u.kvh);
-        __syncwarp();
+        if (lane == 0) *any_odd = 1;
       } else {
         RowStore store;
         store.set(p.o, static_cast<long long>(u.seq0 + tok) * p.ld_o + head * DH, valid_row, lane);
@@ -607,6 +624,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, TMEM_COLS);
   }
+  if (*any_odd && !*abort_flag) recompute_units<F16, DH>(p);
 }
 
 template <bool F16, int DH>

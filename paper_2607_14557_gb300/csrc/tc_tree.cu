@@ -25,8 +25,8 @@
 // 539 MB, 97 us (5.5 TB/s); 12 trees of 16 .. 64 rows over 500 .. 12000, 179 MB, 58 us; one token
 // over 12000 rows 21 us, two over 700 and 433 12.8.
 // Hidden keys and non-finite values are treated as in tc_causal.cu: scores dropped, value
-// rows past the request's end cleared, and a unit whose masked tile holds a non-finite
-// value recomputed row by row.
+// rows past the request's end cleared, and the rows of a piece whose masked tile holds a
+// non-finite value left to recompute_pieces() after the last piece.
 #include <math.h>
 
 #include "attn_math.cuh"
@@ -152,16 +152,15 @@ __device__ __forceinline__ uint64_t visible(const GqaParams& p, const Piece& u, 
 // A slot holds the sums as [column / 4][row] float4, so that a warp stores 512 bytes in one
 // piece (a row's 512 bytes one after the other took 2 us for 128 rows), then each row's
 // (max, weight).
-template <bool F16, int DH>
 struct RowOut {
   uint16_t* o = nullptr;
   float4* part = nullptr;                   // the row's first float4; the next is `rows` on
   float2* stats = nullptr;
   int rows = 0;
 };
-template <bool F16, int DH>
-__device__ __forceinline__ RowOut<F16, DH> row_out(const GqaParams& p, const Piece& u, int tok, int head, int r, int rows) {
-  RowOut<F16, DH> w;
+template <int DH>
+__device__ __forceinline__ RowOut row_out(const GqaParams& p, const Piece& u, int tok, int head, int r, int rows) {
+  RowOut w;
   if (u.part < 0) {
     w.o = static_cast<uint16_t*>(p.o) + static_cast<size_t>(u.q0 + tok) * p.ld_o + head * DH;
   } else {
@@ -173,8 +172,8 @@ __device__ __forceinline__ RowOut<F16, DH> row_out(const GqaParams& p, const Pie
   return w;
 }
 // 8 columns from c on, scaled by inv (output only).
-template <bool F16, int DH>
-__device__ __forceinline__ uint32_t store8(const RowOut<F16, DH>& w, int c, const float (&v)[8], float inv) {
+template <bool F16>
+__device__ __forceinline__ uint32_t store8(const RowOut& w, int c, const float (&v)[8], float inv) {
   if (w.o == nullptr) {
     w.part[(c / 4) * w.rows] = make_float4(v[0], v[1], v[2], v[3]);
     w.part[(c / 4 + 1) * w.rows] = make_float4(v[4], v[5], v[6], v[7]);
@@ -190,58 +189,129 @@ __device__ __forceinline__ uint32_t store8(const RowOut<F16, DH>& w, int c, cons
   return bad;
 }
 
-// One row of a piece from global memory, key by key: only for pieces that met a
-// non-finite value in a masked tile.
-template <bool F16, int DH>
-__device__ __noinline__ uint32_t recompute_row(const GqaParams& p, const Piece* piece, int tok, int head, int r, int rows) {
-  const Piece u = *piece;
-  const uint16_t* q = static_cast<const uint16_t*>(p.q) + static_cast<size_t>(u.q0 + tok) * p.ld_q + head * DH;
-  const uint64_t bits = visible(p, u, tok);
-  const int ctx = u.kv - u.n, begin = u.tile0 * BKV, end = min(u.kv, u.tile1 * BKV);
-  const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(DH));
-  // pool row of key j; -1: hidden, -2: on a page outside the pool (zeros)
-  const auto row_of = [&](int j) -> long long {
-    if (j >= ctx && !((bits >> (j - ctx)) & 1)) return -1;
-    const int page = p.table[static_cast<size_t>(u.b) * p.max_pages + (j >> p.page_shift)];
-    return page < 0 || page >= p.n_pages ? -2 : (static_cast<long long>(page) << p.page_shift) + (j & ((1 << p.page_shift) - 1));
-  };
-  const auto score = [&](long long row) {
-    if (row < 0) return 0.f;
-    const uint32_t* a = reinterpret_cast<const uint32_t*>(q);
-    const uint32_t* b = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.k) + row * p.ld_k + u.kvh * DH);
-    float s = 0.f;
-    for (int d = 0; d < DH / 2; ++d) s += lo16(a[d], F16) * lo16(b[d], F16) + hi16(a[d], F16) * hi16(b[d], F16);
-    return s * scale_log2;
-  };
-  float m = -INFINITY;
-  for (int j = begin; j < end; ++j) {
-    const long long row = row_of(j);
-    if (row != -1) m = fmaxf(m, score(row));
-  }
-  const float base = m == -INFINITY ? 0.f : m;
-  const RowOut<F16, DH> out = row_out<F16, DH>(p, u, tok, head, r, rows);
-  uint32_t bad = 0;
-  float l = 0.f;
-  for (int c = 0; c < DH; c += 8) {
-    float acc[8] = {};
-    l = 0.f;
-    for (int j = begin; j < end; ++j) {
-      const long long row = row_of(j);
-      if (row == -1) continue;
-      const float w = ex2(score(row) - base);
-      l += w;
-      if (row < 0) continue;
-      const uint32_t* b = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.v) + row * p.ld_v + u.kvh * DH + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        acc[2 * e] = fmaf(w, lo16(b[e], F16), acc[2 * e]);
-        acc[2 * e + 1] = fmaf(w, hi16(b[e], F16), acc[2 * e + 1]);
+// A CTA's run [run0, run1) of the line, in shared memory.
+struct Start {
+  long long warp_sum[THREADS / 32];
+  long long run0, run1;
+  long long off;                            // run0 is so many places into request b
+  Request r;
+  int b;
+};
+
+// The pieces of run blockIdx.x, by a whole warp.
+struct PieceWalk {
+  int tpt, extra, lane;
+  int b;                                    // request of the next place, `off` places into it
+  Request r;
+  long long off, at, run1;
+  int window;                               // requests window .. window + 31 in the lanes' registers
+  Request ahead{};
+  Join join{};                              // the unit that begins in the run and does not end there
+  long long join_end = 0;                   // its last place
+
+  __device__ __forceinline__ PieceWalk(const Start& s, int tpt_, int extra_, int lane_)
+      : tpt(tpt_), extra(extra_), lane(lane_), b(s.b), r(s.r), off(s.off), at(s.run0), run1(s.run1), window(s.b - 32) {}
+
+  // The next piece; n < 0: no more.
+  __device__ __forceinline__ Piece next(const GqaParams& p) {
+    const int run = blockIdx.x;
+    Piece u{};
+    while (at < run1) {                     // the next stretch that holds key tiles
+      const long long len = line_length(p, r, tpt, extra);
+      if (off >= len) {                     // on to the next request
+        off -= len;
+        if (++b >= p.B) {                   // the lengths changed under the call
+          at = run1;
+          break;
+        }
+        if (b - window >= 32) {
+          window = b;
+          ahead = read_request(p, window + lane);
+        }
+        r.q0 = __shfl_sync(0xffffffffu, ahead.q0, b - window);
+        r.n = __shfl_sync(0xffffffffu, ahead.n, b - window);
+        r.kv = __shfl_sync(0xffffffffu, ahead.kv, b - window);
+        continue;
       }
+      const int tiles = key_tiles(r.kv), places = tiles + extra, row_tiles = (r.n + tpt - 1) / tpt;
+      const int unit = quotient(off, places);
+      const int first = static_cast<int>(off - static_cast<long long>(unit) * places);
+      const int last = static_cast<int>(min(static_cast<long long>(places), first + (run1 - at)));
+      off += last - first;
+      at += last - first;
+      u.tile0 = max(first - extra, 0);
+      u.tile1 = last - extra;
+      if (u.tile1 <= u.tile0) continue;     // only places without a tile
+      u.q0 = r.q0;
+      u.n = r.n;
+      u.kv = r.kv;
+      u.b = b;
+      u.kvh = unit / row_tiles;
+      u.tok0 = (unit - u.kvh * row_tiles) * tpt;
+      u.part = u.tile0 > 0 ? 2 * run : (u.tile1 < tiles ? 2 * run + 1 : -1);
+      if (u.tile0 == 0 && u.tile1 < tiles) {
+        join = Join{u.q0, u.tok0, u.n, u.kvh, run, 0, {0, 0}};
+        join_end = at + (places - last) - 1;
+      }
+      break;
     }
-    bad |= store8<F16, DH>(out, c, acc, l == 0.f ? 0.f : 1.f / l);
+    if (u.tile1 <= u.tile0) u.n = -1;
+    return u;
   }
-  if (out.stats) *out.stats = make_float2(m, l);
-  return bad;
+};
+
+// The rows that a non-finite value in a masked tile may have reached, from global memory by
+// every warp of the CTA.  Its pieces are looked over once more, so that none need be remembered.
+template <bool F16, int DH>
+__device__ __noinline__ void recompute_pieces(const GqaParams& p, const Start& start) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int G = p.n_heads / p.n_kv, TPT = BQ / G, part_rows = min(TPT, p.max_new) * G;
+  PieceWalk walk(start, TPT, unit_extra(part_rows), lane);
+  uint32_t nonfinite = 0;
+  for (;;) {
+    const Piece u = walk.next(p);
+    if (u.n < 0) break;
+    const int ctx = u.kv - u.n, end = min(u.kv, u.tile1 * BKV);
+    // key j's heads; null on a page outside the pool (zeros)
+    const auto row_of = [&](int j) -> KeyAt {
+      const int page = p.table[static_cast<size_t>(u.b) * p.max_pages + (j >> p.page_shift)];
+      if (page < 0 || page >= p.n_pages) return KeyAt{nullptr, nullptr, true};
+      const size_t row = ((static_cast<size_t>(page) << p.page_shift) + (j & ((1 << p.page_shift) - 1))) * p.ld_k + u.kvh * DH;
+      return KeyAt{static_cast<const uint16_t*>(p.k) + row, static_cast<const uint16_t*>(p.v) + row, true};
+    };
+    const int masked = max(ctx / BKV, u.tile0) * BKV;      // first key of the masked key tiles
+    uint32_t bad = 0;
+    for (int x = threadIdx.x; x < (end - masked) * (DH / 8); x += THREADS) {
+      const KeyAt key = row_of(masked + x / (DH / 8));
+      if (key.v == nullptr) continue;
+      const uint4 a = reinterpret_cast<const uint4*>(key.v)[x % (DH / 8)];
+      bad |= nonfinite_term(a.x, F16) | nonfinite_term(a.y, F16) | nonfinite_term(a.z, F16) | nonfinite_term(a.w, F16);
+    }
+    if (!__syncthreads_or((bad & 0x80008000u) != 0)) continue;
+    const int rows = min(TPT, u.n - u.tok0) * G;
+    for (int r = warp; r < rows; r += THREADS / 32) {
+      const int tok = u.tok0 + r / G, head = u.kvh * G + r % G;
+      const uint64_t bits = visible(p, u, tok);
+      const uint16_t* q = static_cast<const uint16_t*>(p.q) + static_cast<size_t>(u.q0 + tok) * p.ld_q + head * DH;
+      const auto at = [&](int j) { return j < ctx || ((bits >> (j - ctx)) & 1) != 0 ? row_of(j) : KeyAt{nullptr, nullptr, false}; };
+      const RowSums<DH> sums = attend_row<F16, DH>(q, u.tile0 * BKV, end, at, lane);
+      const RowOut out = row_out<DH>(p, u, tok, head, r, part_rows);
+      const float inv = sums.l == 0.f ? 0.f : 1.f / sums.l;
+#pragma unroll
+      for (int e = 0; e < DH / 64; ++e) {
+        const int c = lane * (DH / 32) + 2 * e;
+        if (out.o == nullptr) {
+          reinterpret_cast<float2*>(out.part + (c / 4) * out.rows)[c % 4 / 2] = make_float2(sums.acc[2 * e], sums.acc[2 * e + 1]);
+        } else {
+          const uint32_t x = pack2(sums.acc[2 * e] * inv, sums.acc[2 * e + 1] * inv, F16);
+          nonfinite |= nonfinite_term(x, F16);
+          *reinterpret_cast<uint32_t*>(out.o + c) = x;
+        }
+      }
+      if (out.stats && lane == 0) *out.stats = make_float2(sums.m, sums.l);
+    }
+  }
+  report_range(nonfinite, p.err);
 }
 
 template <bool F16, typename Cfg>
@@ -275,13 +345,8 @@ __global__ void __launch_bounds__(THREADS, 2)
   volatile int* odd = reinterpret_cast<volatile int*>(ring + U_SLOTS);   // [4], as in tc_causal.cu
   uint32_t* tmem_slot = const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(odd + 4));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  struct Start {                             // where this CTA's run begins
-    long long warp_sum[THREADS / 32];
-    long long off;
-    Request r;
-    int b;
-  };
-  constexpr int START_AT = (8 * (7 + 2 * Cfg::BARS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 + 7) & ~7;
+  volatile int* any_odd = abort_flag + 1;    // some piece's rows are left to recompute_pieces()
+  constexpr int START_AT = (8 * (7 + 2 * Cfg::BARS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 12 + 7) & ~7;
   static_assert(START_AT + sizeof(Start) <= BAR_BYTES, "barrier block");
   Start& start = *reinterpret_cast<Start*>(smem + Cfg::OFF_BAR + START_AT);
 
@@ -328,7 +393,7 @@ __global__ void __launch_bounds__(THREADS, 2)
       mbar_init(&u_empty[i], U_READERS);
       odd[i] = 0;
     }
-    *abort_flag = 0;
+    *abort_flag = *any_odd = 0;
     fence_barrier_init();
     tma_prefetch_desc(&mQ);
     tma_prefetch_desc(&mKV);
@@ -370,6 +435,8 @@ __global__ void __launch_bounds__(THREADS, 2)
       const long long n = line_length(p, r, TPT, extra);
       if (run0 < at + n) {
         start.b = b;
+        start.run0 = run0;
+        start.run1 = run1;
         start.off = run0 - at;
         start.r = r;
         break;
@@ -392,13 +459,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     unsigned g = 0;                                       // key tiles loaded
     int pieces = 0;
     bool ok = true;
-    int b = start.b;
-    long long off = start.off, at = run0;
-    Request r = start.r;                                  // request b
-    int window = b - 32;                                  // requests window .. window + 31 in the lanes' registers
-    Request ahead{};
-    Join join{};
-    long long join_end = 0;                               // last place of its unit
+    PieceWalk walk(start, TPT, extra, lane);
     // pool row of this lane's box of key tile j
     const auto box_row = [&](int bb, int kv, int j) {
       const int key = j * BKV + lane * box_rows;
@@ -425,48 +486,7 @@ __global__ void __launch_bounds__(THREADS, 2)
       return true;
     };
     for (int i = 0; ok; ++i) {
-      Piece u{};
-      u.n = -1;
-      while (at < run1) {                                 // the next stretch that holds key tiles
-        const long long len = line_length(p, r, TPT, extra);
-        if (off >= len) {                                 // on to the next request
-          off -= len;
-          if (++b >= p.B) {                               // the lengths changed under the call
-            at = run1;
-            break;
-          }
-          if (b - window >= 32) {
-            window = b;
-            ahead = read_request(p, window + lane);
-          }
-          r.q0 = __shfl_sync(0xffffffffu, ahead.q0, b - window);
-          r.n = __shfl_sync(0xffffffffu, ahead.n, b - window);
-          r.kv = __shfl_sync(0xffffffffu, ahead.kv, b - window);
-          continue;
-        }
-        const int tiles = key_tiles(r.kv), places = tiles + extra, row_tiles = (r.n + TPT - 1) / TPT;
-        const int unit = quotient(off, places);
-        const int first = static_cast<int>(off - static_cast<long long>(unit) * places);
-        const int last = static_cast<int>(min(static_cast<long long>(places), first + (run1 - at)));
-        off += last - first;
-        at += last - first;
-        u.tile0 = max(first - extra, 0);
-        u.tile1 = last - extra;
-        if (u.tile1 <= u.tile0) continue;                 // only places without a tile
-        u.q0 = r.q0;
-        u.n = r.n;
-        u.kv = r.kv;
-        u.b = b;
-        u.kvh = unit / row_tiles;
-        u.tok0 = (unit - u.kvh * row_tiles) * TPT;
-        u.part = u.tile0 > 0 ? 2 * c : (u.tile1 < tiles ? 2 * c + 1 : -1);
-        if (u.tile0 == 0 && u.tile1 < tiles) {
-          join = Join{u.q0, u.tok0, u.n, u.kvh, c, 0, {0, 0}};
-          join_end = at + (places - last) - 1;
-        }
-        break;
-      }
-      if (u.tile1 <= u.tile0) u.n = -1;
+      const Piece u = walk.next(p);
       int next_row = u.n < 0 ? -1 : box_row(u.b, u.kv, u.tile0);   // the page of a tile is looked up a tile ahead
       const int s = i % U_SLOTS;
       if (i >= U_SLOTS && !warp_wait(&u_empty[s], (i / U_SLOTS - 1) & 1, abort_flag, p.err)) break;
@@ -499,8 +519,8 @@ __global__ void __launch_bounds__(THREADS, 2)
         ++g;
       }
     }
-    if (join.n > 0) join.last = run_of(total, join_end, runs);
-    if (lane == 0) joins[c] = join;
+    if (walk.join.n > 0) walk.join.last = run_of(total, walk.join_end, runs);
+    if (lane == 0) joins[c] = walk.join;
     if (*abort_flag && leader) {
       // let copies still in flight land before the CTA's shared memory is released
       if (pieces > 0) mbar_wait_drain(q_full, (pieces - 1) & 1, 20000000ull);
@@ -731,12 +751,11 @@ __global__ void __launch_bounds__(THREADS, 2)
       tc_fence_after();
       const int tok = u->tok0 + rt, head = u->kvh * G + r - rt * G;
       if (odd[i & 3] == i + 1) {
-        if (valid_row) nonfinite |= recompute_row<F16, DH>(p, u, tok, head, r, part_rows);
-        __syncwarp();
+        if (lane == 0) *any_odd = 1;
       } else if (busy) {
         const float inv_l = l == 0.f ? 0.f : 1.f / l;
-        RowOut<F16, DH> out;
-        if (valid_row) out = row_out<F16, DH>(p, *u, tok, head, r, part_rows);
+        RowOut out;
+        if (valid_row) out = row_out<DH>(p, *u, tok, head, r, part_rows);
 #pragma unroll 1
         for (int cc = 0; cc < DH / 32; ++cc) {
           uint32_t rr[32];
@@ -748,7 +767,7 @@ __global__ void __launch_bounds__(THREADS, 2)
               float v[8];
 #pragma unroll
               for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(rr[8 * e + k]);
-              nonfinite |= store8<F16, DH>(out, 32 * cc + 8 * e, v, inv_l);
+              nonfinite |= store8<F16>(out, 32 * cc + 8 * e, v, inv_l);
             }
           }
         }
@@ -767,6 +786,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     tc_fence_after();
     tmem_dealloc(tmem, TMEM_COLS);
   }
+  if (*any_odd && !*abort_flag) recompute_pieces<F16, DH>(p, start);
 }
 
 // Joins the pieces of the unit that begins in run blockIdx.x and ends in a later one, in order
