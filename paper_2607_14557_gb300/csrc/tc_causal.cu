@@ -66,8 +66,8 @@ struct Layout {
 };
 // up to 199680 bytes leave 60 KB of the SM to L1
 static_assert(Layout<128>::BYTES <= 199680, "L1 carve-out");
-// barriers, the unit ring, the odd-value marks, the TMEM base and two flags
-static_assert(8 * (2 + 4 * STAGES + 6 * NT + 2 * U_SLOTS) + 16 * U_SLOTS + 16 * NT + 12 <= BAR_BYTES, "barrier block");
+// barriers, the unit ring, the odd-value marks, the TMEM base and the abort flag
+static_assert(8 * (2 + 4 * STAGES + 6 * NT + 2 * U_SLOTS) + 16 * U_SLOTS + 16 * NT + 8 <= BAR_BYTES, "barrier block");
 
 // seq0 < 0: no more units.
 struct Unit {
@@ -228,7 +228,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   volatile int* odd = reinterpret_cast<volatile int*>(ring + U_SLOTS);
   uint32_t* tmem_slot = const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(odd + 4 * NT));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  volatile int* any_odd = abort_flag + 1;    // some unit's rows are left to recompute_units()
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -260,7 +259,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&u_empty[i], U_READERS);
     }
     for (int i = 0; i < 4 * NT; ++i) odd[i] = 0;
-    *abort_flag = *any_odd = 0;
+    *abort_flag = 0;
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
@@ -581,9 +580,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const float inv_l = l == 0.f ? 0.f : 1.f / l;
       const bool valid_row = rt < TPT && tok < u.L;
       const int head = u.kvh * G + rh;
-      if (odd[4 * t + (i & 3)] == i + 1) {
-        if (lane == 0) *any_odd = 1;
-      } else {
+      if (odd[4 * t + (i & 3)] != i + 1) {        // (else the rows are left to recompute_units())
         RowStore store;
         store.set(p.o, static_cast<long long>(u.seq0 + tok) * p.ld_o + head * DH, valid_row, lane);
         uint32_t top = 0;
@@ -624,7 +621,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, TMEM_COLS);
   }
-  if (*any_odd && !*abort_flag) recompute_units<F16, DH>(p);
+  int any = 0;
+  for (int i = 0; i < 4 * NT; ++i) any |= odd[i];
+  if (any != 0 && !*abort_flag) recompute_units<F16, DH>(p);
 }
 
 template <bool F16, int DH>

@@ -263,7 +263,7 @@ struct PieceWalk {
 // The rows that a non-finite value in a masked tile may have reached, from global memory by
 // every warp of the CTA.  Its pieces are looked over once more, so that none need be remembered.
 template <bool F16, int DH>
-__device__ __noinline__ void recompute_pieces(const GqaParams& p, const Start& start) {
+__device__ __forceinline__ void recompute_pieces(const GqaParams& p, const Start& start) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = p.n_heads / p.n_kv, TPT = BQ / G, part_rows = min(TPT, p.max_new) * G;
   PieceWalk walk(start, TPT, unit_extra(part_rows), lane);
@@ -345,8 +345,7 @@ __global__ void __launch_bounds__(THREADS, 2)
   volatile int* odd = reinterpret_cast<volatile int*>(ring + U_SLOTS);   // [4], as in tc_causal.cu
   uint32_t* tmem_slot = const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(odd + 4));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  volatile int* any_odd = abort_flag + 1;    // some piece's rows are left to recompute_pieces()
-  constexpr int START_AT = (8 * (7 + 2 * Cfg::BARS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 12 + 7) & ~7;
+  constexpr int START_AT = (8 * (7 + 2 * Cfg::BARS + 2 * U_SLOTS) + 36 * U_SLOTS + 16 + 8 + 7) & ~7;
   static_assert(START_AT + sizeof(Start) <= BAR_BYTES, "barrier block");
   Start& start = *reinterpret_cast<Start*>(smem + Cfg::OFF_BAR + START_AT);
 
@@ -393,7 +392,7 @@ __global__ void __launch_bounds__(THREADS, 2)
       mbar_init(&u_empty[i], U_READERS);
       odd[i] = 0;
     }
-    *abort_flag = *any_odd = 0;
+    *abort_flag = 0;
     fence_barrier_init();
     tma_prefetch_desc(&mQ);
     tma_prefetch_desc(&mKV);
@@ -750,9 +749,7 @@ __global__ void __launch_bounds__(THREADS, 2)
       if (!__all_sync(0xffffffffu, mbar_wait(o_done, i & 1, abort_flag, p.err))) break;
       tc_fence_after();
       const int tok = u->tok0 + rt, head = u->kvh * G + r - rt * G;
-      if (odd[i & 3] == i + 1) {
-        if (lane == 0) *any_odd = 1;
-      } else if (busy) {
+      if (busy && odd[i & 3] != i + 1) {      // (else the rows are left to recompute_pieces())
         const float inv_l = l == 0.f ? 0.f : 1.f / l;
         RowOut out;
         if (valid_row) out = row_out<DH>(p, *u, tok, head, r, part_rows);
@@ -786,7 +783,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     tc_fence_after();
     tmem_dealloc(tmem, TMEM_COLS);
   }
-  if (*any_odd && !*abort_flag) recompute_pieces<F16, DH>(p, start);
+  if ((odd[0] | odd[1] | odd[2] | odd[3]) != 0 && !*abort_flag) recompute_pieces<F16, DH>(p, start);
 }
 
 // Joins the pieces of the unit that begins in run blockIdx.x and ends in a later one, in order
