@@ -432,7 +432,9 @@ seer_status seer_kv_accept(seer_dtype dt, const int32_t* cached_len, const int32
  * int32 [B+1], read on the device; rows past cu_seqlens[B] are untouched.  head_dim:
  * 64 or 128 for 16-bit types, a multiple of 4 up to 128 for fp32.  o must not
  * overlap the inputs.  A key that a row does not see never reaches its result, not
- * even an infinite or NaN one.  No workspace. */
+ * even an infinite or NaN one.  Where an offset is below the one before it, that
+ * sequence is left out and recorded, and rows of sequences that then overlap hold
+ * either's result.  No workspace. */
 seer_status seer_attention_causal(const void* q, int ld_q, const void* k, int ld_k, const void* v, int ld_v, void* o,
                                   int ld_o, seer_dtype dt, const int32_t* cu_seqlens, int B, int T_cap, int n_heads,
                                   int n_kv_heads, int head_dim, void* stream);

@@ -75,46 +75,56 @@ __device__ __forceinline__ Span read_span(const GqaParams& p, int b) {
   return s;
 }
 
-// CLUSTER: the blocks of a cluster share a tile's keys.
+// Tiles of a causal call at most.
+__host__ __device__ __forceinline__ long causal_units(const GqaParams& p, int rows) {
+  return (static_cast<long>(p.T_cap) * (p.n_heads / p.n_kv) / rows + p.B) * p.n_kv;
+}
+// Slots of sequence b start at cu[b] * G / BQ + b, at least as far apart as its tiles: the last
+// sequence that starts by `slot`.  Offsets ascend, so a warp looks at 32 at once (2 us of a
+// short call were bisection's loads).
+template <int BQ>
+__device__ __forceinline__ int sequence_at(const GqaParams& p, int G, int slot) {
+  int lo = 0, hi = p.B;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, at = lo + static_cast<int>(threadIdx.x & 31) * step;
+    const bool before = at < hi && (at == lo || static_cast<long long>(p.cu[at]) * G / BQ + at <= slot);
+    lo += (__popc(__ballot_sync(0xffffffffu, before)) - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
+
+// Where some offset falls: the sequence and tile of the slot-th tile, counted over the sequences
+// that lie in the buffers; b = B past the last.  By a whole block.
+template <int BQ>
+__device__ __forceinline__ int2 tile_at(const GqaParams& p, int G, long slot, long* sums) {
+  const auto tiles = [&](int b) -> long {
+    const Span s = read_span<false>(p, b);
+    return s.good ? (static_cast<long>(s.n) * G + BQ - 1) / BQ : 0;
+  };
+  const int each = (p.B + NTH - 1) / NTH;
+  long mine = 0;
+  for (int b = threadIdx.x * each; b < min(p.B, (static_cast<int>(threadIdx.x) + 1) * each); ++b) mine += tiles(b);
+  sums[threadIdx.x] = mine;
+  __syncthreads();
+  int t = 0;
+  while (t < NTH && slot >= sums[t]) slot -= sums[t++];
+  __syncthreads();                            // the sums' memory is free again
+  int b = min(p.B, t * each);
+  for (; b < p.B; ++b) {
+    const long n = tiles(b);
+    if (slot < n) break;
+    slot -= n;
+  }
+  return make_int2(b, static_cast<int>(slot));
+}
+
+// Rows [R0, R0 + BQ) of request b's (token, head) rows.  CLUSTER: the blocks of a cluster share
+// the tile's keys.
 template <bool PAGED, bool CLUSTER, int BQ, int HALVES>
-__global__ void __launch_bounds__(NTH) gqa_simt_kernel(const GqaParams p) {
+__device__ __forceinline__ void attend_tile(const GqaParams& p, int b, int kvh, int R0, const Span& sp, int split) {
   constexpr int TM = BQ / TY, DIMS = 64 * HALVES, ld = row_ld(DIMS);
-  pdl_enter();
-  const int dh = p.head_dim, G = p.n_heads / p.n_kv;
-  const int parts = p.splits, split = CLUSTER ? static_cast<int>(cluster_ctarank()) : (PAGED ? static_cast<int>(blockIdx.x) % parts : 0);
-  // causal: a sequence's last rows, which see the most keys, first
-  const int unit = PAGED ? blockIdx.x / parts : (gridDim.x - 1 - blockIdx.x) / parts;
-  int b, kvh, R0;
-  if (PAGED) {
-    const int tiles = (p.max_new * G + BQ - 1) / BQ;
-    R0 = (unit % tiles) * BQ;
-    kvh = unit / tiles % p.n_kv;
-    b = unit / tiles / p.n_kv;
-  } else {
-    // slots of request b start at cu[b] * G / BQ + b, at least as far apart as its tiles
-    const int slot = unit / p.n_kv;
-    kvh = unit % p.n_kv;
-    // (a warp looks at 32 requests at once: 2 us of a short call were bisection's loads)
-    int lo = 0, hi = p.B;
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 31) / 32, at = lo + static_cast<int>(threadIdx.x & 31) * step;
-      const bool before = at < hi && (at == lo || static_cast<long long>(p.cu[at]) * G / BQ + at <= slot);
-      lo += (__popc(__ballot_sync(0xffffffffu, before)) - 1) * step;
-      hi = min(hi, lo + step);
-    }
-    b = lo;
-    const long long tile = slot - (static_cast<long long>(p.cu[b]) * G / BQ + b);
-    if (blockIdx.x == gridDim.x - 1)          // requests that no block's slot leads to
-      for (int i = threadIdx.x; i < p.B; i += NTH)
-        if (!read_span<PAGED>(p, i).good) record_error(p.err, kErrLayout);
-    if (tile < 0 || tile > 0x7fffffff / BQ) return;
-    R0 = static_cast<int>(tile) * BQ;
-  }
-  const Span sp = read_span<PAGED>(p, b);
-  if (!sp.good) {
-    if (threadIdx.x == 0) record_error(p.err, kErrLayout);
-    return;
-  }
+  const int dh = p.head_dim, G = p.n_heads / p.n_kv, parts = p.splits;
   const long long all_rows = static_cast<long long>(sp.n) * G;
   if (R0 >= all_rows) return;
   const int rows = static_cast<int>(all_rows - R0 < BQ ? all_rows - R0 : BQ);
@@ -363,6 +373,54 @@ __global__ void __launch_bounds__(NTH) gqa_simt_kernel(const GqaParams p) {
   copy_wait<0>();
 }
 
+// The blocks ahead of a causal call's look through all offsets.  Where one falls, the others' slots
+// may have led past some sequences' tiles, so these blocks take all tiles in turn.
+template <bool CLUSTER, int BQ, int HALVES>
+__device__ __noinline__ void take_all_if_one_falls(const GqaParams& p, int worker, int checkers, int split) {
+  int falls = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < p.B; i += NTH) falls |= p.cu[i] > p.cu[i + 1];
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < p.B; i += NTH)
+      if (!read_span<false>(p, i).good) record_error(p.err, kErrLayout);
+  if (!__syncthreads_or(falls)) return;
+  extern __shared__ float4 gqa_smem[];
+  for (long i = worker;; i += checkers) {
+    const int2 at = tile_at<BQ>(p, p.n_heads / p.n_kv, i / p.n_kv, reinterpret_cast<long*>(gqa_smem));
+    if (at.x >= p.B) return;
+    attend_tile<false, CLUSTER, BQ, HALVES>(p, at.x, static_cast<int>(i % p.n_kv), at.y * BQ, read_span<false>(p, at.x), split);
+    __syncthreads();
+  }
+}
+
+// (32 rows of up to 64 dims: shared memory lets four blocks in, so registers have to, too.  600
+// prompts of 1 .. 40 rows 39.6 us, 43 with three)
+template <bool PAGED, bool CLUSTER, int BQ, int HALVES>
+__global__ void __launch_bounds__(NTH, HALVES == 1 && BQ == 32 ? 4 : 1) gqa_simt_kernel(const GqaParams p) {
+  pdl_enter();
+  const int G = p.n_heads / p.n_kv, parts = p.splits;
+  const int split = CLUSTER ? static_cast<int>(cluster_ctarank()) : (PAGED ? static_cast<int>(blockIdx.x) % parts : 0);
+  if constexpr (PAGED) {
+    const int tiles = (p.max_new * G + BQ - 1) / BQ, unit = blockIdx.x / parts;
+    const int R0 = (unit % tiles) * BQ, kvh = unit / tiles % p.n_kv, b = unit / tiles / p.n_kv;
+    const Span sp = read_span<PAGED>(p, b);
+    if (sp.good) attend_tile<PAGED, CLUSTER, BQ, HALVES>(p, b, kvh, R0, sp, split);
+    else if (threadIdx.x == 0) record_error(p.err, kErrLayout);
+  } else {
+    const int units = static_cast<int>(causal_units(p, BQ)), worker = blockIdx.x / parts, checkers = gridDim.x / parts - units;
+    if (worker >= checkers) {
+      const int unit = units - 1 - (worker - checkers);    // a sequence's last rows, which see the most keys, first
+      const int slot = unit / p.n_kv, kvh = unit % p.n_kv, b = sequence_at<BQ>(p, G, slot);
+      const long tile = slot - (static_cast<long>(p.cu[b]) * G / BQ + b);
+      const Span sp = read_span<PAGED>(p, b);
+      if (sp.good && tile >= 0 && tile <= 0x7fffffff / BQ)
+        attend_tile<PAGED, CLUSTER, BQ, HALVES>(p, b, kvh, static_cast<int>(tile) * BQ, sp, split);
+      return;
+    }
+    take_all_if_one_falls<CLUSTER, BQ, HALVES>(p, worker, checkers, split);
+  }
+}
+
 // A warp per (request, key/value head, row): its shares' sums, weighted by exp(max - largest max).
 __global__ void __launch_bounds__(256) gqa_merge_kernel(const GqaParams p) {
   pdl_enter();
@@ -395,7 +453,6 @@ __global__ void __launch_bounds__(256) gqa_merge_kernel(const GqaParams p) {
         make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
 }
 
-long causal_units(const GqaParams& p, int rows) { return (static_cast<long>(p.T_cap) * (p.n_heads / p.n_kv) / rows + p.B) * p.n_kv; }
 long paged_units(int B, int n_heads, int n_kv, int max_new, int rows) {
   return static_cast<long>(B) * n_kv * ((static_cast<long>(max_new) * (n_heads / n_kv) + rows - 1) / rows);
 }
@@ -406,8 +463,10 @@ long paged_units(int B, int n_heads, int n_kv, int max_new, int rows) {
 int block_rows(long units_of_32, int num_sms) { return units_of_32 <= num_sms ? 16 : 32; }
 
 template <bool PAGED, bool CLUSTER, int BQ, int HALVES>
-cudaError_t launch_typed(const GqaParams& p, cudaStream_t st) {
-  const long blocks = (PAGED ? paged_units(p.B, p.n_heads, p.n_kv, p.max_new, BQ) : causal_units(p, BQ)) * p.splits;
+cudaError_t launch_typed(const GqaParams& p, int num_sms, cudaStream_t st) {
+  // (causal: some more ahead, for offsets that fall)
+  const long units = PAGED ? paged_units(p.B, p.n_heads, p.n_kv, p.max_new, BQ) : causal_units(p, BQ) + (num_sms / 4 + p.splits - 1) / p.splits;
+  const long blocks = units * p.splits;
   if (blocks > 0x7fffffffL) return cudaErrorInvalidValue;
   constexpr int smem = 4 * smem_floats(BQ, 64 * HALVES);
   static bool attr_set[64] = {};
@@ -420,12 +479,12 @@ cudaError_t launch_typed(const GqaParams& p, cudaStream_t st) {
   return launch_kernel(gqa_merge_kernel, dim3(static_cast<unsigned>((warps + 7) / 8)), dim3(256), 0, st, p);
 }
 template <bool PAGED, bool CLUSTER, int BQ>
-cudaError_t launch_halves(const GqaParams& p, cudaStream_t st) {
-  return p.head_dim <= 64 ? launch_typed<PAGED, CLUSTER, BQ, 1>(p, st) : launch_typed<PAGED, CLUSTER, BQ, 2>(p, st);
+cudaError_t launch_halves(const GqaParams& p, int num_sms, cudaStream_t st) {
+  return p.head_dim <= 64 ? launch_typed<PAGED, CLUSTER, BQ, 1>(p, num_sms, st) : launch_typed<PAGED, CLUSTER, BQ, 2>(p, num_sms, st);
 }
 template <bool PAGED, bool CLUSTER>
-cudaError_t launch_rows(const GqaParams& p, int rows, cudaStream_t st) {
-  return rows == 16 ? launch_halves<PAGED, CLUSTER, 16>(p, st) : launch_halves<PAGED, CLUSTER, 32>(p, st);
+cudaError_t launch_rows(const GqaParams& p, int rows, int num_sms, cudaStream_t st) {
+  return rows == 16 ? launch_halves<PAGED, CLUSTER, 16>(p, num_sms, st) : launch_halves<PAGED, CLUSTER, 32>(p, num_sms, st);
 }
 
 }  // namespace
@@ -446,14 +505,14 @@ cudaError_t launch_gqa_simt(bool paged, const GqaParams& args, int num_sms, cuda
   GqaParams p = args;
   if (p.T_cap <= 0) return cudaSuccess;
   if (paged)
-    return launch_rows<true, false>(p, block_rows(paged_units(p.B, p.n_heads, p.n_kv, p.max_new, 32), num_sms), st);
+    return launch_rows<true, false>(p, block_rows(paged_units(p.B, p.n_heads, p.n_kv, p.max_new, 32), num_sms), num_sms, st);
   const int rows = block_rows(causal_units(p, 32), num_sms);
   // causal: blocks that share a tile's keys, as many as the SMs hold at once, where
   // prompts have the tiles to share on average
   const long units = causal_units(p, rows);
   p.splits = 1;
   while (p.splits < MAX_PARTS && units * p.splits * 2 <= 4l * num_sms && p.T_cap / p.B >= KT * p.splits) p.splits *= 2;
-  return p.splits > 1 ? launch_rows<false, true>(p, rows, st) : launch_rows<false, false>(p, rows, st);
+  return p.splits > 1 ? launch_rows<false, true>(p, rows, num_sms, st) : launch_rows<false, false>(p, rows, num_sms, st);
 }
 
 }  // namespace seer

@@ -1,0 +1,65 @@
+"""What the paged cache's entry points promise about calls that are odd, but allowed."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import paged_reference as R
+from tests.helpers import cuda, i32
+
+pytestmark = pytest.mark.gpu
+
+S = pytest.importorskip("paper_2607_14557_gb300.seer")
+TDT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    S.seer_check_device()
+    yield
+    torch.cuda.synchronize()
+
+
+def rnd(rng, shape, dt):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(TDT[dt]).to(cuda())
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def close(got, ref, bound):
+    bad = ~(np.abs(got - ref) <= bound + 1e-30)
+    assert not bad.any(), (np.argwhere(bad)[:4].tolist(), got[bad][:4], ref[bad][:4])
+
+
+@pytest.mark.parametrize("dt,dh", [("f32", 64), ("f32", 128), ("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("cu,good", [
+    ([0, 100, 2 ** 31 - 1, 200, 300], [(0, 100), (200, 300)]), ([0, 60, 40, 300], [(0, 40)]), ([-5, 40, 300], [(40, 300)]),
+    ([0, 100, 301], [(0, 100)]), ([0, 300, 100, 400], [(0, 300)]), ([300, 0, 300], [(0, 300)]), ([5, 0, 0], []), ([100, 200, 0, 50], [(100, 200), (0, 50)]),
+    ([0] + [10 * i for i in range(1, 25)] + [-1] + [250 + i for i in range(50)] + [300], [(0, 240), (250, 300)])])
+def test_causal_offsets_that_fall_cost_their_own_rows_alone(dt, dh, cu, good):
+    """good: rows of sequences that lie in the buffers, as far as no other such sequence has them too."""
+    rng = np.random.default_rng(3)
+    hq, hk, T, B = 8, 1, 300, len(cu) - 1
+    x = rnd(rng, (T, (hq + 2 * hk) * dh), dt)
+    h = host(x).reshape(T, hq + 2 * hk, dh)
+    o = torch.full((T, hq * dh), 5.0, dtype=TDT[dt], device=cuda())
+    ld = x.stride(0)
+    S.seer_attention_causal(x, ld, x[:, hq * dh:], ld, x[:, (hq + hk) * dh:], ld, o, o.stride(0), dt, i32(cu), B, T, hq, hk, dh)
+    assert S.seer_check_device() == 2
+    got = host(o).reshape(T, hq, dh)
+    taken = [(a, e) for a, e in zip(cu[:-1], cu[1:]) if 0 <= a <= e <= T]
+    for a, e in taken:
+        rows = [r for r in range(a, e) if any(lo <= r < hi for lo, hi in good)]
+        if rows:
+            ref, bound = R.causal(h[a:e, :hq], h[a:e, hq:hq + hk], h[a:e, hq + hk:], [0, e - a], dt)
+            at = np.array(rows) - a
+            close(got[a:e][at], ref[at], bound[at])
+    free = np.ones(T, bool)                                 # rows of no sequence are as they were
+    for a, e in taken:
+        free[a:e] = False
+    assert (got[free] == 5.0).all()
