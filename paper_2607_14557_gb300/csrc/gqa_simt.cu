@@ -64,8 +64,9 @@ template <bool PAGED>
 __device__ __forceinline__ Span read_span(const GqaParams& p, int b) {
   Span s;
   s.q0 = p.cu[b];
-  s.n = p.cu[b + 1] - s.q0;
-  s.good = s.q0 >= 0 && s.n >= 0 && s.n <= p.T_cap - s.q0;
+  const int end = p.cu[b + 1];
+  s.good = s.q0 >= 0 && end >= s.q0 && end <= p.T_cap;
+  s.n = s.good ? end - s.q0 : 0;
   s.ctx = 0;
   if (PAGED) {
     const int kv = p.kv_len[b];

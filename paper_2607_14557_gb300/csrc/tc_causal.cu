@@ -108,10 +108,10 @@ struct UnitWalk {
   // Units of sequence b per head; 0 where it leaves the buffers.
   __device__ __forceinline__ int groups_of(const GqaParams& p, int b, bool report) const {
     if (b >= p.B) return 0;
-    const int c0 = p.cu[b], n = p.cu[b + 1] - c0;
-    const bool good = c0 >= 0 && n >= 0 && n <= p.T_cap - c0;
+    const int c0 = p.cu[b], c1 = p.cu[b + 1];
+    const bool good = c0 >= 0 && c1 >= c0 && c1 <= p.T_cap;
     if (!good && report) record_error(p.err, kErrLayout);
-    return good ? (n + span - 1) / span : 0;
+    return good ? (c1 - c0 + span - 1) / span : 0;
   }
   // Which of sequences x .. x + 31 have a group g.
   __device__ __forceinline__ uint32_t reach(const GqaParams& p, int x) const {

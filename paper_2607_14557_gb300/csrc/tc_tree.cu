@@ -96,10 +96,12 @@ __device__ __forceinline__ Request read_request(const GqaParams& p, int b) {
   Request r{0, 0, 0, true};
   if (b >= p.B) return r;
   r.q0 = p.cu[b];
-  r.n = p.cu[b + 1] - r.q0;
+  const int end = p.cu[b + 1];
   r.kv = p.kv_len[b];
-  r.good = r.q0 >= 0 && r.n >= 0 && r.n <= p.T_cap - r.q0 && r.n <= p.max_new && r.kv >= r.n &&
-           r.kv <= kMaxKeys && r.kv <= (static_cast<long long>(p.max_pages) << p.page_shift);
+  r.good = r.q0 >= 0 && end >= r.q0 && end <= p.T_cap;
+  r.n = r.good ? end - r.q0 : 0;
+  r.good = r.good && r.n <= p.max_new && r.kv >= r.n && r.kv <= kMaxKeys &&
+           r.kv <= (static_cast<long long>(p.max_pages) << p.page_shift);
   if (!r.good) r.n = r.kv = 0;
   return r;
 }

@@ -63,3 +63,36 @@ def test_causal_offsets_that_fall_cost_their_own_rows_alone(dt, dh, cu, good):
     for a, e in taken:
         free[a:e] = False
     assert (got[free] == 5.0).all()
+
+
+@pytest.mark.parametrize("dt,dh", [("f32", 64), ("bf16", 128), ("f16", 64)])
+def test_offsets_and_lengths_of_minus_2_31(dt, dh):
+    """The difference to an offset of -2^31 passes 2^31: it is inconsistent like any other."""
+    rng = np.random.default_rng(6)
+    hq, hk, T, cu = 8, 1, 300, [0, 7, -2 ** 31, 9, 9, 300]
+    x = rnd(rng, (T, (hq + 2 * hk) * dh), dt)
+    h = host(x).reshape(T, hq + 2 * hk, dh)
+    o = torch.full((T, hq * dh), 5.0, dtype=TDT[dt], device=cuda())
+    ld = x.stride(0)
+    S.seer_attention_causal(x, ld, x[:, hq * dh:], ld, x[:, (hq + hk) * dh:], ld, o, o.stride(0), dt, i32(cu), 5, T, hq, hk, dh)
+    assert S.seer_check_device() == 2
+    got = host(o).reshape(T, hq, dh)
+    for a, e in ((0, 7), (9, 300)):
+        ref, bound = R.causal(h[a:e, :hq], h[a:e, hq:hq + hk], h[a:e, hq + hk:], [0, e - a], dt)
+        close(got[a:e], ref, bound)
+    assert (got[7:9] == 5.0).all()
+    # the same over pages: requests 0, 3 and 4 are well
+    page, kv_len, cu = 16, [40, 9, -2 ** 31, 30, 25], [0, 2, -2 ** 31, 4, 5, 8]
+    tab = np.arange(15).reshape(5, 3)
+    kv = rnd(rng, (15 * page, 2 * hk * dh), dt)
+    table, q = i32(tab), x[:8, :hq * dh].contiguous()
+    pages = S.make_pages(kv, table, 15, page, 3, hk, dh)
+    size = S.seer_attention_tree_workspace_size(dt, 5, hq, hk, dh, 4)
+    ws, o = torch.full((size,), 255, dtype=torch.uint8, device=cuda()), torch.full((8, hq * dh), 5.0, dtype=TDT[dt], device=cuda())
+    S.seer_attention_tree(q, q.stride(0), o, o.stride(0), dt, i32(cu), i32(kv_len), None, 5, 8, hq, 4, pages, ws, size)
+    assert S.seer_check_device() == 2
+    got, kvh = host(o).reshape(8, hq, dh), host(kv).reshape(-1, 2, hk, dh)
+    for b, a, e in ((0, 0, 2), (3, 4, 5), (4, 5, 8)):
+        ref, bound = R.tree(host(q).reshape(8, hq, dh)[a:e], kvh, [tab[b].tolist()], page, [0, e - a], [kv_len[b]], None, dt)
+        close(got[a:e], ref, bound)
+    assert (got[2:4] == 5.0).all()
