@@ -10,6 +10,24 @@ namespace seer {
 constexpr int kAttnRows = 128;     // query rows of a tile
 constexpr int kAttnTiles = 2;      // query tiles of a unit
 
+// Query rows and visible keys of segment i; none where its offsets leave the buffers.
+// (A difference of unchecked offsets may pass 2^31.)
+struct SegmentRows {
+  int L, kv;
+  bool good;
+};
+__device__ __forceinline__ SegmentRows segment_rows(const int* cu, const int* cu_kv, const int* kv_len, int i, int T_cap) {
+  const int c0 = cu[i], c1 = cu[i + 1];
+  SegmentRows r;
+  r.good = c0 >= 0 && c1 >= c0 && c1 <= T_cap;
+  r.L = r.good ? c1 - c0 : 0;
+  const long long Lkv = cu_kv ? static_cast<long long>(cu_kv[i + 1]) - cu_kv[i] : r.L;   // rows of the segment's K/V
+  r.kv = kv_len ? kv_len[i] : static_cast<int>(min(Lkv, 0x7fffffffll));
+  r.good = r.good && Lkv >= 0 && r.kv <= Lkv && (r.L == 0 || r.kv > 0);
+  if (!r.good) r.kv = 0;
+  return r;
+}
+
 // One block: per-segment key counts -> work units (b, h, first q-tile, tiles)
 // of up to NT query tiles, ordered by descending kv length so the longest
 // segments start first.
@@ -24,13 +42,9 @@ __device__ __forceinline__ void attn_schedule_block(const ScheduleArgs& a, int* 
   int* off = sh + 2 * B;     // [B]
   int* rank = sh + 3 * B;    // [B]
   for (int i = threadIdx.x; i < B; i += blockDim.x) {
-    const int L = cu[i + 1] - cu[i];
-    const int Lkv = cu_kv ? cu_kv[i + 1] - cu_kv[i] : L;   // rows of the segment's K/V
-    int kv = kv_len ? kv_len[i] : Lkv;
-    if (L < 0 || cu[i] < 0 || cu[i + 1] > T_cap || kv > Lkv || (L > 0 && kv <= 0)) {
-      record_error(err, kErrLayout);
-      kv = 0;
-    }
+    const SegmentRows r = segment_rows(cu, cu_kv, kv_len, i, T_cap);
+    const int L = r.L, kv = r.kv;
+    if (!r.good) record_error(err, kErrLayout);
     ntile[i] = (kv > 0) ? (L + kAttnRows * kAttnTiles - 1) / (kAttnRows * kAttnTiles) : 0;   // work units (tile groups) per head
     kvs[i] = kv;
   }

@@ -146,13 +146,9 @@ __device__ __forceinline__ int make_inline_schedule(const AttnParams& p, const I
   int* groups = scratch + MAX_INLINE_B;
   const int i = threadIdx.x;
   if (i < p.B) {
-    const int c0 = p.cu[i], c1 = p.cu[i + 1], L = c1 - c0;
-    const int Lkv = p.cu_kv ? p.cu_kv[i + 1] - p.cu_kv[i] : L;
-    int kv = p.kv_len ? p.kv_len[i] : Lkv;
-    if (L < 0 || c0 < 0 || c1 > p.T_cap || kv > Lkv || (L > 0 && kv <= 0)) {
-      record_error(p.err, kErrLayout);
-      kv = 0;
-    }
+    const SegmentRows r = segment_rows(p.cu, p.cu_kv, p.kv_len, i, p.T_cap);
+    const int L = r.L, kv = r.kv;
+    if (!r.good) record_error(p.err, kErrLayout);
     kvs[i] = kv;
     groups[i] = kv > 0 ? (L + BQ * NT - 1) / (BQ * NT) : 0;
   }
