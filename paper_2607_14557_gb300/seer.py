@@ -58,6 +58,7 @@ class seer_pages(ctypes.Structure):
     _fields_ = [("kv", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n_pages", ctypes.c_int),
                 ("page_size", ctypes.c_int), ("max_pages", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
                 ("head_dim", ctypes.c_int)]
+    _held = None                    # of tensors: (dtype code, device index, rows of the table), see make_pages
 
 
 _lib = None
@@ -276,8 +277,10 @@ def seer_attention_noalloc(qkv, o, dt, cu_seqlens, kv_len, B, T_capacity, n_head
 
 
 # ----------------------------------------------------------------- paged K/V cache
-# These go through the extension module _seer_binding: tensors have to be on the current
-# device, index arrays contiguous and of the type that the C entry reads (ValueError).
+# These go through the extension module _seer_binding, which refuses (ValueError) tensors on
+# another device than the current one, index arrays that are not contiguous, of another type
+# than the C entry reads or shorter than the call names, rows of another type than dt or that
+# end behind their memory, and a workspace of fewer than ws_bytes.
 _native_module = None
 
 
@@ -299,7 +302,12 @@ def make_pages(kv, table, n_pages, page_size, max_pages, n_kv_heads, head_dim) -
         raise ValueError("table must be a contiguous int32 tensor")
     if isinstance(kv, torch.Tensor) and isinstance(table, torch.Tensor) and kv.device != table.device:
         raise ValueError("kv and table are on different devices")
-    return seer_pages(_p(kv), _p(table), n_pages, page_size, max_pages, n_kv_heads, head_dim)
+    pages = seer_pages(_p(kv), _p(table), n_pages, page_size, max_pages, n_kv_heads, head_dim)
+    on = next((t.device for t in (kv, table) if isinstance(t, torch.Tensor)), None)
+    pages._held = (_dt(kv.dtype) if isinstance(kv, torch.Tensor) else -1,
+                   -1 if on is None else (on.index if on.type == "cuda" else 1 << 20),
+                   table.numel() // max_pages if isinstance(table, torch.Tensor) and max_pages > 0 else -1)
+    return pages
 
 
 def seer_page_tables(cached_len, new_len, B, page_size, n_pages, free_pages, n_free, free_head, table, max_pages, T_cap,
