@@ -8,9 +8,12 @@ runtime so it shares one runtime instance with PyTorch in the same process.
 from __future__ import annotations
 
 import concurrent.futures
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -36,17 +39,35 @@ def _cuda_lib_dir(nv: str) -> str:
     return os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nv))), "lib64")
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(BINDING):
+def _older(path: str, deps) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(p) > os.path.getmtime(path) for p in deps if os.path.exists(p))
+
+
+def _lib_stale() -> bool:
+    return _older(LIB, [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.join(ROOT, "include", "seer.h"), __file__])
+
+
+def _binding_stale() -> bool:
+    if _older(BINDING, [os.path.join(CSRC, "binding.cpp"), os.path.join(ROOT, "include", "seer.h"), __file__]):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["binding.cpp"]] + [os.path.join(ROOT, "include", "seer.h"), __file__]
-    return any(os.path.getmtime(p) > t for p in deps if os.path.exists(p))
+    try:
+        with open(os.path.join(BUILD, "binding.for")) as f:
+            return f.read() != _binding_for()
+    except OSError:
+        return True
+
+
+def _binding_for() -> str:
+    """The interpreter and torch that the extension module is compiled against."""
+    return f"python {sys.version} torch {importlib.metadata.version('torch')} at {os.path.dirname(importlib.util.find_spec('torch').origin)}"
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    """Compile and link libseer.so if any source is newer; return its path."""
-    if not force and not _stale():
+    """Compile and link what is older than its sources; return libseer.so's path.  Where the
+    extension module cannot be compiled (no Python or torch headers, no host compiler), libseer.so is
+    there all the same when the error is raised."""
+    lib_stale, binding_stale = force or _lib_stale(), force or _binding_stale()
+    if not lib_stale and not binding_stale:
         return LIB
     nv = nvcc()
     os.makedirs(BUILD, exist_ok=True)
@@ -66,17 +87,15 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         return obj
 
     with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        binding = ex.submit(_compile_binding, nv)
-        objs = list(ex.map(compile_one, SOURCES))
-        binding_obj = binding.result()
-    tmp = LIB + ".tmp"
-    libdir = _cuda_lib_dir(nv)
-    cmd = [nv, *ARCH, "-shared", "-cudart", "shared", "-o", tmp, *objs, "-Xlinker", f"-rpath,{libdir}"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, LIB)
-    _link_binding(binding_obj)
+        binding = ex.submit(_compile_binding, nv) if binding_stale else None
+        if lib_stale:
+            objs = list(ex.map(compile_one, SOURCES))
+            tmp = LIB + ".tmp"
+            libdir = _cuda_lib_dir(nv)
+            _run([nv, *ARCH, "-shared", "-cudart", "shared", "-o", tmp, *objs, "-Xlinker", f"-rpath,{libdir}"], "link")
+            os.replace(tmp, LIB)
+    if binding is not None:
+        _link_binding(binding.result())
     return LIB
 
 
@@ -106,8 +125,9 @@ def _link_binding(obj: str) -> None:
     _run([os.environ.get("CXX", "g++"), "-shared", "-o", tmp, obj, "-L", PKG, "-l:libseer.so", "-L", lib, "-ltorch_python", "-lc10_cuda",
           "-lc10", f"-Wl,-rpath,$ORIGIN:{lib}"], "linking the binding")
     os.replace(tmp, BINDING)
+    with open(os.path.join(BUILD, "binding.for"), "w") as f:
+        f.write(_binding_for())
 
 
 if __name__ == "__main__":
-    import sys
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
