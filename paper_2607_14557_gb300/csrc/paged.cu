@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(kAcceptThreads) kv_accept_kernel(const KvAccep
   const int b = blockIdx.y;
   const int c = a.cached[b];
   int n = a.n_accepted[b];
-  bool good = c >= 0 && n >= 0 && n <= a.max_draft;
+  bool good = c >= 0 && n >= 0 && n <= a.max_draft && c <= kMaxKeys - n;
   if (!good) n = 0;
   for (int k = threadIdx.x; k < n; k += kAcceptThreads) {
     const int* list = a.accepted + static_cast<size_t>(b) * a.max_draft;

@@ -96,3 +96,14 @@ def test_offsets_and_lengths_of_minus_2_31(dt, dh):
         ref, bound = R.tree(host(q).reshape(8, hq, dh)[a:e], kvh, [tab[b].tolist()], page, [0, e - a], [kv_len[b]], None, dt)
         close(got[a:e], ref, bound)
     assert (got[2:4] == 5.0).all()
+
+
+def test_accept_past_the_longest_request_keeps_nothing():
+    """A request has at most 2^31 - 1025 rows, so that the lengths after it are still lengths."""
+    kv, table = torch.zeros((5 * 1024, 128), dtype=torch.bfloat16, device=cuda()), torch.zeros((3, 1 << 21), dtype=torch.int32, device=cuda())
+    pages = S.make_pages(kv, table, 5, 1024, 1 << 21, 1, 64)
+    top = 2 ** 31 - 1025
+    for cached, code, want in (([top - 2, 7, 8], 0, [top, 9, 10]), ([top - 1, 7, 8], 2, [top - 1, 9, 10]), ([2 ** 31 - 1024 + 1000, 7, 8], 2, [2 ** 31 - 24, 9, 10])):
+        out = i32([-7] * 3)
+        S.seer_kv_accept("bf16", i32(cached), i32([[0, 1]] * 3), i32([2] * 3), 3, 2, pages, out)
+        assert S.seer_check_device() == code and out.tolist() == want
