@@ -360,7 +360,7 @@ seer_status seer_gather_response(const void* x_packed, seer_dtype dt, const int3
  * What the device finds inconsistent (lengths outside the buffers, pages outside
  * the pool, too few free pages) is recorded (seer_check_device) and that
  * request's or row's part left out; no access leaves the buffers named.  T_cap is at
- * most 2^30; masks are 8-byte aligned.
+ * most 2^30, and where it is 0 row buffers may be NULL; masks are 8-byte aligned.
  * ------------------------------------------------------------------------- */
 #define SEER_MAX_DRAFT 64          /* new rows of a request that a tree can hold */
 #define SEER_MAX_REQUESTS 16384    /* requests of a call */

@@ -168,12 +168,13 @@ seer_status seer_kv_append(const void* qkv, int ld_qkv, seer_dtype dt, int n_hea
   const int dh = pages->head_dim;
   const long long q = static_cast<long long>(n_heads) * dh, k = static_cast<long long>(pages->n_kv_heads) * dh;
   if (q > (1 << 20)) return fail(SEER_ERR_UNSUPPORTED, "append: rows of more than 2^20 query values");
+  if (!(theta == 0.f || theta >= 1.f) || !std::isfinite(theta))
+    return fail(SEER_ERR_INVALID_ARG, "append: theta must be 0 (off) or a finite base from 1 on");
+  if (T_cap == 0) return SEER_OK;             // (empty buffers may have no address)
   SEER_TRY(check_rows("append", "qkv", qkv, ld_qkv, q + 2 * k, dt));
   if (rotated) SEER_TRY(check_rows("append", "rotated", rotated, ld_rotated, q + k, dt));
   if (rotated == qkv && ld_rotated != ld_qkv) return fail(SEER_ERR_INVALID_ARG, "append: in place, rotated has qkv's ld");
   if (!slot) return fail(SEER_ERR_INVALID_ARG, "append: slot is null");
-  if (!(theta == 0.f || theta >= 1.f) || !std::isfinite(theta))
-    return fail(SEER_ERR_INVALID_ARG, "append: theta must be 0 (off) or a finite base from 1 on");
   if (theta > 0.f && !position) return fail(SEER_ERR_INVALID_ARG, "append: rotation needs positions");
   DeviceInfo* di;
   SEER_TRY(device_info(&di));
@@ -234,6 +235,7 @@ seer_status seer_attention_causal(const void* q, int ld_q, const void* k, int ld
   SEER_TRY(check_heads("causal attention", n_heads, n_kv_heads, head_dim, dt));
   SEER_TRY(check_capacity("causal attention", T_cap));
   if (!cu_seqlens) return fail(SEER_ERR_INVALID_ARG, "causal attention: cu_seqlens is null");
+  if (T_cap == 0) return SEER_OK;
   const long long qc = static_cast<long long>(n_heads) * head_dim, kc = static_cast<long long>(n_kv_heads) * head_dim;
   SEER_TRY(check_rows("causal attention", "q", q, ld_q, qc, dt));
   SEER_TRY(check_rows("causal attention", "k", k, ld_k, kc, dt));
@@ -258,7 +260,6 @@ seer_status seer_attention_causal(const void* q, int ld_q, const void* k, int ld
   p.n_kv = n_kv_heads;
   p.head_dim = head_dim;
   p.err = di->err;
-  if (T_cap == 0) return SEER_OK;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (is16(dt)) {
     const int g = n_heads / n_kv_heads;
@@ -303,6 +304,7 @@ seer_status seer_attention_tree(const void* q, int ld_q, void* o, int ld_o, seer
   if (reinterpret_cast<uintptr_t>(mask) % 8 != 0) return fail(SEER_ERR_UNSUPPORTED, "tree attention: mask must be 8-byte aligned");
   if (static_cast<double>(B) * pages->n_kv_heads * max_draft * (static_cast<double>(pages->max_pages) * pages->page_size / 128 + 8) > kMaxTreeTiles)
     return fail(SEER_ERR_UNSUPPORTED, "tree attention: more key tiles than 2^50 fit the tables");
+  if (T_cap == 0) return SEER_OK;
   const long long qc = static_cast<long long>(n_heads) * pages->head_dim;
   SEER_TRY(check_rows("tree attention", "q", q, ld_q, qc, dt));
   SEER_TRY(check_rows("tree attention", "o", o, ld_o, qc, dt));
@@ -337,7 +339,6 @@ seer_status seer_attention_tree(const void* q, int ld_q, void* o, int ld_o, seer
   p.max_pages = pg.max_pages;
   p.part = static_cast<float*>(ws);
   p.err = di->err;
-  if (T_cap == 0) return SEER_OK;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (is16(dt)) {
     const int g = n_heads / pg.n_kv, page = 1 << pg.page_shift;

@@ -107,3 +107,20 @@ def test_accept_past_the_longest_request_keeps_nothing():
         out = i32([-7] * 3)
         S.seer_kv_accept("bf16", i32(cached), i32([[0, 1]] * 3), i32([2] * 3), 3, 2, pages, out)
         assert S.seer_check_device() == code and out.tolist() == want
+
+
+def test_steps_without_rows():
+    """Empty tensors have no address; a step that adds no row calls with them all the same."""
+    B, page, hq, hk, dh = 2, 16, 4, 2, 64
+    kv, table = rnd(np.random.default_rng(0), (10 * page, 2 * hk * dh), "bf16"), i32([[0, 1], [2, 3]])
+    before = kv.clone()
+    pages = S.make_pages(kv, table, 10, page, 2, hk, dh)
+    none = torch.zeros(0, dtype=torch.int32, device=cuda())
+    x, o = torch.zeros((0, (hq + 2 * hk) * dh), dtype=torch.bfloat16, device=cuda()), torch.zeros((0, hq * dh), dtype=torch.bfloat16, device=cuda())
+    ld = (hq + 2 * hk) * dh
+    cu, kv_len, head_out = i32([-7] * 3), i32([-7] * 2), i32([-7])
+    S.seer_page_tables(i32([20, 5]), i32([0, 0]), B, page, 10, none, 0, i32([0]), table, 2, 0, None, cu, kv_len, none, none, None, head_out)
+    S.seer_kv_append(x, ld, "bf16", hq, 0, None, none, none, 10000.0, x, ld, pages)
+    S.seer_attention_causal(x, ld, x, ld, x, ld, o, hq * dh, "bf16", cu, B, 0, hq, hk, dh)
+    S.seer_attention_tree(x, ld, o, hq * dh, "bf16", cu, kv_len, None, B, 0, hq, 4, pages, None, 0)
+    assert cu.tolist() == [0, 0, 0] and kv_len.tolist() == [20, 5] and torch.equal(kv, before) and S.seer_check_device() == 0
