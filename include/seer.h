@@ -396,7 +396,10 @@ typedef struct {
  *                 cu_new_out[B] are untouched
  * With parent or mask_out a request has at most SEER_MAX_DRAFT new rows.  Table
  * entries of taken pages beyond the free list become -1.  No output is an input.
- * Every output depends on the inputs alone, so a call may be repeated. */
+ * Every output depends on the inputs alone, so a call may be repeated.
+ * Entries from ceil(cached_len / page_size) on are written over, whatever they hold:
+ * the pages of rows that the caller drops (rejected drafts, ended requests) are the
+ * caller's to put back, see seer_kv_accept. */
 seer_status seer_page_tables(const int32_t* cached_len, const int32_t* new_len, int B, int page_size, int n_pages,
                              const int32_t* free_pages, int n_free, const int32_t* free_head, int32_t* table,
                              int max_pages, int T_cap, const int32_t* parent, int32_t* cu_new_out, int32_t* kv_len_out,
@@ -421,7 +424,12 @@ seer_status seer_kv_append(const void* qkv, int ld_qkv, seer_dtype dt, int n_hea
  * (accepted ascends strictly, as the rows of a path from the root do), and
  * len_out[b] = cached_len[b] + n_accepted[b] is its next cached_len.  A request with
  * a list that does not ascend, leaves the draft or meets a page outside the pool
- * keeps nothing and is recorded.  One call per layer's pool. */
+ * keeps nothing and is recorded.  One call per layer's pool.
+ * The table is as before: its entries from ceil(len_out[b] / page_size) up to
+ * ceil(kv_len[b] / page_size) are pages that only rejected rows filled.  Before the
+ * next seer_page_tables, which writes over them, the caller puts these k pages back,
+ * e.g. into free_pages[head - k .. head - 1], those already taken, and lowers the free
+ * list's head by k. */
 seer_status seer_kv_accept(seer_dtype dt, const int32_t* cached_len, const int32_t* accepted, const int32_t* n_accepted,
                            int B, int max_draft, const seer_pages* pages, int32_t* len_out, void* stream);
 

@@ -124,3 +124,45 @@ def test_steps_without_rows():
     S.seer_attention_causal(x, ld, x, ld, x, ld, o, hq * dh, "bf16", cu, B, 0, hq, hk, dh)
     S.seer_attention_tree(x, ld, o, hq * dh, "bf16", cu, kv_len, None, B, 0, hq, 4, pages, None, 0)
     assert cu.tolist() == [0, 0, 0] and kv_len.tolist() == [20, 5] and torch.equal(kv, before) and S.seer_check_device() == 0
+
+
+def test_pages_of_rejected_rows_put_back_keep_the_pool_from_running_dry():
+    """Rounds of drafting 24 rows and keeping 1 to 5: every round leaves one or two pages a request that only
+    rejected rows filled.  Put back as seer_kv_accept says, the pool holds for ever; left, it is dry within 20 rounds."""
+    rng = np.random.default_rng(4)
+    B, page, draft, hk, dh, rounds = 4, 16, 24, 1, 64, 60
+    max_pages = (100 + 5 * rounds + draft) // page + 2
+    n_pages = B * ((100 + 5 * rounds + draft) // page + 1)
+    kv = torch.zeros((n_pages * page, 2 * hk * dh), dtype=torch.bfloat16, device=cuda())
+    order = rng.permutation(n_pages)
+    tab = np.full((B, max_pages), -1)
+    tab[:, :7] = order[:7 * B].reshape(B, 7)
+    table, free, head = i32(tab), i32(order), i32([7 * B])
+    pages = S.make_pages(kv, table, n_pages, page, max_pages, hk, dh)
+    cached, new = i32([100] * B), i32([draft] * B)
+    kept_rows = [[] for _ in range(B)]
+    taken = 0
+    for _ in range(rounds):
+        cu, kv_len, slot, pos, head_out, len_out = (torch.zeros(n, dtype=torch.int32, device=cuda()) for n in (B + 1, B, B * draft, B * draft, 1, B))
+        S.seer_page_tables(cached, new, B, page, n_pages, free, n_pages, head, table, max_pages, B * draft, None, cu, kv_len, slot, pos, None, head_out)
+        taken += int(head_out) - int(head)
+        assert (slot >= 0).all() and slot.unique().numel() == B * draft
+        x = rnd(rng, (B * draft, 2 * hk * dh), "bf16")
+        S.seer_kv_append(x, x.stride(0), "bf16", 0, B * draft, None, slot, None, 0.0, None, 0, pages)
+        keep = [sorted(rng.choice(draft, int(rng.integers(1, 6)), replace=False).tolist()) for _ in range(B)]
+        S.seer_kv_accept("bf16", cached, i32([k + [-1] * (draft - len(k)) for k in keep]), i32([len(k) for k in keep]), B, draft, pages, len_out)
+        for b, k in enumerate(keep):
+            kept_rows[b] += [x[b * draft + a] for a in k]
+        col = torch.arange(max_pages, device=cuda())[None]
+        back = (col >= ((len_out + page - 1) // page)[:, None]) & (col < ((kv_len + page - 1) // page)[:, None])
+        k = int(back.sum())
+        free[int(head_out) - k:int(head_out)] = table[back]
+        head.copy_(head_out - k)
+        cached.copy_(len_out)
+        owned = table[col < ((cached + page - 1) // page)[:, None]].tolist() + free[int(head):].tolist()
+        assert sorted(owned) == list(range(n_pages))        # every page in the table or free, once
+    assert taken > 2 * n_pages and S.seer_check_device() == 0
+    for b in range(B):
+        t = torch.arange(100, int(cached[b]), device=cuda())
+        rows = table[b].long()[t // page] * page + t % page
+        assert torch.equal(kv[rows], torch.stack(kept_rows[b]))
