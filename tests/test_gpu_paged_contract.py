@@ -166,3 +166,30 @@ def test_pages_of_rejected_rows_put_back_keep_the_pool_from_running_dry():
         t = torch.arange(100, int(cached[b]), device=cuda())
         rows = table[b].long()[t // page] * page + t % page
         assert torch.equal(kv[rows], torch.stack(kept_rows[b]))
+
+
+@pytest.mark.parametrize("theta", [10000.0, 500000.0, 1.0])
+@pytest.mark.parametrize("top", [2 ** 24, 2 ** 29, 2 ** 31 - 1])
+def test_rotation_of_far_positions_against_a_longer_arithmetic(theta, top):
+    """Angles in 60 decimal digits.  Counted: fp32 sine and cosine of an angle rounded to fp32 in half turns (2^-25
+    of half a turn: pi 2^-25), their 2^-23 each and the products' and sum's 2^-24; the rate's fp64 rounding
+    (3.4 2^-53 of it: exp2, its argument, 2 pi, the division) times the position."""
+    from decimal import Decimal as D, getcontext
+    getcontext().prec = 60
+    two_pi = D("6.28318530717958647692528676655900576839433879875021164194988918")
+    rng = np.random.default_rng(5)
+    dh, T, page = 128, 16, 16
+    pos = [top - int(v) for v in rng.integers(0, top // 2, T - 1)] + [top]
+    kv, x = torch.zeros((page, 2 * dh), device=cuda()), rnd(rng, (T, 3 * dh), "f32")
+    pages = S.make_pages(kv, i32([[0]]), 1, page, 1, 1, dh)
+    out = torch.zeros((T, 2 * dh), device=cuda())
+    S.seer_kv_append(x, 3 * dh, "f32", 1, T, None, i32(range(T)), i32(pos), theta, out, 2 * dh, pages)
+    rate = [D(theta) ** (D(-2 * i) / dh) for i in range(dh // 2)]
+    angle = np.array([[float((D(p) * r) % two_pi) for r in rate] for p in pos])
+    h, got = host(x)[:, :2 * dh].reshape(T, 2, 2, dh // 2), host(out).reshape(T, 2, 2, dh // 2)
+    c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    a, b = h[:, :, 0], h[:, :, 1]
+    ref = np.stack([a * c - b * s, b * c + a * s], 2)
+    bound = (np.abs(a) + np.abs(b))[:, :, None] * (math.pi * 2.0 ** -25 + top * 3.4 * 2.0 ** -53 + 2.0 ** -23 + 3 * 2.0 ** -24)
+    close(got, ref, bound)
+    assert S.seer_check_device() == 0
