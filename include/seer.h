@@ -422,7 +422,7 @@ seer_status seer_page_tables(const int32_t* cached_len, const int32_t* new_len, 
  * NULL) overrides T_cap.  slot -1: nothing is stored for the row; slots of a call
  * are distinct (two rows with one leave pieces of either there).  position: device
  * int32 [T_cap], NULL when theta is 0; theta is 0 or at least 1.  An angle is off by
- * at most 2^-22 rad up to position 2^29 and 2^-20 up to the last; one rounding per
+ * at most 2^-21 rad up to position 2^29 and 2^-20 up to the last; one rounding per
  * value. */
 seer_status seer_kv_append(const void* qkv, int ld_qkv, seer_dtype dt, int n_heads, int T_cap, const int32_t* M_dev,
                            const int32_t* slot, const int32_t* position, float theta, void* rotated, int ld_rotated,
