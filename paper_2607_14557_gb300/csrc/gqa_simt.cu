@@ -5,8 +5,9 @@
 // key/value head, 128 threads with 4 (2) rows x 4 keys each; keys in tiles of 64 with an online softmax (expf),
 // K, V and Q in shared memory by cp.async, the next K under way during a tile's PV and the
 // next V during the next scores.  Lanes as in the fp32 kernels of simt.cu.
-// Bound by shared-memory reads and, for few blocks, by latency: 1500 and 700 rows, 8 / 2 heads of
-// 128, 5.6 GFLOP in 183 us (31 TFLOP/s).
+// Bound, at 4 x 4 values a thread, by shared-memory reads (eight of 16 bytes for 64 multiply-adds)
+// and, for few blocks, by latency: 1500 and 700 rows, 8 / 2 heads of 128, 5.6 GFLOP in 172 us (33
+// TFLOP/s).
 // Few blocks would leave the longest row's tiles in a chain (5 prompts of 1 .. 300 rows, 34 us
 // with one block per tile of rows), so its keys are shared: causal, by a cluster of blocks
 // that merge through distributed shared memory; paged, by blocks whose unnormalised sums
@@ -123,7 +124,12 @@ __device__ __forceinline__ int2 tile_at(const GqaParams& p, int G, long slot, lo
 // Rows [R0, R0 + BQ) of request b's (token, head) rows.  CLUSTER: the blocks of a cluster share
 // the tile's keys.
 template <bool PAGED, bool CLUSTER, int BQ, int HALVES>
-__device__ __forceinline__ void attend_tile(const GqaParams& p, int b, int kvh, int R0, const Span& sp, int split) {
+__device__ __forceinline__ void attend_tile(const GqaParams& p, int b, int kvh, int R0, int split) {
+  const Span sp = read_span<PAGED>(p, b);
+  if (!sp.good) {
+    if (threadIdx.x == 0) record_error(p.err, kErrLayout);
+    return;
+  }
   constexpr int TM = BQ / TY, DIMS = 64 * HALVES, ld = row_ld(DIMS);
   const int dh = p.head_dim, G = p.n_heads / p.n_kv, parts = p.splits;
   const long long all_rows = static_cast<long long>(sp.n) * G;
@@ -389,7 +395,7 @@ __device__ __noinline__ void take_all_if_one_falls(const GqaParams& p, int worke
   for (long i = worker;; i += checkers) {
     const int2 at = tile_at<BQ>(p, p.n_heads / p.n_kv, i / p.n_kv, reinterpret_cast<long*>(gqa_smem));
     if (at.x >= p.B) return;
-    attend_tile<false, CLUSTER, BQ, HALVES>(p, at.x, static_cast<int>(i % p.n_kv), at.y * BQ, read_span<false>(p, at.x), split);
+    attend_tile<false, CLUSTER, BQ, HALVES>(p, at.x, static_cast<int>(i % p.n_kv), at.y * BQ, split);
     __syncthreads();
   }
 }
@@ -404,18 +410,15 @@ __global__ void __launch_bounds__(NTH, HALVES == 1 && BQ == 32 ? 4 : 1) gqa_simt
   if constexpr (PAGED) {
     const int tiles = (p.max_new * G + BQ - 1) / BQ, unit = blockIdx.x / parts;
     const int R0 = (unit % tiles) * BQ, kvh = unit / tiles % p.n_kv, b = unit / tiles / p.n_kv;
-    const Span sp = read_span<PAGED>(p, b);
-    if (sp.good) attend_tile<PAGED, CLUSTER, BQ, HALVES>(p, b, kvh, R0, sp, split);
-    else if (threadIdx.x == 0) record_error(p.err, kErrLayout);
+    attend_tile<PAGED, CLUSTER, BQ, HALVES>(p, b, kvh, R0, split);
   } else {
     const int units = static_cast<int>(causal_units(p, BQ)), worker = blockIdx.x / parts, checkers = gridDim.x / parts - units;
     if (worker >= checkers) {
       const int unit = units - 1 - (worker - checkers);    // a sequence's last rows, which see the most keys, first
       const int slot = unit / p.n_kv, kvh = unit % p.n_kv, b = sequence_at<BQ>(p, G, slot);
       const long tile = slot - (static_cast<long>(p.cu[b]) * G / BQ + b);
-      const Span sp = read_span<PAGED>(p, b);
-      if (sp.good && tile >= 0 && tile <= 0x7fffffff / BQ)
-        attend_tile<PAGED, CLUSTER, BQ, HALVES>(p, b, kvh, static_cast<int>(tile) * BQ, sp, split);
+      if (tile < 0 || tile > 0x7fffffff / BQ) return;
+      attend_tile<PAGED, CLUSTER, BQ, HALVES>(p, b, kvh, static_cast<int>(tile) * BQ, split);
       return;
     }
     take_all_if_one_falls<CLUSTER, BQ, HALVES>(p, worker, checkers, split);
@@ -458,9 +461,9 @@ long paged_units(int B, int n_heads, int n_kv, int max_new, int rows) {
   return static_cast<long>(B) * n_kv * ((static_cast<long>(max_new) * (n_heads / n_kv) + rows - 1) / rows);
 }
 // Rows of a block: 32, or 16 where blocks of 32 would leave SMs idle.  us at 32 / 16: prompts of
-// 1 .. 300 rows, 4 heads of 64 (96 blocks) 16.1 / 13.9; eight drafts of 8 rows over 300 .. 3000
-// (16) 37 / 31; one prompt of 2000, 4 heads of 128 (251) 167 / 204; eight of 300, 8 heads of 64
-// (664) 43.9 / 44.4.
+// 1 .. 300 rows, 4 heads of 64 (96 blocks) 16.5 / 14.2; eight drafts of 8 rows over 300 .. 3000
+// (16) 48 / 41; one prompt of 2000, 4 heads of 128 (251) 141 / 152; eight of 300, 8 heads of 64
+// (664) 43.3 / 45.8.
 int block_rows(long units_of_32, int num_sms) { return units_of_32 <= num_sms ? 16 : 32; }
 
 template <bool PAGED, bool CLUSTER, int BQ, int HALVES>
