@@ -306,7 +306,7 @@ def make_pages(kv, table, n_pages, page_size, max_pages, n_kv_heads, head_dim) -
     on = next((t.device for t in (kv, table) if isinstance(t, torch.Tensor)), None)
     pages._held = (_dt(kv.dtype) if isinstance(kv, torch.Tensor) else -1,
                    -1 if on is None else (on.index if on.type == "cuda" else 1 << 20),
-                   table.numel() // max_pages if isinstance(table, torch.Tensor) and max_pages > 0 else -1)
+                   min(table.numel() // max_pages, MAX_REQUESTS) if isinstance(table, torch.Tensor) and max_pages > 0 else -1)
     return pages
 
 
