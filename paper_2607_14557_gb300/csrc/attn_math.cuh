@@ -91,7 +91,7 @@ __device__ __forceinline__ void load_columns(const uint16_t* row, int lane, floa
 // One row over keys [begin, end) by a warp, in fp32 from global memory: for rows whose tile
 // holds a value that is infinite or NaN and that not every row sees, which the MMA would
 // multiply by the hidden rows' P = 0.  at(j): key j.  One pass, eight keys' loads at a time; it
-// ends early where nothing but NaN can come out.  ~20 ms for 256 rows of 12k keys on one SM.
+// ends early where nothing but NaN can come out.  47 ms for 256 rows of 11.8k keys on one SM.
 template <bool F16, int DH, typename At>
 __device__ __forceinline__ RowSums<DH> attend_row(const uint16_t* q, int begin, int end, const At& at, int lane) {
   constexpr int N = DH / 32, KEYS = 8;

@@ -24,7 +24,8 @@
 //
 // Bound by the softmax chain of the two tiles (a round of both takes 1.36 us against 1.09 of
 // MMA work) and ~2.4 us at a unit's end: one prompt of 11792 rows, 32 / 8 heads of 128, 1.14
-// TFLOP in 0.65 ms (1750 TFLOP/s; 0.72 at the power cap), 16 prompts of 83 .. 1693 rows 0.11 TFLOP in 103 us.
+// TFLOP in 0.64 to 0.76 ms over boxes and power (1510 to 1770 TFLOP/s), 16 prompts of 83 .. 1693
+// rows, 0.11 TFLOP, in 103 to 109 us.
 //
 // P is exponentiated in fp32 and rounded to the 16-bit type that the PV MMA reads; the row
 // sums add the rounded values, so numerator and normaliser carry the same rounding.

@@ -22,8 +22,8 @@
 //   warp 1     MMA issuer: S = Q K_j^T, then O += P V_j with P written over S
 //   warps 2-5  softmax, a thread per row; warps without a row of the tile only pass on
 // Measured (32 / 8 heads of 128): one token for each of 64 requests over 200 .. 8000 cached rows,
-// 539 MB, 97 us (5.5 TB/s); 12 trees of 16 .. 64 rows over 500 .. 12000, 179 MB, 58 us; one token
-// over 12000 rows 21 us, two over 700 and 433 12.8.
+// 539 MB, 98 us (5.5 TB/s); 12 trees of 16 .. 64 rows over 500 .. 12000, 179 MB, 60 us; one token
+// over 12000 rows 21 us, two over 700 and 433 13.3.  The softmax warps spill 180 .. 230 bytes.
 // Hidden keys and non-finite values are treated as in tc_causal.cu: scores dropped, value
 // rows past the request's end cleared, and the rows of a piece whose masked tile holds a
 // non-finite value left to recompute_pieces() after the last piece.
