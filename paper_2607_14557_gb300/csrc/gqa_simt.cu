@@ -383,7 +383,7 @@ __device__ __forceinline__ void attend_tile(const GqaParams& p, int b, int kvh, 
 // The blocks ahead of a causal call's look through all offsets.  Where one falls, the others' slots
 // may have led past some sequences' tiles, so these blocks take all tiles in turn.
 template <bool CLUSTER, int BQ, int HALVES>
-__device__ __noinline__ void take_all_if_one_falls(const GqaParams& p, int worker, int checkers, int split) {
+__device__ __noinline__ void take_all_if_one_falls(const GqaParams& p, int worker, int scouts, int split) {
   int falls = 0;
 #pragma unroll 4
   for (int i = threadIdx.x; i < p.B; i += NTH) falls |= p.cu[i] > p.cu[i + 1];
@@ -392,7 +392,7 @@ __device__ __noinline__ void take_all_if_one_falls(const GqaParams& p, int worke
       if (!read_span<false>(p, i).good) record_error(p.err, kErrLayout);
   if (!__syncthreads_or(falls)) return;
   extern __shared__ float4 gqa_smem[];
-  for (long i = worker;; i += checkers) {
+  for (long i = worker;; i += scouts) {
     const int2 at = tile_at<BQ>(p, p.n_heads / p.n_kv, i / p.n_kv, reinterpret_cast<long*>(gqa_smem));
     if (at.x >= p.B) return;
     attend_tile<false, CLUSTER, BQ, HALVES>(p, at.x, static_cast<int>(i % p.n_kv), at.y * BQ, split);
@@ -412,16 +412,16 @@ __global__ void __launch_bounds__(NTH, HALVES == 1 && BQ == 32 ? 4 : 1) gqa_simt
     const int R0 = (unit % tiles) * BQ, kvh = unit / tiles % p.n_kv, b = unit / tiles / p.n_kv;
     attend_tile<PAGED, CLUSTER, BQ, HALVES>(p, b, kvh, R0, split);
   } else {
-    const int units = static_cast<int>(causal_units(p, BQ)), worker = blockIdx.x / parts, checkers = gridDim.x / parts - units;
-    if (worker >= checkers) {
-      const int unit = units - 1 - (worker - checkers);    // a sequence's last rows, which see the most keys, first
+    const int units = static_cast<int>(causal_units(p, BQ)), worker = blockIdx.x / parts, scouts = gridDim.x / parts - units;
+    if (worker >= scouts) {
+      const int unit = units - 1 - (worker - scouts);    // a sequence's last rows, which see the most keys, first
       const int slot = unit / p.n_kv, kvh = unit % p.n_kv, b = sequence_at<BQ>(p, G, slot);
       const long tile = slot - (static_cast<long>(p.cu[b]) * G / BQ + b);
       if (tile < 0 || tile > 0x7fffffff / BQ) return;
       attend_tile<PAGED, CLUSTER, BQ, HALVES>(p, b, kvh, static_cast<int>(tile) * BQ, split);
       return;
     }
-    take_all_if_one_falls<CLUSTER, BQ, HALVES>(p, worker, checkers, split);
+    take_all_if_one_falls<CLUSTER, BQ, HALVES>(p, worker, scouts, split);
   }
 }
 
