@@ -471,6 +471,128 @@ seer_status seer_attention_tree_workspace_size(seer_dtype dt, int B, int n_heads
                                                int max_draft, size_t* bytes);
 
 /* ---------------------------------------------------------------------------
+ * A paged cache under a budget, for servers whose prompts outgrow the positions that a
+ * model was trained on and the memory that a request may hold: positions scaled for
+ * long contexts, and the cached rows dropped that the queries look at least.  A step:
+ *   seer_page_tables, seer_kv_append_rotary (positions count the rows dropped so far),
+ *   attention, seer_attention_mass, and for requests past their budget
+ *   seer_evict_select and seer_kv_evict.
+ * Attention does not depend on the order of cached rows (a key carries its position), so
+ * an evicted row's place is taken by a row from the cache's end and nothing else moves.
+ * Two numbers are kept for row t of request b, at [b * ld_mass + t]: mass (fp32), the
+ * attention weight it has gathered, and birth (int32), its position.  gone[b] counts the
+ * rows that the request has lost: kv_len[b] + gone[b] is its next position.  Lengths are
+ * the same in every layer, so one page table goes on serving all; mass, birth and the
+ * choice of rows may be each layer's own or shared.
+ * What the device finds inconsistent is recorded (seer_check_device) and that request
+ * left out; no access leaves the buffers named.  A call repeats itself bit by bit.
+ * ------------------------------------------------------------------------- */
+typedef enum {
+  SEER_ROTARY_PLAIN = 0,
+  SEER_ROTARY_LINEAR = 1,   /* every rate divided by factor */
+  SEER_ROTARY_TURNS = 2,    /* by the turns n a pair makes over original_len: as it is from
+                               high turns on, divided by factor up to low, between them
+                               rate * (g + (1 - g) / factor), g = (n - low) / (high - low) */
+  SEER_ROTARY_PAIRS = 3     /* by the pair's number i: rate * (1 - t + t / factor), t rising
+                               from 0 at pair first to 1 at pair last, the (floored, ceiled)
+                               pairs that make high and low turns over original_len; first
+                               at least 0, last at most rotary_dim - 1 and above first by
+                               0.001 where it would not be */
+} seer_rotary_scaling;
+
+typedef struct {
+  double theta;             /* pair i turns by theta^(-2i / rotary_dim) per position; >= 1 */
+  double factor;            /* scalings: >= 1 */
+  double low, high;         /* TURNS, PAIRS: 0 < low < high */
+  double magnitude;         /* cosines and sines are multiplied by it (1: a rotation) */
+  int original_len;         /* TURNS, PAIRS: > 0 */
+  int rotary_dim;           /* the head's first values that turn: even, from 2 to head_dim */
+  int interleaved;          /* 0: pairs (i, i + rotary_dim / 2); 1: pairs (2i, 2i + 1) */
+  int scaling;              /* seer_rotary_scaling */
+} seer_rotary;
+
+/* out[r] = the n_heads heads of x[r] turned by position[r] (device int32 [T_cap], may be
+ * negative): (a, b) of a pair becomes magnitude * (a cos - b sin, b cos + a sin); values
+ * from rotary_dim on are copied as they are.  Rows of x and out are ld_* values apart;
+ * out may be x itself with its ld, else they must not overlap.  M_dev (device int32, may
+ * be NULL) overrides T_cap; rows past it are untouched.  head_dim: a multiple of 16 (fp32:
+ * of 8) up to 128; without interleaving rotary_dim is a multiple of 4 (fp32: of 2).  An
+ * angle is off by at most 2^-20 rad up to position 2^29 and 2^-18 up to the last; one
+ * rounding per value. */
+seer_status seer_rotate(const void* x, int ld_x, seer_dtype dt, int n_heads, int head_dim, int T_cap,
+                        const int32_t* M_dev, const int32_t* position, const seer_rotary* rotary, void* out, int ld_out,
+                        void* stream);
+
+/* seer_kv_append with the rotation that `rotary` describes (NULL: none), each row turned
+ * by its position + shift of its request: row r of request b, cu_new[b] <= r <
+ * cu_new[b+1], by position[r] + shift[b] (shift NULL: by position[r], cu_new may then be
+ * NULL; rows outside the requests are not shifted).  shift is the gone of a cache that
+ * has lost rows and position what seer_page_tables gives. */
+seer_status seer_kv_append_rotary(const void* qkv, int ld_qkv, seer_dtype dt, int n_heads, int T_cap,
+                                  const int32_t* M_dev, const int32_t* slot, const int32_t* position,
+                                  const int32_t* cu_new, const int32_t* shift, int B, const seer_rotary* rotary,
+                                  void* rotated, int ld_rotated, const seer_pages* pages, void* stream);
+
+/* Attention weight that each cached row receives from the request's last new rows, summed
+ * over them and over all query heads:
+ *   mass_out[b, t] = (t < c ? keep * mass_in[b, t] : 0) + sum_h sum_i p_h(i, t), t < kv_len[b]
+ * with c = kv_len[b] - n rows from before the step, n new rows (their keys stored), of which
+ * the last w = min(n, window) look: new row i sees rows t <= c + i, and p_h(i, .) is the
+ * softmax of q_h(i) k_t / sqrt(head_dim) over them.  The sum over a softmax's row is 1, so
+ * the new weight of a request adds up to w * n_heads.  Also birth[b, c + i] = c + i +
+ * gone[b] of all new rows (birth NULL: not kept; gone NULL: zeros).
+ * q               rows of n_heads heads, turned as the keys are; request b's new rows are
+ *                 rows cu_new[b] .. cu_new[b+1] - 1
+ * accepted        NULL: n = cu_new[b+1] - cu_new[b].  Else, after seer_kv_accept with the
+ *                 same lists: n = n_accepted[b], and new row i's query is row cu_new[b] +
+ *                 accepted[b * max_draft + i]; kv_len is then seer_kv_accept's len_out.  A
+ *                 row whose entry is outside its draft is recorded and does not look
+ * window          rows that look at most, 1 .. SEER_MAX_DRAFT
+ * T_kv_cap        the requests' kv_len add up to at most this; requests past it are left
+ *                 out and recorded
+ * mass_in         may be mass_out itself (not overlap it otherwise); NULL where keep is 0
+ * Entries from kv_len[b] to ld_mass are untouched.  A request without new rows keeps
+ * keep * mass_in.  A row's infinite or NaN scores make its weights NaN for the rows that
+ * it sees.  Pages outside the pool read as zeros and are recorded.  Types, heads and
+ * head_dim as for seer_attention_tree; weights and sums are fp32.
+ * ws: seer_attention_mass_workspace_size() bytes, 16-byte aligned; calls that share one
+ * must not overlap on the GPU; nothing in it needs to start at zero. */
+seer_status seer_attention_mass(const void* q, int ld_q, seer_dtype dt, const int32_t* cu_new, const int32_t* kv_len,
+                                const int32_t* accepted, const int32_t* n_accepted, int max_draft, int window, int B,
+                                int T_cap, int T_kv_cap, int n_heads, const seer_pages* pages, float keep,
+                                const int32_t* gone, const float* mass_in, float* mass_out, int32_t* birth,
+                                int ld_mass, void* ws, size_t ws_bytes, void* stream);
+seer_status seer_attention_mass_workspace_size(seer_dtype dt, int B, int T_kv_cap, int n_heads, int n_kv_heads,
+                                               int head_dim, int window, size_t* bytes);
+
+/* Which rows each request keeps under its budget, and the moves that close the gaps.
+ * K = min(budget[b], kv_len[b]) rows stay: first those born at kv_len[b] + gone[b] -
+ * min(recent, K) or later, then those born before `sinks`, then the others by mass, the
+ * most first (NaN above all); among equals the lower row.  The kept rows t >= K,
+ * ascending, go to the places t < K of rows that are not kept, ascending:
+ *   len_out[b]  = K, gone_out[b] = gone[b] + kv_len[b] - K, n_moves[b] = m, and
+ *   row move_from[b * ld_move + i] becomes row move_to[b * ld_move + i], i < m
+ * (entries from m on are untouched; gone NULL: zeros).  m is at most min(K, kv_len[b] -
+ * K); where ld_move is less than that, where budget[b] is negative or kv_len[b] outside
+ * 0 .. ld_mass the request is recorded and stays as it is (len_out = kv_len, m = 0).
+ * gone_out may be gone itself and len_out kv_len itself. */
+seer_status seer_evict_select(const float* mass, const int32_t* birth, int ld_mass, const int32_t* kv_len,
+                              const int32_t* gone, const int32_t* budget, int B, int sinks, int recent,
+                              int32_t* len_out, int32_t* gone_out, int32_t* n_moves, int32_t* move_from,
+                              int32_t* move_to, int ld_move, void* stream);
+
+/* Makes the moves in a pool, and in mass and birth (each may be NULL): one call per
+ * layer's pool, mass and birth once.  kv_len is the length before the choice (NULL: the
+ * rows that the table holds); moves from or to rows outside it, or pages outside the
+ * pool, are left out and recorded.  No row is both a source and a place, as
+ * seer_evict_select leaves it.  The table is as before: its entries from ceil(len_out[b] /
+ * page_size) up to ceil(kv_len[b] / page_size) are pages to put back, as after
+ * seer_kv_accept. */
+seer_status seer_kv_evict(seer_dtype dt, const int32_t* kv_len, const int32_t* n_moves, const int32_t* move_from,
+                          const int32_t* move_to, int ld_move, int B, const seer_pages* pages, float* mass,
+                          int32_t* birth, int ld_mass, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Diagnostics.
  * ------------------------------------------------------------------------- */
 /* Thread-local message describing the last failure of this thread. */

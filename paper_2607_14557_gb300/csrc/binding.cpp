@@ -42,7 +42,7 @@ void* address(PyObject* o, int device, const c10::ScalarType* type) {
   throw Refused(std::string("expected a tensor, an address or None, got ") + Py_TYPE(o)->tp_name);
 }
 
-constexpr c10::ScalarType kInt32 = c10::ScalarType::Int, kInt64 = c10::ScalarType::Long;
+constexpr c10::ScalarType kInt32 = c10::ScalarType::Int, kInt64 = c10::ScalarType::Long, kFloat = c10::ScalarType::Float;
 
 template <typename T>
 struct Arg {                                // integers
@@ -90,15 +90,31 @@ struct Arg<uint64_t*> {
   static uint64_t* get(PyObject* o, int d) { return static_cast<uint64_t*>(address(o, d, &kInt64)); }
 };
 template <>
-struct Arg<const seer_pages*> {             // the ctypes struct
-  static const seer_pages* get(PyObject* o, int) {
-    Py_buffer b;
-    if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) throw PythonError();
-    const void* p = b.buf;
-    const bool fits = b.len == static_cast<Py_ssize_t>(sizeof(seer_pages));
-    PyBuffer_Release(&b);
-    if (!fits) throw Refused("pages is not a seer_pages");
-    return static_cast<const seer_pages*>(p);
+struct Arg<const float*> {
+  static const float* get(PyObject* o, int d) { return static_cast<const float*>(address(o, d, &kFloat)); }
+};
+template <>
+struct Arg<float*> {
+  static float* get(PyObject* o, int d) { return static_cast<float*>(address(o, d, &kFloat)); }
+};
+template <typename S>
+const S* structure(PyObject* o, const char* refusal) {   // the ctypes struct
+  Py_buffer b;
+  if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) throw PythonError();
+  const void* p = b.buf;
+  const bool fits = b.len == static_cast<Py_ssize_t>(sizeof(S));
+  PyBuffer_Release(&b);
+  if (!fits) throw Refused(refusal);
+  return static_cast<const S*>(p);
+}
+template <>
+struct Arg<const seer_pages*> {
+  static const seer_pages* get(PyObject* o, int) { return structure<seer_pages>(o, "pages is not a seer_pages"); }
+};
+template <>
+struct Arg<const seer_rotary*> {
+  static const seer_rotary* get(PyObject* o, int) {
+    return o == Py_None ? nullptr : structure<seer_rotary>(o, "rotary is not a seer_rotary");
   }
 };
 
@@ -145,6 +161,14 @@ void rows_hold(const char* name, PyObject* o, long long dt, long long rows, long
   if ((rows - 1) * ld + cols > have)
     throw Refused(std::string(name) + ": " + std::to_string(rows) + " rows of " + std::to_string(cols) + " values, " + std::to_string(ld) +
                   " apart, end behind the tensor's memory");
+}
+
+// A workspace of `bytes`.
+void workspace_holds(PyObject* o, long long bytes) {
+  const at::Tensor* ws = tensor(o);
+  if (ws != nullptr && (!ws->is_contiguous() || static_cast<long long>(ws->nbytes()) < bytes))
+    throw Refused("ws holds " + std::to_string(ws->nbytes()) + " bytes" + (ws->is_contiguous() ? "" : ", not contiguous") + ", the call names " +
+                  std::to_string(bytes));
 }
 
 // A pool of type dt and a table of B rows: make_pages leaves (dtype code, device, rows of the table) as _held,
@@ -246,11 +270,92 @@ void check<&seer_attention_tree>(PyObject* const* a) {
   rows_hold("o", a[2], dt, cap, integer(a[3]), cols);
   holds("cu_new", a[5], B + 1);
   holds("kv_len", a[6], B);
-  const at::Tensor* ws = tensor(a[13]);
-  if (ws != nullptr && (!ws->is_contiguous() || static_cast<long long>(ws->nbytes()) < bytes))
-    throw Refused("ws holds " + std::to_string(ws->nbytes()) + " bytes" + (ws->is_contiguous() ? "" : ", not contiguous") + ", the call names " +
-                  std::to_string(bytes));
+  workspace_holds(a[13], bytes);
   pages_hold(a[12], dt, B, false);
+}
+
+template <>
+void check<&seer_rotate>(PyObject* const* a) {
+  const long long dt = integer(a[2]), cap = integer(a[5]), cols = integer(a[3]) * integer(a[4]);
+  rows_hold("x", a[0], dt, cap, integer(a[1]), cols);
+  holds("M_dev", a[6], 1);
+  holds("position", a[7], cap);
+  rows_hold("out", a[9], dt, cap, integer(a[10]), cols);
+  Arg<const seer_rotary*>::get(a[8], 0);
+}
+
+template <>
+constexpr int kPages<&seer_kv_append_rotary> = 14;
+template <>
+void check<&seer_kv_append_rotary>(PyObject* const* a) {
+  const long long ld = integer(a[1]), dt = integer(a[2]), heads = integer(a[3]), cap = integer(a[4]), B = integer(a[10]), ld_rot = integer(a[13]);
+  const seer_pages g = pages_of(a[14]);
+  rows_hold("qkv", a[0], dt, cap, ld, (heads + 2ll * g.n_kv_heads) * g.head_dim);
+  holds("M_dev", a[5], 1);
+  holds("slot", a[6], cap);
+  holds("position", a[7], cap);
+  if (a[9] != Py_None) {
+    holds("cu_new", a[8], B + 1);
+    holds("shift", a[9], B);
+  }
+  rows_hold("rotated", a[12], dt, cap, ld_rot, (heads + g.n_kv_heads) * g.head_dim);
+  Arg<const seer_rotary*>::get(a[11], 0);
+  pages_hold(a[14], dt, 0, false);
+}
+
+template <>
+constexpr int kPages<&seer_attention_mass> = 13;
+template <>
+void check<&seer_attention_mass>(PyObject* const* a) {
+  const long long dt = integer(a[2]), draft = integer(a[7]), B = integer(a[9]), cap = integer(a[10]), ld = integer(a[19]);
+  const long long bytes = Arg<size_t>::get(a[21], 0);
+  const seer_pages g = pages_of(a[13]);
+  rows_hold("q", a[0], dt, cap, integer(a[1]), integer(a[12]) * g.head_dim);
+  holds("cu_new", a[3], B + 1);
+  holds("kv_len", a[4], B);
+  if (B <= SEER_MAX_REQUESTS) {
+    holds("accepted", a[5], B * draft);
+    holds("mass_in", a[16], B * ld);
+    holds("mass_out", a[17], B * ld);
+    holds("birth", a[18], B * ld);
+  }
+  holds("n_accepted", a[6], B);
+  holds("gone", a[15], B);
+  workspace_holds(a[20], bytes);
+  pages_hold(a[13], dt, B, false);
+}
+
+template <>
+void check<&seer_evict_select>(PyObject* const* a) {
+  const long long ld = integer(a[2]), B = integer(a[6]), ld_move = integer(a[14]);
+  if (B <= SEER_MAX_REQUESTS) {
+    holds("mass", a[0], B * ld);
+    holds("birth", a[1], B * ld);
+    holds("move_from", a[12], B * ld_move);
+    holds("move_to", a[13], B * ld_move);
+  }
+  holds("kv_len", a[3], B);
+  holds("gone", a[4], B);
+  holds("budget", a[5], B);
+  holds("len_out", a[9], B);
+  holds("gone_out", a[10], B);
+  holds("n_moves", a[11], B);
+}
+
+template <>
+constexpr int kPages<&seer_kv_evict> = 7;
+template <>
+void check<&seer_kv_evict>(PyObject* const* a) {
+  const long long ld_move = integer(a[5]), B = integer(a[6]), ld = integer(a[10]);
+  holds("kv_len", a[1], B);
+  holds("n_moves", a[2], B);
+  if (B <= SEER_MAX_REQUESTS) {
+    holds("move_from", a[3], B * ld_move);
+    holds("move_to", a[4], B * ld_move);
+    holds("mass", a[8], B * ld);
+    holds("birth", a[9], B * ld);
+  }
+  pages_hold(a[7], integer(a[0]), B, false);
 }
 
 template <auto Fn>
@@ -286,7 +391,9 @@ struct Call<Fn> {
 
 #define SEER_ENTRY(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&Call<&f>::entry)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {SEER_ENTRY(seer_page_tables), SEER_ENTRY(seer_kv_append), SEER_ENTRY(seer_kv_accept),
-                          SEER_ENTRY(seer_attention_causal), SEER_ENTRY(seer_attention_tree), {nullptr, nullptr, 0, nullptr}};
+                          SEER_ENTRY(seer_attention_causal), SEER_ENTRY(seer_attention_tree), SEER_ENTRY(seer_rotate),
+                          SEER_ENTRY(seer_kv_append_rotary), SEER_ENTRY(seer_attention_mass), SEER_ENTRY(seer_evict_select),
+                          SEER_ENTRY(seer_kv_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_seer_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,321 @@
+// Eviction from a paged cache: the rows to keep by accumulated weight (a radix selection per
+// request), and the moves that close the gaps.
+#include "budget.h"
+#include "common.cuh"
+
+namespace seer {
+namespace {
+
+// ------------------------------------------------------------------ the choice
+// The K first rows in the order (recent, sink, mass, lower row) stay.  A row's place in it is a
+// 32-bit key: the mass as an ordered integer below the three values that NaN, sinks and recent
+// rows take.  The K-th largest key is found 11, 11 and 10 bits at a time by histograms, the
+// rows equal to it that stay are the lowest, and two counts over the rows number the moves.
+// A cluster of CTAs takes a request, each a stretch of its rows, whose keys stay in shared
+// memory across the passes (from the matrices again where they do not fit); histograms and
+// counts meet through distributed shared memory.  Sums of integers: the order of the atomics
+// leaves no trace.
+constexpr int kSelThreads = 512;
+constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kSelKeys = 16384;             // keys of a CTA in shared memory
+constexpr int kBins = 2048;
+constexpr uint32_t kKeyRecent = 0xffffffffu, kKeySink = 0xfffffffeu, kKeyNan = 0xfffffffdu;
+
+struct SelShared {
+  unsigned hist[2][kBins];                  // of this CTA, by turns
+  unsigned counts[kSelWarps][4];            // per warp: rows above / at the key before K, and behind
+  unsigned warp_sum[kSelWarps];
+  unsigned found_bin, found_above;
+  uint32_t keys[kSelKeys];
+};
+
+__device__ __forceinline__ unsigned ld_cluster(uint32_t addr) {
+  unsigned v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ uint32_t mass_key(float m) {
+  if (m != m) return kKeyNan;
+  const uint32_t u = __float_as_uint(m + 0.f);            // -0 and 0 are one value
+  return u ^ ((u >> 31) != 0 ? 0xffffffffu : 0x80000000u);
+}
+
+__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectArgs a, const int ranks) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  SelShared& sh = *reinterpret_cast<SelShared*>(smem);
+  pdl_enter();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int b = blockIdx.x / ranks, rank = blockIdx.x % ranks;
+  const int L0 = a.kv_len[b], budget = a.budget[b], gone = a.gone ? a.gone[b] : 0;
+  bool good = L0 >= 0 && L0 <= a.ld_mass && budget >= 0;
+  const int L = good ? L0 : 0, K = good ? min(budget, L) : 0;
+  if (good && min(K, L - K) > a.ld_move) good = false;
+  if (!good || K == L || K == 0) {          // nothing to choose; every rank has read the lengths before one writes
+    if (ranks > 1) cluster_sync();
+    if (rank == 0 && tid == 0) {
+      if (!good) record_error(a.err, L0 >= 0 && L0 <= a.ld_mass && budget >= 0 ? kErrCapacity : kErrLayout);
+      a.len_out[b] = good ? K : L0;
+      a.gone_out[b] = gone + (good ? L - K : 0);
+      a.n_moves[b] = 0;
+    }
+    return;
+  }
+  const long long young = static_cast<long long>(L) + gone - min(a.recent, K);
+  // rank's rows [r0, r1), a warp's [w0, w1) of them: both multiples of 32 from their starts
+  const int share = ((L + ranks - 1) / ranks + 31) / 32 * 32;
+  const int r0 = static_cast<int>(min(static_cast<long long>(L), static_cast<long long>(share) * rank));
+  const int r1 = static_cast<int>(min(static_cast<long long>(L), static_cast<long long>(r0) + share));
+  const bool held = r1 - r0 <= kSelKeys;
+  const float* mass = a.mass + static_cast<size_t>(b) * a.ld_mass;
+  const int* birth = a.birth + static_cast<size_t>(b) * a.ld_mass;
+  const auto read_key = [&](int t) {
+    const int born = birth[t];
+    return born >= young ? kKeyRecent : (born < a.sinks ? kKeySink : mass_key(mass[t]));
+  };
+  const auto key_of = [&](int t) { return held ? sh.keys[t - r0] : read_key(t); };
+
+  // ---- the K-th largest key
+  for (int i = tid; i < 2 * kBins; i += kSelThreads) (&sh.hist[0][0])[i] = 0;
+  __syncthreads();
+  uint32_t prefix = 0;
+  unsigned need = K;                        // rows with the prefix that stay
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    constexpr int kShift[3] = {21, 10, 0};
+    const int shift = kShift[pass], bins = pass == 2 ? 1024 : kBins;
+    unsigned* hist = sh.hist[pass & 1];
+    for (int t = r0 + tid; t < r1; t += kSelThreads) {
+      uint32_t k;
+      if (pass == 0) {
+        k = read_key(t);
+        if (held) sh.keys[t - r0] = k;
+      } else {
+        k = key_of(t);
+      }
+      const int above = pass == 0 ? 32 : kShift[pass == 0 ? 0 : pass - 1];
+      if (pass == 0 || (k >> above) == (prefix >> above)) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+    }
+    if (ranks > 1) cluster_sync();
+    else __syncthreads();
+    // thread i owns bins [4 i, 4 i + 4) counted from the top
+    unsigned mine[4], sum = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int bin = bins - 1 - (4 * tid + e);
+      unsigned v = 0;
+      if (bin >= 0) {
+        if (ranks == 1) v = hist[bin];
+        else
+          for (int r = 0; r < ranks; ++r) v += ld_cluster(cluster_addr(&hist[bin], r));
+      }
+      mine[e] = v;
+      sum += v;
+    }
+    unsigned inc = sum;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned v = __shfl_up_sync(0xffffffffu, inc, off);
+      if (lane >= off) inc += v;
+    }
+    if (lane == 31) sh.warp_sum[warp] = inc;
+    __syncthreads();
+    unsigned before = inc - sum;
+    for (int w = 0; w < warp; ++w) before += sh.warp_sum[w];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (before < need && need <= before + mine[e]) {   // one thread's bin
+        sh.found_bin = bins - 1 - (4 * tid + e);
+        sh.found_above = before;
+      }
+      before += mine[e];
+    }
+    if (pass == 1)                          // pass 2 uses the first histogram again; every rank has read it (the sync above)
+      for (int i = tid; i < kBins; i += kSelThreads) sh.hist[0][i] = 0;
+    __syncthreads();
+    prefix |= sh.found_bin << shift;
+    need -= sh.found_above;
+    __syncthreads();
+  }
+
+  // ---- counts per warp: rows above the key and at it, before row K and behind
+  const int wshare = (share / 32 + kSelWarps - 1) / kSelWarps * 32;
+  const int w0 = min(r1, r0 + warp * wshare), w1 = min(r1, w0 + wshare);
+  unsigned n[4] = {0, 0, 0, 0};
+  for (int t = w0 + lane; t - lane < w1; t += 32) {
+    const uint32_t k = t < w1 ? key_of(t) : 0;
+    const bool over = t < w1 && k > prefix, at = t < w1 && k == prefix;
+    const unsigned first = __ballot_sync(0xffffffffu, t < K);
+    const unsigned m = __ballot_sync(0xffffffffu, over), e = __ballot_sync(0xffffffffu, at);
+    n[0] += __popc(m & first);
+    n[1] += __popc(e & first);
+    n[2] += __popc(m & ~first);
+    n[3] += __popc(e & ~first);
+  }
+  if (lane < 4) sh.counts[warp][lane] = n[lane & 3];
+  if (ranks > 1) cluster_sync();
+  else __syncthreads();
+  // rows above / at the key in warps before this one, and in all of them before row K
+  unsigned above = 0, equal = 0, above_k = 0, equal_k = 0;
+  for (int i = lane; i < ranks * kSelWarps; i += 32) {
+    const int r = i / kSelWarps, w = i % kSelWarps;
+    unsigned c[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = ranks == 1 ? sh.counts[w][e] : ld_cluster(cluster_addr(&sh.counts[w][e], r));
+    above_k += c[0];
+    equal_k += c[1];
+    if (i < rank * kSelWarps + warp) {
+      above += c[0] + c[2];
+      equal += c[1] + c[3];
+    }
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    above += __shfl_xor_sync(0xffffffffu, above, off);
+    equal += __shfl_xor_sync(0xffffffffu, equal, off);
+    above_k += __shfl_xor_sync(0xffffffffu, above_k, off);
+    equal_k += __shfl_xor_sync(0xffffffffu, equal_k, off);
+  }
+  if (ranks > 1) cluster_sync();            // nobody reads another CTA's memory from here on
+  const unsigned kept_k = above_k + min(need, equal_k);    // rows before K that stay
+  if (rank == 0 && tid == 0) {
+    a.len_out[b] = K;
+    a.gone_out[b] = gone + (L - K);
+    a.n_moves[b] = K - static_cast<int>(kept_k);
+  }
+
+  // ---- the moves: place i of the holes before K, row i of the kept behind
+  int* from = a.move_from + static_cast<size_t>(b) * a.ld_move;
+  int* to = a.move_to + static_cast<size_t>(b) * a.ld_move;
+  for (int t = w0 + lane; t - lane < w1; t += 32) {
+    const uint32_t k = t < w1 ? key_of(t) : 0;
+    const bool over = t < w1 && k > prefix, at = t < w1 && k == prefix;
+    const unsigned m = __ballot_sync(0xffffffffu, over), e = __ballot_sync(0xffffffffu, at);
+    const unsigned less = (1u << lane) - 1;
+    const unsigned ties = equal + __popc(e & less);
+    const unsigned kept = above + __popc(m & less) + min(ties, need);   // rows before t that stay
+    const bool keep = over || (at && ties < need);
+    if (t < w1) {
+      if (t < K && !keep) to[t - kept] = t;
+      if (t >= K && keep) from[kept - kept_k] = t;
+    }
+    above += __popc(m);
+    equal += __popc(e);
+  }
+}
+
+// ------------------------------------------------------------------ the moves
+// Row move_from of a request becomes its row move_to; sources and places are apart, so all
+// moves go at once.  Bound by HBM: each moved row is read once and written once.  All requests'
+// moves form one line; a warp takes 2 KB of a row at a time, its loads ahead of its stores.
+constexpr int kEvictThreads = 256;
+constexpr int kSeg = 2048;
+
+__global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const EvictArgs a) {
+  extern __shared__ int first[];            // [B + 1] a request's first move on the line, cut at 2^31 - 1
+  __shared__ long long warp_sum[kEvictThreads / 32];
+  pdl_enter();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const auto moves_of = [&](int b, bool report) {
+    const int n = a.n_moves[b];
+    if (n >= 0 && n <= a.ld_move) return n;
+    if (report) record_error(a.err, kErrLayout);
+    return 0;
+  };
+  long long sum = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kEvictThreads) {
+    const int b = b0 + tid;
+    const long long v = b < a.B ? moves_of(b, blockIdx.x == 0) : 0;
+    long long inc = v;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, inc, off);
+      if (lane >= off) inc += x;
+    }
+    if (lane == 31) warp_sum[warp] = inc;
+    __syncthreads();
+    long long before = sum, all = 0;
+    for (int w = 0; w < kEvictThreads / 32; ++w) {
+      if (w < warp) before += warp_sum[w];
+      all += warp_sum[w];
+    }
+    if (b < a.B) first[b] = static_cast<int>(min(before + inc - v, 0x7fffffffll));
+    sum += all;
+    __syncthreads();
+  }
+  if (tid == 0) first[a.B] = static_cast<int>(min(sum, 0x7fffffffll));
+  __syncthreads();
+
+  const int segs = (a.row_bytes + kSeg - 1) / kSeg;
+  const long long total = static_cast<long long>(first[a.B]) * segs, step = static_cast<long long>(gridDim.x) * (kEvictThreads / 32);
+  for (long long x = static_cast<long long>(blockIdx.x) * (kEvictThreads / 32) + warp; x < total; x += step) {
+    const int move = static_cast<int>(x / segs), seg = static_cast<int>(x - static_cast<long long>(move) * segs);
+    int lo = 0, hi = a.B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= move) lo = mid; else hi = mid;
+    }
+    const size_t at = static_cast<size_t>(lo) * a.ld_move + (move - first[lo]);
+    const int t[2] = {a.move_from[at], a.move_to[at]};
+    const long long room = min(static_cast<long long>(a.pages.max_pages) << a.pages.page_shift,
+                               a.kv_len ? static_cast<long long>(a.kv_len[lo]) : 0x7fffffffll);
+    size_t row[2];
+    bool good = true;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      int page = -1;
+      if (t[e] >= 0 && t[e] < room && (t[e] < a.ld_mass || (!a.mass && !a.birth)))
+        page = a.pages.table[static_cast<size_t>(lo) * a.pages.max_pages + (t[e] >> a.pages.page_shift)];
+      if (page < 0 || page >= a.pages.n_pages) good = false;
+      row[e] = (static_cast<size_t>(page) << a.pages.page_shift) + (t[e] & ((1 << a.pages.page_shift) - 1));
+    }
+    if (!good) {
+      if (lane == 0) record_error(a.err, kErrLayout);
+      continue;
+    }
+    uint8_t* kv = static_cast<uint8_t*>(a.pages.kv);
+    const int begin = seg * kSeg + lane * 16;
+    uint4 w[kSeg / 512];
+#pragma unroll
+    for (int e = 0; e < kSeg / 512; ++e)
+      if (begin + e * 512 < a.row_bytes) w[e] = *reinterpret_cast<const uint4*>(kv + row[0] * a.row_bytes + begin + e * 512);
+#pragma unroll
+    for (int e = 0; e < kSeg / 512; ++e)
+      if (begin + e * 512 < a.row_bytes) *reinterpret_cast<uint4*>(kv + row[1] * a.row_bytes + begin + e * 512) = w[e];
+    if (seg == 0 && lane == 0) {
+      const size_t base = static_cast<size_t>(lo) * a.ld_mass;
+      if (a.mass) a.mass[base + t[1]] = a.mass[base + t[0]];
+      if (a.birth) a.birth[base + t[1]] = a.birth[base + t[0]];
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_evict_select(const SelectArgs& a, int num_sms, cudaStream_t st) {
+  // CTAs of a request: as many as its longest row count gives work, and the GPU has room for
+  int ranks = 1;
+  while (ranks < 8 && a.ld_mass > 4096l * ranks && a.B * ranks < 2 * num_sms) ranks *= 2;
+  static bool attr_set[64] = {};
+  const int smem = static_cast<int>(sizeof(SelShared));
+  const cudaError_t e = set_smem_limit_once(evict_select_kernel, smem, attr_set);
+  if (e != cudaSuccess) return e;
+  return launch_kernel_overlap(launch_overlap_enabled(), ranks, evict_select_kernel, dim3(a.B * ranks), dim3(kSelThreads), smem,
+                               st, a, ranks);
+}
+
+cudaError_t launch_kv_evict(const EvictArgs& a, int num_sms, cudaStream_t st) {
+  if (a.B > kPageTableMaxB) return cudaErrorInvalidValue;
+  const int smem = (a.B + 1) * static_cast<int>(sizeof(int));
+  if (smem > 46 * 1024) {
+    static bool attr_set[64] = {};
+    const cudaError_t e = set_smem_limit_once(kv_evict_kernel, (kPageTableMaxB + 1) * static_cast<int>(sizeof(int)), attr_set);
+    if (e != cudaSuccess) return e;
+  }
+  const long long segs = (a.row_bytes + kSeg - 1) / kSeg;
+  const long long work = (static_cast<long long>(a.B) * a.ld_move * segs + kEvictThreads / 32 - 1) / (kEvictThreads / 32);
+  const long long most = 8ll * num_sms;
+  return launch_kernel(kv_evict_kernel, dim3(static_cast<unsigned>(work < 1 ? 1 : (work < most ? work : most))), dim3(kEvictThreads), smem, st, a);
+}
+
+}  // namespace seer

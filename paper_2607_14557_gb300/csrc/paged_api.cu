@@ -1,8 +1,10 @@
 // C ABI of the paged K/V cache (declared in include/seer.h): argument checks and
-// launches; the arithmetic runs in paged.cu and the grouped-head attention kernels.
+// launches; the arithmetic runs in paged.cu, rotary.cu, mass.cu, evict.cu and the
+// grouped-head attention kernels.
 #include <cmath>
 
 #include "api.h"
+#include "budget.h"
 #include "common.cuh"
 #include "kernels.h"
 #include "paged.h"
@@ -101,6 +103,59 @@ seer_status map_heads(CUtensorMap* m, const void* base, seer_dtype dt, long rows
                             const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(SEER_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+  return SEER_OK;
+}
+
+// Rates of a head's pairs as fractions of a turn per position, in fp64; pairs turn by at most
+// one radian per position.
+seer_status rotary_rates(const char* what, const seer_rotary* r, int head_dim, seer_dtype dt, TurnRates* out) {
+  if (!(r->theta >= 1.0) || !std::isfinite(r->theta)) return fail(SEER_ERR_INVALID_ARG, "%s: theta must be a finite base from 1 on", what);
+  if (r->scaling < SEER_ROTARY_PLAIN || r->scaling > SEER_ROTARY_PAIRS) return fail(SEER_ERR_INVALID_ARG, "%s: unknown rotary scaling %d", what, r->scaling);
+  if (r->interleaved != 0 && r->interleaved != 1) return fail(SEER_ERR_INVALID_ARG, "%s: interleaved must be 0 or 1", what);
+  if (!std::isfinite(r->magnitude)) return fail(SEER_ERR_INVALID_ARG, "%s: magnitude must be finite", what);
+  const int rd = r->rotary_dim;
+  if (rd < 2 || rd > head_dim || rd % 2 != 0)
+    return fail(SEER_ERR_INVALID_ARG, "%s: rotary_dim must be even, from 2 to head_dim (got %d of %d)", what, rd, head_dim);
+  if (!r->interleaved && rd / 2 * static_cast<int>(esize(dt)) % 4 != 0)
+    return fail(SEER_ERR_UNSUPPORTED, "%s: half a 16-bit rotary_dim must be even (got %d)", what, rd / 2);
+  if (r->scaling != SEER_ROTARY_PLAIN && (!(r->factor >= 1.0) || !std::isfinite(r->factor)))
+    return fail(SEER_ERR_INVALID_ARG, "%s: a rotary factor must be finite and at least 1", what);
+  const bool ramp = r->scaling == SEER_ROTARY_TURNS || r->scaling == SEER_ROTARY_PAIRS;
+  if (ramp && (!(r->low > 0.0) || !(r->high > r->low) || !std::isfinite(r->high) || r->original_len <= 0))
+    return fail(SEER_ERR_INVALID_ARG, "%s: rotary scaling needs 0 < low < high and a positive original_len", what);
+  if (r->scaling == SEER_ROTARY_PAIRS && r->theta == 1.0)
+    return fail(SEER_ERR_INVALID_ARG, "%s: pairs of base 1 all make the same turns", what);
+  const double turn = 6.283185307179586476925;
+  double first = 0, last = 0;
+  if (r->scaling == SEER_ROTARY_PAIRS) {
+    const auto pair_of = [&](double turns) { return rd * std::log(r->original_len / (turn * turns)) / (2 * std::log(r->theta)); };
+    first = std::fmax(std::floor(pair_of(r->high)), 0.0);
+    last = std::fmin(std::ceil(pair_of(r->low)), rd - 1.0);
+    if (last <= first) last = first + 0.001;
+  }
+  for (int i = 0; i < rd / 2; ++i) {
+    double rate = std::exp2(-2.0 * i / rd * std::log2(r->theta));
+    if (r->scaling == SEER_ROTARY_LINEAR) {
+      rate /= r->factor;
+    } else if (ramp) {
+      // the share that keeps its rate
+      double g = r->scaling == SEER_ROTARY_TURNS ? (r->original_len * rate / turn - r->low) / (r->high - r->low)
+                                                 : 1.0 - (i - first) / (last - first);
+      g = std::fmin(std::fmax(g, 0.0), 1.0);
+      rate *= g + (1.0 - g) / r->factor;
+    }
+    out->rate[i] = static_cast<uint64_t>(rate / turn * 18446744073709551616.0);
+  }
+  return SEER_OK;
+}
+
+// Types and sizes of a mass call that its workspace follows from.
+seer_status check_mass(int B, int T_kv_cap, int n_heads, int n_kv, int head_dim, int window, seer_dtype dt) {
+  SEER_TRY(check_requests("attention mass", B));
+  SEER_TRY(check_heads("attention mass", n_heads, n_kv, head_dim, dt));
+  if (T_kv_cap < 0) return fail(SEER_ERR_INVALID_ARG, "attention mass: bad sizes");
+  if (window < 1 || window > SEER_MAX_DRAFT)
+    return fail(SEER_ERR_INVALID_ARG, "attention mass: window must be in [1, %d]", SEER_MAX_DRAFT);
   return SEER_OK;
 }
 
@@ -353,6 +408,233 @@ seer_status seer_attention_tree(const void* q, int ld_q, void* o, int ld_o, seer
   p.splits = gqa_simt_splits(B, n_heads, pg.n_kv, max_draft, di->num_sms);
   Phase ph(PH_ATTN, st);
   SEER_CUDA(launch_gqa_simt(true, p, di->num_sms, st), "tree attention launch");
+  return SEER_OK;
+}
+
+seer_status seer_rotate(const void* x, int ld_x, seer_dtype dt, int n_heads, int head_dim, int T_cap,
+                        const int32_t* M_dev, const int32_t* position, const seer_rotary* rotary, void* out, int ld_out,
+                        void* stream) {
+  if (!valid_dt(dt)) return fail(SEER_ERR_INVALID_ARG, "rotate: unknown dtype");
+  if (!rotary) return fail(SEER_ERR_INVALID_ARG, "rotate: rotary is null");
+  if (n_heads <= 0 || head_dim <= 0) return fail(SEER_ERR_INVALID_ARG, "rotate: heads and head_dim must be positive");
+  const int step = dt == SEER_F32 ? 8 : 16;
+  if (head_dim > 128 || head_dim % step != 0)
+    return fail(SEER_ERR_UNSUPPORTED, "rotate: head_dim must be a multiple of %d and at most 128 (got %d)", step, head_dim);
+  const long long cols = static_cast<long long>(n_heads) * head_dim;
+  if (cols > (1 << 20)) return fail(SEER_ERR_UNSUPPORTED, "rotate: rows of more than 2^20 values");
+  SEER_TRY(check_capacity("rotate", T_cap));
+  TurnRates rates{};
+  SEER_TRY(rotary_rates("rotate", rotary, head_dim, dt, &rates));
+  if (T_cap == 0) return SEER_OK;
+  SEER_TRY(check_rows("rotate", "x", x, ld_x, cols, dt));
+  SEER_TRY(check_rows("rotate", "out", out, ld_out, cols, dt));
+  if (out == x && ld_out != ld_x) return fail(SEER_ERR_INVALID_ARG, "rotate: in place, out has x's ld");
+  if (!position) return fail(SEER_ERR_INVALID_ARG, "rotate: position is null");
+  DeviceInfo* di;
+  SEER_TRY(device_info(&di));
+  const long es = static_cast<long>(esize(dt));
+  RotateArgs a{};
+  a.x = static_cast<const uint8_t*>(x);
+  a.ld = ld_x * es;
+  a.out = static_cast<uint8_t*>(out);
+  a.ld_out = ld_out * es;
+  a.n_turned = n_heads;
+  a.first_stored = n_heads;
+  a.head_dim = head_dim;
+  a.half = rotary->rotary_dim / 2;
+  a.position = position;
+  a.M_dev = M_dev;
+  a.T_cap = T_cap;
+  a.magnitude = static_cast<float>(rotary->magnitude);
+  a.err = di->err;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Phase ph(PH_KV, st);
+  SEER_CUDA(launch_rotate(dt, rotary->interleaved != 0, a, rates, di->num_sms, st), "rotate launch");
+  return SEER_OK;
+}
+
+seer_status seer_kv_append_rotary(const void* qkv, int ld_qkv, seer_dtype dt, int n_heads, int T_cap,
+                                  const int32_t* M_dev, const int32_t* slot, const int32_t* position,
+                                  const int32_t* cu_new, const int32_t* shift, int B, const seer_rotary* rotary,
+                                  void* rotated, int ld_rotated, const seer_pages* pages, void* stream) {
+  PagedKv pg;
+  SEER_TRY(check_pages("rotary append", pages, dt, &pg));
+  if (n_heads < 0) return fail(SEER_ERR_INVALID_ARG, "rotary append: bad sizes");
+  SEER_TRY(check_capacity("rotary append", T_cap));
+  const int dh = pages->head_dim;
+  const long long q = static_cast<long long>(n_heads) * dh, k = static_cast<long long>(pages->n_kv_heads) * dh;
+  if (q > (1 << 20)) return fail(SEER_ERR_UNSUPPORTED, "rotary append: rows of more than 2^20 query values");
+  TurnRates rates{};
+  if (rotary) SEER_TRY(rotary_rates("rotary append", rotary, dh, dt, &rates));
+  if (shift) {
+    SEER_TRY(check_requests("rotary append", B));
+    if (!cu_new) return fail(SEER_ERR_INVALID_ARG, "rotary append: a shift needs cu_new");
+  }
+  if (T_cap == 0) return SEER_OK;
+  SEER_TRY(check_rows("rotary append", "qkv", qkv, ld_qkv, q + 2 * k, dt));
+  if (rotated) SEER_TRY(check_rows("rotary append", "rotated", rotated, ld_rotated, q + k, dt));
+  if (rotated == qkv && ld_rotated != ld_qkv) return fail(SEER_ERR_INVALID_ARG, "rotary append: in place, rotated has qkv's ld");
+  if (!slot) return fail(SEER_ERR_INVALID_ARG, "rotary append: slot is null");
+  if (rotary && !position) return fail(SEER_ERR_INVALID_ARG, "rotary append: rotation needs positions");
+  DeviceInfo* di;
+  SEER_TRY(device_info(&di));
+  const long es = static_cast<long>(esize(dt));
+  RotateArgs a{};
+  a.x = static_cast<const uint8_t*>(qkv);
+  a.ld = ld_qkv * es;
+  a.out = static_cast<uint8_t*>(rotated);
+  a.ld_out = ld_rotated * es;
+  a.n_turned = n_heads + pages->n_kv_heads;
+  a.n_plain = pages->n_kv_heads;
+  a.first_stored = n_heads;
+  a.head_dim = dh;
+  a.half = rotary ? rotary->rotary_dim / 2 : 0;
+  a.slot = slot;
+  a.position = rotary ? position : nullptr;
+  a.M_dev = M_dev;
+  a.T_cap = T_cap;
+  a.cu = cu_new;
+  a.shift = rotary ? shift : nullptr;
+  a.B = B;
+  a.magnitude = rotary ? static_cast<float>(rotary->magnitude) : 1.f;
+  a.kv = pg.kv;
+  a.pool_rows = pg.n_pages << pg.page_shift;
+  a.err = di->err;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Phase ph(PH_KV, st);
+  SEER_CUDA(launch_rotate(dt, rotary && rotary->interleaved != 0, a, rates, di->num_sms, st), "rotary append launch");
+  return SEER_OK;
+}
+
+seer_status seer_attention_mass_workspace_size(seer_dtype dt, int B, int T_kv_cap, int n_heads, int n_kv_heads,
+                                               int head_dim, int window, size_t* bytes) {
+  SEER_TRY(check_mass(B, T_kv_cap, n_heads, n_kv_heads, head_dim, window, dt));
+  if (!bytes) return fail(SEER_ERR_INVALID_ARG, "attention mass: bytes is null");
+  DeviceInfo* di;
+  SEER_TRY(device_info(&di));
+  *bytes = mass_workspace(dt, B, T_kv_cap, n_heads, n_kv_heads, head_dim, window, di->num_sms);
+  return SEER_OK;
+}
+
+seer_status seer_attention_mass(const void* q, int ld_q, seer_dtype dt, const int32_t* cu_new, const int32_t* kv_len,
+                                const int32_t* accepted, const int32_t* n_accepted, int max_draft, int window, int B,
+                                int T_cap, int T_kv_cap, int n_heads, const seer_pages* pages, float keep,
+                                const int32_t* gone, const float* mass_in, float* mass_out, int32_t* birth,
+                                int ld_mass, void* ws, size_t ws_bytes, void* stream) {
+  MassArgs a{};
+  SEER_TRY(check_pages("attention mass", pages, dt, &a.pages));
+  SEER_TRY(check_mass(B, T_kv_cap, n_heads, pages->n_kv_heads, pages->head_dim, window, dt));
+  SEER_TRY(check_capacity("attention mass", T_cap));
+  if (!cu_new || !kv_len || !mass_out) return fail(SEER_ERR_INVALID_ARG, "attention mass: null pointer");
+  if ((accepted == nullptr) != (n_accepted == nullptr)) return fail(SEER_ERR_INVALID_ARG, "attention mass: accepted comes with n_accepted");
+  if (accepted && (max_draft < 1 || max_draft > SEER_MAX_DRAFT))
+    return fail(SEER_ERR_INVALID_ARG, "attention mass: max_draft must be in [1, %d]", SEER_MAX_DRAFT);
+  if (!std::isfinite(keep)) return fail(SEER_ERR_INVALID_ARG, "attention mass: keep must be finite");
+  if (keep != 0.f && !mass_in) return fail(SEER_ERR_INVALID_ARG, "attention mass: mass_in is null");
+  if (ld_mass <= 0) return fail(SEER_ERR_INVALID_ARG, "attention mass: ld_mass must be positive");
+  if (T_cap > 0) SEER_TRY(check_rows("attention mass", "q", q, ld_q, static_cast<long long>(n_heads) * pages->head_dim, dt));
+  size_t need = 0;
+  SEER_TRY(seer_attention_mass_workspace_size(dt, B, T_kv_cap, n_heads, pages->n_kv_heads, pages->head_dim, window, &need));
+  if (!ws || ws_bytes < need) return fail(SEER_ERR_WORKSPACE, "attention mass needs %zu bytes of workspace", need);
+  if (!aligned16(ws)) return fail(SEER_ERR_UNSUPPORTED, "attention mass: the workspace must be 16-byte aligned");
+  DeviceInfo* di;
+  SEER_TRY(device_info(&di));
+  a.q = q;
+  a.ld_q = ld_q;
+  a.cu = cu_new;
+  a.kv_len = kv_len;
+  a.accepted = accepted;
+  a.n_accepted = n_accepted;
+  a.max_draft = max_draft;
+  a.window = window;
+  a.B = B;
+  a.T_cap = T_cap;
+  a.cap_tiles = T_kv_cap / kMassKeys + B;
+  a.n_heads = n_heads;
+  a.keep = keep;
+  a.gone = gone;
+  a.mass_in = mass_in;
+  a.mass_out = mass_out;
+  a.birth = birth;
+  a.ld_mass = ld_mass;
+  a.ws = ws;
+  a.err = di->err;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Phase ph(PH_ATTN, st);
+  SEER_CUDA(launch_mass(dt, a, di->num_sms, st), "attention mass launch");
+  return SEER_OK;
+}
+
+seer_status seer_evict_select(const float* mass, const int32_t* birth, int ld_mass, const int32_t* kv_len,
+                              const int32_t* gone, const int32_t* budget, int B, int sinks, int recent,
+                              int32_t* len_out, int32_t* gone_out, int32_t* n_moves, int32_t* move_from,
+                              int32_t* move_to, int ld_move, void* stream) {
+  SEER_TRY(check_requests("evict select", B));
+  if (!mass || !birth || !kv_len || !budget || !len_out || !gone_out || !n_moves || !move_from || !move_to)
+    return fail(SEER_ERR_INVALID_ARG, "evict select: null pointer");
+  if (ld_mass <= 0 || ld_move <= 0) return fail(SEER_ERR_INVALID_ARG, "evict select: ld_mass and ld_move must be positive");
+  if (ld_mass > kMaxKeys) return fail(SEER_ERR_UNSUPPORTED, "evict select: at most %d rows of a request", kMaxKeys);
+  if (sinks < 0 || recent < 0) return fail(SEER_ERR_INVALID_ARG, "evict select: sinks and recent must not be negative");
+  // a request's CTAs read what others write: len_out and gone_out alone may replace their own inputs
+  const void* const in[] = {mass, birth, kv_len, gone, budget};
+  const void* const out[] = {len_out, gone_out, n_moves, move_from, move_to};
+  for (const void* i : in)
+    for (const void* o : out)
+      if (i != nullptr && i == o && !(i == kv_len && o == len_out) && !(i == gone && o == gone_out))
+        return fail(SEER_ERR_INVALID_ARG, "evict select: an output is also an input");
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (out[i] == out[j]) return fail(SEER_ERR_INVALID_ARG, "evict select: two outputs share an address");
+  DeviceInfo* di;
+  SEER_TRY(device_info(&di));
+  SelectArgs a{};
+  a.mass = mass;
+  a.birth = birth;
+  a.ld_mass = ld_mass;
+  a.kv_len = kv_len;
+  a.gone = gone;
+  a.budget = budget;
+  a.B = B;
+  a.sinks = sinks;
+  a.recent = recent;
+  a.len_out = len_out;
+  a.gone_out = gone_out;
+  a.n_moves = n_moves;
+  a.move_from = move_from;
+  a.move_to = move_to;
+  a.ld_move = ld_move;
+  a.err = di->err;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Phase ph(PH_KV, st);
+  SEER_CUDA(launch_evict_select(a, di->num_sms, st), "evict select launch");
+  return SEER_OK;
+}
+
+seer_status seer_kv_evict(seer_dtype dt, const int32_t* kv_len, const int32_t* n_moves, const int32_t* move_from,
+                          const int32_t* move_to, int ld_move, int B, const seer_pages* pages, float* mass,
+                          int32_t* birth, int ld_mass, void* stream) {
+  EvictArgs a{};
+  SEER_TRY(check_requests("evict", B));
+  SEER_TRY(check_pages("evict", pages, dt, &a.pages));
+  if (!n_moves || !move_from || !move_to) return fail(SEER_ERR_INVALID_ARG, "evict: null pointer");
+  if (ld_move <= 0) return fail(SEER_ERR_INVALID_ARG, "evict: ld_move must be positive");
+  if ((mass || birth) && ld_mass <= 0) return fail(SEER_ERR_INVALID_ARG, "evict: ld_mass must be positive");
+  DeviceInfo* di;
+  SEER_TRY(device_info(&di));
+  a.kv_len = kv_len;
+  a.n_moves = n_moves;
+  a.move_from = move_from;
+  a.move_to = move_to;
+  a.ld_move = ld_move;
+  a.B = B;
+  a.row_bytes = 2 * pages->n_kv_heads * pages->head_dim * static_cast<int>(esize(dt));
+  a.mass = mass;
+  a.birth = birth;
+  a.ld_mass = ld_mass;
+  a.err = di->err;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Phase ph(PH_KV, st);
+  SEER_CUDA(launch_kv_evict(a, di->num_sms, st), "evict launch");
   return SEER_OK;
 }
 

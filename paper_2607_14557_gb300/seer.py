@@ -61,6 +61,12 @@ class seer_pages(ctypes.Structure):
     _held = None                    # of tensors: (dtype code, device index, rows of the table), see make_pages
 
 
+class seer_rotary(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("magnitude", ctypes.c_double), ("original_len", ctypes.c_int), ("rotary_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("scaling", ctypes.c_int)]
+
+
 _lib = None
 
 
@@ -104,6 +110,14 @@ def lib() -> ctypes.CDLL:
             "seer_attention_tree": [vp, i32, vp, i32, i32, vp, vp, vp, i32, i32, i32, i32, ctypes.POINTER(seer_pages), vp,
                                     sz, vp],
             "seer_attention_tree_workspace_size": [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
+            "seer_rotate": [vp, i32, i32, i32, i32, i32, vp, vp, ctypes.POINTER(seer_rotary), vp, i32, vp],
+            "seer_kv_append_rotary": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, ctypes.POINTER(seer_rotary), vp, i32,
+                                      ctypes.POINTER(seer_pages), vp],
+            "seer_attention_mass": [vp, i32, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, ctypes.POINTER(seer_pages),
+                                    ctypes.c_float, vp, vp, vp, vp, i32, vp, sz, vp],
+            "seer_attention_mass_workspace_size": [i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
+            "seer_evict_select": [vp, vp, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp],
+            "seer_kv_evict": [i32, vp, vp, vp, vp, i32, i32, ctypes.POINTER(seer_pages), vp, vp, i32, vp],
             "seer_check_device": [ctypes.POINTER(ctypes.c_int)],
             "seer_selftest_wait_timeout": [i32, vp],
             "seer_profile_enable": [i32],
@@ -346,6 +360,51 @@ def seer_attention_tree_workspace_size(dt, B, n_heads, n_kv_heads, head_dim, max
     _check(lib().seer_attention_tree_workspace_size(_dt(dt), B, n_heads, n_kv_heads, head_dim, max_draft,
                                                     ctypes.byref(out)))
     return out.value
+
+
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "turns": 2, "pairs": 3}
+
+
+def make_rotary(theta, rotary_dim, interleaved=False, scaling="none", factor=1.0, low=1.0, high=1.0, original_len=1,
+                magnitude=1.0) -> seer_rotary:
+    """scaling: a name of ROTARY_SCALINGS or its code."""
+    return seer_rotary(theta, factor, low, high, magnitude, original_len, rotary_dim, int(interleaved),
+                       ROTARY_SCALINGS.get(scaling, scaling))
+
+
+def seer_rotate(x, ld_x, dt, n_heads, head_dim, T_cap, M_dev, position, rotary, out, ld_out, stream=None):
+    _check(_native().seer_rotate(x, ld_x, _dt(dt), n_heads, head_dim, T_cap, M_dev, position, rotary, out, ld_out, stream))
+
+
+def seer_kv_append_rotary(qkv, ld_qkv, dt, n_heads, T_cap, M_dev, slot, position, cu_new, shift, B, rotary, rotated,
+                          ld_rotated, pages, stream=None):
+    _check(_native().seer_kv_append_rotary(qkv, ld_qkv, _dt(dt), n_heads, T_cap, M_dev, slot, position, cu_new, shift, B,
+                                           rotary, rotated, ld_rotated, pages, stream))
+
+
+def seer_attention_mass(q, ld_q, dt, cu_new, kv_len, accepted, n_accepted, max_draft, window, B, T_cap, T_kv_cap, n_heads,
+                        pages, keep, gone, mass_in, mass_out, birth, ld_mass, ws, ws_bytes, stream=None):
+    _check(_native().seer_attention_mass(q, ld_q, _dt(dt), cu_new, kv_len, accepted, n_accepted, max_draft, window, B,
+                                         T_cap, T_kv_cap, n_heads, pages, keep, gone, mass_in, mass_out, birth, ld_mass,
+                                         ws, ws_bytes, stream))
+
+
+def seer_attention_mass_workspace_size(dt, B, T_kv_cap, n_heads, n_kv_heads, head_dim, window) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().seer_attention_mass_workspace_size(_dt(dt), B, T_kv_cap, n_heads, n_kv_heads, head_dim, window,
+                                                    ctypes.byref(out)))
+    return out.value
+
+
+def seer_evict_select(mass, birth, ld_mass, kv_len, gone, budget, B, sinks, recent, len_out, gone_out, n_moves, move_from,
+                      move_to, ld_move, stream=None):
+    _check(_native().seer_evict_select(mass, birth, ld_mass, kv_len, gone, budget, B, sinks, recent, len_out, gone_out,
+                                       n_moves, move_from, move_to, ld_move, stream))
+
+
+def seer_kv_evict(dt, kv_len, n_moves, move_from, move_to, ld_move, B, pages, mass, birth, ld_mass, stream=None):
+    _check(_native().seer_kv_evict(_dt(dt), kv_len, n_moves, move_from, move_to, ld_move, B, pages, mass, birth, ld_mass,
+                                   stream))
 
 
 def seer_check_device() -> int:
