@@ -128,6 +128,15 @@ __device__ __forceinline__ float2 join(float2 x, float2 y) {
 // (m, 1 / l) as the weights take it: 2^(s - m) / l.
 __device__ __forceinline__ float2 finish(float2 x) { return make_float2(x.x == -INFINITY ? 0.f : x.x, 1.f / x.y); }
 
+// Key t's new weight into the matrices.
+__device__ __forceinline__ void store_mass(const MassArgs& a, const Request& r, int b, int t, float w) {
+  const size_t at = static_cast<size_t>(b) * a.ld_mass + t;
+  const int c = r.kv - r.n;
+  if (t < c && a.keep != 0.f) w = fmaf(a.keep, a.mass_in[at], w);
+  a.mass_out[at] = w;
+  if (a.birth && t >= c) a.birth[at] = t + (a.gone ? a.gone[b] : 0);
+}
+
 // Workspace of the general path: per piece of a request's tiles and column (m, l), then per
 // request and column (m, 1 / l).
 __host__ __device__ inline long columns(const MassArgs& a) { return static_cast<long>(a.n_heads) * a.window; }
@@ -316,36 +325,301 @@ __global__ void __launch_bounds__(kThreads) mass_weights_kernel(const MassArgs a
       float w = 0.f;
 #pragma unroll
       for (int e = 0; e < kThreads / KEYS; ++e) w += sums[e * KEYS + tid];
-      const size_t at = static_cast<size_t>(b) * a.ld_mass + t;
-      const int c = r.kv - r.n;
-      if (t < c && a.keep != 0.f) w = fmaf(a.keep, a.mass_in[at], w);
-      a.mass_out[at] = w;
-      if (a.birth && t >= c) a.birth[at] = t + (a.gone ? a.gone[b] : 0);
+      store_mass(a, r, b, t, w);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ few columns, 16-bit
+// Where a key/value head has at most 16 columns (a decoded token of up to 16 heads) the scores
+// are kept: 4 bytes a column and key beside the key's 2 head_dim bytes, so the cache is read
+// once and the second kernel reads the scores, mostly from L2.  Bound by HBM.
+// A warp takes 16 keys of a head at a time straight from global memory into the fragments of
+// m16n8k16: the order of a product's terms is free, so a lane's 16 bytes of a row serve as the
+// k-indices that the fragment wants from it (and Q is cut alike), and nothing passes through
+// shared memory.  The next keys are under way while these are multiplied, their pages are
+// looked up a step earlier.  A lane keeps the maxima and sums of its two columns over its keys.
+constexpr int kFewCols = 16;                // columns of a key/value head at most
+constexpr int kFewStats = 1024;             // of all heads
+constexpr int GROUP = 16;                   // keys of a step
+
+// Workspace: per piece and column (m, l), then the scores as [tile][column][64].
+struct FewWork {
+  float2* stats;
+  float* scores;
+};
+__host__ __device__ inline size_t few_stats(int B, int runs, long cols) { return ((runs + static_cast<size_t>(B)) * cols + 1) / 2 * 2; }
+__device__ __forceinline__ FewWork few_work(const MassArgs& a) {
+  float2* st = static_cast<float2*>(a.ws);
+  return FewWork{st, reinterpret_cast<float*>(st + few_stats(a.B, a.runs, columns(a)))};
+}
+
+template <bool F16>
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16 keys of a head in a lane: rows lane / 4 and lane / 4 + 8, bytes 16 (lane % 4) of every 64.
+template <int DH>
+struct KeyRegs {
+  uint4 lo[DH / 32], hi[DH / 32];
+};
+
+template <bool F16, int DH, int NT>
+__global__ void __launch_bounds__(kThreads, 2) mass_scores_kernel(const MassArgs a, const float scale) {
+  pdl_enter();
+  extern __shared__ int first[];
+  __shared__ long long warp_sum[kThreads / 32];
+  __shared__ float2 shares[kThreads / 32][NT * 8];
+  tile_line(a, first, warp_sum, blockIdx.x == 0);
+  const int total = first[a.B], runs = min(a.runs, total), run = blockIdx.x;
+  if (run >= runs) return;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, row = lane >> 2;
+  const int hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window;
+  const FewWork w = few_work(a);
+  // warps of a head: its keys are dealt to them 16 at a time
+  const int per_head = hk >= 8 ? 1 : 8 / hk, heads = hk >= 8 ? 8 : hk;
+  const int sub = warp / heads;
+  const bool busy = sub < per_head;
+  const long row_elems = 2l * hk * DH;
+  const int page_mask = (1 << a.pages.page_shift) - 1;
+  int at = cut(total, run, runs);
+  const int end = cut(total, run + 1, runs);
+  for (int b = request_at(first, a.B, at); at < end; ++b) {
+    if (first[b + 1] <= at) continue;
+    const Request r = read_request(a, b);
+    const int tile0 = at - first[b], tile1 = min(first[b + 1], end) - first[b];
+    at += tile1 - tile0;
+    const int cols = r.look * g;
+    if (cols == 0) continue;
+    const int groups = min(tile1 * KEYS, r.kv + GROUP - 1) / GROUP;      // key groups [tile0 * 4, groups)
+    const int free_to = r.kv - r.look;                                   // keys up to it are seen by every row
+    const int* table = a.pages.table + static_cast<size_t>(b) * a.pages.max_pages;
+    for (int kvh = warp % heads; kvh < (hk + heads - 1) / heads * heads; kvh += heads) {
+      const bool mine = busy && kvh < hk;
+      float m[NT][2], l[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          m[nt][e] = -INFINITY;
+          l[nt][e] = 0.f;
+        }
+      if (mine) {
+        uint4 q[NT][DH / 32];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int col = nt * 8 + row;
+          const int qr = col < cols ? query_row(a, r, b, col / g, false) : -1;
+          const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (qr < 0 ? 0 : qr * a.ld_q + static_cast<long>(kvh * g + col % g) * DH));
+#pragma unroll
+          for (int j = 0; j < DH / 32; ++j) q[nt][j] = qr < 0 ? make_uint4(0, 0, 0, 0) : src[4 * j + quad];
+        }
+        const uint16_t* keys = static_cast<const uint16_t*>(a.pages.kv) + static_cast<long>(kvh) * DH + 8 * quad;
+        const auto look_up = [&](int gi, int (&page)[2]) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int t = gi * GROUP + row + 8 * e;
+            page[e] = gi < groups && t < r.kv ? table[t >> a.pages.page_shift] : -1;
+          }
+        };
+        const auto load = [&](int gi, const int (&page)[2], KeyRegs<DH>& k) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int t = gi * GROUP + row + 8 * e;
+            uint4* to = e == 0 ? k.lo : k.hi;
+            const bool there = page[e] >= 0 && page[e] < a.pages.n_pages;
+            if (!there && gi < groups && t < r.kv) record_error(a.err, kErrLayout);
+            const uint4* src = reinterpret_cast<const uint4*>(keys + ((static_cast<long>(there ? page[e] : 0) << a.pages.page_shift) + (t & page_mask)) * row_elems);
+#pragma unroll
+            for (int j = 0; j < DH / 32; ++j) to[j] = there ? src[4 * j] : make_uint4(0, 0, 0, 0);
+          }
+        };
+        const auto compute = [&](int gi, const KeyRegs<DH>& k) {
+          const int t = gi * GROUP + row;
+          float* out = w.scores + (static_cast<size_t>(first[b] + (gi >> 2)) * hk + kvh) * cc * KEYS + (gi & 3) * GROUP + row;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < DH / 32; ++j) {
+              mma16816<F16>(d, k.lo[j].x, k.hi[j].x, k.lo[j].y, k.hi[j].y, q[nt][j].x, q[nt][j].y);
+              mma16816<F16>(d, k.lo[j].z, k.hi[j].z, k.lo[j].w, k.hi[j].w, q[nt][j].z, q[nt][j].w);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int col = nt * 8 + 2 * quad + e;
+              float s0 = d[e] * scale, s1 = d[2 + e] * scale;
+              if (col < cols) {
+                out[col * KEYS] = s0;
+                out[col * KEYS + 8] = s1;
+              }
+              if (t + 8 > free_to) {          // (column col sees keys up to free_to + col / g)
+                const int last = free_to + col / g;
+                if (t > last) s0 = -INFINITY;
+                if (t + 8 > last) s1 = -INFINITY;
+              }
+              const float top = max3(m[nt][e], s0, s1), base = top == -INFINITY ? 0.f : top;
+              l[nt][e] = l[nt][e] * ex2(m[nt][e] - base) + ex2(s0 - base) + ex2(s1 - base);
+              m[nt][e] = top;
+            }
+          }
+        };
+        KeyRegs<DH> k[2];
+        int page[2];
+        int gi = tile0 * (KEYS / GROUP) + sub;
+        look_up(gi, page);
+        load(gi, page, k[0]);
+        look_up(gi + per_head, page);
+        while (gi < groups) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            load(gi + per_head, page, k[x ^ 1]);
+            look_up(gi + 2 * per_head, page);
+            if (gi < groups) compute(gi, k[x]);
+            gi += per_head;
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float2 s = make_float2(m[nt][e], l[nt][e]);
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1)
+              s = join(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, off), __shfl_xor_sync(0xffffffffu, s.y, off)));
+            if (row == 0) shares[warp][nt * 8 + 2 * quad + e] = s;
+          }
+      }
+      __syncthreads();
+      float2* out = w.stats + (run + static_cast<long>(b)) * hk * cc;
+      for (int x = tid; x < heads * cols; x += kThreads) {
+        const int h = x / cols, col = x - h * cols, head = kvh - warp % heads + h;
+        if (head >= hk) continue;
+        float2 s = shares[h][col];
+        for (int e = 1; e < per_head; ++e) s = join(s, shares[h + e * heads][col]);
+        out[static_cast<long>(head) * cc + col] = s;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 4) mass_sums_kernel(const MassArgs a) {
+  pdl_enter();
+  extern __shared__ int first[];
+  __shared__ long long warp_sum[kThreads / 32];
+  __shared__ float sums[kThreads];
+  __shared__ float4 stat[kFewStats];          // (m, 1 / l, the column's place, keys behind free_to that it sees)
+  tile_line(a, first, warp_sum, false);
+  const int total = first[a.B], runs = min(a.runs, total);       // of the kernel before
+  const int blocks = min(static_cast<int>(gridDim.x), total);
+  if (static_cast<int>(blockIdx.x) >= blocks) return;
+  const int tid = threadIdx.x, hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window;
+  const FewWork w = few_work(a);
+  int at = cut(total, blockIdx.x, blocks);
+  const int end = cut(total, blockIdx.x + 1, blocks);
+  for (int b = request_at(first, a.B, at); at < end; ++b) {
+    if (first[b + 1] <= at) continue;
+    const Request r = read_request(a, b);
+    const int cols = r.look * g, all = hk * cols;
+    const int c0 = run_of(total, first[b], runs), c1 = run_of(total, first[b + 1] - 1, runs);
+    __syncthreads();
+    for (int x = tid; x < all; x += kThreads) {
+      const int kvh = x / cols, col = x - kvh * cols;
+      float2 s = make_float2(-INFINITY, 0.f);
+      for (int c = c0; c <= c1; ++c) s = join(s, w.stats[(c + static_cast<long>(b)) * hk * cc + static_cast<long>(kvh) * cc + col]);
+      const float2 f = query_row(a, r, b, col / g, kvh == 0 && at == first[b]) < 0 ? make_float2(0.f, 0.f) : finish(s);
+      stat[x] = make_float4(f.x, f.y, __int_as_float(kvh * cc + col), __int_as_float(col / g));
+    }
+    __syncthreads();
+    const int stop = min(first[b + 1], end);
+    for (; at < stop; ++at) {
+      const int t = (at - first[b]) * KEYS + tid % KEYS;
+      float sum = 0.f;
+      if (t < r.kv) {
+        const float* src = w.scores + static_cast<size_t>(at) * hk * cc * KEYS + tid % KEYS;
+        const int free_to = r.kv - r.look;
+#pragma unroll 8
+        for (int x = tid / KEYS; x < all; x += kThreads / KEYS) {
+          const float4 st = stat[x];
+          const float s = src[__float_as_int(st.z) * KEYS];
+          if (st.y != 0.f && t <= free_to + __float_as_int(st.w)) sum += ex2(s - st.x) * st.y;
+        }
+      }
+      sums[tid] = sum;
+      __syncthreads();
+      if (tid < KEYS && t < r.kv) {
+        float v = 0.f;
+#pragma unroll
+        for (int e = 0; e < kThreads / KEYS; ++e) v += sums[e * KEYS + tid];
+        store_mass(a, r, b, t, v);
+      }
+      __syncthreads();
     }
   }
 }
 
 int general_runs(int num_sms) { return 2 * num_sms; }
+int few_runs(int num_sms) { return 2 * num_sms; }
+bool few_columns(int type, int n_heads, int n_kv, int window) {
+  const long cols = static_cast<long>(n_heads / n_kv) * window;
+  return type != kF32 && cols <= kFewCols && cols * n_kv <= kFewStats;
+}
 
 }  // namespace
 
 size_t mass_workspace(int type, int B, int T_kv_cap, int n_heads, int n_kv, int head_dim, int window, int num_sms) {
   const size_t cols = static_cast<size_t>(n_heads) * window, unit = static_cast<size_t>(n_heads / n_kv) * window;
+  if (few_columns(type, n_heads, n_kv, window))
+    return 8 * few_stats(B, few_runs(num_sms), cols) + 4 * KEYS * cols * (static_cast<size_t>(T_kv_cap) / KEYS + B);
   return 8 * (B * cols + (general_runs(num_sms) + static_cast<size_t>(B) * n_kv) * unit);
 }
 
 cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_t st) {
   MassArgs a = args;
   const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(a.pages.head_dim));
+  const int line = (a.B + 1) * static_cast<int>(sizeof(int)), most_line = (kPageTableMaxB + 1) * static_cast<int>(sizeof(int));
+  if (few_columns(type, a.n_heads, a.pages.n_kv, a.window)) {
+    a.runs = few_runs(num_sms);
+    const dim3 grid(a.cap_tiles < a.runs ? a.cap_tiles : a.runs), sums(a.cap_tiles < 4 * num_sms ? a.cap_tiles : 4 * num_sms);
+    const int wide = a.n_heads / a.pages.n_kv * a.window > 8;
+    cudaError_t e = cudaErrorInvalidValue;
+#define SEER_FEW(F, D, N)                                                                       \
+  if ((type == kF16) == F && a.pages.head_dim == D && wide == N - 1) {                          \
+    static bool set[64] = {};                                                                   \
+    e = set_smem_limit_once(mass_scores_kernel<F, D, N>, most_line, set);                       \
+    if (e == cudaSuccess) e = launch_kernel(mass_scores_kernel<F, D, N>, grid, dim3(kThreads), line, st, a, scale); \
+  }
+    SEER_FEW(false, 64, 1)
+    SEER_FEW(false, 64, 2)
+    SEER_FEW(false, 128, 1)
+    SEER_FEW(false, 128, 2)
+    SEER_FEW(true, 64, 1)
+    SEER_FEW(true, 64, 2)
+    SEER_FEW(true, 128, 1)
+    SEER_FEW(true, 128, 2)
+#undef SEER_FEW
+    static bool set[64] = {};
+    if (e == cudaSuccess) e = set_smem_limit_once(mass_sums_kernel, most_line, set);
+    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel, sums, dim3(kThreads), line, st, a);
+    return e;
+  }
   a.runs = general_runs(num_sms);
-  const int line = (a.B + 1) * static_cast<int>(sizeof(int)), smem = static_cast<int>(sizeof(TileShared)) + line;
-  const int most = static_cast<int>(sizeof(TileShared)) + (kPageTableMaxB + 1) * static_cast<int>(sizeof(int));
+  const int smem = static_cast<int>(sizeof(TileShared)) + line, most = static_cast<int>(sizeof(TileShared)) + most_line;
   const long units = static_cast<long>(a.B) * a.pages.n_kv;
   const int joins = static_cast<int>(units < 4l * num_sms ? units : 4l * num_sms);
   const int tiles = a.cap_tiles < 4 * num_sms ? a.cap_tiles : 4 * num_sms;
   {
     static bool set[64] = {};
-    const cudaError_t e = set_smem_limit_once(mass_join_kernel, (kPageTableMaxB + 1) * static_cast<int>(sizeof(int)), set);
+    const cudaError_t e = set_smem_limit_once(mass_join_kernel, most_line, set);
     if (e != cudaSuccess) return e;
   }
 #define SEER_MASS(T)                                                                                          \
