@@ -23,8 +23,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libseer.so")
 BINDING = os.path.join(PKG, "_seer_binding.so")
 SOURCES = ["seer_api.cu", "tc_gemm.cu", "tc_attn.cu", "simt.cu", "aux_kernels.cu", "seer_noalloc.cu", "paged_api.cu",
-           "paged.cu", "gqa_simt.cu", "tc_causal.cu", "tc_tree.cu", "rotary.cu", "mass.cu", "evict.cu"]
-HEADERS = ["common.cuh", "kernels.h", "attn_schedule.cuh", "api.h", "paged.h", "budget.h", "attn_math.cuh"]
+           "paged.cu", "gqa_simt.cu", "tc_causal.cu", "tc_tree.cu", "rotary.cu", "mass.cu", "tc_mass.cu", "evict.cu"]
+HEADERS = ["common.cuh", "kernels.h", "attn_schedule.cuh", "api.h", "paged.h", "budget.h", "mass_common.cuh", "attn_math.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

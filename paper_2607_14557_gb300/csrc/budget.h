@@ -46,7 +46,7 @@ struct MassArgs {
   int max_draft;
   int window;
   int B, T_cap;
-  int cap_tiles;          // key tiles that the call's T_kv_cap allows
+  int T_kv_cap;           // keys of all requests
   int n_heads;
   PagedKv pages;
   float keep;
@@ -59,9 +59,14 @@ struct MassArgs {
   int runs;               // runs that the tiles are cut into at most (set by the launch)
   int* err;
 };
-constexpr int kMassKeys = 64;               // keys of a tile
 size_t mass_workspace(int type, int B, int T_kv_cap, int n_heads, int n_kv, int head_dim, int window, int num_sms);
 cudaError_t launch_mass(int type, const MassArgs& a, int num_sms, cudaStream_t st);
+// The tensor-core path (tc_mass.cu): 16-bit calls of more columns than launch_mass keeps scores for.
+// mK: the pool as [rows][2 * n_kv][head_dim] in boxes of tc_mass_box_keys() x 1 x 64, with the 128-byte swizzle.
+bool mass_on_tensor_cores(int type, int n_heads, int n_kv, int window);
+int tc_mass_box_keys(int page_size);
+size_t tc_mass_workspace(int B, int T_kv_cap, int n_heads, int n_kv, int window, int num_sms);
+cudaError_t launch_tc_mass(const CUtensorMap& mK, const MassArgs& a, bool f16, int num_sms, cudaStream_t st);
 
 struct SelectArgs {
   const float* mass;      // [B, ld_mass]

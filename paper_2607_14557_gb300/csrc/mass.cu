@@ -4,50 +4,27 @@
 //   m_hi = max_t s_hi(t),  l_hi = sum_t 2^(s_hi(t) - m_hi).
 // A column is one query row of one head.  A softmax's weight needs its whole row first, so the
 // keys are gone through twice: for every column's maximum and sum, then for the weights.
-#include <math.h>
-
-#include "attn_math.cuh"
-#include "budget.h"
-#include "common.cuh"
+#include "mass_common.cuh"
 
 namespace seer {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int KEYS = kMassKeys;
+constexpr int KEYS = 64;                     // keys of a tile
 
-// ------------------------------------------------------------------ requests and their key tiles
-struct Request {
-  int q0, rows;           // its first row of q, and how many the batch gives it
-  int n, look, kv;        // new rows, those that look, keys
-  bool good;
-};
-__device__ __forceinline__ Request read_request(const MassArgs& a, int b) {
-  Request r{};
-  const int q0 = a.cu[b], end = a.cu[b + 1], kv = a.kv_len[b];
-  r.good = q0 >= 0 && end >= q0 && end <= a.T_cap;
-  const int rows = r.good ? end - q0 : 0;
-  const int n = a.accepted ? a.n_accepted[b] : rows;
-  r.good = r.good && n >= 0 && n <= rows && (!a.accepted || n <= a.max_draft) && kv >= n && kv <= a.ld_mass && kv <= kMaxKeys &&
-           kv <= (static_cast<long long>(a.pages.max_pages) << a.pages.page_shift);
-  if (!r.good) return r;
-  r.q0 = q0;
-  r.rows = rows;
-  r.n = n;
-  r.look = min(n, a.window);
-  r.kv = kv;
-  return r;
-}
-__device__ __forceinline__ int tiles_of(const Request& r) { return (r.kv + KEYS - 1) / KEYS; }
+__device__ __forceinline__ int tiles_of(const MassRequest& r) { return (r.kv + KEYS - 1) / KEYS; }
+// Key tiles that the call's key capacity allows.
+__host__ __device__ inline int tile_capacity(const MassArgs& a) { return a.T_kv_cap / KEYS + a.B; }
 
 // first[b] = key tiles of the requests before b, first[B] all; by the whole block.  Requests
 // past the call's key capacity have no tiles, nor has any behind them.
 __device__ __forceinline__ void tile_line(const MassArgs& a, int* first, long long* warp_sum, bool report) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const long long cap = tile_capacity(a);
   long long sum = 0;
   for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
     const int b = b0 + tid;
-    Request r{};
+    MassRequest r{};
     if (b < a.B) {
       r = read_request(a, b);
       if (!r.good && report) record_error(a.err, kErrLayout);
@@ -67,8 +44,8 @@ __device__ __forceinline__ void tile_line(const MassArgs& a, int* first, long lo
       sum += warp_sum[w];
     }
     if (b < a.B) {
-      if (before + inc > a.cap_tiles && v > 0 && report) record_error(a.err, kErrCapacity);
-      first[b + 1] = static_cast<int>(before + inc > a.cap_tiles ? -1 : before + inc);
+      if (before + inc > cap && v > 0 && report) record_error(a.err, kErrCapacity);
+      first[b + 1] = static_cast<int>(before + inc > cap ? -1 : before + inc);
     }
     __syncthreads();
   }
@@ -87,56 +64,6 @@ __device__ __forceinline__ void tile_line(const MassArgs& a, int* first, long lo
     __syncthreads();
   }
 }
-// The request of place x on the line.
-__device__ __forceinline__ int request_at(const int* first, int B, int x) {
-  int lo = 0, hi = B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= x) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-// Run c of n over `total` places: [cut(c), cut(c + 1)), and the run that holds x.
-__device__ __forceinline__ int cut(long long total, int c, int n) { return static_cast<int>(total * c / n); }
-__device__ __forceinline__ int run_of(long long total, long long x, int n) { return static_cast<int>(((x + 1) * n - 1) / total); }
-
-// Row of q of a request's i-th looking row, or -1 (an accepted entry outside the draft).
-__device__ __forceinline__ int query_row(const MassArgs& a, const Request& r, int b, int i, bool report) {
-  const int k = r.n - r.look + i;
-  if (!a.accepted) return r.q0 + k;
-  const int e = a.accepted[static_cast<size_t>(b) * a.max_draft + k];
-  if (e >= 0 && e < r.rows) return r.q0 + e;
-  if (report) record_error(a.err, kErrLayout);
-  return -1;
-}
-// Pool row of key t of request b, or -1.
-__device__ __forceinline__ long key_row(const MassArgs& a, int b, int t, bool report) {
-  const int page = a.pages.table[static_cast<size_t>(b) * a.pages.max_pages + (t >> a.pages.page_shift)];
-  if (page < 0 || page >= a.pages.n_pages) {
-    if (report) record_error(a.err, kErrLayout);
-    return -1;
-  }
-  return (static_cast<long>(page) << a.pages.page_shift) + (t & ((1 << a.pages.page_shift) - 1));
-}
-
-// (m, l) of two sets of keys; m = -inf: nothing but hidden or -inf scores.
-__device__ __forceinline__ float2 join(float2 x, float2 y) {
-  const float m = fmaxf(x.x, y.x);
-  const float base = m == -INFINITY ? 0.f : m;
-  return make_float2(m, x.y * ex2(x.x - base) + y.y * ex2(y.x - base));
-}
-// (m, 1 / l) as the weights take it: 2^(s - m) / l.
-__device__ __forceinline__ float2 finish(float2 x) { return make_float2(x.x == -INFINITY ? 0.f : x.x, 1.f / x.y); }
-
-// Key t's new weight into the matrices.
-__device__ __forceinline__ void store_mass(const MassArgs& a, const Request& r, int b, int t, float w) {
-  const size_t at = static_cast<size_t>(b) * a.ld_mass + t;
-  const int c = r.kv - r.n;
-  if (t < c && a.keep != 0.f) w = fmaf(a.keep, a.mass_in[at], w);
-  a.mass_out[at] = w;
-  if (a.birth && t >= c) a.birth[at] = t + (a.gone ? a.gone[b] : 0);
-}
-
 // Workspace of the general path: per piece of a request's tiles and column (m, l), then per
 // request and column (m, 1 / l).
 __host__ __device__ inline long columns(const MassArgs& a) { return static_cast<long>(a.n_heads) * a.window; }
@@ -159,7 +86,7 @@ struct TileShared {
   int col_row[COLS];                          // new row of a column counted from the first that looks, -1: none
 };
 template <int T>
-__device__ __forceinline__ void load_queries(const MassArgs& a, const Request& r, int b, int kvh, int col0, TileShared& sh) {
+__device__ __forceinline__ void load_queries(const MassArgs& a, const MassRequest& r, int b, int kvh, int col0, TileShared& sh) {
   const int dh = a.pages.head_dim, g = a.n_heads / a.pages.n_kv;
   for (int x = threadIdx.x; x < COLS * dh; x += kThreads) {
     const int j = x / dh, d = x - j * dh, col = col0 + j, i = col / g;
@@ -170,7 +97,7 @@ __device__ __forceinline__ void load_queries(const MassArgs& a, const Request& r
   }
 }
 template <int T>
-__device__ __forceinline__ void load_keys(const MassArgs& a, const Request& r, int b, int kvh, int t0, TileShared& sh, bool report) {
+__device__ __forceinline__ void load_keys(const MassArgs& a, const MassRequest& r, int b, int kvh, int t0, TileShared& sh, bool report) {
   const int dh = a.pages.head_dim;
   for (int x = threadIdx.x; x < KEYS * dh; x += kThreads) {
     const int j = x / dh, d = x - j * dh;
@@ -214,7 +141,7 @@ __global__ void __launch_bounds__(kThreads) mass_stats_kernel(const MassArgs a, 
   while (at < end) {
     // unit (b, kvh): tiles first[b] * hk + kvh * tiles ..
     const int b = request_at(first, a.B, static_cast<int>(at / hk));
-    const Request r = read_request(a, b);
+    const MassRequest r = read_request(a, b);
     const int tiles = tiles_of(r);
     const long long inside = at - static_cast<long long>(first[b]) * hk;
     const int kvh = static_cast<int>(inside / tiles), tile0 = static_cast<int>(inside - static_cast<long long>(kvh) * tiles);
@@ -269,7 +196,7 @@ __global__ void __launch_bounds__(kThreads) mass_join_kernel(const MassArgs a) {
     const int b = static_cast<int>(unit / hk), kvh = static_cast<int>(unit % hk);
     const int tiles = first[b + 1] - first[b];
     if (tiles == 0) continue;
-    const Request r = read_request(a, b);
+    const MassRequest r = read_request(a, b);
     const long long at = static_cast<long long>(first[b]) * hk + static_cast<long long>(kvh) * tiles;
     const int c0 = run_of(total, at, runs), c1 = run_of(total, at + tiles - 1, runs);
     for (int col = threadIdx.x; col < r.look * g; col += kThreads) {
@@ -296,7 +223,7 @@ __global__ void __launch_bounds__(kThreads) mass_weights_kernel(const MassArgs a
   const int hk = a.pages.n_kv, tid = threadIdx.x, g = a.n_heads / hk;
   for (int x = blockIdx.x; x < first[a.B]; x += gridDim.x) {
     const int b = request_at(first, a.B, x);
-    const Request r = read_request(a, b);
+    const MassRequest r = read_request(a, b);
     const int t0 = (x - first[b]) * KEYS, t = t0 + tid % KEYS;
     float sum = 0.f;
     if (r.look > 0)
@@ -394,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 2) mass_scores_kernel(const MassArgs
   const int end = cut(total, run + 1, runs);
   for (int b = request_at(first, a.B, at); at < end; ++b) {
     if (first[b + 1] <= at) continue;
-    const Request r = read_request(a, b);
+    const MassRequest r = read_request(a, b);
     const int tile0 = at - first[b], tile1 = min(first[b + 1], end) - first[b];
     at += tile1 - tile0;
     const int cols = r.look * g;
@@ -528,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 4) mass_sums_kernel(const MassArgs a
   const int end = cut(total, blockIdx.x + 1, blocks);
   for (int b = request_at(first, a.B, at); at < end; ++b) {
     if (first[b + 1] <= at) continue;
-    const Request r = read_request(a, b);
+    const MassRequest r = read_request(a, b);
     const int cols = r.look * g, all = hk * cols;
     const int c0 = run_of(total, first[b], runs), c1 = run_of(total, first[b + 1] - 1, runs);
     __syncthreads();
@@ -576,8 +503,11 @@ bool few_columns(int type, int n_heads, int n_kv, int window) {
 
 }  // namespace
 
+bool mass_on_tensor_cores(int type, int n_heads, int n_kv, int window) { return type != kF32 && !few_columns(type, n_heads, n_kv, window); }
+
 size_t mass_workspace(int type, int B, int T_kv_cap, int n_heads, int n_kv, int head_dim, int window, int num_sms) {
   const size_t cols = static_cast<size_t>(n_heads) * window, unit = static_cast<size_t>(n_heads / n_kv) * window;
+  if (mass_on_tensor_cores(type, n_heads, n_kv, window)) return tc_mass_workspace(B, T_kv_cap, n_heads, n_kv, window, num_sms);
   if (few_columns(type, n_heads, n_kv, window))
     return 8 * few_stats(B, few_runs(num_sms), cols) + 4 * KEYS * cols * (static_cast<size_t>(T_kv_cap) / KEYS + B);
   return 8 * (B * cols + (general_runs(num_sms) + static_cast<size_t>(B) * n_kv) * unit);
@@ -589,7 +519,8 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
   const int line = (a.B + 1) * static_cast<int>(sizeof(int)), most_line = (kPageTableMaxB + 1) * static_cast<int>(sizeof(int));
   if (few_columns(type, a.n_heads, a.pages.n_kv, a.window)) {
     a.runs = few_runs(num_sms);
-    const dim3 grid(a.cap_tiles < a.runs ? a.cap_tiles : a.runs), sums(a.cap_tiles < 4 * num_sms ? a.cap_tiles : 4 * num_sms);
+    const int most_tiles = tile_capacity(a);
+    const dim3 grid(most_tiles < a.runs ? most_tiles : a.runs), sums(most_tiles < 4 * num_sms ? most_tiles : 4 * num_sms);
     const int wide = a.n_heads / a.pages.n_kv * a.window > 8;
     cudaError_t e = cudaErrorInvalidValue;
 #define SEER_FEW(F, D, N)                                                                       \
@@ -616,7 +547,7 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
   const int smem = static_cast<int>(sizeof(TileShared)) + line, most = static_cast<int>(sizeof(TileShared)) + most_line;
   const long units = static_cast<long>(a.B) * a.pages.n_kv;
   const int joins = static_cast<int>(units < 4l * num_sms ? units : 4l * num_sms);
-  const int tiles = a.cap_tiles < 4 * num_sms ? a.cap_tiles : 4 * num_sms;
+  const int tiles = tile_capacity(a) < 4 * num_sms ? tile_capacity(a) : 4 * num_sms;
   {
     static bool set[64] = {};
     const cudaError_t e = set_smem_limit_once(mass_join_kernel, most_line, set);
@@ -633,8 +564,6 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
     return e;                                                                                                 \
   }
   SEER_MASS(kF32)
-  SEER_MASS(kBF16)
-  SEER_MASS(kF16)
 #undef SEER_MASS
   return cudaErrorInvalidValue;
 }

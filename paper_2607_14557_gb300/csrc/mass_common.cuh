@@ -1,0 +1,86 @@
+// What the kernels of the attention mass share: requests as they check them, the line of key
+// tiles that runs are cut from, and the arithmetic of joined softmax sums.
+#pragma once
+
+#include <math.h>
+
+#include "attn_math.cuh"
+#include "budget.h"
+#include "common.cuh"
+
+namespace seer {
+
+struct MassRequest {
+  int q0, rows;           // its first row of q, and how many the batch gives it
+  int n, look, kv;        // new rows, those that look, keys
+  bool good;
+};
+__device__ __forceinline__ MassRequest read_request(const MassArgs& a, int b) {
+  MassRequest r{};
+  const int q0 = a.cu[b], end = a.cu[b + 1], kv = a.kv_len[b];
+  r.good = q0 >= 0 && end >= q0 && end <= a.T_cap;
+  const int rows = r.good ? end - q0 : 0;
+  const int n = a.accepted ? a.n_accepted[b] : rows;
+  r.good = r.good && n >= 0 && n <= rows && (!a.accepted || n <= a.max_draft) && kv >= n && kv <= a.ld_mass && kv <= kMaxKeys &&
+           kv <= (static_cast<long long>(a.pages.max_pages) << a.pages.page_shift);
+  if (!r.good) return r;
+  r.q0 = q0;
+  r.rows = rows;
+  r.n = n;
+  r.look = min(n, a.window);
+  r.kv = kv;
+  return r;
+}
+
+// The request of place x on the line.
+template <typename P>
+__device__ __forceinline__ int request_at(const P* first, int B, P x) {
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+// Run c of n over `total` places: [cut(c), cut(c + 1)), and the run that holds x.
+__device__ __forceinline__ int cut(long long total, int c, int n) { return static_cast<int>(total * c / n); }
+__device__ __forceinline__ int run_of(long long total, long long x, int n) { return static_cast<int>(((x + 1) * n - 1) / total); }
+
+// Row of q of a request's i-th looking row, or -1 (an accepted entry outside the draft).
+__device__ __forceinline__ int query_row(const MassArgs& a, const MassRequest& r, int b, int i, bool report) {
+  const int k = r.n - r.look + i;
+  if (!a.accepted) return r.q0 + k;
+  const int e = a.accepted[static_cast<size_t>(b) * a.max_draft + k];
+  if (e >= 0 && e < r.rows) return r.q0 + e;
+  if (report) record_error(a.err, kErrLayout);
+  return -1;
+}
+// Pool row of key t of request b, or -1.
+__device__ __forceinline__ long key_row(const MassArgs& a, int b, int t, bool report) {
+  const int page = a.pages.table[static_cast<size_t>(b) * a.pages.max_pages + (t >> a.pages.page_shift)];
+  if (page < 0 || page >= a.pages.n_pages) {
+    if (report) record_error(a.err, kErrLayout);
+    return -1;
+  }
+  return (static_cast<long>(page) << a.pages.page_shift) + (t & ((1 << a.pages.page_shift) - 1));
+}
+
+// (m, l) of two sets of keys; m = -inf: nothing but hidden or -inf scores.
+__device__ __forceinline__ float2 join(float2 x, float2 y) {
+  const float m = fmaxf(x.x, y.x);
+  const float base = m == -INFINITY ? 0.f : m;
+  return make_float2(m, x.y * ex2(x.x - base) + y.y * ex2(y.x - base));
+}
+// (m, 1 / l) as the weights take it: 2^(s - m) / l.
+__device__ __forceinline__ float2 finish(float2 x) { return make_float2(x.x == -INFINITY ? 0.f : x.x, 1.f / x.y); }
+
+// Key t's new weight into the matrices.
+__device__ __forceinline__ void store_mass(const MassArgs& a, const MassRequest& r, int b, int t, float w) {
+  const size_t at = static_cast<size_t>(b) * a.ld_mass + t;
+  const int c = r.kv - r.n;
+  if (t < c && a.keep != 0.f) w = fmaf(a.keep, a.mass_in[at], w);
+  a.mass_out[at] = w;
+  if (a.birth && t >= c) a.birth[at] = t + (a.gone ? a.gone[b] : 0);
+}
+
+}  // namespace seer

@@ -1,0 +1,543 @@
+// Attention mass of many columns (windows of rows, wide groups of heads) on tcgen05 for sm_103a:
+// head_dim 64 or 128, q and the cache both f16 or both bf16.
+//   mass[t] += sum over columns of 2^(s - m) / l   (mass.cu has the definition)
+// The scores of a column block, up to 256 columns, times every key do not fit anywhere, so they
+// are multiplied twice: once for each column's maximum and sum, once for the weights.
+//   first pass   S = Q K^T, a column a TMEM lane: maximum and sum need no other thread
+//   second pass  S^T = K Q^T, a key a lane: the sum over the columns needs no other thread
+// Both passes are one kernel: the same loads, rings and roles, with A and B changed about.  A
+// product's terms are added in the same order either way, so both passes see the same scores.
+//
+// A unit is (request, key/value head, column block); its work the 128-key tiles of the cache.  All
+// units' tiles form one line, cut into equal runs, one per CTA.  A piece of a unit leaves its
+// columns' (m, l) in the workspace; the second pass joins a unit's pieces when it begins one, and
+// leaves each key's sum per unit, which the last kernel adds up in order.
+//
+// One CTA per SM:
+//   warp 0       producer: key tiles by TMA, a box per page and lane, a ring of three
+//   warp 1       MMA issuer, two score tiles of 256 columns ahead in tensor memory
+//   warps 2-9    exponentials: two warps a lane quarter
+//   warps 10-13  queries of the next piece into shared memory, and its joined statistics
+// Bound by the exponentials: two a (column, key).
+#include "mass_common.cuh"
+
+namespace seer {
+namespace {
+
+constexpr int KEYS = 128;                   // keys of a tile
+constexpr int COLS = 256;                   // columns of a block, two tiles of 128 rows of Q
+constexpr int RING = 3;
+constexpr int THREADS = 448;
+constexpr int SOFT_WARP = 2, LOAD_WARP = 10;
+constexpr uint32_t TMEM_COLS = 512;
+constexpr uint64_t kDrainNs = 20000000ull;
+
+template <int DH>
+struct Layout {
+  static constexpr int PANELS = DH / 64;
+  static constexpr int K_PANEL = KEYS * 128, K_TILE = PANELS * K_PANEL;
+  static constexpr int Q_PANEL = COLS * 128, Q_TILE = PANELS * Q_PANEL;
+  static constexpr int OFF_K = 2 * Q_TILE;
+  static constexpr int OFF_STAT = OFF_K + RING * K_TILE;   // of the second pass: -m, 1 / l, token
+  static constexpr int OFF_BAR = OFF_STAT + COLS * 9;
+  static constexpr int BYTES = OFF_BAR + 256;
+  static_assert(BYTES <= 227 * 1024 && OFF_BAR % 8 == 0, "shared memory of an SM");
+};
+
+// Workspace: prefix sums over the requests, the pieces' (m, l), the keys' sums per unit.
+struct Work {
+  int* tiles;             // [B + 1] key tiles of the requests before b
+  long long* places;      // [B + 1] places on the line
+  float2* stats;          // [runs + B * slices][256]
+  float* sums;            // [2 * slices][capacity tiles][128]
+};
+struct Sizes {
+  int tpt, slices, blocks;                  // tokens of a tile of Q; units and column blocks of a request at most
+};
+__host__ __device__ inline Sizes sizes_of(int n_heads, int n_kv, int window) {
+  Sizes z;
+  z.tpt = 128 / (n_heads / n_kv);
+  z.blocks = (window + 2 * z.tpt - 1) / (2 * z.tpt);
+  z.slices = n_kv * z.blocks;
+  return z;
+}
+__host__ __device__ inline size_t work_tiles(int T_kv_cap, int B) { return static_cast<size_t>(T_kv_cap) / KEYS + B; }
+__host__ __device__ inline size_t prefix_bytes(int B) { return (12 * (static_cast<size_t>(B) + 2) + 15) / 16 * 16; }
+__device__ __forceinline__ Work work_of(const MassArgs& a, const Sizes& z) {
+  Work w;
+  uint8_t* p = static_cast<uint8_t*>(a.ws);
+  w.places = reinterpret_cast<long long*>(p);
+  w.tiles = reinterpret_cast<int*>(w.places + a.B + 1);
+  w.stats = reinterpret_cast<float2*>(p + prefix_bytes(a.B));
+  w.sums = reinterpret_cast<float*>(w.stats + (a.runs + static_cast<size_t>(a.B) * z.slices) * COLS);
+  return w;
+}
+
+// ------------------------------------------------------------------ the line
+__global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
+  pdl_enter();
+  __shared__ long long warp_sum[2][32];
+  const Sizes z = sizes_of(a.n_heads, a.pages.n_kv, a.window);
+  const Work w = work_of(a, z);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long cap = static_cast<long long>(work_tiles(a.T_kv_cap, a.B));
+  long long tiles = 0, places = 0;          // of the requests before
+  for (int b0 = 0; b0 < a.B; b0 += 1024) {
+    const int b = b0 + tid;
+    long long v[2] = {0, 0};
+    if (b < a.B) {
+      const MassRequest r = read_request(a, b);
+      if (!r.good) record_error(a.err, kErrLayout);
+      v[0] = (r.kv + KEYS - 1) / KEYS;
+      v[1] = v[0] * a.pages.n_kv * ((r.look + 2 * z.tpt - 1) / (2 * z.tpt));
+    }
+    long long inc[2] = {v[0], v[1]};
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, inc[0], off), y = __shfl_up_sync(0xffffffffu, inc[1], off);
+      if (lane >= off) {
+        inc[0] += x;
+        inc[1] += y;
+      }
+    }
+    if (lane == 31) {
+      warp_sum[0][warp] = inc[0];
+      warp_sum[1][warp] = inc[1];
+    }
+    __syncthreads();
+    long long before[2] = {tiles, places};
+    for (int x = 0; x < 32; ++x) {
+      if (x < warp) {
+        before[0] += warp_sum[0][x];
+        before[1] += warp_sum[1][x];
+      }
+      tiles += warp_sum[0][x];
+      places += warp_sum[1][x];
+    }
+    if (b < a.B) {
+      // past the key capacity nobody has tiles: such a request begins and ends where the last good one did
+      const bool fits = before[0] + inc[0] <= cap;
+      if (!fits && v[0] > 0) record_error(a.err, kErrCapacity);
+      w.tiles[b + 1] = fits ? static_cast<int>(before[0] + inc[0]) : -1;
+      w.places[b + 1] = before[1] + inc[1];
+    }
+    __syncthreads();
+  }
+  if (tid == 0) {
+    w.tiles[0] = 0;
+    w.places[0] = 0;
+  }
+  __syncthreads();
+  if (w.tiles[a.B] >= 0) return;
+  int lo = 0, hi = a.B;                     // tiles[lo] >= 0, tiles[hi] < 0
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (w.tiles[mid] >= 0) lo = mid; else hi = mid;
+  }
+  const int end = w.tiles[lo];
+  const long long last = w.places[lo];
+  __syncthreads();
+  for (int b = lo + 1 + tid; b <= a.B; b += 1024) {
+    w.tiles[b] = end;
+    w.places[b] = last;
+  }
+}
+
+// A piece of a unit: key tiles [tile0, tile1).
+struct Piece {
+  int b, kvh, tok0;       // tok0: the block's first token among the rows that look
+  int tile0, tile1, tiles;
+  int slice;
+  MassRequest r;
+};
+// The pieces of run blockIdx.x, the same for every role of the CTA.
+struct Walk {
+  const MassArgs& a;
+  const Sizes z;
+  const Work w;
+  long long at, end, total;
+  int runs, b = 0;
+  bool fresh = true;
+
+  __device__ __forceinline__ Walk(const MassArgs& a_) : a(a_), z(sizes_of(a_.n_heads, a_.pages.n_kv, a_.window)), w(work_of(a_, z)) {
+    total = w.places[a.B];
+    runs = static_cast<int>(min(static_cast<long long>(a.runs), total));
+    const int run = blockIdx.x;
+    at = run < runs ? total * run / runs : 0;
+    end = run < runs ? total * (run + 1) / runs : 0;
+  }
+  __device__ __forceinline__ int run_at(long long x) const { return static_cast<int>(((x + 1) * runs - 1) / total); }
+  __device__ __forceinline__ bool next(Piece& p) {
+    if (at >= end) return false;
+    if (fresh || w.places[b + 1] <= at) {
+      fresh = false;
+      b = request_at(w.places, a.B, at);
+      p.r = read_request(a, b);
+    }
+    p.b = b;
+    p.tiles = w.tiles[b + 1] - w.tiles[b];
+    const long long off = at - w.places[b];
+    const int unit = static_cast<int>(off / p.tiles), blocks = (p.r.look + 2 * z.tpt - 1) / (2 * z.tpt);
+    p.tile0 = static_cast<int>(off - static_cast<long long>(unit) * p.tiles);
+    p.tile1 = static_cast<int>(min(static_cast<long long>(p.tiles), p.tile0 + (end - at)));
+    at += p.tile1 - p.tile0;
+    p.kvh = unit / blocks;
+    p.tok0 = (unit - p.kvh * blocks) * 2 * z.tpt;
+    p.slice = p.kvh * z.blocks + (unit - p.kvh * blocks);
+    return true;
+  }
+};
+
+// ------------------------------------------------------------------ both passes
+template <bool F16, int DH, bool WEIGHTS>
+__global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_constant__ CUtensorMap mK, const MassArgs a, const float scale) {
+  using L = Layout<DH>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  if ((smem_u32(smem) & 1023u) != 0) {
+    pdl_enter();
+    if (threadIdx.x == 0) record_error(a.err, kErrLayout);
+    return;
+  }
+  float* neg_m = reinterpret_cast<float*>(smem + L::OFF_STAT);
+  float* inv_l = neg_m + COLS;
+  uint8_t* token = reinterpret_cast<uint8_t*>(inv_l + COLS);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
+  uint64_t* k_full = bars;                  // [RING]
+  uint64_t* k_empty = k_full + RING;        // [RING]
+  uint64_t* q_full = k_empty + RING;        // [2]
+  uint64_t* q_empty = q_full + 2;           // [2]
+  uint64_t* s_full = q_empty + 2;           // [2]
+  uint64_t* s_empty = s_full + 2;           // [2]
+  uint64_t* stat_full = s_empty + 2;
+  uint64_t* stat_empty = stat_full + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(stat_empty + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  static_assert(8 * (2 * RING + 10) + 8 <= 256, "barrier block");
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < RING; ++i) {
+      mbar_init(&k_full[i], 1);
+      mbar_init(&k_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_full[i], 4);
+      mbar_init(&q_empty[i], 1);
+      mbar_init(&s_full[i], 1);
+      mbar_init(&s_empty[i], 8);
+    }
+    mbar_init(stat_full, 4);
+    mbar_init(stat_empty, 8);
+    *abort_flag = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&mK);
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
+  pdl_enter();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int G = a.n_heads / a.pages.n_kv;
+  Walk walk(a);
+  const int tpt = walk.z.tpt;
+  Piece p{};
+
+  if (warp == 0) {
+    // -------------------------------------------------- producer
+    const bool leader = elect_one();
+    const int box_rows = min(KEYS, 1 << a.pages.page_shift), boxes = KEYS / box_rows;
+    const int out_of_pool = a.pages.n_pages << a.pages.page_shift;    // a row that the tensor map fills with zeros
+    const auto box_row = [&](const Piece& u, int j) {
+      const int key = j * KEYS + lane * box_rows;
+      if (lane >= boxes || key >= u.r.kv) return -1;
+      const int page = a.pages.table[static_cast<size_t>(u.b) * a.pages.max_pages + (key >> a.pages.page_shift)];
+      if (page < 0 || page >= a.pages.n_pages) {
+        record_error(a.err, kErrLayout);
+        return out_of_pool;
+      }
+      return (page << a.pages.page_shift) + (key & ((1 << a.pages.page_shift) - 1));
+    };
+    unsigned g = 0;
+    bool ok = true;
+    while (ok && walk.next(p)) {
+      int next_row = box_row(p, p.tile0);                 // the page of a tile is looked up a tile ahead
+      for (int j = p.tile0; j < p.tile1; ++j, ++g) {
+        const int row = next_row, s = g % RING;
+        if (j + 1 < p.tile1) next_row = box_row(p, j + 1);
+        if (g >= RING && !warp_wait(&k_empty[s], (g / RING - 1) & 1, abort_flag, a.err)) {
+          ok = false;
+          break;
+        }
+        const int bytes = __popc(__ballot_sync(0xffffffffu, row >= 0)) * box_rows * 128 * L::PANELS;
+        if (leader) mbar_arrive_expect_tx(&k_full[s], bytes);
+        __syncwarp();
+        if (row >= 0)
+          for (int x = 0; x < L::PANELS; ++x)
+            tma_load_3d(smem + L::OFF_K + s * L::K_TILE + x * L::K_PANEL + lane * box_rows * 128, &mK, &k_full[s], 64 * x, p.kvh, row);
+        __syncwarp();
+      }
+    }
+    if (*abort_flag && leader)                            // copies still in flight land before the memory is released
+      for (unsigned j = g > RING ? g - RING : 0; j < g; ++j) mbar_wait_drain(&k_full[j % RING], (j / RING) & 1, kDrainNs);
+  } else if (warp == 1) {
+    // -------------------------------------------------- MMA issuer
+    const bool leader = elect_one();
+    const uint64_t base = make_sdesc_sw128(smem_u32(smem), 16, 1024);
+    unsigned g = 0;
+    bool ok = true;
+    for (int i = 0; ok && walk.next(p); ++i) {
+      const int qb = i & 1;
+      const int ntok = p.r.look - p.tok0, rows1 = min(max(ntok - tpt, 0), tpt) * G;
+      const bool two = rows1 > 0;
+      // columns of the second pass: whole 16s (rows of Q behind the block's are zeros)
+      const uint32_t n = two ? 128 + (rows1 + 15) / 16 * 16 : (ntok * G + 15) / 16 * 16;
+      const uint32_t idesc = WEIGHTS ? make_idesc(KEYS, n, 0, F16) : make_idesc(128, KEYS, 0, F16);
+      if (!warp_wait(&q_full[qb], (i / 2) & 1, abort_flag, a.err)) break;
+      for (int j = p.tile0; j < p.tile1; ++j, ++g) {
+        const int s = g % RING, buf = g & 1;
+        if (!warp_wait(&k_full[s], (g / RING) & 1, abort_flag, a.err) ||
+            (g >= 2 && !warp_wait(&s_empty[buf], (g / 2 - 1) & 1, abort_flag, a.err))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        if (leader) {
+          const uint64_t dk = base + ((L::OFF_K + s * L::K_TILE) >> 4), dq = base + ((qb * L::Q_TILE) >> 4);
+          const uint32_t d = tmem + buf * COLS;
+          for (int t = 0; t < (WEIGHTS || !two ? 1 : 2); ++t)
+#pragma unroll
+            for (int k = 0; k < DH / 16; ++k) {
+              const uint64_t ok_ = dk + (((k >> 2) * L::K_PANEL + (k & 3) * 32) >> 4);
+              const uint64_t oq = dq + (((k >> 2) * L::Q_PANEL + t * 128 * 128 + (k & 3) * 32) >> 4);
+              tc_mma_f16(d + t * 128, WEIGHTS ? ok_ : oq, WEIGHTS ? oq : ok_, idesc, k > 0 ? 1u : 0u);
+            }
+          tc_commit(&s_full[buf]);
+          tc_commit(&k_empty[s]);
+          if (j + 1 == p.tile1) tc_commit(&q_empty[qb]);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp < LOAD_WARP) {
+    // -------------------------------------------------- exponentials, warps 2 .. 9
+    const int half = (warp - SOFT_WARP) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
+    unsigned g = 0;
+    bool ok = true;
+    for (int i = 0; ok && walk.next(p); ++i) {
+      const int ntok = p.r.look - p.tok0, rows0 = min(ntok, tpt) * G, rows1 = min(max(ntok - tpt, 0), tpt) * G;
+      const bool two = rows1 > 0;
+      const int free_to = p.r.kv - p.r.look + p.tok0;     // keys up to it are seen by every column of the block
+      if constexpr (!WEIGHTS) {
+        // a lane a column: tile `half` of Q, or with one tile half of its keys
+        const int rows = two && half == 1 ? rows1 : rows0;
+        const bool busy = quarter * 32 < rows;
+        const int last = free_to + (two ? half * tpt : 0) + r / G;      // the last key that the column sees
+        const int col0 = two ? half * 128 : half * 64, cols = two ? 128 : 64, key0 = two ? 0 : half * 64;
+        float m = -INFINITY, l = 0.f;                     // m of unscaled scores
+        for (int j = p.tile0; j < p.tile1; ++j, ++g) {
+          const int buf = g & 1;
+          if (!warp_wait(&s_full[buf], (g / 2) & 1, abort_flag, a.err)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (busy) {
+            for (int c = 0; c < cols; c += 64) {
+              uint32_t v[2][32];
+              tmem_ld32(tmem + lane_off + buf * COLS + col0 + c, v[0]);
+              tmem_ld32(tmem + lane_off + buf * COLS + col0 + c + 32, v[1]);
+              tmem_ld_wait();
+              const int t0 = j * KEYS + key0 + c;
+              if (t0 + 63 > free_to) {                    // some column does not see all of these
+                const int seen = last - t0 + 1;
+#pragma unroll
+                for (int x = 0; x < 64; ++x)
+                  if (x >= seen) v[x / 32][x % 32] = 0xff800000u;
+              }
+              float top = m;
+#pragma unroll
+              for (int x = 0; x < 64; x += 2) top = max3(top, __uint_as_float(v[x / 32][x % 32]), __uint_as_float(v[x / 32][x % 32 + 1]));
+              const float base = top == -INFINITY ? 0.f : __fmul_rn(top, scale);
+              l *= m == -INFINITY ? 0.f : ex2(__fmul_rn(m, scale) - base);
+              m = top;
+              float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int x = 0; x < 64; ++x) sum[x & 3] += ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x / 32][x % 32]), scale), -base));
+              l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_empty[buf]);
+        }
+        if (ok && r < rows)
+          walk.w.stats[(blockIdx.x + static_cast<size_t>(p.b) * walk.z.slices + p.slice) * COLS + half * 128 + r] =
+              make_float2(m == -INFINITY ? m : __fmul_rn(m, scale), l);
+      } else {
+        // a lane a key: every second 32 columns
+        if (!warp_wait(stat_full, i & 1, abort_flag, a.err)) break;
+        for (int j = p.tile0; j < p.tile1; ++j, ++g) {
+          const int buf = g & 1;
+          if (!warp_wait(&s_full[buf], (g / 2) & 1, abort_flag, a.err)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const int t = j * KEYS + r;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int c = half * 32; c < COLS; c += 64) {
+            const int left = c < 128 ? rows0 - c : rows1 - (c - 128);   // columns from c on in this tile of Q
+            if (left <= 0) continue;
+            uint32_t v[32];
+            tmem_ld32(tmem + lane_off + buf * COLS + c, v);
+            tmem_ld_wait();
+            if (j * KEYS + KEYS - 1 > free_to || left < 32) {
+#pragma unroll
+              for (int x = 0; x < 32; ++x) {
+                const float w = ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x]), scale), neg_m[c + x])) * inv_l[c + x];
+                if (x < left && t <= free_to + token[c + x]) sum[x & 3] += w;
+              }
+            } else {
+#pragma unroll
+              for (int x = 0; x < 32; x += 4) {
+                const float4 nm = *reinterpret_cast<const float4*>(neg_m + c + x), il = *reinterpret_cast<const float4*>(inv_l + c + x);
+                sum[0] = fmaf(ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x]), scale), nm.x)), il.x, sum[0]);
+                sum[1] = fmaf(ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x + 1]), scale), nm.y)), il.y, sum[1]);
+                sum[2] = fmaf(ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x + 2]), scale), nm.z)), il.z, sum[2]);
+                sum[3] = fmaf(ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x + 3]), scale), nm.w)), il.w, sum[3]);
+              }
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_empty[buf]);
+          walk.w.sums[((2 * static_cast<size_t>(p.slice) + half) * work_tiles(a.T_kv_cap, a.B) + walk.w.tiles[p.b] + j) * KEYS + r] =
+              (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(stat_empty);
+      }
+    }
+  } else {
+    // -------------------------------------------------- queries and statistics, warps 10 .. 13
+    const int w = warp - LOAD_WARP, tid = w * 32 + lane;
+    constexpr int CHUNKS = DH / 8, STEP = 32 / CHUNKS;    // 16-byte chunks of a row, rows of a warp's load
+    bool ok = true;
+    for (int i = 0; ok && walk.next(p); ++i) {
+      const int qb = i & 1;
+      const int ntok = p.r.look - p.tok0, rows0 = min(ntok, tpt) * G, rows1 = min(max(ntok - tpt, 0), tpt) * G;
+      // the row of q of a column of the block: x of tile t; -1: none
+      const auto row_of = [&](int t, int x, bool report) {
+        const int tok = p.tok0 + t * tpt + x / G;
+        return x < (t == 0 ? rows0 : rows1) ? query_row(a, p.r, p.b, tok, report) : -1;
+      };
+      if (i >= 2 && !warp_wait(&q_empty[qb], (i / 2 - 1) & 1, abort_flag, a.err)) break;
+      for (int t = 0; t < (rows1 > 0 ? 2 : 1); ++t) {
+        uint8_t* q = smem + qb * L::Q_TILE + t * 128 * 128;
+        const int c = lane % CHUNKS, first = w * 32 + lane / CHUNKS;
+#pragma unroll 8
+        for (int y = 0; y < 32; y += STEP) {
+          const int x = first + y, qr = row_of(t, x, false);
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (qr >= 0) v = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + qr * a.ld_q + static_cast<long>(p.kvh * G + x % G) * DH)[c];
+          *reinterpret_cast<uint4*>(q + (c / 8) * L::Q_PANEL + x * 128 + (((c & 7) ^ (x & 7)) << 4)) = v;
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[qb]);
+      if constexpr (WEIGHTS) {
+        // columns tid and tid + 128: their pieces in order of the keys
+        float2 s[2];
+        const long long unit0 = walk.w.places[p.b] + static_cast<long long>(p.kvh * ((p.r.look + 2 * tpt - 1) / (2 * tpt)) + p.tok0 / (2 * tpt)) * p.tiles;
+        const int c0 = walk.run_at(unit0), c1 = walk.run_at(unit0 + p.tiles - 1);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          s[t] = make_float2(-INFINITY, 0.f);
+          for (int c = c0; c <= c1; ++c) {
+            const float2* st = walk.w.stats + (c + static_cast<size_t>(p.b) * walk.z.slices + p.slice) * COLS;
+            if (tid < (t == 0 ? rows0 : rows1)) s[t] = join(s[t], st[t * 128 + tid]);
+            if (t == 0 && rows1 == 0 && tid < rows0) s[0] = join(s[0], st[128 + tid]);     // the other half of its keys
+          }
+          const bool looks = row_of(t, tid, p.kvh == 0 && p.tile0 == 0) >= 0;
+          s[t] = looks ? finish(s[t]) : make_float2(INFINITY, 0.f);
+        }
+        if (i >= 1 && !warp_wait(stat_empty, (i - 1) & 1, abort_flag, a.err)) break;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          neg_m[t * 128 + tid] = -s[t].x;
+          inv_l[t * 128 + tid] = s[t].y;
+          token[t * 128 + tid] = static_cast<uint8_t>(min(255, t * tpt + tid / G));
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(stat_full);
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+// A key's sums of all units, in order, and what came in.
+constexpr int FINAL_THREADS = 128;
+__global__ void __launch_bounds__(FINAL_THREADS) mass_final_kernel(const MassArgs a) {
+  pdl_enter();
+  const Sizes z = sizes_of(a.n_heads, a.pages.n_kv, a.window);
+  const Work w = work_of(a, z);
+  const size_t tiles = work_tiles(a.T_kv_cap, a.B);
+  const int total = w.tiles[a.B];
+  for (int x = blockIdx.x; x < total; x += gridDim.x) {
+    const int b = request_at(w.tiles, a.B, x);
+    const MassRequest r = read_request(a, b);
+    const int t = (x - w.tiles[b]) * KEYS + threadIdx.x;
+    if (t >= r.kv) continue;
+    const int blocks = (r.look + 2 * z.tpt - 1) / (2 * z.tpt);
+    float sum = 0.f;
+    const float* src = w.sums + static_cast<size_t>(x) * KEYS + threadIdx.x;
+    for (int h = 0; h < a.pages.n_kv; ++h)
+#pragma unroll 4
+      for (int y = 0; y < 2 * blocks; ++y) sum += src[(2 * static_cast<size_t>(h) * z.blocks + y) * tiles * KEYS];
+    store_mass(a, r, b, t, sum);
+  }
+}
+
+template <bool F16, int DH>
+cudaError_t launch_typed(const CUtensorMap& mK, const MassArgs& a, float scale, cudaStream_t st) {
+  static bool set0[64] = {}, set1[64] = {};
+  cudaError_t e = set_smem_limit_once(tc_mass_kernel<F16, DH, false>, Layout<DH>::BYTES, set0);
+  if (e == cudaSuccess) e = set_smem_limit_once(tc_mass_kernel<F16, DH, true>, Layout<DH>::BYTES, set1);
+  if (e == cudaSuccess) e = launch_kernel(tc_mass_kernel<F16, DH, false>, dim3(a.runs), dim3(THREADS), Layout<DH>::BYTES, st, mK, a, scale);
+  if (e == cudaSuccess) e = launch_kernel(tc_mass_kernel<F16, DH, true>, dim3(a.runs), dim3(THREADS), Layout<DH>::BYTES, st, mK, a, scale);
+  return e;
+}
+
+}  // namespace
+
+int tc_mass_box_keys(int page_size) { return page_size < KEYS ? page_size : KEYS; }
+
+size_t tc_mass_workspace(int B, int T_kv_cap, int n_heads, int n_kv, int window, int num_sms) {
+  const Sizes z = sizes_of(n_heads, n_kv, window);
+  return prefix_bytes(B) + 8 * (num_sms + static_cast<size_t>(B) * z.slices) * COLS + 8 * static_cast<size_t>(z.slices) * work_tiles(T_kv_cap, B) * KEYS;
+}
+
+cudaError_t launch_tc_mass(const CUtensorMap& mK, const MassArgs& args, bool f16, int num_sms, cudaStream_t st) {
+  MassArgs a = args;
+  a.runs = num_sms;
+  const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(a.pages.head_dim));
+  cudaError_t e = launch_kernel(mass_line_kernel, dim3(1), dim3(1024), 0, st, a);
+  if (e != cudaSuccess) return e;
+  if (a.pages.head_dim == 64) e = f16 ? launch_typed<true, 64>(mK, a, scale, st) : launch_typed<false, 64>(mK, a, scale, st);
+  else e = f16 ? launch_typed<true, 128>(mK, a, scale, st) : launch_typed<false, 128>(mK, a, scale, st);
+  if (e != cudaSuccess) return e;
+  const size_t tiles = work_tiles(a.T_kv_cap, a.B);
+  return launch_kernel(mass_final_kernel, dim3(static_cast<unsigned>(tiles < 8ul * num_sms ? tiles : 8ul * num_sms)), dim3(FINAL_THREADS), 0, st, a);
+}
+
+}  // namespace seer
