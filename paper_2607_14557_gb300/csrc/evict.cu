@@ -69,11 +69,8 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
   const bool held = r1 - r0 <= kSelKeys;
   const float* mass = a.mass + static_cast<size_t>(b) * a.ld_mass;
   const int* birth = a.birth + static_cast<size_t>(b) * a.ld_mass;
-  const auto read_key = [&](int t) {
-    const int born = birth[t];
-    return born >= young ? kKeyRecent : (born < a.sinks ? kKeySink : mass_key(mass[t]));
-  };
-  const auto key_of = [&](int t) { return held ? sh.keys[t - r0] : read_key(t); };
+  const auto row_key = [&](int born, float m) { return born >= young ? kKeyRecent : (born < a.sinks ? kKeySink : mass_key(m)); };
+  const auto key_of = [&](int t) { return held ? sh.keys[t - r0] : row_key(birth[t], mass[t]); };
 
   // ---- the K-th largest key
   for (int i = tid; i < 2 * kBins; i += kSelThreads) (&sh.hist[0][0])[i] = 0;
@@ -85,16 +82,31 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     constexpr int kShift[3] = {21, 10, 0};
     const int shift = kShift[pass], bins = pass == 2 ? 1024 : kBins;
     unsigned* hist = sh.hist[pass & 1];
-    for (int t = r0 + tid; t < r1; t += kSelThreads) {
-      uint32_t k;
-      if (pass == 0) {
-        k = read_key(t);
-        if (held) sh.keys[t - r0] = k;
+    const int above = kShift[pass == 0 ? 0 : pass - 1];
+    for (int t0 = r0 + tid; t0 < r1; t0 += 8 * kSelThreads) {
+      uint32_t k[8];
+      if (pass == 0) {                      // all loads first
+        int born[8];
+        float m[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int t = min(t0 + e * kSelThreads, r1 - 1);
+          born[e] = birth[t];
+          m[e] = mass[t];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k[e] = row_key(born[e], m[e]);
       } else {
-        k = key_of(t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k[e] = key_of(min(t0 + e * kSelThreads, r1 - 1));
       }
-      const int above = pass == 0 ? 32 : kShift[pass == 0 ? 0 : pass - 1];
-      if (pass == 0 || (k >> above) == (prefix >> above)) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int t = t0 + e * kSelThreads;
+        if (t >= r1) break;
+        if (pass == 0 && held) sh.keys[t - r0] = k[e];
+        if (pass == 0 || (k[e] >> above) == (prefix >> above)) atomicAdd(&hist[(k[e] >> shift) & (bins - 1)], 1u);
+      }
     }
     if (ranks > 1) cluster_sync();
     else __syncthreads();

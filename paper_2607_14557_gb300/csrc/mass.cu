@@ -443,7 +443,6 @@ __global__ void __launch_bounds__(kThreads, 4) mass_sums_kernel(const MassArgs a
   pdl_enter();
   extern __shared__ int first[];
   __shared__ long long warp_sum[kThreads / 32];
-  __shared__ float sums[kThreads];
   __shared__ float4 stat[kFewStats];          // (m, 1 / l, the column's place, keys behind free_to that it sees)
   tile_line(a, first, warp_sum, false);
   const int total = first[a.B], runs = min(a.runs, total);       // of the kernel before
@@ -462,35 +461,41 @@ __global__ void __launch_bounds__(kThreads, 4) mass_sums_kernel(const MassArgs a
     for (int x = tid; x < all; x += kThreads) {
       const int kvh = x / cols, col = x - kvh * cols;
       float2 s = make_float2(-INFINITY, 0.f);
-      for (int c = c0; c <= c1; ++c) s = join(s, w.stats[(c + static_cast<long>(b)) * hk * cc + static_cast<long>(kvh) * cc + col]);
+      const float2* src = w.stats + static_cast<long>(b) * hk * cc + static_cast<long>(kvh) * cc + col;
+      for (int c = c0; c <= c1; c += 8) {       // in order of the keys, eight loads under way
+        float2 piece[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) piece[e] = c + e <= c1 ? src[static_cast<long>(c + e) * hk * cc] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = join(s, piece[e]);
+      }
       const float2 f = query_row(a, r, b, col / g, kvh == 0 && at == first[b]) < 0 ? make_float2(0.f, 0.f) : finish(s);
       stat[x] = make_float4(f.x, f.y, __int_as_float(kvh * cc + col), __int_as_float(col / g));
     }
     __syncthreads();
+    // four tiles at once, a thread a key
     const int stop = min(first[b + 1], end);
-    for (; at < stop; ++at) {
-      const int t = (at - first[b]) * KEYS + tid % KEYS;
+    for (; at < stop; at += kThreads / KEYS) {
+      const int tile = at + tid / KEYS;
+      const int t = (tile - first[b]) * KEYS + tid % KEYS;
+      if (tile >= stop || t >= r.kv) continue;
+      const float* src = w.scores + static_cast<size_t>(tile) * hk * cc * KEYS + tid % KEYS;
+      const int free_to = r.kv - r.look;
       float sum = 0.f;
-      if (t < r.kv) {
-        const float* src = w.scores + static_cast<size_t>(at) * hk * cc * KEYS + tid % KEYS;
-        const int free_to = r.kv - r.look;
-#pragma unroll 8
-        for (int x = tid / KEYS; x < all; x += kThreads / KEYS) {
-          const float4 st = stat[x];
-          const float s = src[__float_as_int(st.z) * KEYS];
-          if (st.y != 0.f && t <= free_to + __float_as_int(st.w)) sum += ex2(s - st.x) * st.y;
+      for (int x0 = 0; x0 < all; x0 += 16) {
+        float s[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = x0 + e < all ? src[__float_as_int(stat[x0 + e].z) * KEYS] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if (x0 + e >= all) break;
+          const float4 st = stat[x0 + e];
+          if (st.y != 0.f && t <= free_to + __float_as_int(st.w)) sum += ex2(s[e] - st.x) * st.y;
         }
       }
-      sums[tid] = sum;
-      __syncthreads();
-      if (tid < KEYS && t < r.kv) {
-        float v = 0.f;
-#pragma unroll
-        for (int e = 0; e < kThreads / KEYS; ++e) v += sums[e * KEYS + tid];
-        store_mass(a, r, b, t, v);
-      }
-      __syncthreads();
+      store_mass(a, r, b, t, sum);
     }
+    at = stop;
   }
 }
 

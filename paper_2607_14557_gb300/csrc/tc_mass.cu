@@ -437,12 +437,18 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
       for (int t = 0; t < (rows1 > 0 ? 2 : 1); ++t) {
         uint8_t* q = smem + qb * L::Q_TILE + t * 128 * 128;
         const int c = lane % CHUNKS, first = w * 32 + lane / CHUNKS;
-#pragma unroll 8
-        for (int y = 0; y < 32; y += STEP) {
-          const int x = first + y, qr = row_of(t, x, false);
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (qr >= 0) v = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + qr * a.ld_q + static_cast<long>(p.kvh * G + x % G) * DH)[c];
-          *reinterpret_cast<uint4*>(q + (c / 8) * L::Q_PANEL + x * 128 + (((c & 7) ^ (x & 7)) << 4)) = v;
+        // all of the warp's loads first: one by one with their stores a piece took 26 us
+        uint4 v[CHUNKS];
+#pragma unroll
+        for (int y = 0; y < CHUNKS; ++y) {
+          const int x = first + y * STEP, qr = row_of(t, x, false);
+          v[y] = make_uint4(0, 0, 0, 0);
+          if (qr >= 0) v[y] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + qr * a.ld_q + static_cast<long>(p.kvh * G + x % G) * DH) + c);
+        }
+#pragma unroll
+        for (int y = 0; y < CHUNKS; ++y) {
+          const int x = first + y * STEP;
+          *reinterpret_cast<uint4*>(q + (c / 8) * L::Q_PANEL + x * 128 + (((c & 7) ^ (x & 7)) << 4)) = v[y];
         }
       }
       fence_proxy_async_smem();
