@@ -53,6 +53,16 @@ __device__ __forceinline__ void ffma2(float a0, float a1, float b0, float b1, fl
       : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
 }
 
+// (s0, s1) += (a0, a1) in one instruction.
+__device__ __forceinline__ void fadd2(float& s0, float& s1, float a0, float a1) {
+  asm("{\n\t.reg .b64 ra, rb;\n\t"
+      "mov.b64 ra, {%0, %1};\n\t"
+      "mov.b64 rb, {%2, %3};\n\t"
+      "add.rn.f32x2 ra, ra, rb;\n\t"
+      "mov.b64 {%0, %1}, ra;\n\t}"
+      : "+f"(s0), "+f"(s1) : "f"(a0), "f"(a1));
+}
+
 // The largest magnitude of the 16-bit values seen, NaN included, two at a time.
 template <bool F16>
 __device__ __forceinline__ uint32_t max_abs2(uint32_t m, uint32_t w) {

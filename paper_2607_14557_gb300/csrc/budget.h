@@ -62,11 +62,13 @@ struct MassArgs {
 size_t mass_workspace(int type, int B, int T_kv_cap, int n_heads, int n_kv, int head_dim, int window, int num_sms);
 cudaError_t launch_mass(int type, const MassArgs& a, int num_sms, cudaStream_t st);
 // The tensor-core path (tc_mass.cu): 16-bit calls of more columns than launch_mass keeps scores for.
-// mK: the pool as [rows][2 * n_kv][head_dim] in boxes of tc_mass_box_keys() x 1 x 64, with the 128-byte swizzle.
+// mQ: q as [T_cap][n_heads][head_dim] in boxes of tc_mass_box_tokens() x n_heads / n_kv x 64 (unused with
+// accepted rows); mK: the pool as [rows][2 * n_kv][head_dim] in boxes of tc_mass_box_keys() x 1 x 64, with the 128-byte swizzle.
 bool mass_on_tensor_cores(int type, int n_heads, int n_kv, int window);
+int tc_mass_box_tokens(int n_heads, int n_kv, int window);
 int tc_mass_box_keys(int page_size);
 size_t tc_mass_workspace(int B, int T_kv_cap, int n_heads, int n_kv, int window, int num_sms);
-cudaError_t launch_tc_mass(const CUtensorMap& mK, const MassArgs& a, bool f16, int num_sms, cudaStream_t st);
+cudaError_t launch_tc_mass(const CUtensorMap& mQ, const CUtensorMap& mK, const MassArgs& a, bool f16, int num_sms, cudaStream_t st);
 
 struct SelectArgs {
   const float* mass;      // [B, ld_mass]

@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 2) mass_scores_kernel(const MassArgs
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int col = nt * 8 + 2 * quad + e;
-              float s0 = d[e] * scale, s1 = d[2 + e] * scale;
+              float s0 = __fmul_rn(d[e], scale), s1 = __fmul_rn(d[2 + e], scale);   // as they are kept
               if (col < cols) {
                 out[col * KEYS] = s0;
                 out[col * KEYS + 8] = s1;

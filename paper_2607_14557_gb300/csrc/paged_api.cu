@@ -561,12 +561,15 @@ seer_status seer_attention_mass(const void* q, int ld_q, seer_dtype dt, const in
   a.err = di->err;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (mass_on_tensor_cores(dt, n_heads, pages->n_kv_heads, window)) {
-    CUtensorMap mk;
+    CUtensorMap mq{}, mk;
+    if (!accepted && T_cap > 0)
+      SEER_TRY(map_heads(&mq, q, dt, T_cap, ld_q, n_heads, pages->head_dim, tc_mass_box_tokens(n_heads, pages->n_kv_heads, window),
+                         n_heads / pages->n_kv_heads));
     SEER_TRY(map_heads(&mk, a.pages.kv, dt, static_cast<long>(a.pages.n_pages) << a.pages.page_shift,
                        2l * a.pages.n_kv * a.pages.head_dim, 2 * a.pages.n_kv, a.pages.head_dim,
                        tc_mass_box_keys(1 << a.pages.page_shift), 1));
     Phase ph(PH_ATTN, st);
-    SEER_CUDA(launch_tc_mass(mk, a, dt == SEER_F16, di->num_sms, st), "attention mass launch");
+    SEER_CUDA(launch_tc_mass(mq, mk, a, dt == SEER_F16, di->num_sms, st), "attention mass launch");
     return SEER_OK;
   }
   Phase ph(PH_ATTN, st);

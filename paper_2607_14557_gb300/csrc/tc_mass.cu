@@ -14,10 +14,12 @@
 // leaves each key's sum per unit, which the last kernel adds up in order.
 //
 // One CTA per SM:
-//   warp 0       producer: key tiles by TMA, a box per page and lane, a ring of three
+//   warp 0       producer: queries of the next piece and key tiles by TMA, of the keys a box per
+//                page and lane, a ring of three
 //   warp 1       MMA issuer, two score tiles of 256 columns ahead in tensor memory
 //   warps 2-9    exponentials: two warps a lane quarter
-//   warps 10-13  queries of the next piece into shared memory, and its joined statistics
+//   warps 10-13  the joined statistics of the next piece, and of accepted drafts its queries, whose
+//                rows lie anywhere
 // Bound by the exponentials: two a (column, key).
 #include "mass_common.cuh"
 
@@ -167,11 +169,24 @@ struct Walk {
     end = run < runs ? total * (run + 1) / runs : 0;
   }
   __device__ __forceinline__ int run_at(long long x) const { return static_cast<int>(((x + 1) * runs - 1) / total); }
+  // The request of place x, by a whole warp: the prefix sums are narrowed 32-fold a step.
+  __device__ __forceinline__ int find(long long x) const {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = a.B;                    // among [lo, lo + n)
+    while (n > 1) {
+      const int step = (n + 31) / 32, k = lane * step;
+      const unsigned below = __ballot_sync(0xffffffffu, k < n && w.places[lo + k] <= x);
+      const int last = 31 - __clz(below);   // (places[lo] <= x)
+      lo += last * step;
+      n = min(step, n - last * step);
+    }
+    return lo;
+  }
   __device__ __forceinline__ bool next(Piece& p) {
     if (at >= end) return false;
     if (fresh || w.places[b + 1] <= at) {
       fresh = false;
-      b = request_at(w.places, a.B, at);
+      b = find(at);
       p.r = read_request(a, b);
     }
     p.b = b;
@@ -190,7 +205,9 @@ struct Walk {
 
 // ------------------------------------------------------------------ both passes
 template <bool F16, int DH, bool WEIGHTS>
-__global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_constant__ CUtensorMap mK, const MassArgs a, const float scale) {
+__global__ void __launch_bounds__(THREADS, 1)
+    tc_mass_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mK, const MassArgs a, const int q_box,
+                   const float scale) {
   using L = Layout<DH>;
   extern __shared__ __align__(1024) uint8_t smem[];
   if ((smem_u32(smem) & 1023u) != 0) {
@@ -221,7 +238,7 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
       mbar_init(&k_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&q_full[i], 4);
+      mbar_init(&q_full[i], a.accepted ? 4 : 1);
       mbar_init(&q_empty[i], 1);
       mbar_init(&s_full[i], 1);
       mbar_init(&s_empty[i], 8);
@@ -231,6 +248,7 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
     *abort_flag = 0;
     fence_barrier_init();
     tma_prefetch_desc(&mK);
+    if (!a.accepted && a.T_cap > 0) tma_prefetch_desc(&mQ);
   }
   if (warp == 1) tmem_alloc(tmem_slot, TMEM_COLS);
   pdl_enter();
@@ -260,8 +278,21 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
     };
     unsigned g = 0;
     bool ok = true;
-    while (ok && walk.next(p)) {
+    int pieces = 0;
+    for (; ok && walk.next(p); ++pieces) {
       int next_row = box_row(p, p.tile0);                 // the page of a tile is looked up a tile ahead
+      if (!a.accepted) {                                  // the block's rows of q: tokens x heads of the group
+        const int qb = pieces & 1, parts = p.r.look - p.tok0 > tpt ? 2 : 1;
+        if (pieces >= 2 && !warp_wait(&q_empty[qb], (pieces / 2 - 1) & 1, abort_flag, a.err)) break;
+        if (leader) {
+          mbar_arrive_expect_tx(&q_full[qb], parts * L::PANELS * q_box * G * 128);
+          for (int y = 0; y < parts; ++y)
+            for (int x = 0; x < L::PANELS; ++x)
+              tma_load_3d(smem + qb * L::Q_TILE + x * L::Q_PANEL + y * 128 * 128, &mQ, &q_full[qb], 64 * x, p.kvh * G,
+                          p.r.q0 + p.r.n - p.r.look + p.tok0 + y * tpt);
+        }
+        __syncwarp();
+      }
       for (int j = p.tile0; j < p.tile1; ++j, ++g) {
         const int row = next_row, s = g % RING;
         if (j + 1 < p.tile1) next_row = box_row(p, j + 1);
@@ -278,8 +309,11 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
         __syncwarp();
       }
     }
-    if (*abort_flag && leader)                            // copies still in flight land before the memory is released
+    if (*abort_flag && leader) {                          // copies still in flight land before the memory is released
+      if (!a.accepted)
+        for (int j = pieces > 2 ? pieces - 2 : 0; j <= pieces; ++j) mbar_wait_drain(&q_full[j & 1], (j / 2) & 1, kDrainNs);
       for (unsigned j = g > RING ? g - RING : 0; j < g; ++j) mbar_wait_drain(&k_full[j % RING], (j / RING) & 1, kDrainNs);
+    }
   } else if (warp == 1) {
     // -------------------------------------------------- MMA issuer
     const bool leader = elect_one();
@@ -364,7 +398,11 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
               m = top;
               float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int x = 0; x < 64; ++x) sum[x & 3] += ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x / 32][x % 32]), scale), -base));
+              for (int x = 0; x < 64; x += 2) {
+                float e0, e1;
+                ffma2(__uint_as_float(v[x / 32][x % 32]), __uint_as_float(v[x / 32][x % 32 + 1]), scale, scale, -base, -base, e0, e1);
+                fadd2(sum[x & 2], sum[(x & 2) + 1], ex2(e0), ex2(e1));
+              }
               l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             }
           }
@@ -396,17 +434,18 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
             if (j * KEYS + KEYS - 1 > free_to || left < 32) {
 #pragma unroll
               for (int x = 0; x < 32; ++x) {
-                const float w = ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x]), scale), neg_m[c + x])) * inv_l[c + x];
+                const float w = ex2(fmaf(__uint_as_float(v[x]), scale, neg_m[c + x])) * inv_l[c + x];
                 if (x < left && t <= free_to + token[c + x]) sum[x & 3] += w;
               }
             } else {
 #pragma unroll
               for (int x = 0; x < 32; x += 4) {
                 const float4 nm = *reinterpret_cast<const float4*>(neg_m + c + x), il = *reinterpret_cast<const float4*>(inv_l + c + x);
-                sum[0] = fmaf(ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x]), scale), nm.x)), il.x, sum[0]);
-                sum[1] = fmaf(ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x + 1]), scale), nm.y)), il.y, sum[1]);
-                sum[2] = fmaf(ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x + 2]), scale), nm.z)), il.z, sum[2]);
-                sum[3] = fmaf(ex2(__fadd_rn(__fmul_rn(__uint_as_float(v[x + 3]), scale), nm.w)), il.w, sum[3]);
+                float e[4];
+                ffma2(__uint_as_float(v[x]), __uint_as_float(v[x + 1]), scale, scale, nm.x, nm.y, e[0], e[1]);
+                ffma2(__uint_as_float(v[x + 2]), __uint_as_float(v[x + 3]), scale, scale, nm.z, nm.w, e[2], e[3]);
+                ffma2(ex2(e[0]), ex2(e[1]), il.x, il.y, sum[0], sum[1], sum[0], sum[1]);
+                ffma2(ex2(e[2]), ex2(e[3]), il.z, il.w, sum[2], sum[3], sum[2], sum[3]);
               }
             }
           }
@@ -433,8 +472,8 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
         const int tok = p.tok0 + t * tpt + x / G;
         return x < (t == 0 ? rows0 : rows1) ? query_row(a, p.r, p.b, tok, report) : -1;
       };
-      if (i >= 2 && !warp_wait(&q_empty[qb], (i / 2 - 1) & 1, abort_flag, a.err)) break;
-      for (int t = 0; t < (rows1 > 0 ? 2 : 1); ++t) {
+      if (a.accepted && i >= 2 && !warp_wait(&q_empty[qb], (i / 2 - 1) & 1, abort_flag, a.err)) break;
+      for (int t = 0; a.accepted && t < (rows1 > 0 ? 2 : 1); ++t) {
         uint8_t* q = smem + qb * L::Q_TILE + t * 128 * 128;
         const int c = lane % CHUNKS, first = w * 32 + lane / CHUNKS;
         // all of the warp's loads first: one by one with their stores a piece took 26 us
@@ -451,9 +490,11 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
           *reinterpret_cast<uint4*>(q + (c / 8) * L::Q_PANEL + x * 128 + (((c & 7) ^ (x & 7)) << 4)) = v[y];
         }
       }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&q_full[qb]);
+      if (a.accepted) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full[qb]);
+      }
       if constexpr (WEIGHTS) {
         // columns tid and tid + 128: their pieces in order of the keys
         float2 s[2];
@@ -491,41 +532,62 @@ __global__ void __launch_bounds__(THREADS, 1) tc_mass_kernel(const __grid_consta
   }
 }
 
-// A key's sums of all units, in order, and what came in.
+// A key's sums of all units, in order, and what came in.  A tile a block; latency: the sums of the
+// first 16 are loaded before it is known whose they are (any tile's memory is there).
 constexpr int FINAL_THREADS = 128;
 __global__ void __launch_bounds__(FINAL_THREADS) mass_final_kernel(const MassArgs a) {
   pdl_enter();
   const Sizes z = sizes_of(a.n_heads, a.pages.n_kv, a.window);
   const Work w = work_of(a, z);
-  const size_t tiles = work_tiles(a.T_kv_cap, a.B);
-  const int total = w.tiles[a.B];
-  for (int x = blockIdx.x; x < total; x += gridDim.x) {
-    const int b = request_at(w.tiles, a.B, x);
-    const MassRequest r = read_request(a, b);
-    const int t = (x - w.tiles[b]) * KEYS + threadIdx.x;
-    if (t >= r.kv) continue;
-    const int blocks = (r.look + 2 * z.tpt - 1) / (2 * z.tpt);
-    float sum = 0.f;
-    const float* src = w.sums + static_cast<size_t>(x) * KEYS + threadIdx.x;
-    for (int h = 0; h < a.pages.n_kv; ++h)
-#pragma unroll 4
-      for (int y = 0; y < 2 * blocks; ++y) sum += src[(2 * static_cast<size_t>(h) * z.blocks + y) * tiles * KEYS];
-    store_mass(a, r, b, t, sum);
+  const size_t step = work_tiles(a.T_kv_cap, a.B) * KEYS;
+  const int x = blockIdx.x, lane = threadIdx.x & 31;
+  const float* src = w.sums + static_cast<size_t>(x) * KEYS + threadIdx.x;
+  float s[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[e] = e < 2 * z.slices ? src[e * step] : 0.f;
+  if (x >= w.tiles[a.B]) return;
+  int b = 0, left = a.B;                    // the request of tile x, the prefix sums narrowed 32-fold a step
+  while (left > 1) {
+    const int hop = (left + 31) / 32, k = lane * hop;
+    const unsigned below = __ballot_sync(0xffffffffu, k < left && w.tiles[b + k] <= x);
+    const int last = 31 - __clz(below);
+    b += last * hop;
+    left = min(hop, left - last * hop);
   }
+  const MassRequest r = read_request(a, b);
+  const int t = (x - w.tiles[b]) * KEYS + threadIdx.x;
+  if (t >= r.kv) return;
+  const int blocks = (r.look + 2 * z.tpt - 1) / (2 * z.tpt);      // column blocks that the request has
+  float sum = 0.f;
+  for (int i0 = 0; i0 < 2 * z.slices; i0 += 16) {
+    if (i0 > 0) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = i0 + e < 2 * z.slices ? src[(i0 + e) * step] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (i0 + e < 2 * z.slices && (i0 + e) / 2 % z.blocks < blocks) sum += s[e];
+  }
+  store_mass(a, r, b, t, sum);
 }
 
 template <bool F16, int DH>
-cudaError_t launch_typed(const CUtensorMap& mK, const MassArgs& a, float scale, cudaStream_t st) {
+cudaError_t launch_typed(const CUtensorMap& mQ, const CUtensorMap& mK, const MassArgs& a, float scale, cudaStream_t st) {
   static bool set0[64] = {}, set1[64] = {};
+  const int box = tc_mass_box_tokens(a.n_heads, a.pages.n_kv, a.window);
   cudaError_t e = set_smem_limit_once(tc_mass_kernel<F16, DH, false>, Layout<DH>::BYTES, set0);
   if (e == cudaSuccess) e = set_smem_limit_once(tc_mass_kernel<F16, DH, true>, Layout<DH>::BYTES, set1);
-  if (e == cudaSuccess) e = launch_kernel(tc_mass_kernel<F16, DH, false>, dim3(a.runs), dim3(THREADS), Layout<DH>::BYTES, st, mK, a, scale);
-  if (e == cudaSuccess) e = launch_kernel(tc_mass_kernel<F16, DH, true>, dim3(a.runs), dim3(THREADS), Layout<DH>::BYTES, st, mK, a, scale);
+  if (e == cudaSuccess) e = launch_kernel(tc_mass_kernel<F16, DH, false>, dim3(a.runs), dim3(THREADS), Layout<DH>::BYTES, st, mQ, mK, a, box, scale);
+  if (e == cudaSuccess) e = launch_kernel(tc_mass_kernel<F16, DH, true>, dim3(a.runs), dim3(THREADS), Layout<DH>::BYTES, st, mQ, mK, a, box, scale);
   return e;
 }
 
 }  // namespace
 
+int tc_mass_box_tokens(int n_heads, int n_kv, int window) {
+  const int tpt = 128 / (n_heads / n_kv);
+  return tpt < window ? tpt : window;
+}
 int tc_mass_box_keys(int page_size) { return page_size < KEYS ? page_size : KEYS; }
 
 size_t tc_mass_workspace(int B, int T_kv_cap, int n_heads, int n_kv, int window, int num_sms) {
@@ -533,17 +595,16 @@ size_t tc_mass_workspace(int B, int T_kv_cap, int n_heads, int n_kv, int window,
   return prefix_bytes(B) + 8 * (num_sms + static_cast<size_t>(B) * z.slices) * COLS + 8 * static_cast<size_t>(z.slices) * work_tiles(T_kv_cap, B) * KEYS;
 }
 
-cudaError_t launch_tc_mass(const CUtensorMap& mK, const MassArgs& args, bool f16, int num_sms, cudaStream_t st) {
+cudaError_t launch_tc_mass(const CUtensorMap& mQ, const CUtensorMap& mK, const MassArgs& args, bool f16, int num_sms, cudaStream_t st) {
   MassArgs a = args;
   a.runs = num_sms;
   const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(a.pages.head_dim));
   cudaError_t e = launch_kernel(mass_line_kernel, dim3(1), dim3(1024), 0, st, a);
   if (e != cudaSuccess) return e;
-  if (a.pages.head_dim == 64) e = f16 ? launch_typed<true, 64>(mK, a, scale, st) : launch_typed<false, 64>(mK, a, scale, st);
-  else e = f16 ? launch_typed<true, 128>(mK, a, scale, st) : launch_typed<false, 128>(mK, a, scale, st);
+  if (a.pages.head_dim == 64) e = f16 ? launch_typed<true, 64>(mQ, mK, a, scale, st) : launch_typed<false, 64>(mQ, mK, a, scale, st);
+  else e = f16 ? launch_typed<true, 128>(mQ, mK, a, scale, st) : launch_typed<false, 128>(mQ, mK, a, scale, st);
   if (e != cudaSuccess) return e;
-  const size_t tiles = work_tiles(a.T_kv_cap, a.B);
-  return launch_kernel(mass_final_kernel, dim3(static_cast<unsigned>(tiles < 8ul * num_sms ? tiles : 8ul * num_sms)), dim3(FINAL_THREADS), 0, st, a);
+  return launch_kernel(mass_final_kernel, dim3(static_cast<unsigned>(work_tiles(a.T_kv_cap, a.B))), dim3(FINAL_THREADS), 0, st, a);
 }
 
 }  // namespace seer
