@@ -19,20 +19,42 @@ constexpr int kSelThreads = 512;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelKeys = 16384;             // keys of a CTA in shared memory
 constexpr int kBins = 2048;
+constexpr int kAhead = 4;                   // rows of a thread whose loads are under way
 constexpr uint32_t kKeyRecent = 0xffffffffu, kKeySink = 0xfffffffeu, kKeyNan = 0xfffffffdu;
 
 struct SelShared {
   unsigned hist[2][kBins];                  // of this CTA, by turns
-  unsigned counts[kSelWarps][4];            // per warp: rows above / at the key before K, and behind
+  uint4 counts[kSelWarps];                  // per warp: rows above, at the key before K, above, at it behind
   unsigned warp_sum[kSelWarps];
   unsigned found_bin, found_above;
   uint32_t keys[kSelKeys];
 };
 
-__device__ __forceinline__ unsigned ld_cluster(uint32_t addr) {
-  unsigned v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ uint4 ld_cluster4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
+}
+// The four words at p, summed over the cluster's CTAs.
+template <int RANKS>
+__device__ __forceinline__ uint4 sum_over_ranks(const unsigned* p) {
+  if constexpr (RANKS == 1) return *reinterpret_cast<const uint4*>(p);
+  uint4 v[RANKS], s = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int r = 0; r < RANKS; ++r) v[r] = ld_cluster4(cluster_addr(p, r));
+#pragma unroll
+  for (int r = 0; r < RANKS; ++r) {
+    s.x += v[r].x;
+    s.y += v[r].y;
+    s.z += v[r].z;
+    s.w += v[r].w;
+  }
+  return s;
+}
+template <int RANKS>
+__device__ __forceinline__ void sync_ranks() {
+  if constexpr (RANKS > 1) cluster_sync();
+  else __syncthreads();
 }
 
 __device__ __forceinline__ uint32_t mass_key(float m) {
@@ -41,7 +63,9 @@ __device__ __forceinline__ uint32_t mass_key(float m) {
   return u ^ ((u >> 31) != 0 ? 0xffffffffu : 0x80000000u);
 }
 
-__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectArgs a, const int ranks) {
+template <int RANKS>
+__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectArgs a) {
+  constexpr int ranks = RANKS;
   extern __shared__ __align__(16) uint8_t smem[];
   SelShared& sh = *reinterpret_cast<SelShared*>(smem);
   pdl_enter();
@@ -52,7 +76,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
   const int L = good ? L0 : 0, K = good ? min(budget, L) : 0;
   if (good && min(K, L - K) > a.ld_move) good = false;
   if (!good || K == L || K == 0) {          // nothing to choose; every rank has read the lengths before one writes
-    if (ranks > 1) cluster_sync();
+    sync_ranks<RANKS>();
     if (rank == 0 && tid == 0) {
       if (!good) record_error(a.err, L0 >= 0 && L0 <= a.ld_mass && budget >= 0 ? kErrCapacity : kErrLayout);
       a.len_out[b] = good ? K : L0;
@@ -77,53 +101,45 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
   __syncthreads();
   uint32_t prefix = 0;
   unsigned need = K;                        // rows with the prefix that stay
-#pragma unroll
+#pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
-    constexpr int kShift[3] = {21, 10, 0};
-    const int shift = kShift[pass], bins = pass == 2 ? 1024 : kBins;
+    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? kBins / 2 : kBins;
     unsigned* hist = sh.hist[pass & 1];
-    const int above = kShift[pass == 0 ? 0 : pass - 1];
-    for (int t0 = r0 + tid; t0 < r1; t0 += 8 * kSelThreads) {
-      uint32_t k[8];
-      if (pass == 0) {                      // all loads first
-        int born[8];
-        float m[8];
+    if (pass == 0) {
+#pragma unroll 1
+      for (int t0 = r0 + tid; t0 < r1; t0 += kAhead * kSelThreads) {
+        int born[kAhead];
+        float m[kAhead];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < kAhead; ++e) {  // all loads first
           const int t = min(t0 + e * kSelThreads, r1 - 1);
           born[e] = birth[t];
           m[e] = mass[t];
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) k[e] = row_key(born[e], m[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) k[e] = key_of(min(t0 + e * kSelThreads, r1 - 1));
+        for (int e = 0; e < kAhead; ++e) {
+          const int t = t0 + e * kSelThreads;
+          const uint32_t k = row_key(born[e], m[e]);
+          if (t < r1) {
+            if (held) sh.keys[t - r0] = k;
+            atomicAdd(&hist[k >> 21], 1u);
+          }
+        }
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int t = t0 + e * kSelThreads;
-        if (t >= r1) break;
-        if (pass == 0 && held) sh.keys[t - r0] = k[e];
-        if (pass == 0 || (k[e] >> above) == (prefix >> above)) atomicAdd(&hist[(k[e] >> shift) & (bins - 1)], 1u);
+    } else {
+      const int above = pass == 1 ? 21 : 10;
+#pragma unroll 1
+      for (int t = r0 + tid; t < r1; t += kSelThreads) {
+        const uint32_t k = key_of(t);
+        if ((k >> above) == (prefix >> above)) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
       }
     }
-    if (ranks > 1) cluster_sync();
-    else __syncthreads();
-    // thread i owns bins [4 i, 4 i + 4) counted from the top
-    unsigned mine[4], sum = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int bin = bins - 1 - (4 * tid + e);
-      unsigned v = 0;
-      if (bin >= 0) {
-        if (ranks == 1) v = hist[bin];
-        else
-          for (int r = 0; r < ranks; ++r) v += ld_cluster(cluster_addr(&hist[bin], r));
-      }
-      mine[e] = v;
-      sum += v;
-    }
+    sync_ranks<RANKS>();
+    // thread i owns the bins [4 i, 4 i + 4) counted from the top
+    uint4 own = make_uint4(0, 0, 0, 0);
+    const int low = bins - 4 - 4 * tid;
+    if (low >= 0) own = sum_over_ranks<RANKS>(hist + low);
+    const unsigned sum = own.x + own.y + own.z + own.w;
     unsigned inc = sum;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -133,14 +149,27 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     if (lane == 31) sh.warp_sum[warp] = inc;
     __syncthreads();
     unsigned before = inc - sum;
+#pragma unroll 1
     for (int w = 0; w < warp; ++w) before += sh.warp_sum[w];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (before < need && need <= before + mine[e]) {   // one thread's bin
-        sh.found_bin = bins - 1 - (4 * tid + e);
-        sh.found_above = before;
+    if (before < need && need <= before + sum) {           // one thread's bins
+      int bin = 3;
+      unsigned count = own.w;
+      if (need > before + count) {
+        before += count;
+        count = own.z;
+        bin = 2;
       }
-      before += mine[e];
+      if (bin == 2 && need > before + count) {
+        before += count;
+        count = own.y;
+        bin = 1;
+      }
+      if (bin == 1 && need > before + count) {
+        before += count;
+        bin = 0;
+      }
+      sh.found_bin = low + bin;
+      sh.found_above = before;
     }
     if (pass == 1)                          // pass 2 uses the first histogram again; every rank has read it (the sync above)
       for (int i = tid; i < kBins; i += kSelThreads) sh.hist[0][i] = 0;
@@ -153,42 +182,39 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
   // ---- counts per warp: rows above the key and at it, before row K and behind
   const int wshare = (share / 32 + kSelWarps - 1) / kSelWarps * 32;
   const int w0 = min(r1, r0 + warp * wshare), w1 = min(r1, w0 + wshare);
-  unsigned n[4] = {0, 0, 0, 0};
+  uint4 n = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
   for (int t = w0 + lane; t - lane < w1; t += 32) {
     const uint32_t k = t < w1 ? key_of(t) : 0;
     const bool over = t < w1 && k > prefix, at = t < w1 && k == prefix;
     const unsigned first = __ballot_sync(0xffffffffu, t < K);
     const unsigned m = __ballot_sync(0xffffffffu, over), e = __ballot_sync(0xffffffffu, at);
-    n[0] += __popc(m & first);
-    n[1] += __popc(e & first);
-    n[2] += __popc(m & ~first);
-    n[3] += __popc(e & ~first);
+    n.x += __popc(m & first);
+    n.y += __popc(e & first);
+    n.z += __popc(m & ~first);
+    n.w += __popc(e & ~first);
   }
-  if (lane < 4) sh.counts[warp][lane] = n[lane & 3];
-  if (ranks > 1) cluster_sync();
-  else __syncthreads();
+  if (lane == 0) sh.counts[warp] = n;
+  sync_ranks<RANKS>();
   // rows above / at the key in warps before this one, and in all of them before row K
   unsigned above = 0, equal = 0, above_k = 0, equal_k = 0;
-  for (int i = lane; i < ranks * kSelWarps; i += 32) {
-    const int r = i / kSelWarps, w = i % kSelWarps;
-    unsigned c[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c[e] = ranks == 1 ? sh.counts[w][e] : ld_cluster(cluster_addr(&sh.counts[w][e], r));
-    above_k += c[0];
-    equal_k += c[1];
+  for (int x = 0; x < (RANKS * kSelWarps + 31) / 32; ++x) {
+    const int i = x * 32 + lane, r = i / kSelWarps, w = i % kSelWarps;
+    uint4 c = make_uint4(0, 0, 0, 0);
+    if (i < RANKS * kSelWarps) c = RANKS == 1 ? sh.counts[w] : ld_cluster4(cluster_addr(&sh.counts[w], r));
+    above_k += c.x;
+    equal_k += c.y;
     if (i < rank * kSelWarps + warp) {
-      above += c[0] + c[2];
-      equal += c[1] + c[3];
+      above += c.x + c.z;
+      equal += c.y + c.w;
     }
   }
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    above += __shfl_xor_sync(0xffffffffu, above, off);
-    equal += __shfl_xor_sync(0xffffffffu, equal, off);
-    above_k += __shfl_xor_sync(0xffffffffu, above_k, off);
-    equal_k += __shfl_xor_sync(0xffffffffu, equal_k, off);
-  }
-  if (ranks > 1) cluster_sync();            // nobody reads another CTA's memory from here on
+  above = __reduce_add_sync(0xffffffffu, above);
+  equal = __reduce_add_sync(0xffffffffu, equal);
+  above_k = __reduce_add_sync(0xffffffffu, above_k);
+  equal_k = __reduce_add_sync(0xffffffffu, equal_k);
+  if (RANKS > 1) cluster_sync();            // nobody reads another CTA's memory from here on
   const unsigned kept_k = above_k + min(need, equal_k);    // rows before K that stay
   if (rank == 0 && tid == 0) {
     a.len_out[b] = K;
@@ -199,6 +225,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
   // ---- the moves: place i of the holes before K, row i of the kept behind
   int* from = a.move_from + static_cast<size_t>(b) * a.ld_move;
   int* to = a.move_to + static_cast<size_t>(b) * a.ld_move;
+#pragma unroll 1
   for (int t = w0 + lane; t - lane < w1; t += 32) {
     const uint32_t k = t < w1 ? key_of(t) : 0;
     const bool over = t < w1 && k > prefix, at = t < w1 && k == prefix;
@@ -302,18 +329,22 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const EvictArgs
   }
 }
 
+template <int RANKS>
+cudaError_t launch_ranks(const SelectArgs& a, cudaStream_t st) {
+  static bool attr_set[64] = {};
+  const int smem = static_cast<int>(sizeof(SelShared));
+  const cudaError_t e = set_smem_limit_once(evict_select_kernel<RANKS>, smem, attr_set);
+  if (e != cudaSuccess) return e;
+  return launch_kernel_overlap(launch_overlap_enabled(), RANKS, evict_select_kernel<RANKS>, dim3(a.B * RANKS), dim3(kSelThreads), smem, st, a);
+}
+
 }  // namespace
 
 cudaError_t launch_evict_select(const SelectArgs& a, int num_sms, cudaStream_t st) {
   // CTAs of a request: as many as its longest row count gives work, and the GPU has room for
   int ranks = 1;
   while (ranks < 8 && a.ld_mass > 4096l * ranks && a.B * ranks < 2 * num_sms) ranks *= 2;
-  static bool attr_set[64] = {};
-  const int smem = static_cast<int>(sizeof(SelShared));
-  const cudaError_t e = set_smem_limit_once(evict_select_kernel, smem, attr_set);
-  if (e != cudaSuccess) return e;
-  return launch_kernel_overlap(launch_overlap_enabled(), ranks, evict_select_kernel, dim3(a.B * ranks), dim3(kSelThreads), smem,
-                               st, a, ranks);
+  return ranks == 1 ? launch_ranks<1>(a, st) : (ranks == 2 ? launch_ranks<2>(a, st) : (ranks == 4 ? launch_ranks<4>(a, st) : launch_ranks<8>(a, st)));
 }
 
 cudaError_t launch_kv_evict(const EvictArgs& a, int num_sms, cudaStream_t st) {

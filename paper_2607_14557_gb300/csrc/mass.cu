@@ -22,30 +22,32 @@ __device__ __forceinline__ void tile_line(const MassArgs& a, int* first, long lo
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const long long cap = tile_capacity(a);
   long long sum = 0;
+#pragma unroll 1
   for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
     const int b = b0 + tid;
-    MassRequest r{};
+    int v = 0;                                  // at most 2^25, so a warp's sum has 32 bits
     if (b < a.B) {
-      r = read_request(a, b);
+      const MassRequest r = read_request(a, b);
       if (!r.good && report) record_error(a.err, kErrLayout);
+      v = tiles_of(r);
     }
-    const long long v = tiles_of(r);
-    long long inc = v;
+    int inc = v;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-      const long long x = __shfl_up_sync(0xffffffffu, inc, off);
+      const int x = __shfl_up_sync(0xffffffffu, inc, off);
       if (lane >= off) inc += x;
     }
     if (lane == 31) warp_sum[warp] = inc;
     __syncthreads();
-    long long before = sum;
+    long long before = sum + inc;
+#pragma unroll 1
     for (int w = 0; w < warps; ++w) {
       if (w < warp) before += warp_sum[w];
       sum += warp_sum[w];
     }
     if (b < a.B) {
-      if (before + inc > cap && v > 0 && report) record_error(a.err, kErrCapacity);
-      first[b + 1] = static_cast<int>(before + inc > cap ? -1 : before + inc);
+      if (before > cap && v > 0 && report) record_error(a.err, kErrCapacity);
+      first[b + 1] = static_cast<int>(before > cap ? -1 : before);
     }
     __syncthreads();
   }
@@ -54,16 +56,19 @@ __device__ __forceinline__ void tile_line(const MassArgs& a, int* first, long lo
   // -1 marks the capacity's end: later requests start and end where the last good one did
   if (first[a.B] < 0) {
     int lo = 0, hi = a.B;                       // first[lo] >= 0, first[hi] < 0
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (first[mid] >= 0) lo = mid; else hi = mid;
     }
     const int end = first[lo];
     __syncthreads();
+#pragma unroll 1
     for (int b = lo + 1 + tid; b <= a.B; b += blockDim.x) first[b] = end;
     __syncthreads();
   }
 }
+
 // Workspace of the general path: per piece of a request's tiles and column (m, l), then per
 // request and column (m, 1 / l).
 __host__ __device__ inline long columns(const MassArgs& a) { return static_cast<long>(a.n_heads) * a.window; }
@@ -133,19 +138,16 @@ __global__ void __launch_bounds__(kThreads) mass_stats_kernel(const MassArgs a, 
   __shared__ float2 halves[kThreads / 32][4];
   tile_line(a, first, warp_sum, blockIdx.x == 0);
   const int hk = a.pages.n_kv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = a.n_heads / hk;
-  const long long total = static_cast<long long>(first[a.B]) * hk;
-  const int runs = static_cast<int>(min(static_cast<long long>(a.runs), total)), run = blockIdx.x;
-  if (run >= runs) return;
-  long long at = total * run / runs;
-  const long long end = total * (run + 1) / runs;
+  const int total = first[a.B] * hk, length = run_length(total, a.runs), run = blockIdx.x;
+  int at = min(run * length, total);
+  const int end = min(at + length, total);
   while (at < end) {
     // unit (b, kvh): tiles first[b] * hk + kvh * tiles ..
-    const int b = request_at(first, a.B, static_cast<int>(at / hk));
+    const int b = request_at(first, a.B, at / hk);
     const MassRequest r = read_request(a, b);
     const int tiles = tiles_of(r);
-    const long long inside = at - static_cast<long long>(first[b]) * hk;
-    const int kvh = static_cast<int>(inside / tiles), tile0 = static_cast<int>(inside - static_cast<long long>(kvh) * tiles);
-    const int tile1 = static_cast<int>(min(static_cast<long long>(tiles), tile0 + (end - at)));
+    const int inside = at - first[b] * hk, kvh = inside / tiles, tile0 = inside - kvh * tiles;
+    const int tile1 = min(tiles, tile0 + (end - at));
     at += tile1 - tile0;
     float2* out = piece_stats(a) + (run + static_cast<long>(b) * hk + kvh) * (static_cast<long>(g) * a.window);
     for (int col0 = 0; col0 < r.look * g; col0 += COLS) {
@@ -190,15 +192,13 @@ __global__ void __launch_bounds__(kThreads) mass_join_kernel(const MassArgs a) {
   __shared__ long long warp_sum[kThreads / 32];
   tile_line(a, first, warp_sum, false);
   const int hk = a.pages.n_kv, g = a.n_heads / hk;
-  const long long total = static_cast<long long>(first[a.B]) * hk;
-  const int runs = static_cast<int>(min(static_cast<long long>(a.runs), total));
+  const int total = first[a.B] * hk, length = run_length(total, a.runs);
   for (long long unit = blockIdx.x; unit < static_cast<long long>(a.B) * hk; unit += gridDim.x) {
     const int b = static_cast<int>(unit / hk), kvh = static_cast<int>(unit % hk);
     const int tiles = first[b + 1] - first[b];
     if (tiles == 0) continue;
     const MassRequest r = read_request(a, b);
-    const long long at = static_cast<long long>(first[b]) * hk + static_cast<long long>(kvh) * tiles;
-    const int c0 = run_of(total, at, runs), c1 = run_of(total, at + tiles - 1, runs);
+    const int at = first[b] * hk + kvh * tiles, c0 = at / length, c1 = (at + tiles - 1) / length;
     for (int col = threadIdx.x; col < r.look * g; col += kThreads) {
       float2 s = make_float2(-INFINITY, 0.f);
       for (int c = c0; c <= c1; ++c) s = join(s, piece_stats(a)[(c + unit) * (static_cast<long>(g) * a.window) + col]);
@@ -270,15 +270,18 @@ constexpr int kFewCols = 16;                // columns of a key/value head at mo
 constexpr int kFewStats = 1024;             // of all heads
 constexpr int GROUP = 16;                   // keys of a step
 
-// Workspace: per piece and column (m, l), then the scores as [tile][column][64].
+// Workspace: the prefix sums of the tiles, per piece and column (m, l), the scores as
+// [tile][column][64].
 struct FewWork {
+  int* first;             // [B + 1]
   float2* stats;
   float* scores;
 };
+__host__ __device__ inline size_t few_first(int B) { return (4 * (static_cast<size_t>(B) + 1) + 15) / 16 * 16; }
 __host__ __device__ inline size_t few_stats(int B, int runs, long cols) { return ((runs + static_cast<size_t>(B)) * cols + 1) / 2 * 2; }
 __device__ __forceinline__ FewWork few_work(const MassArgs& a) {
-  float2* st = static_cast<float2*>(a.ws);
-  return FewWork{st, reinterpret_cast<float*>(st + few_stats(a.B, a.runs, columns(a)))};
+  float2* st = reinterpret_cast<float2*>(static_cast<uint8_t*>(a.ws) + few_first(a.B));
+  return FewWork{static_cast<int*>(a.ws), st, reinterpret_cast<float*>(st + few_stats(a.B, a.runs, columns(a)))};
 }
 
 template <bool F16>
@@ -306,8 +309,10 @@ __global__ void __launch_bounds__(kThreads, 2) mass_scores_kernel(const MassArgs
   __shared__ long long warp_sum[kThreads / 32];
   __shared__ float2 shares[kThreads / 32][NT * 8];
   tile_line(a, first, warp_sum, blockIdx.x == 0);
-  const int total = first[a.B], runs = min(a.runs, total), run = blockIdx.x;
-  if (run >= runs) return;
+  const int total = first[a.B], length = run_length(total, a.runs), run = blockIdx.x;
+  if (run == 0)
+    for (int b = threadIdx.x; b <= a.B; b += kThreads) few_work(a).first[b] = first[b];
+  if (run * length >= total) return;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, row = lane >> 2;
   const int hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window;
   const FewWork w = few_work(a);
@@ -317,8 +322,8 @@ __global__ void __launch_bounds__(kThreads, 2) mass_scores_kernel(const MassArgs
   const bool busy = sub < per_head;
   const long row_elems = 2l * hk * DH;
   const int page_mask = (1 << a.pages.page_shift) - 1;
-  int at = cut(total, run, runs);
-  const int end = cut(total, run + 1, runs);
+  int at = run * length;
+  const int end = min(at + length, total);
   for (int b = request_at(first, a.B, at); at < end; ++b) {
     if (first[b + 1] <= at) continue;
     const MassRequest r = read_request(a, b);
@@ -439,64 +444,66 @@ __global__ void __launch_bounds__(kThreads, 2) mass_scores_kernel(const MassArgs
   }
 }
 
-__global__ void __launch_bounds__(kThreads, 4) mass_sums_kernel(const MassArgs a) {
+// A tile a block, four threads a key with every fourth eight columns.  Bound by latency, so a
+// thread's first scores are loaded before it is known whose the tile is (any tile's memory is
+// there), and the code is kept short: its first instructions come from memory too.
+constexpr int kEarly = 8;
+__global__ void __launch_bounds__(kThreads) mass_sums_kernel(const MassArgs a) {
   pdl_enter();
-  extern __shared__ int first[];
-  __shared__ long long warp_sum[kThreads / 32];
-  __shared__ float4 stat[kFewStats];          // (m, 1 / l, the column's place, keys behind free_to that it sees)
-  tile_line(a, first, warp_sum, false);
-  const int total = first[a.B], runs = min(a.runs, total);       // of the kernel before
-  const int blocks = min(static_cast<int>(gridDim.x), total);
-  if (static_cast<int>(blockIdx.x) >= blocks) return;
-  const int tid = threadIdx.x, hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window;
+  __shared__ float2 stat[kFewStats + kEarly];   // (m, 1 / l) of every column
+  __shared__ uint8_t row_of[kFewStats + kEarly];   // its row among those that look
+  __shared__ float sums[kThreads];
+  const int tid = threadIdx.x, part = tid / KEYS, key = tid % KEYS, tile = blockIdx.x;
+  const int hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window, all = hk * cc;
   const FewWork w = few_work(a);
-  int at = cut(total, blockIdx.x, blocks);
-  const int end = cut(total, blockIdx.x + 1, blocks);
-  for (int b = request_at(first, a.B, at); at < end; ++b) {
-    if (first[b + 1] <= at) continue;
-    const MassRequest r = read_request(a, b);
-    const int cols = r.look * g, all = hk * cols;
-    const int c0 = run_of(total, first[b], runs), c1 = run_of(total, first[b + 1] - 1, runs);
-    __syncthreads();
-    for (int x = tid; x < all; x += kThreads) {
-      const int kvh = x / cols, col = x - kvh * cols;
-      float2 s = make_float2(-INFINITY, 0.f);
-      const float2* src = w.stats + static_cast<long>(b) * hk * cc + static_cast<long>(kvh) * cc + col;
+  const float* src = w.scores + (static_cast<size_t>(tile) * all + part * kEarly) * KEYS + key;
+  float s[kEarly];
+#pragma unroll
+  for (int e = 0; e < kEarly; ++e) s[e] = part * kEarly + e < all ? src[e * KEYS] : 0.f;
+  const int total = w.first[a.B];
+  if (tile >= total) return;
+  const int b = request_at(w.first, a.B, tile);
+  const int t0 = w.first[b], length = run_length(total, a.runs);
+  const int c0 = t0 / length, c1 = (w.first[b + 1] - 1) / length;
+  const MassRequest r = read_request(a, b);
+#pragma unroll 1
+  for (int x = tid; x < all; x += kThreads) {
+    float2 f = make_float2(-INFINITY, 0.f);
+    const int col = x % cc;
+    if (col < r.look * g) {
+      const float2* from = w.stats + (static_cast<size_t>(b) + c0) * all + x;
+#pragma unroll 1
       for (int c = c0; c <= c1; c += 8) {       // in order of the keys, eight loads under way
         float2 piece[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) piece[e] = c + e <= c1 ? src[static_cast<long>(c + e) * hk * cc] : make_float2(-INFINITY, 0.f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = join(s, piece[e]);
+        for (int e = 0; e < 8; ++e) piece[e] = c + e <= c1 ? from[e * all] : make_float2(-INFINITY, 0.f);
+        f = join8(f, piece);
+        from += 8 * all;
       }
-      const float2 f = query_row(a, r, b, col / g, kvh == 0 && at == first[b]) < 0 ? make_float2(0.f, 0.f) : finish(s);
-      stat[x] = make_float4(f.x, f.y, __int_as_float(kvh * cc + col), __int_as_float(col / g));
+      f = query_row(a, r, b, col / g, x < cc && tile == t0) < 0 ? make_float2(0.f, 0.f) : finish(f);
     }
-    __syncthreads();
-    // four tiles at once, a thread a key
-    const int stop = min(first[b + 1], end);
-    for (; at < stop; at += kThreads / KEYS) {
-      const int tile = at + tid / KEYS;
-      const int t = (tile - first[b]) * KEYS + tid % KEYS;
-      if (tile >= stop || t >= r.kv) continue;
-      const float* src = w.scores + static_cast<size_t>(tile) * hk * cc * KEYS + tid % KEYS;
-      const int free_to = r.kv - r.look;
-      float sum = 0.f;
-      for (int x0 = 0; x0 < all; x0 += 16) {
-        float s[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = x0 + e < all ? src[__float_as_int(stat[x0 + e].z) * KEYS] : 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (x0 + e >= all) break;
-          const float4 st = stat[x0 + e];
-          if (st.y != 0.f && t <= free_to + __float_as_int(st.w)) sum += ex2(s[e] - st.x) * st.y;
-        }
-      }
-      store_mass(a, r, b, t, sum);
-    }
-    at = stop;
+    stat[x] = f;                                // (no weights: 1 / l is 0)
+    row_of[x] = static_cast<uint8_t>(col / g);
   }
+  if (tid < kEarly) stat[all + tid] = make_float2(0.f, 0.f);
+  __syncthreads();
+  const int t = (tile - t0) * KEYS + key, behind = t - (r.kv - r.look);   // > 0: only columns from that row on see it
+  float sum = 0.f;
+#pragma unroll 1
+  for (int x0 = part * kEarly; x0 < all; x0 += kThreads / KEYS * kEarly) {
+#pragma unroll
+    for (int e = 0; e < kEarly; ++e) {
+      const float2 st = stat[x0 + e];
+      const bool seen = st.y != 0.f && (behind <= 0 || behind <= row_of[x0 + e]);
+      sum += seen ? ex2(s[e] - st.x) * st.y : 0.f;
+    }
+    src += kThreads / KEYS * kEarly * KEYS;
+#pragma unroll
+    for (int e = 0; e < kEarly; ++e) s[e] = x0 + kThreads / KEYS * kEarly + e < all ? src[e * KEYS] : 0.f;
+  }
+  sums[tid] = sum;
+  __syncthreads();
+  if (tid < KEYS && t < r.kv) store_mass(a, r, b, t, (sums[tid] + sums[KEYS + tid]) + (sums[2 * KEYS + tid] + sums[3 * KEYS + tid]));
 }
 
 int general_runs(int num_sms) { return 2 * num_sms; }
@@ -514,7 +521,7 @@ size_t mass_workspace(int type, int B, int T_kv_cap, int n_heads, int n_kv, int 
   const size_t cols = static_cast<size_t>(n_heads) * window, unit = static_cast<size_t>(n_heads / n_kv) * window;
   if (mass_on_tensor_cores(type, n_heads, n_kv, window)) return tc_mass_workspace(B, T_kv_cap, n_heads, n_kv, window, num_sms);
   if (few_columns(type, n_heads, n_kv, window))
-    return 8 * few_stats(B, few_runs(num_sms), cols) + 4 * KEYS * cols * (static_cast<size_t>(T_kv_cap) / KEYS + B);
+    return few_first(B) + 8 * few_stats(B, few_runs(num_sms), cols) + 4 * KEYS * cols * (static_cast<size_t>(T_kv_cap) / KEYS + B);
   return 8 * (B * cols + (general_runs(num_sms) + static_cast<size_t>(B) * n_kv) * unit);
 }
 
@@ -525,7 +532,7 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
   if (few_columns(type, a.n_heads, a.pages.n_kv, a.window)) {
     a.runs = few_runs(num_sms);
     const int most_tiles = tile_capacity(a);
-    const dim3 grid(most_tiles < a.runs ? most_tiles : a.runs), sums(most_tiles < 4 * num_sms ? most_tiles : 4 * num_sms);
+    const dim3 grid(most_tiles < a.runs ? most_tiles : a.runs), sums(most_tiles);
     const int wide = a.n_heads / a.pages.n_kv * a.window > 8;
     cudaError_t e = cudaErrorInvalidValue;
 #define SEER_FEW(F, D, N)                                                                       \
@@ -543,9 +550,7 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
     SEER_FEW(true, 128, 1)
     SEER_FEW(true, 128, 2)
 #undef SEER_FEW
-    static bool set[64] = {};
-    if (e == cudaSuccess) e = set_smem_limit_once(mass_sums_kernel, most_line, set);
-    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel, sums, dim3(kThreads), line, st, a);
+    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel, sums, dim3(kThreads), 0, st, a);
     return e;
   }
   a.runs = general_runs(num_sms);

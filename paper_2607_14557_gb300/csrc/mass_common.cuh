@@ -32,19 +32,24 @@ __device__ __forceinline__ MassRequest read_request(const MassArgs& a, int b) {
   return r;
 }
 
-// The request of place x on the line.
-template <typename P>
-__device__ __forceinline__ int request_at(const P* first, int B, P x) {
-  int lo = 0, hi = B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= x) lo = mid; else hi = mid;
+// The request of place x on a line, first[b] the places before request b: by a whole warp, the
+// prefix sums narrowed 32-fold a step.
+__device__ __forceinline__ int request_at(const int* first, int B, int x) {
+  const int lane = threadIdx.x & 31;
+  int b = 0, left = B;
+#pragma unroll 1
+  while (left > 1) {
+    const int hop = (left + 31) / 32, k = lane * hop;
+    const unsigned below = __ballot_sync(0xffffffffu, k < left && first[b + k] <= x);
+    const int last = 31 - __clz(below);         // (first[b] <= x)
+    b += last * hop;
+    left = min(hop, left - last * hop);
   }
-  return lo;
+  return b;
 }
-// Run c of n over `total` places: [cut(c), cut(c + 1)), and the run that holds x.
-__device__ __forceinline__ int cut(long long total, int c, int n) { return static_cast<int>(total * c / n); }
-__device__ __forceinline__ int run_of(long long total, long long x, int n) { return static_cast<int>(((x + 1) * n - 1) / total); }
+// Places of a run: `total` places cut into at most n equal runs, the last one shorter.  Run c holds
+// places [c * run, (c + 1) * run), so a place's run is one 32-bit division (total < 2^31).
+__device__ __forceinline__ int run_length(int total, int n) { return max(1, (total + n - 1) / n); }
 
 // Row of q of a request's i-th looking row, or -1 (an accepted entry outside the draft).
 __device__ __forceinline__ int query_row(const MassArgs& a, const MassRequest& r, int b, int i, bool report) {
@@ -71,9 +76,23 @@ __device__ __forceinline__ float2 join(float2 x, float2 y) {
   const float base = m == -INFINITY ? 0.f : m;
   return make_float2(m, x.y * ex2(x.x - base) + y.y * ex2(y.x - base));
 }
-// (m, 1 / l) as the weights take it: 2^(s - m) / l.
-__device__ __forceinline__ float2 finish(float2 x) { return make_float2(x.x == -INFINITY ? 0.f : x.x, 1.f / x.y); }
-
+// Eight more at once: one maximum, then independent terms.
+__device__ __forceinline__ float2 join8(float2 x, const float2 (&y)[8]) {
+  float m = x.x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = fmaxf(m, y[e].x);
+  const float base = m == -INFINITY ? 0.f : m;
+  float l = x.y * ex2(x.x - base);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) l = fmaf(y[e].y, ex2(y[e].x - base), l);
+  return make_float2(m, l);
+}
+// (m, 1 / l) as the weights take it: 2^(s - m) / l.  The reciprocal is off by at most 2^-23 of itself.
+__device__ __forceinline__ float2 finish(float2 x) {
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(x.y));
+  return make_float2(x.x == -INFINITY ? 0.f : x.x, inv);
+}
 // Key t's new weight into the matrices.
 __device__ __forceinline__ void store_mass(const MassArgs& a, const MassRequest& r, int b, int t, float w) {
   const size_t at = static_cast<size_t>(b) * a.ld_mass + t;

@@ -49,7 +49,7 @@ struct Layout {
 // Workspace: prefix sums over the requests, the pieces' (m, l), the keys' sums per unit.
 struct Work {
   int* tiles;             // [B + 1] key tiles of the requests before b
-  long long* places;      // [B + 1] places on the line
+  int* places;            // [B + 1] places on the line
   float2* stats;          // [runs + B * slices][256]
   float* sums;            // [2 * slices][capacity tiles][128]
 };
@@ -64,12 +64,12 @@ __host__ __device__ inline Sizes sizes_of(int n_heads, int n_kv, int window) {
   return z;
 }
 __host__ __device__ inline size_t work_tiles(int T_kv_cap, int B) { return static_cast<size_t>(T_kv_cap) / KEYS + B; }
-__host__ __device__ inline size_t prefix_bytes(int B) { return (12 * (static_cast<size_t>(B) + 2) + 15) / 16 * 16; }
+__host__ __device__ inline size_t prefix_bytes(int B) { return (8 * (static_cast<size_t>(B) + 1) + 15) / 16 * 16; }
 __device__ __forceinline__ Work work_of(const MassArgs& a, const Sizes& z) {
   Work w;
   uint8_t* p = static_cast<uint8_t*>(a.ws);
-  w.places = reinterpret_cast<long long*>(p);
-  w.tiles = reinterpret_cast<int*>(w.places + a.B + 1);
+  w.places = reinterpret_cast<int*>(p);
+  w.tiles = w.places + a.B + 1;
   w.stats = reinterpret_cast<float2*>(p + prefix_bytes(a.B));
   w.sums = reinterpret_cast<float*>(w.stats + (a.runs + static_cast<size_t>(a.B) * z.slices) * COLS);
   return w;
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
       const bool fits = before[0] + inc[0] <= cap;
       if (!fits && v[0] > 0) record_error(a.err, kErrCapacity);
       w.tiles[b + 1] = fits ? static_cast<int>(before[0] + inc[0]) : -1;
-      w.places[b + 1] = before[1] + inc[1];
+      w.places[b + 1] = static_cast<int>(before[1] + inc[1]);   // below 2^31 where it fits
     }
     __syncthreads();
   }
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
     if (w.tiles[mid] >= 0) lo = mid; else hi = mid;
   }
   const int end = w.tiles[lo];
-  const long long last = w.places[lo];
+  const int last = w.places[lo];
   __syncthreads();
   for (int b = lo + 1 + tid; b <= a.B; b += 1024) {
     w.tiles[b] = end;
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
 struct Piece {
   int b, kvh, tok0;       // tok0: the block's first token among the rows that look
   int tile0, tile1, tiles;
-  int slice;
+  int slice, first;       // first: the unit's first place
   MassRequest r;
 };
 // The pieces of run blockIdx.x, the same for every role of the CTA.
@@ -157,44 +157,29 @@ struct Walk {
   const MassArgs& a;
   const Sizes z;
   const Work w;
-  long long at, end, total;
-  int runs, b = 0;
+  int at, end, length;                      // of a run: places
+  int b = 0;
   bool fresh = true;
 
   __device__ __forceinline__ Walk(const MassArgs& a_) : a(a_), z(sizes_of(a_.n_heads, a_.pages.n_kv, a_.window)), w(work_of(a_, z)) {
-    total = w.places[a.B];
-    runs = static_cast<int>(min(static_cast<long long>(a.runs), total));
-    const int run = blockIdx.x;
-    at = run < runs ? total * run / runs : 0;
-    end = run < runs ? total * (run + 1) / runs : 0;
-  }
-  __device__ __forceinline__ int run_at(long long x) const { return static_cast<int>(((x + 1) * runs - 1) / total); }
-  // The request of place x, by a whole warp: the prefix sums are narrowed 32-fold a step.
-  __device__ __forceinline__ int find(long long x) const {
-    const int lane = threadIdx.x & 31;
-    int lo = 0, n = a.B;                    // among [lo, lo + n)
-    while (n > 1) {
-      const int step = (n + 31) / 32, k = lane * step;
-      const unsigned below = __ballot_sync(0xffffffffu, k < n && w.places[lo + k] <= x);
-      const int last = 31 - __clz(below);   // (places[lo] <= x)
-      lo += last * step;
-      n = min(step, n - last * step);
-    }
-    return lo;
+    const int total = w.places[a.B];
+    length = run_length(total, a.runs);
+    at = min(static_cast<int>(blockIdx.x) * length, total);
+    end = min(at + length, total);
   }
   __device__ __forceinline__ bool next(Piece& p) {
     if (at >= end) return false;
     if (fresh || w.places[b + 1] <= at) {
       fresh = false;
-      b = find(at);
+      b = request_at(w.places, a.B, at);
       p.r = read_request(a, b);
     }
     p.b = b;
     p.tiles = w.tiles[b + 1] - w.tiles[b];
-    const long long off = at - w.places[b];
-    const int unit = static_cast<int>(off / p.tiles), blocks = (p.r.look + 2 * z.tpt - 1) / (2 * z.tpt);
-    p.tile0 = static_cast<int>(off - static_cast<long long>(unit) * p.tiles);
-    p.tile1 = static_cast<int>(min(static_cast<long long>(p.tiles), p.tile0 + (end - at)));
+    const int off = at - w.places[b], unit = off / p.tiles, blocks = (p.r.look + 2 * z.tpt - 1) / (2 * z.tpt);
+    p.first = at - (off - unit * p.tiles);
+    p.tile0 = off - unit * p.tiles;
+    p.tile1 = min(p.tiles, p.tile0 + (end - at));
     at += p.tile1 - p.tile0;
     p.kvh = unit / blocks;
     p.tok0 = (unit - p.kvh * blocks) * 2 * z.tpt;
@@ -498,8 +483,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       if constexpr (WEIGHTS) {
         // columns tid and tid + 128: their pieces in order of the keys
         float2 s[2];
-        const long long unit0 = walk.w.places[p.b] + static_cast<long long>(p.kvh * ((p.r.look + 2 * tpt - 1) / (2 * tpt)) + p.tok0 / (2 * tpt)) * p.tiles;
-        const int c0 = walk.run_at(unit0), c1 = walk.run_at(unit0 + p.tiles - 1);
+        const int c0 = p.first / walk.length, c1 = (p.first + p.tiles - 1) / walk.length;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           s[t] = make_float2(-INFINITY, 0.f);
@@ -540,33 +524,25 @@ __global__ void __launch_bounds__(FINAL_THREADS) mass_final_kernel(const MassArg
   const Sizes z = sizes_of(a.n_heads, a.pages.n_kv, a.window);
   const Work w = work_of(a, z);
   const size_t step = work_tiles(a.T_kv_cap, a.B) * KEYS;
-  const int x = blockIdx.x, lane = threadIdx.x & 31;
+  const int x = blockIdx.x;
   const float* src = w.sums + static_cast<size_t>(x) * KEYS + threadIdx.x;
   float s[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) s[e] = e < 2 * z.slices ? src[e * step] : 0.f;
   if (x >= w.tiles[a.B]) return;
-  int b = 0, left = a.B;                    // the request of tile x, the prefix sums narrowed 32-fold a step
-  while (left > 1) {
-    const int hop = (left + 31) / 32, k = lane * hop;
-    const unsigned below = __ballot_sync(0xffffffffu, k < left && w.tiles[b + k] <= x);
-    const int last = 31 - __clz(below);
-    b += last * hop;
-    left = min(hop, left - last * hop);
-  }
+  const int b = request_at(w.tiles, a.B, x);
   const MassRequest r = read_request(a, b);
   const int t = (x - w.tiles[b]) * KEYS + threadIdx.x;
   if (t >= r.kv) return;
   const int blocks = (r.look + 2 * z.tpt - 1) / (2 * z.tpt);      // column blocks that the request has
   float sum = 0.f;
+#pragma unroll 1
   for (int i0 = 0; i0 < 2 * z.slices; i0 += 16) {
-    if (i0 > 0) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = i0 + e < 2 * z.slices ? src[(i0 + e) * step] : 0.f;
-    }
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-      if (i0 + e < 2 * z.slices && (i0 + e) / 2 % z.blocks < blocks) sum += s[e];
+      if (i0 + e < 2 * z.slices && (z.blocks == 1 ? blocks > 0 : (i0 + e) / 2 % z.blocks < blocks)) sum += s[e];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = i0 + 16 + e < 2 * z.slices ? src[(i0 + 16 + e) * step] : 0.f;
   }
   store_mass(a, r, b, t, sum);
 }
