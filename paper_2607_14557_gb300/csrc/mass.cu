@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kThreads) mass_weights_kernel(const MassArgs a
       float w = 0.f;
 #pragma unroll
       for (int e = 0; e < kThreads / KEYS; ++e) w += sums[e * KEYS + tid];
-      store_mass(a, r, b, t, w);
+      store_mass(a, r, b, t, w, old_mass(a, r, b, t));
     }
   }
 }
@@ -261,11 +261,9 @@ __global__ void __launch_bounds__(kThreads) mass_weights_kernel(const MassArgs a
 // Where a key/value head has at most 16 columns (a decoded token of up to 16 heads) the scores
 // are kept: 4 bytes a column and key beside the key's 2 head_dim bytes, so the cache is read
 // once and the second kernel reads the scores, mostly from L2.  Bound by HBM.
-// A warp takes 16 keys of a head at a time straight from global memory into the fragments of
-// m16n8k16: the order of a product's terms is free, so a lane's 16 bytes of a row serve as the
-// k-indices that the fragment wants from it (and Q is cut alike), and nothing passes through
-// shared memory.  The next keys are under way while these are multiplied, their pages are
-// looked up a step earlier.  A lane keeps the maxima and sums of its two columns over its keys.
+// A warp multiplies 16 keys of a head at a time by m16n8k16: the order of a product's terms is
+// free, so a lane's 16 bytes of a row serve as the k-indices that the fragment wants from it, and Q
+// is cut alike.  A lane keeps the maxima and sums of its two columns over its keys.
 constexpr int kFewCols = 16;                // columns of a key/value head at most
 constexpr int kFewStats = 1024;             // of all heads
 constexpr int GROUP = 16;                   // keys of a step
@@ -296,163 +294,222 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 16 keys of a head in a lane: rows lane / 4 and lane / 4 + 8, bytes 16 (lane % 4) of every 64.
-template <int DH>
-struct KeyRegs {
-  uint4 lo[DH / 32], hi[DH / 32];
-};
+// A CTA: eight warps that multiply and one that loads.  A stage is what the eight take at once, 16
+// keys of eight heads, or of fewer heads more keys; a key's heads lie side by side in the pool and
+// come as one bulk copy, rows of a stage 64 bytes further apart than they are long, so that the
+// fragments' 16-byte reads meet in no bank.  Two CTAs per SM, three stages each.
+constexpr int kStages = 3, kScoreThreads = kThreads + 32, kWarps = kThreads / 32;
+__host__ __device__ constexpr int stage_bytes(int heads, int dh) { return kWarps / heads * GROUP * (heads * dh * 2 + 64); }
+__host__ __device__ constexpr int ring_bytes(int n_kv, int dh) { return kStages * stage_bytes(n_kv < kWarps ? n_kv : kWarps, dh); }
+
+__device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, int bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_u32(smem_dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
 
 template <bool F16, int DH, int NT>
-__global__ void __launch_bounds__(kThreads, 2) mass_scores_kernel(const MassArgs a, const float scale) {
+__global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const MassArgs a, const float scale) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  int* first = reinterpret_cast<int*>(ring + ring_bytes(a.pages.n_kv, DH));
+  __shared__ long long warp_sum[kScoreThreads / 32];
+  __shared__ float2 shares[kWarps][NT * 8];
+  __shared__ uint64_t full[kStages], empty[kStages];
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], kWarps);
+    }
+    abort_word = 0;
+    fence_barrier_init();
+  }
   pdl_enter();
-  extern __shared__ int first[];
-  __shared__ long long warp_sum[kThreads / 32];
-  __shared__ float2 shares[kThreads / 32][NT * 8];
   tile_line(a, first, warp_sum, blockIdx.x == 0);
   const int total = first[a.B], length = run_length(total, a.runs), run = blockIdx.x;
   if (run == 0)
-    for (int b = threadIdx.x; b <= a.B; b += kThreads) few_work(a).first[b] = first[b];
-  if (run * length >= total) return;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, row = lane >> 2;
+    for (int b = tid; b <= a.B; b += kScoreThreads) few_work(a).first[b] = first[b];
+  int at = run * length;
+  const int end = min(at + length, total);
+  if (at >= end) return;
   const int hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window;
   const FewWork w = few_work(a);
   // warps of a head: its keys are dealt to them 16 at a time
-  const int per_head = hk >= 8 ? 1 : 8 / hk, heads = hk >= 8 ? 8 : hk;
-  const int sub = warp / heads;
-  const bool busy = sub < per_head;
-  const long row_elems = 2l * hk * DH;
+  const int heads = min(hk, kWarps), per_head = kWarps / heads;
+  const int pitch = heads * DH * 2 + 64, stage = stage_bytes(heads, DH);
   const int page_mask = (1 << a.pages.page_shift) - 1;
-  int at = run * length;
-  const int end = min(at + length, total);
-  for (int b = request_at(first, a.B, at); at < end; ++b) {
+  unsigned step = 0;                            // stages used
+  bool ok = true;
+#pragma unroll 1
+  for (int b = request_at(first, a.B, at); ok && at < end; ++b) {
     if (first[b + 1] <= at) continue;
     const MassRequest r = read_request(a, b);
     const int tile0 = at - first[b], tile1 = min(first[b + 1], end) - first[b];
     at += tile1 - tile0;
     const int cols = r.look * g;
     if (cols == 0) continue;
-    const int groups = min(tile1 * KEYS, r.kv + GROUP - 1) / GROUP;      // key groups [tile0 * 4, groups)
-    const int free_to = r.kv - r.look;                                   // keys up to it are seen by every row
-    const int* table = a.pages.table + static_cast<size_t>(b) * a.pages.max_pages;
-    for (int kvh = warp % heads; kvh < (hk + heads - 1) / heads * heads; kvh += heads) {
-      const bool mine = busy && kvh < hk;
-      float m[NT][2], l[NT][2];
+    const int groups = min(tile1 * KEYS, r.kv + GROUP - 1) / GROUP;      // key groups [4 tile0, groups)
+    const int group0 = tile0 * (KEYS / GROUP), steps = (groups - group0 + per_head - 1) / per_head;
+#pragma unroll 1
+    for (int head0 = 0; ok && head0 < hk; head0 += heads) {
+      const int here = min(heads, hk - head0);
+      if (warp == kWarps) {
+        // ---- loads: a lane a key, its page looked up a stage ahead
+        const int keys = per_head * GROUP, bytes = here * DH * 2;
+        const long row_bytes = 4l * hk * DH;
+        const uint8_t* pool = static_cast<const uint8_t*>(a.pages.kv) + head0 * DH * 2;
+        const int* table = a.pages.table + static_cast<size_t>(b) * a.pages.max_pages;
+        constexpr int MORE = kWarps * GROUP / 32;            // keys of a lane at most
+        int page[MORE];
+        const auto look_up = [&](int i) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+          for (int e = 0; e < MORE; ++e) {
+            const int k = lane + 32 * e, t = (group0 + i * per_head) * GROUP + k;
+            page[e] = i < steps && k < keys && t < r.kv ? table[t >> a.pages.page_shift] : -1;
+          }
+        };
+        look_up(0);
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i, ++step) {
+          const int s = step % kStages;
+          if (step >= kStages && !warp_wait(&empty[s], (step / kStages - 1) & 1, abort_flag, a.err)) {
+            ok = false;
+            break;
+          }
+          int mine = 0;
+          uint8_t* dst = ring + s * stage + lane * pitch;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          m[nt][e] = -INFINITY;
-          l[nt][e] = 0.f;
+          for (int e = 0; e < MORE; ++e) {
+            const int k = lane + 32 * e, t = (group0 + i * per_head) * GROUP + k;
+            if (k >= keys || t >= r.kv) page[e] = -2;        // (no key)
+            else if (page[e] < 0 || page[e] >= a.pages.n_pages) {
+              record_error(a.err, kErrLayout);               // reads as zeros
+              for (int x = 0; x < bytes; x += 16) *reinterpret_cast<uint4*>(dst + e * 32 * pitch + x) = make_uint4(0, 0, 0, 0);
+              fence_proxy_async_smem();
+              page[e] = -2;
+            } else {
+              ++mine;
+            }
+          }
+          const int rows = __reduce_add_sync(0xffffffffu, mine);
+          if (lane == 0) mbar_arrive_expect_tx(&full[s], rows * bytes);
+          __syncwarp();
+#pragma unroll
+          for (int e = 0; e < MORE; ++e) {
+            const int t = (group0 + i * per_head) * GROUP + lane + 32 * e;
+            if (page[e] >= 0)
+              bulk_load(dst + e * 32 * pitch, pool + ((static_cast<long>(page[e]) << a.pages.page_shift) + (t & page_mask)) * row_bytes, bytes, &full[s]);
+          }
+          look_up(i + 1);
         }
-      if (mine) {
-        uint4 q[NT][DH / 32];
+        continue;
+      }
+      // ---- products
+      const int h = warp % heads, sub = warp / heads, quad = lane & 3, row = lane >> 2, kvh = head0 + h;
+      const bool busy = sub < per_head && h < here;
+      float m[NT][2], l[NT][2];
+      uint4 q[NT][DH / 32];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        m[nt][0] = m[nt][1] = -INFINITY;
+        l[nt][0] = l[nt][1] = 0.f;
+        const int col = nt * 8 + row;
+        const int qr = busy && col < cols ? query_row(a, r, b, col / g, false) : -1;
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (qr < 0 ? 0 : qr * a.ld_q + static_cast<long>(kvh * g + col % g) * DH));
+#pragma unroll
+        for (int j = 0; j < DH / 32; ++j) q[nt][j] = qr < 0 ? make_uint4(0, 0, 0, 0) : src[4 * j + quad];
+      }
+      const int free_to = r.kv - r.look;                     // keys up to it are seen by every row
+      const uint8_t* mine = ring + (sub * GROUP + row) * pitch + h * DH * 2 + quad * 16;
+#pragma unroll 1
+      for (int i = 0; i < steps; ++i, ++step) {
+        const int s = step % kStages, gi = group0 + i * per_head + sub, t = gi * GROUP + row;
+        if (!warp_wait(&full[s], (step / kStages) & 1, abort_flag, a.err)) {
+          ok = false;
+          break;
+        }
+        uint4 lo[DH / 32], hi[DH / 32];
+        if (busy) {
+#pragma unroll
+          for (int j = 0; j < DH / 32; ++j) {
+            lo[j] = *reinterpret_cast<const uint4*>(mine + s * stage + j * 64);
+            hi[j] = *reinterpret_cast<const uint4*>(mine + s * stage + 8 * pitch + j * 64);
+          }
+        }
+        __syncwarp();
+        if (!busy || gi >= groups) {
+          if (lane == 0) mbar_arrive(&empty[s]);
+          continue;
+        }
+        float d[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          const int col = nt * 8 + row;
-          const int qr = col < cols ? query_row(a, r, b, col / g, false) : -1;
-          const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (qr < 0 ? 0 : qr * a.ld_q + static_cast<long>(kvh * g + col % g) * DH));
+          d[nt][0] = d[nt][1] = d[nt][2] = d[nt][3] = 0.f;
 #pragma unroll
-          for (int j = 0; j < DH / 32; ++j) q[nt][j] = qr < 0 ? make_uint4(0, 0, 0, 0) : src[4 * j + quad];
-        }
-        const uint16_t* keys = static_cast<const uint16_t*>(a.pages.kv) + static_cast<long>(kvh) * DH + 8 * quad;
-        const auto look_up = [&](int gi, int (&page)[2]) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int t = gi * GROUP + row + 8 * e;
-            page[e] = gi < groups && t < r.kv ? table[t >> a.pages.page_shift] : -1;
-          }
-        };
-        const auto load = [&](int gi, const int (&page)[2], KeyRegs<DH>& k) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int t = gi * GROUP + row + 8 * e;
-            uint4* to = e == 0 ? k.lo : k.hi;
-            const bool there = page[e] >= 0 && page[e] < a.pages.n_pages;
-            if (!there && gi < groups && t < r.kv) record_error(a.err, kErrLayout);
-            const uint4* src = reinterpret_cast<const uint4*>(keys + ((static_cast<long>(there ? page[e] : 0) << a.pages.page_shift) + (t & page_mask)) * row_elems);
-#pragma unroll
-            for (int j = 0; j < DH / 32; ++j) to[j] = there ? src[4 * j] : make_uint4(0, 0, 0, 0);
-          }
-        };
-        const auto compute = [&](int gi, const KeyRegs<DH>& k) {
-          const int t = gi * GROUP + row;
-          float* out = w.scores + (static_cast<size_t>(first[b] + (gi >> 2)) * hk + kvh) * cc * KEYS + (gi & 3) * GROUP + row;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float d[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < DH / 32; ++j) {
-              mma16816<F16>(d, k.lo[j].x, k.hi[j].x, k.lo[j].y, k.hi[j].y, q[nt][j].x, q[nt][j].y);
-              mma16816<F16>(d, k.lo[j].z, k.hi[j].z, k.lo[j].w, k.hi[j].w, q[nt][j].z, q[nt][j].w);
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int col = nt * 8 + 2 * quad + e;
-              float s0 = __fmul_rn(d[e], scale), s1 = __fmul_rn(d[2 + e], scale);   // as they are kept
-              if (col < cols) {
-                out[col * KEYS] = s0;
-                out[col * KEYS + 8] = s1;
-              }
-              if (t + 8 > free_to) {          // (column col sees keys up to free_to + col / g)
-                const int last = free_to + col / g;
-                if (t > last) s0 = -INFINITY;
-                if (t + 8 > last) s1 = -INFINITY;
-              }
-              const float top = max3(m[nt][e], s0, s1), base = top == -INFINITY ? 0.f : top;
-              l[nt][e] = l[nt][e] * ex2(m[nt][e] - base) + ex2(s0 - base) + ex2(s1 - base);
-              m[nt][e] = top;
-            }
-          }
-        };
-        KeyRegs<DH> k[2];
-        int page[2];
-        int gi = tile0 * (KEYS / GROUP) + sub;
-        look_up(gi, page);
-        load(gi, page, k[0]);
-        look_up(gi + per_head, page);
-        while (gi < groups) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            load(gi + per_head, page, k[x ^ 1]);
-            look_up(gi + 2 * per_head, page);
-            if (gi < groups) compute(gi, k[x]);
-            gi += per_head;
+          for (int j = 0; j < DH / 32; ++j) {
+            mma16816<F16>(d[nt], lo[j].x, hi[j].x, lo[j].y, hi[j].y, q[nt][j].x, q[nt][j].y);
+            mma16816<F16>(d[nt], lo[j].z, hi[j].z, lo[j].w, hi[j].w, q[nt][j].z, q[nt][j].w);
           }
         }
+        if (lane == 0) mbar_arrive(&empty[s]);               // (the fragments are in registers)
+        float* out = w.scores + (static_cast<size_t>(first[b] + (gi >> 2)) * hk + kvh) * cc * KEYS + (gi & 3) * GROUP + row;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float2 s = make_float2(m[nt][e], l[nt][e]);
-#pragma unroll
-            for (int off = 4; off < 32; off <<= 1)
-              s = join(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, off), __shfl_xor_sync(0xffffffffu, s.y, off)));
-            if (row == 0) shares[warp][nt * 8 + 2 * quad + e] = s;
+            const int col = nt * 8 + 2 * quad + e;
+            float s0 = __fmul_rn(d[nt][e], scale), s1 = __fmul_rn(d[nt][2 + e], scale);   // as they are kept
+            if (col < cols) {
+              out[col * KEYS] = s0;
+              out[col * KEYS + 8] = s1;
+            }
+            if (t + 8 > free_to) {              // (column col sees keys up to free_to + col / g)
+              const int last = free_to + col / g;
+              if (t > last) s0 = -INFINITY;
+              if (t + 8 > last) s1 = -INFINITY;
+            }
+            const float top = max3(m[nt][e], s0, s1), base = top == -INFINITY ? 0.f : top;
+            l[nt][e] = l[nt][e] * ex2(m[nt][e] - base) + ex2(s0 - base) + ex2(s1 - base);
+            m[nt][e] = top;
           }
       }
-      __syncthreads();
-      float2* out = w.stats + (run + static_cast<long>(b)) * hk * cc;
-      for (int x = tid; x < heads * cols; x += kThreads) {
-        const int h = x / cols, col = x - h * cols, head = kvh - warp % heads + h;
-        if (head >= hk) continue;
-        float2 s = shares[h][col];
-        for (int e = 1; e < per_head; ++e) s = join(s, shares[h + e * heads][col]);
-        out[static_cast<long>(head) * cc + col] = s;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float2 x = make_float2(m[nt][e], l[nt][e]);
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1)
+            x = join(x, make_float2(__shfl_xor_sync(0xffffffffu, x.x, off), __shfl_xor_sync(0xffffffffu, x.y, off)));
+          if (row == 0) shares[warp][nt * 8 + 2 * quad + e] = x;
+        }
+      asm volatile("bar.sync 1, %0;" ::"r"(kThreads) : "memory");
+      float2* out = w.stats + (static_cast<size_t>(run) + b) * hk * cc;
+#pragma unroll 1
+      for (int x = tid; x < here * cols; x += kThreads) {
+        const int head = x / cols, col = x - head * cols;
+        float2 st = shares[head][col];
+        for (int e = 1; e < per_head; ++e) st = join(st, shares[head + e * heads][col]);
+        out[static_cast<size_t>(head0 + head) * cc + col] = st;
       }
-      __syncthreads();
+      asm volatile("bar.sync 1, %0;" ::"r"(kThreads) : "memory");
     }
   }
+  if (warp == kWarps && *abort_flag && lane == 0)            // copies still in flight land before the memory is released
+    for (unsigned j = step > kStages ? step - kStages : 0; j <= step; ++j) mbar_wait_drain(&full[j % kStages], (j / kStages) & 1, 20000000ull);
 }
 
-// A tile a block, four threads a key with every fourth eight columns.  Bound by latency, so a
+// A tile a block, two threads a key with every second 16 columns.  Bound by latency, so a
 // thread's first scores are loaded before it is known whose the tile is (any tile's memory is
 // there), and the code is kept short: its first instructions come from memory too.
-constexpr int kEarly = 8;
-__global__ void __launch_bounds__(kThreads) mass_sums_kernel(const MassArgs a) {
+constexpr int kEarly = 16, kSumThreads = 2 * KEYS;
+__global__ void __launch_bounds__(kSumThreads) mass_sums_kernel(const MassArgs a) {
   pdl_enter();
   __shared__ float2 stat[kFewStats + kEarly];   // (m, 1 / l) of every column
   __shared__ uint8_t row_of[kFewStats + kEarly];   // its row among those that look
-  __shared__ float sums[kThreads];
+  __shared__ float sums[kSumThreads];
   const int tid = threadIdx.x, part = tid / KEYS, key = tid % KEYS, tile = blockIdx.x;
   const int hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window, all = hk * cc;
   const FewWork w = few_work(a);
@@ -466,8 +523,10 @@ __global__ void __launch_bounds__(kThreads) mass_sums_kernel(const MassArgs a) {
   const int t0 = w.first[b], length = run_length(total, a.runs);
   const int c0 = t0 / length, c1 = (w.first[b + 1] - 1) / length;
   const MassRequest r = read_request(a, b);
+  const int t = (tile - t0) * KEYS + key;
+  const float old = tid < KEYS && t < r.kv ? old_mass(a, r, b, t) : 0.f;
 #pragma unroll 1
-  for (int x = tid; x < all; x += kThreads) {
+  for (int x = tid; x < all; x += kSumThreads) {
     float2 f = make_float2(-INFINITY, 0.f);
     const int col = x % cc;
     if (col < r.look * g) {
@@ -487,23 +546,23 @@ __global__ void __launch_bounds__(kThreads) mass_sums_kernel(const MassArgs a) {
   }
   if (tid < kEarly) stat[all + tid] = make_float2(0.f, 0.f);
   __syncthreads();
-  const int t = (tile - t0) * KEYS + key, behind = t - (r.kv - r.look);   // > 0: only columns from that row on see it
+  const int behind = t - (r.kv - r.look);       // > 0: only columns from that row on see it
   float sum = 0.f;
 #pragma unroll 1
-  for (int x0 = part * kEarly; x0 < all; x0 += kThreads / KEYS * kEarly) {
+  for (int x0 = part * kEarly; x0 < all; x0 += kSumThreads / KEYS * kEarly) {
 #pragma unroll
     for (int e = 0; e < kEarly; ++e) {
       const float2 st = stat[x0 + e];
       const bool seen = st.y != 0.f && (behind <= 0 || behind <= row_of[x0 + e]);
       sum += seen ? ex2(s[e] - st.x) * st.y : 0.f;
     }
-    src += kThreads / KEYS * kEarly * KEYS;
+    src += kSumThreads / KEYS * kEarly * KEYS;
 #pragma unroll
-    for (int e = 0; e < kEarly; ++e) s[e] = x0 + kThreads / KEYS * kEarly + e < all ? src[e * KEYS] : 0.f;
+    for (int e = 0; e < kEarly; ++e) s[e] = x0 + kSumThreads / KEYS * kEarly + e < all ? src[e * KEYS] : 0.f;
   }
   sums[tid] = sum;
   __syncthreads();
-  if (tid < KEYS && t < r.kv) store_mass(a, r, b, t, (sums[tid] + sums[KEYS + tid]) + (sums[2 * KEYS + tid] + sums[3 * KEYS + tid]));
+  if (tid < KEYS && t < r.kv) store_mass(a, r, b, t, sums[tid] + sums[KEYS + tid], old);
 }
 
 int general_runs(int num_sms) { return 2 * num_sms; }
@@ -538,8 +597,9 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
 #define SEER_FEW(F, D, N)                                                                       \
   if ((type == kF16) == F && a.pages.head_dim == D && wide == N - 1) {                          \
     static bool set[64] = {};                                                                   \
-    e = set_smem_limit_once(mass_scores_kernel<F, D, N>, most_line, set);                       \
-    if (e == cudaSuccess) e = launch_kernel(mass_scores_kernel<F, D, N>, grid, dim3(kThreads), line, st, a, scale); \
+    e = set_smem_limit_once(mass_scores_kernel<F, D, N>, ring_bytes(1, D) + most_line, set);       \
+    if (e == cudaSuccess)                                                                       \
+      e = launch_kernel(mass_scores_kernel<F, D, N>, grid, dim3(kScoreThreads), ring_bytes(a.pages.n_kv, D) + line, st, a, scale); \
   }
     SEER_FEW(false, 64, 1)
     SEER_FEW(false, 64, 2)
@@ -550,7 +610,7 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
     SEER_FEW(true, 128, 1)
     SEER_FEW(true, 128, 2)
 #undef SEER_FEW
-    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel, sums, dim3(kThreads), 0, st, a);
+    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel, sums, dim3(kSumThreads), 0, st, a);
     return e;
   }
   a.runs = general_runs(num_sms);

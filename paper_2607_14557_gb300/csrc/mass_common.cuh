@@ -33,15 +33,20 @@ __device__ __forceinline__ MassRequest read_request(const MassArgs& a, int b) {
 }
 
 // The request of place x on a line, first[b] the places before request b: by a whole warp, the
-// prefix sums narrowed 32-fold a step.
+// prefix sums narrowed 128-fold a step (four loads a lane, one after the other's heels).
 __device__ __forceinline__ int request_at(const int* first, int B, int x) {
   const int lane = threadIdx.x & 31;
   int b = 0, left = B;
 #pragma unroll 1
   while (left > 1) {
-    const int hop = (left + 31) / 32, k = lane * hop;
-    const unsigned below = __ballot_sync(0xffffffffu, k < left && first[b + k] <= x);
-    const int last = 31 - __clz(below);         // (first[b] <= x)
+    const int hop = (left + 127) / 128;
+    int below = 0;                              // of 128 starts, those at or before x
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int k = (4 * lane + e) * hop;
+      below += k < left && first[b + k] <= x;
+    }
+    const int last = __reduce_add_sync(0xffffffffu, below) - 1;     // (first[b] <= x)
     b += last * hop;
     left = min(hop, left - last * hop);
   }
@@ -93,13 +98,15 @@ __device__ __forceinline__ float2 finish(float2 x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(x.y));
   return make_float2(x.x == -INFINITY ? 0.f : x.x, inv);
 }
-// Key t's new weight into the matrices.
-__device__ __forceinline__ void store_mass(const MassArgs& a, const MassRequest& r, int b, int t, float w) {
+
+// Key t's new weight into the matrices; what it adds to is read before.
+__device__ __forceinline__ float old_mass(const MassArgs& a, const MassRequest& r, int b, int t) {
+  return t < r.kv - r.n && a.keep != 0.f ? a.mass_in[static_cast<size_t>(b) * a.ld_mass + t] : 0.f;
+}
+__device__ __forceinline__ void store_mass(const MassArgs& a, const MassRequest& r, int b, int t, float w, float old) {
   const size_t at = static_cast<size_t>(b) * a.ld_mass + t;
-  const int c = r.kv - r.n;
-  if (t < c && a.keep != 0.f) w = fmaf(a.keep, a.mass_in[at], w);
-  a.mass_out[at] = w;
-  if (a.birth && t >= c) a.birth[at] = t + (a.gone ? a.gone[b] : 0);
+  a.mass_out[at] = fmaf(a.keep, old, w);
+  if (a.birth && t >= r.kv - r.n) a.birth[at] = t + (a.gone ? a.gone[b] : 0);
 }
 
 }  // namespace seer

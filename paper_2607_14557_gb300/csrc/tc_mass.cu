@@ -534,6 +534,7 @@ __global__ void __launch_bounds__(FINAL_THREADS) mass_final_kernel(const MassArg
   const MassRequest r = read_request(a, b);
   const int t = (x - w.tiles[b]) * KEYS + threadIdx.x;
   if (t >= r.kv) return;
+  const float old = old_mass(a, r, b, t);
   const int blocks = (r.look + 2 * z.tpt - 1) / (2 * z.tpt);      // column blocks that the request has
   float sum = 0.f;
 #pragma unroll 1
@@ -544,7 +545,7 @@ __global__ void __launch_bounds__(FINAL_THREADS) mass_final_kernel(const MassArg
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = i0 + 16 + e < 2 * z.slices ? src[(i0 + 16 + e) * step] : 0.f;
   }
-  store_mass(a, r, b, t, sum);
+  store_mass(a, r, b, t, sum, old);
 }
 
 template <bool F16, int DH>
