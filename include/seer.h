@@ -554,7 +554,8 @@ seer_status seer_kv_append_rotary(const void* qkv, int ld_qkv, seer_dtype dt, in
  * Entries from kv_len[b] to ld_mass are untouched.  A request without new rows keeps
  * keep * mass_in.  A row's infinite or NaN scores make its weights NaN for the rows that
  * it sees.  Pages outside the pool read as zeros and are recorded.  Types, heads and
- * head_dim as for seer_attention_tree; weights and sums are fp32.
+ * head_dim as for seer_attention_tree (fp32: n_heads * window at most 16384); weights and
+ * sums are fp32.
  * ws: seer_attention_mass_workspace_size() bytes, 16-byte aligned; calls that share one
  * must not overlap on the GPU; nothing in it needs to start at zero. */
 seer_status seer_attention_mass(const void* q, int ld_q, seer_dtype dt, const int32_t* cu_new, const int32_t* kv_len,

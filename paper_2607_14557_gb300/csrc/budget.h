@@ -59,6 +59,7 @@ struct MassArgs {
   int runs;               // runs that the tiles are cut into at most (set by the launch)
   int* err;
 };
+constexpr int kMassColumns = 16384;          // fp32: n_heads * window at most (their statistics are in a block's shared memory)
 size_t mass_workspace(int type, int B, int T_kv_cap, int n_heads, int n_kv, int head_dim, int window, int num_sms);
 cudaError_t launch_mass(int type, const MassArgs& a, int num_sms, cudaStream_t st);
 // The tensor-core path (tc_mass.cu): 16-bit calls of more columns than launch_mass keeps scores for.

@@ -2,8 +2,10 @@
 // rows, summed over them and over all query heads.
 //   mass[t] = keep mass[t] + sum_h sum_i 2^(s_hi(t) - m_hi) / l_hi,  s = q k log2(e) / sqrt(dh),
 //   m_hi = max_t s_hi(t),  l_hi = sum_t 2^(s_hi(t) - m_hi).
-// A column is one query row of one head.  A softmax's weight needs its whole row first, so the
-// keys are gone through twice: for every column's maximum and sum, then for the weights.
+// A column is one query row of one head.  A softmax's weight needs its whole row first.  Here the
+// scores of one pass over the keys are kept, with each run's maxima and sums per column, and a
+// second kernel joins these and adds up the weights: for fp32, and for 16-bit calls of few columns.
+// (tc_mass.cu: many columns, whose scores would be more than the keys, are multiplied twice.)
 #include "mass_common.cuh"
 
 namespace seer {
@@ -69,67 +71,44 @@ __device__ __forceinline__ void tile_line(const MassArgs& a, int* first, long lo
   }
 }
 
-// Workspace of the general path: per piece of a request's tiles and column (m, l), then per
-// request and column (m, 1 / l).
-__host__ __device__ inline long columns(const MassArgs& a) { return static_cast<long>(a.n_heads) * a.window; }
-__device__ __forceinline__ float2* final_stats(const MassArgs& a) { return static_cast<float2*>(a.ws); }
-__device__ __forceinline__ float2* piece_stats(const MassArgs& a) { return final_stats(a) + a.B * columns(a); }
-
-// ------------------------------------------------------------------ the general path
-// Scores of one 64-key tile and 16 columns on the CUDA cores: keys and queries of a head in
-// shared memory as fp32, a thread 4 columns of one key.
+// Workspace: the prefix sums of the tiles, per piece and column (m, l), the scores as
+// [tile][column][64].
+struct ScoreWork {
+  int* first;             // [B + 1]
+  float2* stats;
+  float* scores;
+};
+__host__ __device__ inline int columns(const MassArgs& a) { return a.n_heads * a.window; }
+__host__ __device__ inline size_t first_bytes(int B) { return (4 * (static_cast<size_t>(B) + 1) + 15) / 16 * 16; }
+// fp32: a unit is 16 columns of a key/value head; a piece's statistics are a unit's.  16-bit: a piece
+// holds all columns.
 constexpr int COLS = 16;
-template <int T>
-__device__ __forceinline__ float load1(const void* p, long i) {
-  if constexpr (T == kF32) return static_cast<const float*>(p)[i];
-  else if constexpr (T == kBF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-  else return __half2float(static_cast<const __half*>(p)[i]);
+__host__ __device__ inline int unit_blocks(int n_heads, int n_kv, int window) { return (n_heads / n_kv * window + COLS - 1) / COLS; }
+__host__ __device__ inline size_t stat_count(bool f32, int B, int runs, int n_heads, int n_kv, int window) {
+  if (f32) {
+    const size_t units = static_cast<size_t>(n_kv) * unit_blocks(n_heads, n_kv, window);
+    return (runs + B * units) * COLS;
+  }
+  return ((runs + static_cast<size_t>(B)) * n_heads * window + 1) / 2 * 2;
 }
+__device__ __forceinline__ ScoreWork score_work(const MassArgs& a, bool f32) {
+  float2* st = reinterpret_cast<float2*>(static_cast<uint8_t*>(a.ws) + first_bytes(a.B));
+  return ScoreWork{static_cast<int*>(a.ws), st, reinterpret_cast<float*>(st + stat_count(f32, a.B, a.runs, a.n_heads, a.pages.n_kv, a.window))};
+}
+
+// ------------------------------------------------------------------ fp32
+// Scores of a 64-key tile and 16 columns at a time on the CUDA cores: keys and queries of a head in
+// shared memory, a thread 4 columns of one key.  Units (request, key/value head, 16 columns) times
+// tiles form the line, so that a small call spreads over the GPU; a run's tiles of a unit leave one
+// (m, l) per column.  Bound by the latency of a step for small calls, by shared memory for large.
 struct TileShared {
   float k[KEYS][132];
   float q[COLS][128];
-  int col_row[COLS];                          // new row of a column counted from the first that looks, -1: none
+  long row[2][KEYS];                          // pool rows of this tile's keys and the next one's, -1: zeros
+  int place[COLS];                            // a column's row among those that look, -1: none
 };
-template <int T>
-__device__ __forceinline__ void load_queries(const MassArgs& a, const MassRequest& r, int b, int kvh, int col0, TileShared& sh) {
-  const int dh = a.pages.head_dim, g = a.n_heads / a.pages.n_kv;
-  for (int x = threadIdx.x; x < COLS * dh; x += kThreads) {
-    const int j = x / dh, d = x - j * dh, col = col0 + j, i = col / g;
-    int row = -1;
-    if (i < r.look) row = query_row(a, r, b, i, false);
-    sh.q[j][d] = row < 0 ? 0.f : load1<T>(a.q, row * a.ld_q + static_cast<long>(kvh * g + col % g) * dh + d);
-    if (d == 0) sh.col_row[j] = row < 0 ? -1 : i;
-  }
-}
-template <int T>
-__device__ __forceinline__ void load_keys(const MassArgs& a, const MassRequest& r, int b, int kvh, int t0, TileShared& sh, bool report) {
-  const int dh = a.pages.head_dim;
-  for (int x = threadIdx.x; x < KEYS * dh; x += kThreads) {
-    const int j = x / dh, d = x - j * dh;
-    const long row = t0 + j < r.kv ? key_row(a, b, t0 + j, report && d == 0) : -1;
-    sh.k[j][d] = row < 0 ? 0.f : load1<T>(a.pages.kv, (row * 2 * a.pages.n_kv + kvh) * dh + d);
-  }
-}
-// Scores of this thread's key (threadIdx.x % 64) and columns 4 (threadIdx.x / 64) .. + 3.
-__device__ __forceinline__ void tile_scores(int dh, float scale, const TileShared& sh, float (&s)[4]) {
-  const int key = threadIdx.x % KEYS, c0 = threadIdx.x / KEYS * 4;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) s[e] = 0.f;
-  for (int d = 0; d < dh; d += 4) {
-    const float4 k = *reinterpret_cast<const float4*>(&sh.k[key][d]);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float4 q = *reinterpret_cast<const float4*>(&sh.q[c0 + e][d]);
-      s[e] = fmaf(k.w, q.w, fmaf(k.z, q.z, fmaf(k.y, q.y, fmaf(k.x, q.x, s[e]))));
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) s[e] = __fmul_rn(s[e], scale);   // rounded: both passes then see one value
-}
 
-// Maxima and sums: the tiles of all requests and key/value heads on one line, a run a block.
-template <int T>
-__global__ void __launch_bounds__(kThreads) mass_stats_kernel(const MassArgs a, const float scale) {
+__global__ void __launch_bounds__(kThreads) mass_scores_f32_kernel(const MassArgs a, const float scale) {
   pdl_enter();
   extern __shared__ __align__(16) uint8_t smem[];
   TileShared& sh = *reinterpret_cast<TileShared*>(smem);
@@ -137,123 +116,93 @@ __global__ void __launch_bounds__(kThreads) mass_stats_kernel(const MassArgs a, 
   __shared__ long long warp_sum[kThreads / 32];
   __shared__ float2 halves[kThreads / 32][4];
   tile_line(a, first, warp_sum, blockIdx.x == 0);
-  const int hk = a.pages.n_kv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = a.n_heads / hk;
-  const int total = first[a.B] * hk, length = run_length(total, a.runs), run = blockIdx.x;
-  int at = min(run * length, total);
-  const int end = min(at + length, total);
+  const ScoreWork w = score_work(a, true);
+  const int hk = a.pages.n_kv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = a.n_heads / hk, cc = g * a.window;
+  const int blocks = unit_blocks(a.n_heads, hk, a.window), units = hk * blocks, dh = a.pages.head_dim, chunks = dh / 4;
+  if (blockIdx.x == 0)
+    for (int b = tid; b <= a.B; b += kThreads) w.first[b] = first[b];
+  const int total = first[a.B] * units, length = run_length(total, a.runs), run = blockIdx.x;
+  int at = min(static_cast<long long>(run) * length, static_cast<long long>(total));
+  const int end = min(static_cast<long long>(at) + length, static_cast<long long>(total));
+#pragma unroll 1
   while (at < end) {
-    // unit (b, kvh): tiles first[b] * hk + kvh * tiles ..
-    const int b = request_at(first, a.B, at / hk);
+    const int b = request_at(first, a.B, at / units);
     const MassRequest r = read_request(a, b);
-    const int tiles = tiles_of(r);
-    const int inside = at - first[b] * hk, kvh = inside / tiles, tile0 = inside - kvh * tiles;
-    const int tile1 = min(tiles, tile0 + (end - at));
+    const int tiles = tiles_of(r), inside = at - first[b] * units, unit = inside / tiles, tile0 = inside - unit * tiles;
+    const int tile1 = min(tiles, tile0 + (end - at)), kvh = unit / blocks, col0 = (unit - kvh * blocks) * COLS;
     at += tile1 - tile0;
-    float2* out = piece_stats(a) + (run + static_cast<long>(b) * hk + kvh) * (static_cast<long>(g) * a.window);
-    for (int col0 = 0; col0 < r.look * g; col0 += COLS) {
-      __syncthreads();
-      load_queries<T>(a, r, b, kvh, col0, sh);
-      float2 stat[4];
+    if (col0 >= r.look * g) continue;
+    const auto look_up = [&](int tile, long (&rows)[KEYS]) {
+      if (tid < KEYS) rows[tid] = tile < tile1 && tile * KEYS + tid < r.kv ? key_row(a, b, tile * KEYS + tid, true) : -1;
+    };
+    __syncthreads();                            // the unit before is done with the queries
+    look_up(tile0, sh.row[0]);
+#pragma unroll 2
+    for (int x = tid; x < COLS * chunks; x += kThreads) {
+      const int j = x / chunks, c = x - j * chunks, col = col0 + j, i = col / g;
+      const int row = i < r.look && col < cc ? query_row(a, r, b, i, false) : -1;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row >= 0) v = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + row * a.ld_q + static_cast<long>(kvh * g + col % g) * dh)[c];
+      *reinterpret_cast<float4*>(&sh.q[j][4 * c]) = v;
+      if (c == 0) sh.place[j] = row < 0 ? -1 : i;
+    }
+    float2 stat[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) stat[e] = make_float2(-INFINITY, 0.f);
-      for (int tile = tile0; tile < tile1; ++tile) {
-        __syncthreads();
-        load_keys<T>(a, r, b, kvh, tile * KEYS, sh, true);
-        __syncthreads();
-        float s[4];
-        tile_scores(a.pages.head_dim, scale, sh, s);
-        const int t = tile * KEYS + tid % KEYS;
+    for (int e = 0; e < 4; ++e) stat[e] = make_float2(-INFINITY, 0.f);
+    const int key = tid % KEYS, c0 = tid / KEYS * 4;
+#pragma unroll 1
+    for (int tile = tile0; tile < tile1; ++tile) {
+      const int now = (tile - tile0) & 1;
+      __syncthreads();                          // rows are there, the tile before is done with the keys
+#pragma unroll 1
+      for (int x0 = tid; x0 < KEYS * chunks; x0 += 4 * kThreads) {
+        float4 v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int i = sh.col_row[tid / KEYS * 4 + e];
-          if (i >= 0 && t <= r.kv - r.look + i && t < r.kv) stat[e] = join(stat[e], make_float2(s[e] == s[e] ? s[e] : -INFINITY, s[e] == s[e] ? 1.f : s[e]));
+          const int x = min(x0 + e * kThreads, KEYS * chunks - 1), j = x / chunks;
+          const long row = sh.row[now][j];
+          v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (row >= 0) v[e] = reinterpret_cast<const float4*>(static_cast<const float*>(a.pages.kv) + (row * 2 * hk + kvh) * dh)[x - j * chunks];
         }
-      }
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float2 other = make_float2(__shfl_xor_sync(0xffffffffu, stat[e].x, off), __shfl_xor_sync(0xffffffffu, stat[e].y, off));
-          stat[e] = join(stat[e], other);
-        }
-      if (lane == 0)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) halves[warp][e] = stat[e];
-      __syncthreads();
-      if (tid < COLS && col0 + tid < r.look * g) out[col0 + tid] = join(halves[tid / 4 * 2][tid % 4], halves[tid / 4 * 2 + 1][tid % 4]);
-    }
-  }
-}
-
-// A column's pieces in order of their keys: a block per (request, key/value head).
-__global__ void __launch_bounds__(kThreads) mass_join_kernel(const MassArgs a) {
-  pdl_enter();
-  extern __shared__ int first[];
-  __shared__ long long warp_sum[kThreads / 32];
-  tile_line(a, first, warp_sum, false);
-  const int hk = a.pages.n_kv, g = a.n_heads / hk;
-  const int total = first[a.B] * hk, length = run_length(total, a.runs);
-  for (long long unit = blockIdx.x; unit < static_cast<long long>(a.B) * hk; unit += gridDim.x) {
-    const int b = static_cast<int>(unit / hk), kvh = static_cast<int>(unit % hk);
-    const int tiles = first[b + 1] - first[b];
-    if (tiles == 0) continue;
-    const MassRequest r = read_request(a, b);
-    const int at = first[b] * hk + kvh * tiles, c0 = at / length, c1 = (at + tiles - 1) / length;
-    for (int col = threadIdx.x; col < r.look * g; col += kThreads) {
-      float2 s = make_float2(-INFINITY, 0.f);
-      for (int c = c0; c <= c1; ++c) s = join(s, piece_stats(a)[(c + unit) * (static_cast<long>(g) * a.window) + col]);
-      // an entry outside the draft has no weights
-      final_stats(a)[b * columns(a) + static_cast<long>(kvh) * g * a.window + col] =
-          query_row(a, r, b, col / g, kvh == 0) < 0 ? make_float2(0.f, 0.f) : finish(s);
-    }
-  }
-}
-
-// The weights: a block a tile of keys, all heads' columns in order.
-template <int T>
-__global__ void __launch_bounds__(kThreads) mass_weights_kernel(const MassArgs a, const float scale) {
-  pdl_enter();
-  extern __shared__ __align__(16) uint8_t smem[];
-  TileShared& sh = *reinterpret_cast<TileShared*>(smem);
-  int* first = reinterpret_cast<int*>(smem + sizeof(TileShared));
-  __shared__ long long warp_sum[kThreads / 32];
-  __shared__ float sums[kThreads];
-  __shared__ float2 stat[COLS];
-  tile_line(a, first, warp_sum, false);
-  const int hk = a.pages.n_kv, tid = threadIdx.x, g = a.n_heads / hk;
-  for (int x = blockIdx.x; x < first[a.B]; x += gridDim.x) {
-    const int b = request_at(first, a.B, x);
-    const MassRequest r = read_request(a, b);
-    const int t0 = (x - first[b]) * KEYS, t = t0 + tid % KEYS;
-    float sum = 0.f;
-    if (r.look > 0)
-      for (int kvh = 0; kvh < hk; ++kvh) {
-        __syncthreads();
-        load_keys<T>(a, r, b, kvh, t0, sh, false);
-        for (int col0 = 0; col0 < r.look * g; col0 += COLS) {
-          __syncthreads();
-          load_queries<T>(a, r, b, kvh, col0, sh);
-          if (tid < COLS && col0 + tid < r.look * g)
-            stat[tid] = final_stats(a)[b * columns(a) + static_cast<long>(kvh) * g * a.window + col0 + tid];
-          __syncthreads();
-          float s[4];
-          tile_scores(a.pages.head_dim, scale, sh, s);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int j = tid / KEYS * 4 + e, i = sh.col_row[j];
-            if (i >= 0 && t <= r.kv - r.look + i) sum += ex2(s[e] - stat[j].x) * stat[j].y;
-          }
+          const int x = min(x0 + e * kThreads, KEYS * chunks - 1), j = x / chunks;
+          *reinterpret_cast<float4*>(&sh.k[j][4 * (x - j * chunks)]) = v[e];
         }
       }
-    __syncthreads();
-    sums[tid] = sum;
-    __syncthreads();
-    if (tid < KEYS && t < r.kv) {
-      float w = 0.f;
+      look_up(tile + 1, sh.row[now ^ 1]);
+      __syncthreads();
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+      for (int d = 0; d < dh; d += 4) {
+        const float4 k = *reinterpret_cast<const float4*>(&sh.k[key][d]);
 #pragma unroll
-      for (int e = 0; e < kThreads / KEYS; ++e) w += sums[e * KEYS + tid];
-      store_mass(a, r, b, t, w, old_mass(a, r, b, t));
+        for (int e = 0; e < 4; ++e) {
+          const float4 q = *reinterpret_cast<const float4*>(&sh.q[c0 + e][d]);
+          s[e] = fmaf(k.w, q.w, fmaf(k.z, q.z, fmaf(k.y, q.y, fmaf(k.x, q.x, s[e]))));
+        }
+      }
+      const int t = tile * KEYS + key;
+      float* out = w.scores + (static_cast<size_t>(first[b] + tile) * hk + kvh) * cc * KEYS + key;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = __fmul_rn(s[e], scale);  // as it is kept
+        if (col0 + c0 + e < cc) out[(col0 + c0 + e) * KEYS] = v;
+        const int i = sh.place[c0 + e];
+        if (i >= 0 && t <= r.kv - r.look + i) stat[e] = join(stat[e], make_float2(v == v ? v : -INFINITY, v == v ? 1.f : v));
+      }
     }
+#pragma unroll 1
+    for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        stat[e] = join(stat[e], make_float2(__shfl_xor_sync(0xffffffffu, stat[e].x, off), __shfl_xor_sync(0xffffffffu, stat[e].y, off)));
+    if (lane == 0)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) halves[warp][e] = stat[e];
+    __syncthreads();
+    if (tid < COLS)
+      w.stats[(run + static_cast<size_t>(b) * units + unit) * COLS + tid] = join(halves[tid / 4 * 2][tid % 4], halves[tid / 4 * 2 + 1][tid % 4]);
   }
 }
 
@@ -265,22 +214,8 @@ __global__ void __launch_bounds__(kThreads) mass_weights_kernel(const MassArgs a
 // free, so a lane's 16 bytes of a row serve as the k-indices that the fragment wants from it, and Q
 // is cut alike.  A lane keeps the maxima and sums of its two columns over its keys.
 constexpr int kFewCols = 16;                // columns of a key/value head at most
-constexpr int kFewStats = 1024;             // of all heads
+constexpr int kFewAll = 1024;               // of all heads
 constexpr int GROUP = 16;                   // keys of a step
-
-// Workspace: the prefix sums of the tiles, per piece and column (m, l), the scores as
-// [tile][column][64].
-struct FewWork {
-  int* first;             // [B + 1]
-  float2* stats;
-  float* scores;
-};
-__host__ __device__ inline size_t few_first(int B) { return (4 * (static_cast<size_t>(B) + 1) + 15) / 16 * 16; }
-__host__ __device__ inline size_t few_stats(int B, int runs, long cols) { return ((runs + static_cast<size_t>(B)) * cols + 1) / 2 * 2; }
-__device__ __forceinline__ FewWork few_work(const MassArgs& a) {
-  float2* st = reinterpret_cast<float2*>(static_cast<uint8_t*>(a.ws) + few_first(a.B));
-  return FewWork{static_cast<int*>(a.ws), st, reinterpret_cast<float*>(st + few_stats(a.B, a.runs, columns(a)))};
-}
 
 template <bool F16>
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -330,12 +265,12 @@ __global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const Mas
   tile_line(a, first, warp_sum, blockIdx.x == 0);
   const int total = first[a.B], length = run_length(total, a.runs), run = blockIdx.x;
   if (run == 0)
-    for (int b = tid; b <= a.B; b += kScoreThreads) few_work(a).first[b] = first[b];
+    for (int b = tid; b <= a.B; b += kScoreThreads) score_work(a, false).first[b] = first[b];
   int at = run * length;
   const int end = min(at + length, total);
   if (at >= end) return;
   const int hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window;
-  const FewWork w = few_work(a);
+  const ScoreWork w = score_work(a, false);
   // warps of a head: its keys are dealt to them 16 at a time
   const int heads = min(hk, kWarps), per_head = kWarps / heads;
   const int pitch = heads * DH * 2 + 64, stage = stage_bytes(heads, DH);
@@ -505,14 +440,15 @@ __global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const Mas
 // thread's first scores are loaded before it is known whose the tile is (any tile's memory is
 // there), and the code is kept short: its first instructions come from memory too.
 constexpr int kEarly = 16, kSumThreads = 2 * KEYS;
+template <bool F32>
 __global__ void __launch_bounds__(kSumThreads) mass_sums_kernel(const MassArgs a) {
   pdl_enter();
-  __shared__ float2 stat[kFewStats + kEarly];   // (m, 1 / l) of every column
-  __shared__ uint8_t row_of[kFewStats + kEarly];   // its row among those that look
+  extern __shared__ float2 stat[];              // (m, 1 / l) of every column
   __shared__ float sums[kSumThreads];
   const int tid = threadIdx.x, part = tid / KEYS, key = tid % KEYS, tile = blockIdx.x;
   const int hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window, all = hk * cc;
-  const FewWork w = few_work(a);
+  uint8_t* row_of = reinterpret_cast<uint8_t*>(stat + all + kEarly);      // a column's row among those that look
+  const ScoreWork w = score_work(a, F32);
   const float* src = w.scores + (static_cast<size_t>(tile) * all + part * kEarly) * KEYS + key;
   float s[kEarly];
 #pragma unroll
@@ -520,8 +456,8 @@ __global__ void __launch_bounds__(kSumThreads) mass_sums_kernel(const MassArgs a
   const int total = w.first[a.B];
   if (tile >= total) return;
   const int b = request_at(w.first, a.B, tile);
-  const int t0 = w.first[b], length = run_length(total, a.runs);
-  const int c0 = t0 / length, c1 = (w.first[b + 1] - 1) / length;
+  const int blocks = unit_blocks(a.n_heads, hk, a.window), units = F32 ? hk * blocks : 1;
+  const int t0 = w.first[b], tiles = w.first[b + 1] - t0, length = run_length(total * units, a.runs);
   const MassRequest r = read_request(a, b);
   const int t = (tile - t0) * KEYS + key;
   const float old = tid < KEYS && t < r.kv ? old_mass(a, r, b, t) : 0.f;
@@ -530,14 +466,16 @@ __global__ void __launch_bounds__(kSumThreads) mass_sums_kernel(const MassArgs a
     float2 f = make_float2(-INFINITY, 0.f);
     const int col = x % cc;
     if (col < r.look * g) {
-      const float2* from = w.stats + (static_cast<size_t>(b) + c0) * all + x;
+      const int kvh = x / cc, unit = F32 ? kvh * blocks + col / COLS : 0, place = t0 * units + unit * tiles;
+      const int c0 = place / length, c1 = (place + tiles - 1) / length, hop = F32 ? COLS : all;
+      const float2* from = w.stats + (static_cast<size_t>(b) * units + unit + c0) * hop + (F32 ? col % COLS : x);
 #pragma unroll 1
       for (int c = c0; c <= c1; c += 8) {       // in order of the keys, eight loads under way
         float2 piece[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) piece[e] = c + e <= c1 ? from[e * all] : make_float2(-INFINITY, 0.f);
+        for (int e = 0; e < 8; ++e) piece[e] = c + e <= c1 ? from[e * hop] : make_float2(-INFINITY, 0.f);
         f = join8(f, piece);
-        from += 8 * all;
+        from += 8 * hop;
       }
       f = query_row(a, r, b, col / g, x < cc && tile == t0) < 0 ? make_float2(0.f, 0.f) : finish(f);
     }
@@ -565,77 +503,60 @@ __global__ void __launch_bounds__(kSumThreads) mass_sums_kernel(const MassArgs a
   if (tid < KEYS && t < r.kv) store_mass(a, r, b, t, sums[tid] + sums[KEYS + tid], old);
 }
 
-int general_runs(int num_sms) { return 2 * num_sms; }
-int few_runs(int num_sms) { return 2 * num_sms; }
-bool few_columns(int type, int n_heads, int n_kv, int window) {
-  const long cols = static_cast<long>(n_heads / n_kv) * window;
-  return type != kF32 && cols <= kFewCols && cols * n_kv <= kFewStats;
+int score_runs(bool f32, int num_sms) { return (f32 ? 4 : 2) * num_sms; }
+bool few_columns(int n_heads, int n_kv, int window) {
+  return n_heads / n_kv * window <= kFewCols && n_heads * window <= kFewAll;
 }
 
 }  // namespace
 
-bool mass_on_tensor_cores(int type, int n_heads, int n_kv, int window) { return type != kF32 && !few_columns(type, n_heads, n_kv, window); }
+bool mass_on_tensor_cores(int type, int n_heads, int n_kv, int window) { return type != kF32 && !few_columns(n_heads, n_kv, window); }
 
 size_t mass_workspace(int type, int B, int T_kv_cap, int n_heads, int n_kv, int head_dim, int window, int num_sms) {
-  const size_t cols = static_cast<size_t>(n_heads) * window, unit = static_cast<size_t>(n_heads / n_kv) * window;
   if (mass_on_tensor_cores(type, n_heads, n_kv, window)) return tc_mass_workspace(B, T_kv_cap, n_heads, n_kv, window, num_sms);
-  if (few_columns(type, n_heads, n_kv, window))
-    return few_first(B) + 8 * few_stats(B, few_runs(num_sms), cols) + 4 * KEYS * cols * (static_cast<size_t>(T_kv_cap) / KEYS + B);
-  return 8 * (B * cols + (general_runs(num_sms) + static_cast<size_t>(B) * n_kv) * unit);
+  const bool f32 = type == kF32;
+  return first_bytes(B) + 8 * stat_count(f32, B, score_runs(f32, num_sms), n_heads, n_kv, window) +
+         4 * KEYS * static_cast<size_t>(n_heads) * window * (static_cast<size_t>(T_kv_cap) / KEYS + B);
 }
 
 cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_t st) {
   MassArgs a = args;
+  const bool f32 = type == kF32;
   const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(a.pages.head_dim));
   const int line = (a.B + 1) * static_cast<int>(sizeof(int)), most_line = (kPageTableMaxB + 1) * static_cast<int>(sizeof(int));
-  if (few_columns(type, a.n_heads, a.pages.n_kv, a.window)) {
-    a.runs = few_runs(num_sms);
-    const int most_tiles = tile_capacity(a);
-    const dim3 grid(most_tiles < a.runs ? most_tiles : a.runs), sums(most_tiles);
-    const int wide = a.n_heads / a.pages.n_kv * a.window > 8;
-    cudaError_t e = cudaErrorInvalidValue;
+  const int most_tiles = tile_capacity(a), sums_smem = 9 * (columns(a) + kEarly);
+  a.runs = score_runs(f32, num_sms);
+  cudaError_t e = cudaErrorInvalidValue;
+  if (f32) {
+    static bool set0[64] = {}, set1[64] = {};
+    const long places = static_cast<long>(most_tiles) * a.pages.n_kv * unit_blocks(a.n_heads, a.pages.n_kv, a.window);
+    const dim3 grid(static_cast<unsigned>(places < a.runs ? places : a.runs));
+    e = set_smem_limit_once(mass_scores_f32_kernel, static_cast<int>(sizeof(TileShared)) + most_line, set0);
+    if (e == cudaSuccess) e = set_smem_limit_once(mass_sums_kernel<true>, 9 * (kMassColumns + kEarly), set1);
+    if (e == cudaSuccess) e = launch_kernel(mass_scores_f32_kernel, grid, dim3(kThreads), sizeof(TileShared) + line, st, a, scale);
+    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel<true>, dim3(most_tiles), dim3(kSumThreads), sums_smem, st, a);
+    return e;
+  }
+  const dim3 grid(most_tiles < a.runs ? most_tiles : a.runs);
+  const int wide = a.n_heads / a.pages.n_kv * a.window > 8;
 #define SEER_FEW(F, D, N)                                                                       \
   if ((type == kF16) == F && a.pages.head_dim == D && wide == N - 1) {                          \
     static bool set[64] = {};                                                                   \
-    e = set_smem_limit_once(mass_scores_kernel<F, D, N>, ring_bytes(1, D) + most_line, set);       \
+    e = set_smem_limit_once(mass_scores_kernel<F, D, N>, ring_bytes(1, D) + most_line, set);    \
     if (e == cudaSuccess)                                                                       \
       e = launch_kernel(mass_scores_kernel<F, D, N>, grid, dim3(kScoreThreads), ring_bytes(a.pages.n_kv, D) + line, st, a, scale); \
   }
-    SEER_FEW(false, 64, 1)
-    SEER_FEW(false, 64, 2)
-    SEER_FEW(false, 128, 1)
-    SEER_FEW(false, 128, 2)
-    SEER_FEW(true, 64, 1)
-    SEER_FEW(true, 64, 2)
-    SEER_FEW(true, 128, 1)
-    SEER_FEW(true, 128, 2)
+  SEER_FEW(false, 64, 1)
+  SEER_FEW(false, 64, 2)
+  SEER_FEW(false, 128, 1)
+  SEER_FEW(false, 128, 2)
+  SEER_FEW(true, 64, 1)
+  SEER_FEW(true, 64, 2)
+  SEER_FEW(true, 128, 1)
+  SEER_FEW(true, 128, 2)
 #undef SEER_FEW
-    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel, sums, dim3(kSumThreads), 0, st, a);
-    return e;
-  }
-  a.runs = general_runs(num_sms);
-  const int smem = static_cast<int>(sizeof(TileShared)) + line, most = static_cast<int>(sizeof(TileShared)) + most_line;
-  const long units = static_cast<long>(a.B) * a.pages.n_kv;
-  const int joins = static_cast<int>(units < 4l * num_sms ? units : 4l * num_sms);
-  const int tiles = tile_capacity(a) < 4 * num_sms ? tile_capacity(a) : 4 * num_sms;
-  {
-    static bool set[64] = {};
-    const cudaError_t e = set_smem_limit_once(mass_join_kernel, most_line, set);
-    if (e != cudaSuccess) return e;
-  }
-#define SEER_MASS(T)                                                                                          \
-  if (type == T) {                                                                                            \
-    static bool set0[64] = {}, set1[64] = {};                                                                 \
-    cudaError_t e = set_smem_limit_once(mass_stats_kernel<T>, most, set0);                                    \
-    if (e == cudaSuccess) e = set_smem_limit_once(mass_weights_kernel<T>, most, set1);                        \
-    if (e == cudaSuccess) e = launch_kernel(mass_stats_kernel<T>, dim3(a.runs), dim3(kThreads), smem, st, a, scale); \
-    if (e == cudaSuccess) e = launch_kernel(mass_join_kernel, dim3(joins), dim3(kThreads), line, st, a);      \
-    if (e == cudaSuccess) e = launch_kernel(mass_weights_kernel<T>, dim3(tiles), dim3(kThreads), smem, st, a, scale); \
-    return e;                                                                                                 \
-  }
-  SEER_MASS(kF32)
-#undef SEER_MASS
-  return cudaErrorInvalidValue;
+  if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel<false>, dim3(most_tiles), dim3(kSumThreads), sums_smem, st, a);
+  return e;
 }
 
 }  // namespace seer

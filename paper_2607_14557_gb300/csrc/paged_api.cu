@@ -156,8 +156,10 @@ seer_status check_mass(int B, int T_kv_cap, int n_heads, int n_kv, int head_dim,
   if (T_kv_cap < 0) return fail(SEER_ERR_INVALID_ARG, "attention mass: bad sizes");
   if (window < 1 || window > SEER_MAX_DRAFT)
     return fail(SEER_ERR_INVALID_ARG, "attention mass: window must be in [1, %d]", SEER_MAX_DRAFT);
-  // tiles of 64 keys times heads times column blocks are counted in 32 bits
-  if ((T_kv_cap / 64.0 + B) * n_kv * (static_cast<double>(n_heads) / n_kv * window / 128 + 1) > 2147483647.0)
+  if (dt == SEER_F32 && static_cast<long long>(n_heads) * window > kMassColumns)
+    return fail(SEER_ERR_UNSUPPORTED, "attention mass: fp32 takes at most %d heads times rows", kMassColumns);
+  // tiles of 64 keys times heads times blocks of 16 columns are counted in 32 bits
+  if ((T_kv_cap / 64.0 + B) * n_kv * (static_cast<double>(n_heads) / n_kv * window / 16 + 1) > 2147483647.0)
     return fail(SEER_ERR_UNSUPPORTED, "attention mass: more than 2^31 key tiles");
   return SEER_OK;
 }

@@ -93,7 +93,8 @@ def mass(pg=None, **kw):
     (dict(acc=P, n_acc=P, draft=65), INVALID), (dict(window=0), INVALID), (dict(window=65), INVALID), (dict(B=0), INVALID),
     (dict(B=S.MAX_REQUESTS + 1), UNSUPPORTED), (dict(T=-1), INVALID), (dict(T_kv=-1), INVALID), (dict(hq=3), INVALID),
     (dict(keep=math.nan), INVALID), (dict(mass_in=None), INVALID), (dict(mass_out=None), INVALID), (dict(ld_mass=0), INVALID),
-    (dict(pg=dict(head_dim=80)), UNSUPPORTED), (dict(pg=dict(table=None)), INVALID), (dict(pages=None), INVALID)])
+    (dict(pg=dict(head_dim=80)), UNSUPPORTED), (dict(pg=dict(table=None)), INVALID), (dict(pages=None), INVALID),
+    (dict(dt=0, hq=1026, ld=1026 * 64, window=16), UNSUPPORTED), (dict(B=16384, T_kv=2 ** 31 - 1, window=64, hq=128, ld=8192), UNSUPPORTED)])
 def test_mass_refuses(kw, status):
     assert mass(**kw) == status
 
