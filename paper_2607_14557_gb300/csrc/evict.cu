@@ -11,45 +11,37 @@ namespace {
 // 32-bit key: the mass as an ordered integer below the three values that NaN, sinks and recent
 // rows take.  The K-th largest key is found 11, 11 and 10 bits at a time by histograms, the
 // rows equal to it that stay are the lowest, and two counts over the rows number the moves.
-// A cluster of CTAs takes a request, each a stretch of its rows, whose keys stay in shared
-// memory across the passes (from the matrices again where they do not fit); histograms and
-// counts meet through distributed shared memory.  Sums of integers: the order of the atomics
+// A CTA takes a request, or a cluster of CTAs a long one, each a stretch of its rows, whose keys stay
+// in shared memory across the passes (from the matrices again where they do not fit).  In a cluster
+// the CTAs add their histograms' filled bins to the first one's, which finds the bin and tells the
+// others (all reading all: 5 us a pass of 16 CTAs).  Sums of integers: the order of the atomics
 // leaves no trace.
-constexpr int kSelThreads = 512;
+constexpr int kSelThreads = 1024;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelKeys = 16384;             // keys of a CTA in shared memory
 constexpr int kBins = 2048;
+constexpr long kRankRows = 8192;            // of a request per CTA, while the GPU has room for more CTAs
+constexpr int kMostRanks = 16;
 constexpr int kAhead = 4;                   // rows of a thread whose loads are under way
 constexpr uint32_t kKeyRecent = 0xffffffffu, kKeySink = 0xfffffffeu, kKeyNan = 0xfffffffdu;
 
 struct SelShared {
-  unsigned hist[2][kBins];                  // of this CTA, by turns
-  uint4 counts[kSelWarps];                  // per warp: rows above, at the key before K, above, at it behind
+  unsigned hist[3][kBins];                  // of this CTA; the first one's become the cluster's
+  uint4 totals[kMostRanks];                 // per CTA: rows above / at the key before K, above / at it behind
+  uint4 counts[kSelWarps];                  // the same per warp of this CTA
   unsigned warp_sum[kSelWarps];
   unsigned found_bin, found_above;
   uint32_t keys[kSelKeys];
 };
 
-__device__ __forceinline__ uint4 ld_cluster4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void add_cluster(uint32_t addr, unsigned v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
-// The four words at p, summed over the cluster's CTAs.
-template <int RANKS>
-__device__ __forceinline__ uint4 sum_over_ranks(const unsigned* p) {
-  if constexpr (RANKS == 1) return *reinterpret_cast<const uint4*>(p);
-  uint4 v[RANKS], s = make_uint4(0, 0, 0, 0);
-#pragma unroll
-  for (int r = 0; r < RANKS; ++r) v[r] = ld_cluster4(cluster_addr(p, r));
-#pragma unroll
-  for (int r = 0; r < RANKS; ++r) {
-    s.x += v[r].x;
-    s.y += v[r].y;
-    s.z += v[r].z;
-    s.w += v[r].w;
-  }
-  return s;
+__device__ __forceinline__ void st_cluster(uint32_t addr, unsigned v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void st_cluster4(uint32_t addr, uint4 v) {
+  asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 template <int RANKS>
 __device__ __forceinline__ void sync_ranks() {
@@ -65,20 +57,20 @@ __device__ __forceinline__ uint32_t mass_key(float m) {
 
 template <int RANKS>
 __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectArgs a) {
-  constexpr int ranks = RANKS;
   extern __shared__ __align__(16) uint8_t smem[];
   SelShared& sh = *reinterpret_cast<SelShared*>(smem);
-  pdl_enter();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int b = blockIdx.x / ranks, rank = blockIdx.x % ranks;
+  for (int i = tid; i < 3 * kBins; i += kSelThreads) (&sh.hist[0][0])[i] = 0;
+  pdl_enter();
+  const int b = blockIdx.x / RANKS, rank = blockIdx.x % RANKS;
   const int L0 = a.kv_len[b], budget = a.budget[b], gone = a.gone ? a.gone[b] : 0;
-  bool good = L0 >= 0 && L0 <= a.ld_mass && budget >= 0;
-  const int L = good ? L0 : 0, K = good ? min(budget, L) : 0;
-  if (good && min(K, L - K) > a.ld_move) good = false;
-  if (!good || K == L || K == 0) {          // nothing to choose; every rank has read the lengths before one writes
-    sync_ranks<RANKS>();
+  sync_ranks<RANKS>();                      // every CTA's histograms are zero, and the lengths read before one writes
+  const bool sound = L0 >= 0 && L0 <= a.ld_mass && budget >= 0;
+  const int L = sound ? L0 : 0, K = sound ? min(budget, L) : 0;
+  const bool good = sound && min(K, L - K) <= a.ld_move;
+  if (!good || K == L || K == 0) {          // nothing to choose
     if (rank == 0 && tid == 0) {
-      if (!good) record_error(a.err, L0 >= 0 && L0 <= a.ld_mass && budget >= 0 ? kErrCapacity : kErrLayout);
+      if (!good) record_error(a.err, sound ? kErrCapacity : kErrLayout);
       a.len_out[b] = good ? K : L0;
       a.gone_out[b] = gone + (good ? L - K : 0);
       a.n_moves[b] = 0;
@@ -87,7 +79,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
   }
   const long long young = static_cast<long long>(L) + gone - min(a.recent, K);
   // rank's rows [r0, r1), a warp's [w0, w1) of them: both multiples of 32 from their starts
-  const int share = ((L + ranks - 1) / ranks + 31) / 32 * 32;
+  const int share = ((L + RANKS - 1) / RANKS + 31) / 32 * 32;
   const int r0 = static_cast<int>(min(static_cast<long long>(L), static_cast<long long>(share) * rank));
   const int r1 = static_cast<int>(min(static_cast<long long>(L), static_cast<long long>(r0) + share));
   const bool held = r1 - r0 <= kSelKeys;
@@ -97,14 +89,12 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
   const auto key_of = [&](int t) { return held ? sh.keys[t - r0] : row_key(birth[t], mass[t]); };
 
   // ---- the K-th largest key
-  for (int i = tid; i < 2 * kBins; i += kSelThreads) (&sh.hist[0][0])[i] = 0;
-  __syncthreads();
   uint32_t prefix = 0;
   unsigned need = K;                        // rows with the prefix that stay
 #pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? kBins / 2 : kBins;
-    unsigned* hist = sh.hist[pass & 1];
+    unsigned* hist = sh.hist[pass];
     if (pass == 0) {
 #pragma unroll 1
       for (int t0 = r0 + tid; t0 < r1; t0 += kAhead * kSelThreads) {
@@ -128,62 +118,61 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
       }
     } else {
       const int above = pass == 1 ? 21 : 10;
-#pragma unroll 1
+#pragma unroll 2
       for (int t = r0 + tid; t < r1; t += kSelThreads) {
         const uint32_t k = key_of(t);
         if ((k >> above) == (prefix >> above)) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
       }
     }
+    if (RANKS > 1) {
+      __syncthreads();
+      if (rank != 0)
+        for (int i = tid; i < bins; i += kSelThreads) {
+          const unsigned v = hist[i];
+          if (v != 0) add_cluster(cluster_addr(hist + i, 0), v);
+        }
+    }
     sync_ranks<RANKS>();
-    // thread i owns the bins [4 i, 4 i + 4) counted from the top
-    uint4 own = make_uint4(0, 0, 0, 0);
-    const int low = bins - 4 - 4 * tid;
-    if (low >= 0) own = sum_over_ranks<RANKS>(hist + low);
-    const unsigned sum = own.x + own.y + own.z + own.w;
-    unsigned inc = sum;
+    if (rank == 0) {
+      // thread i owns the bins 2 i and 2 i + 1 counted from the top
+      const int low = bins - 2 - 2 * tid;
+      uint2 own = make_uint2(0, 0);
+      if (low >= 0) own = *reinterpret_cast<const uint2*>(hist + low);
+      const unsigned sum = own.x + own.y;
+      unsigned inc = sum;
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const unsigned v = __shfl_up_sync(0xffffffffu, inc, off);
-      if (lane >= off) inc += v;
+      for (int off = 1; off < 32; off <<= 1) {
+        const unsigned v = __shfl_up_sync(0xffffffffu, inc, off);
+        if (lane >= off) inc += v;
+      }
+      if (lane == 31) sh.warp_sum[warp] = inc;
+      __syncthreads();
+      unsigned before = inc - sum + __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_sum[lane] : 0u);
+      if (before < need && need <= before + sum) {         // one thread's bins
+        const bool upper = need <= before + own.y;
+        const unsigned bin = low + upper, over = upper ? before : before + own.y;
+        if (RANKS == 1) {
+          sh.found_bin = bin;
+          sh.found_above = over;
+        } else {
+          for (int r = 0; r < RANKS; ++r) {
+            st_cluster(cluster_addr(&sh.found_bin, r), bin);
+            st_cluster(cluster_addr(&sh.found_above, r), over);
+          }
+        }
+      }
     }
-    if (lane == 31) sh.warp_sum[warp] = inc;
-    __syncthreads();
-    unsigned before = inc - sum;
-#pragma unroll 1
-    for (int w = 0; w < warp; ++w) before += sh.warp_sum[w];
-    if (before < need && need <= before + sum) {           // one thread's bins
-      int bin = 3;
-      unsigned count = own.w;
-      if (need > before + count) {
-        before += count;
-        count = own.z;
-        bin = 2;
-      }
-      if (bin == 2 && need > before + count) {
-        before += count;
-        count = own.y;
-        bin = 1;
-      }
-      if (bin == 1 && need > before + count) {
-        before += count;
-        bin = 0;
-      }
-      sh.found_bin = low + bin;
-      sh.found_above = before;
-    }
-    if (pass == 1)                          // pass 2 uses the first histogram again; every rank has read it (the sync above)
-      for (int i = tid; i < kBins; i += kSelThreads) sh.hist[0][i] = 0;
-    __syncthreads();
+    sync_ranks<RANKS>();
     prefix |= sh.found_bin << shift;
     need -= sh.found_above;
-    __syncthreads();
+    // (the next found is written behind a barrier that every thread reaches after this)
   }
 
   // ---- counts per warp: rows above the key and at it, before row K and behind
   const int wshare = (share / 32 + kSelWarps - 1) / kSelWarps * 32;
   const int w0 = min(r1, r0 + warp * wshare), w1 = min(r1, w0 + wshare);
   uint4 n = make_uint4(0, 0, 0, 0);
-#pragma unroll 1
+#pragma unroll 2
   for (int t = w0 + lane; t - lane < w1; t += 32) {
     const uint32_t k = t < w1 ? key_of(t) : 0;
     const bool over = t < w1 && k > prefix, at = t < w1 && k == prefix;
@@ -195,26 +184,25 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     n.w += __popc(e & ~first);
   }
   if (lane == 0) sh.counts[warp] = n;
-  sync_ranks<RANKS>();
-  // rows above / at the key in warps before this one, and in all of them before row K
-  unsigned above = 0, equal = 0, above_k = 0, equal_k = 0;
-#pragma unroll
-  for (int x = 0; x < (RANKS * kSelWarps + 31) / 32; ++x) {
-    const int i = x * 32 + lane, r = i / kSelWarps, w = i % kSelWarps;
-    uint4 c = make_uint4(0, 0, 0, 0);
-    if (i < RANKS * kSelWarps) c = RANKS == 1 ? sh.counts[w] : ld_cluster4(cluster_addr(&sh.counts[w], r));
-    above_k += c.x;
-    equal_k += c.y;
-    if (i < rank * kSelWarps + warp) {
-      above += c.x + c.z;
-      equal += c.y + c.w;
-    }
+  __syncthreads();
+  // of all warps before this one, and of the whole CTA
+  uint4 c = sh.counts[lane], all;
+  all.x = __reduce_add_sync(0xffffffffu, c.x);
+  all.y = __reduce_add_sync(0xffffffffu, c.y);
+  all.z = __reduce_add_sync(0xffffffffu, c.z);
+  all.w = __reduce_add_sync(0xffffffffu, c.w);
+  unsigned above = __reduce_add_sync(0xffffffffu, lane < warp ? c.x + c.z : 0u);
+  unsigned equal = __reduce_add_sync(0xffffffffu, lane < warp ? c.y + c.w : 0u);
+  unsigned above_k = all.x, equal_k = all.y;
+  if (RANKS > 1) {
+    if (tid < RANKS) st_cluster4(cluster_addr(&sh.totals[rank], tid), all);
+    cluster_sync();                         // nobody touches another CTA's memory from here on
+    c = lane < RANKS ? sh.totals[lane & (kMostRanks - 1)] : make_uint4(0, 0, 0, 0);
+    above_k = __reduce_add_sync(0xffffffffu, c.x);
+    equal_k = __reduce_add_sync(0xffffffffu, c.y);
+    above += __reduce_add_sync(0xffffffffu, lane < rank ? c.x + c.z : 0u);
+    equal += __reduce_add_sync(0xffffffffu, lane < rank ? c.y + c.w : 0u);
   }
-  above = __reduce_add_sync(0xffffffffu, above);
-  equal = __reduce_add_sync(0xffffffffu, equal);
-  above_k = __reduce_add_sync(0xffffffffu, above_k);
-  equal_k = __reduce_add_sync(0xffffffffu, equal_k);
-  if (RANKS > 1) cluster_sync();            // nobody reads another CTA's memory from here on
   const unsigned kept_k = above_k + min(need, equal_k);    // rows before K that stay
   if (rank == 0 && tid == 0) {
     a.len_out[b] = K;
@@ -225,7 +213,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
   // ---- the moves: place i of the holes before K, row i of the kept behind
   int* from = a.move_from + static_cast<size_t>(b) * a.ld_move;
   int* to = a.move_to + static_cast<size_t>(b) * a.ld_move;
-#pragma unroll 1
+#pragma unroll 2
   for (int t = w0 + lane; t - lane < w1; t += 32) {
     const uint32_t k = t < w1 ? key_of(t) : 0;
     const bool over = t < w1 && k > prefix, at = t < w1 && k == prefix;
@@ -332,10 +320,12 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const EvictArgs
 template <int RANKS>
 cudaError_t launch_ranks(const SelectArgs& a, cudaStream_t st) {
   static bool attr_set[64] = {};
-  const int smem = static_cast<int>(sizeof(SelShared));
-  const cudaError_t e = set_smem_limit_once(evict_select_kernel<RANKS>, smem, attr_set);
+  cudaError_t e = cudaSuccess;
+  if (RANKS > 8) e = cudaFuncSetAttribute(evict_select_kernel<RANKS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) e = set_smem_limit_once(evict_select_kernel<RANKS>, static_cast<int>(sizeof(SelShared)), attr_set);
   if (e != cudaSuccess) return e;
-  return launch_kernel_overlap(launch_overlap_enabled(), RANKS, evict_select_kernel<RANKS>, dim3(a.B * RANKS), dim3(kSelThreads), smem, st, a);
+  return launch_kernel_overlap(launch_overlap_enabled(), RANKS, evict_select_kernel<RANKS>, dim3(a.B * RANKS), dim3(kSelThreads),
+                               sizeof(SelShared), st, a);
 }
 
 }  // namespace
@@ -343,8 +333,14 @@ cudaError_t launch_ranks(const SelectArgs& a, cudaStream_t st) {
 cudaError_t launch_evict_select(const SelectArgs& a, int num_sms, cudaStream_t st) {
   // CTAs of a request: as many as its longest row count gives work, and the GPU has room for
   int ranks = 1;
-  while (ranks < 8 && a.ld_mass > 4096l * ranks && a.B * ranks < 2 * num_sms) ranks *= 2;
-  return ranks == 1 ? launch_ranks<1>(a, st) : (ranks == 2 ? launch_ranks<2>(a, st) : (ranks == 4 ? launch_ranks<4>(a, st) : launch_ranks<8>(a, st)));
+  while (ranks < kMostRanks && a.ld_mass > kRankRows * ranks && a.B * ranks < 2 * num_sms) ranks *= 2;
+  switch (ranks) {
+    case 1: return launch_ranks<1>(a, st);
+    case 2: return launch_ranks<2>(a, st);
+    case 4: return launch_ranks<4>(a, st);
+    case 8: return launch_ranks<8>(a, st);
+    default: return launch_ranks<16>(a, st);
+  }
 }
 
 cudaError_t launch_kv_evict(const EvictArgs& a, int num_sms, cudaStream_t st) {

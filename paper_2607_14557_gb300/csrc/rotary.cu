@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotRows = 4;
+constexpr int kUnroll = 3;
 
 // W 32-bit words at once.
 template <int W>
@@ -89,7 +90,7 @@ template <int T, int W, bool INTER>
 __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const RotateArgs a, const __grid_constant__ TurnRates rates) {
   pdl_enter();
   constexpr int es = T == kF32 ? 4 : 2, N = 4 * W / es;      // values of W words
-  constexpr int Q = N < 4 ? N : 4, UNROLL = 3, ROW = 64;
+  constexpr int Q = N < 4 ? N : 4, UNROLL = kUnroll, ROW = 64;
   __shared__ __align__(16) float cosines[kRotRows][ROW], sines[kRotRows][ROW];
   __shared__ long long positions[kRotRows];
   __shared__ int slots[kRotRows];
@@ -222,12 +223,27 @@ cudaError_t launch_rotate(int type, bool interleaved, const RotateArgs& args, co
                           cudaStream_t st) {
   if (args.T_cap <= 0) return cudaSuccess;
   RotateArgs a = args;
-  a.rows_per_block = a.T_cap >= 2 * kRotRows * num_sms ? kRotRows : 1;
-  const int groups = (a.T_cap + a.rows_per_block - 1) / a.rows_per_block;
-  const dim3 grid(groups < 8 * num_sms ? groups : 8 * num_sms);
   // the widest words that both sides of a pair are aligned to
   const int es = type == kF32 ? 4 : 2, side = a.half * es;
   const int words = interleaved || side % 16 == 0 ? 4 : (side % 8 == 0 ? 2 : 1);
+  // rows of a block: those whose items fill its threads' loads best (32 heads of 128: three rows 47
+  // us, four 53)
+  a.rows_per_block = 1;
+  if (a.T_cap >= 2 * kRotRows * num_sms) {
+    const int pair = 2 * 4 * words / es, round = kUnroll * kRotThreads;
+    const bool turning = a.out == a.x && a.n_plain == 0 && a.slot == nullptr;
+    const int items = (a.n_turned + a.n_plain) * (turning ? (2 * a.half + pair - 1) / pair : a.head_dim / pair);
+    double best = 0;
+    for (int rows = kRotRows; rows >= 1; --rows) {
+      const double used = static_cast<double>(rows * items) / ((rows * items + round - 1) / round * round);
+      if (used > best + 0.01) {
+        best = used;
+        a.rows_per_block = rows;
+      }
+    }
+  }
+  const int groups = (a.T_cap + a.rows_per_block - 1) / a.rows_per_block;
+  const dim3 grid(groups < 8 * num_sms ? groups : 8 * num_sms);
 #define SEER_ROTATE(T, W, I) \
   if (type == T && words == W && interleaved == I) return launch_kernel(rotate_kernel<T, W, I>, grid, dim3(kRotThreads), 0, st, a, rates);
 #define SEER_ROTATE_TYPE(T) \
