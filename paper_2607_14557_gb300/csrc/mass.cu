@@ -229,11 +229,11 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// A CTA: eight warps that multiply and one that loads.  A stage is what the eight take at once, 16
+// A CTA: eight warps that multiply and two that load.  A stage is what the eight take at once, 16
 // keys of eight heads, or of fewer heads more keys; a key's heads lie side by side in the pool and
 // come as one bulk copy, rows of a stage 64 bytes further apart than they are long, so that the
 // fragments' 16-byte reads meet in no bank.  Two CTAs per SM, three stages each.
-constexpr int kStages = 3, kScoreThreads = kThreads + 32, kWarps = kThreads / 32;
+constexpr int kStages = 3, kLoaders = 2, kScoreThreads = kThreads + 32 * kLoaders, kWarps = kThreads / 32;
 __host__ __device__ constexpr int stage_bytes(int heads, int dh) { return kWarps / heads * GROUP * (heads * dh * 2 + 64); }
 __host__ __device__ constexpr int ring_bytes(int n_kv, int dh) { return kStages * stage_bytes(n_kv < kWarps ? n_kv : kWarps, dh); }
 
@@ -253,12 +253,13 @@ __global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const Mas
   __shared__ long long warp_sum[kScoreThreads / 32];
   __shared__ float2 shares[kWarps][NT * 8];
   __shared__ uint64_t full[kStages], empty[kStages];
+  __shared__ int pages[kWarps * GROUP];         // of the next keys to load
   __shared__ int abort_word;
   volatile int* abort_flag = &abort_word;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(&full[i], 1);
+      mbar_init(&full[i], kLoaders);
       mbar_init(&empty[i], kWarps);
     }
     abort_word = 0;
@@ -293,28 +294,33 @@ __global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const Mas
 #pragma unroll 1
     for (int head0 = 0; ok && head0 < hk; head0 += heads) {
       const int here = min(heads, hk - head0);
-      if (warp == kWarps) {
-        // ---- loads: a lane a key, 32 keys at a time; the first 32's pages are looked up three stages
-        // ahead (one ahead, the first stages went out 0.9 us apart)
-        const int keys = per_head * GROUP, bytes = here * DH * 2;
+      if (warp >= kWarps) {
+        // ---- loads: a lane a key, the loading warps in turn (a warp's copies go out 50 ns apart); the
+        // pages of 128 keys are looked up together
+        const int loader = warp - kWarps;
+        const int keys = per_head * GROUP, bytes = here * DH * 2, batch = kWarps * GROUP / keys;
         const long row_bytes = 4l * hk * DH;
         const uint8_t* pool = static_cast<const uint8_t*>(a.pages.kv) + head0 * DH * 2;
         const int* table = a.pages.table + static_cast<size_t>(b) * a.pages.max_pages;
-        const auto look_up = [&](int i, int k) {
-          const int t = (group0 + i * per_head) * GROUP + k;
-          return i < steps && k < keys && t < r.kv ? table[t >> a.pages.page_shift] : -1;
-        };
-        int page0 = look_up(0, lane), page1 = look_up(1, lane), page2 = look_up(2, lane);
 #pragma unroll 1
         for (int i = 0; i < steps; ++i, ++step) {
           const int s = step % kStages;
+          if (i % batch == 0) {
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < kWarps * GROUP / kLoaders / 32; ++e) {
+              const int k = (lane + 32 * e) * kLoaders + loader, t = (group0 + i * per_head) * GROUP + k;
+              pages[k] = t < r.kv ? table[t >> a.pages.page_shift] : -1;
+            }
+            __syncwarp();
+          }
           if (step >= kStages && !warp_wait(&empty[s], (step / kStages - 1) & 1, abort_flag, a.err)) {
             ok = false;
             break;
           }
 #pragma unroll 1
-          for (int k = lane; k - lane < keys; k += 32) {
-            const int page = k == lane ? page0 : look_up(i, k), t = (group0 + i * per_head) * GROUP + k;
+          for (int k = lane * kLoaders + loader; k - lane * kLoaders < keys; k += 32 * kLoaders) {
+            const int t = (group0 + i * per_head) * GROUP + k, page = k < keys ? pages[i % batch * keys + k] : -1;
             const bool wanted = k < keys && t < r.kv, there = wanted && page >= 0 && page < a.pages.n_pages;
             uint8_t* dst = ring + s * stage + k * pitch;
             const int rows = __popc(__ballot_sync(0xffffffffu, there));
@@ -331,9 +337,6 @@ __global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const Mas
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&full[s]);
-          page0 = page1;
-          page1 = page2;
-          page2 = look_up(i + 3, lane);
         }
         continue;
       }
@@ -428,7 +431,7 @@ __global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const Mas
       asm volatile("bar.sync 1, %0;" ::"r"(kThreads) : "memory");
     }
   }
-  if (warp == kWarps && *abort_flag && lane == 0)            // copies still in flight land before the memory is released
+  if (warp >= kWarps && *abort_flag && lane == 0)            // copies still in flight land before the memory is released
     for (unsigned j = step > kStages ? step - kStages : 0; j <= step; ++j) mbar_wait_drain(&full[j % kStages], (j / kStages) & 1, 20000000ull);
 }
 
