@@ -586,9 +586,9 @@ seer_status seer_evict_select(const float* mass, const int32_t* birth, int ld_ma
  * layer's pool, mass and birth once.  kv_len is the length before the choice (NULL: the
  * rows that the table holds); moves from or to rows outside it, or pages outside the
  * pool, are left out and recorded.  No row is both a source and a place, as
- * seer_evict_select leaves it.  The table is as before: its entries from ceil(len_out[b] /
- * page_size) up to ceil(kv_len[b] / page_size) are pages to put back, as after
- * seer_kv_accept. */
+ * seer_evict_select leaves it, and no page that is moved to belongs to two requests.  The
+ * table is as before: its entries from ceil(len_out[b] / page_size) up to ceil(kv_len[b] /
+ * page_size) are pages to put back, as after seer_kv_accept. */
 seer_status seer_kv_evict(seer_dtype dt, const int32_t* kv_len, const int32_t* n_moves, const int32_t* move_from,
                           const int32_t* move_to, int ld_move, int B, const seer_pages* pages, float* mass,
                           int32_t* birth, int ld_mass, void* stream);

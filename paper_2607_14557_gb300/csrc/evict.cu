@@ -320,9 +320,11 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const EvictArgs
 template <int RANKS>
 cudaError_t launch_ranks(const SelectArgs& a, cudaStream_t st) {
   static bool attr_set[64] = {};
-  cudaError_t e = cudaSuccess;
-  if (RANKS > 8) e = cudaFuncSetAttribute(evict_select_kernel<RANKS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  if (e == cudaSuccess) e = set_smem_limit_once(evict_select_kernel<RANKS>, static_cast<int>(sizeof(SelShared)), attr_set);
+  if (RANKS > 8) {
+    const cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<RANKS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
+  const cudaError_t e = set_smem_limit_once(evict_select_kernel<RANKS>, static_cast<int>(sizeof(SelShared)), attr_set);
   if (e != cudaSuccess) return e;
   return launch_kernel_overlap(launch_overlap_enabled(), RANKS, evict_select_kernel<RANKS>, dim3(a.B * RANKS), dim3(kSelThreads),
                                sizeof(SelShared), st, a);

@@ -197,8 +197,16 @@ __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const RotateArgs a,
               w = fmaf(w0, cs, p0 * sn);
             }
           }
+          const Words<W> a0 = lo[u], b0 = hi[u];
           lo[u] = pack<T, W>(x);
           hi[u] = pack<T, W>(y);
+          if (INTER && (c + 1) * N > a.half) {     // what does not turn keeps its bits, a NaN's too
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              if (c * N + i * 4 / (2 * es) >= a.half) lo[u].w[i] = a0.w[i];
+              if (c * N + (W + i) * 4 / (2 * es) >= a.half) hi[u].w[i] = b0.w[i];
+            }
+          }
         }
         long xo, yo;
         offsets(head[u], c, xo, yo);
