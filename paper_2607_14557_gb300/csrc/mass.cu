@@ -437,69 +437,75 @@ __global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const Mas
 
 // A tile a block, two threads a key with every second 16 columns.  Bound by latency, so a
 // thread's first scores are loaded before it is known whose the tile is (any tile's memory is
-// there), and the code is kept short: its first instructions come from memory too.
+// there; of a capacity far above the keys that there are, only a GPU's worth of tiles is), and the code is kept short: its first instructions come from memory too.
 constexpr int kEarly = 16, kSumThreads = 2 * KEYS;
 template <bool F32>
 __global__ void __launch_bounds__(kSumThreads) mass_sums_kernel(const MassArgs a) {
   pdl_enter();
   extern __shared__ float2 stat[];              // (m, 1 / l) of every column
   __shared__ float sums[kSumThreads];
-  const int tid = threadIdx.x, part = tid / KEYS, key = tid % KEYS, tile = blockIdx.x;
+  const int tid = threadIdx.x, part = tid / KEYS, key = tid % KEYS;
   const int hk = a.pages.n_kv, g = a.n_heads / hk, cc = g * a.window, all = hk * cc;
   uint8_t* row_of = reinterpret_cast<uint8_t*>(stat + all + kEarly);      // a column's row among those that look
   const ScoreWork w = score_work(a, F32);
-  const float* src = w.scores + (static_cast<size_t>(tile) * all + part * kEarly) * KEYS + key;
+  int tile = blockIdx.x;
   float s[kEarly];
+  const auto load_from = [&](int column) {
+    const float* src = w.scores + (static_cast<size_t>(tile) * all + column) * KEYS + key;
 #pragma unroll
-  for (int e = 0; e < kEarly; ++e) s[e] = part * kEarly + e < all ? src[e * KEYS] : 0.f;
+    for (int e = 0; e < kEarly; ++e) s[e] = column + e < all ? src[e * KEYS] : 0.f;
+  };
+  load_from(part * kEarly);
   const int total = w.first[a.B];
-  if (tile >= total) return;
-  const int b = request_at(w.first, a.B, tile);
-  const int blocks = unit_blocks(a.n_heads, hk, a.window), units = F32 ? hk * blocks : 1;
-  const int t0 = w.first[b], tiles = w.first[b + 1] - t0, length = run_length(total * units, a.runs);
-  const MassRequest r = read_request(a, b);
-  const int t = (tile - t0) * KEYS + key;
-  const float old = tid < KEYS && t < r.kv ? old_mass(a, r, b, t) : 0.f;
-#pragma unroll 1
-  for (int x = tid; x < all; x += kSumThreads) {
-    float2 f = make_float2(-INFINITY, 0.f);
-    const int col = x % cc;
-    if (col < r.look * g) {
-      const int kvh = x / cc, unit = F32 ? kvh * blocks + col / COLS : 0, place = t0 * units + unit * tiles;
-      const int c0 = place / length, c1 = (place + tiles - 1) / length, hop = F32 ? COLS : all;
-      const float2* from = w.stats + (static_cast<size_t>(b) * units + unit + c0) * hop + (F32 ? col % COLS : x);
-#pragma unroll 1
-      for (int c = c0; c <= c1; c += 8) {       // in order of the keys, eight loads under way
-        float2 piece[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) piece[e] = c + e <= c1 ? from[e * hop] : make_float2(-INFINITY, 0.f);
-        f = join8(f, piece);
-        from += 8 * hop;
-      }
-      f = query_row(a, r, b, col / g, x < cc && tile == t0) < 0 ? make_float2(0.f, 0.f) : finish(f);
-    }
-    stat[x] = f;                                // (no weights: 1 / l is 0)
-    row_of[x] = static_cast<uint8_t>(col / g);
-  }
+  const int blocks = unit_blocks(a.n_heads, hk, a.window), units = F32 ? hk * blocks : 1, length = run_length(total * units, a.runs);
   if (tid < kEarly) stat[all + tid] = make_float2(0.f, 0.f);
-  __syncthreads();
-  const int behind = t - (r.kv - r.look);       // > 0: only columns from that row on see it
-  float sum = 0.f;
 #pragma unroll 1
-  for (int x0 = part * kEarly; x0 < all; x0 += kSumThreads / KEYS * kEarly) {
+  while (tile < total) {
+    const int b = request_at(w.first, a.B, tile);
+    const int t0 = w.first[b], tiles = w.first[b + 1] - t0;
+    const MassRequest r = read_request(a, b);
+    const int t = (tile - t0) * KEYS + key;
+    const float old = tid < KEYS && t < r.kv ? old_mass(a, r, b, t) : 0.f;
+#pragma unroll 1
+    for (int x = tid; x < all; x += kSumThreads) {
+      float2 f = make_float2(-INFINITY, 0.f);
+      const int col = x % cc;
+      if (col < r.look * g) {
+        const int kvh = x / cc, unit = F32 ? kvh * blocks + col / COLS : 0, place = t0 * units + unit * tiles;
+        const int c0 = place / length, c1 = (place + tiles - 1) / length, hop = F32 ? COLS : all;
+        const float2* from = w.stats + (static_cast<size_t>(b) * units + unit + c0) * hop + (F32 ? col % COLS : x);
+#pragma unroll 1
+        for (int c = c0; c <= c1; c += 8) {     // in order of the keys, eight loads under way
+          float2 piece[8];
 #pragma unroll
-    for (int e = 0; e < kEarly; ++e) {
-      const float2 st = stat[x0 + e];
-      const bool seen = st.y != 0.f && (behind <= 0 || behind <= row_of[x0 + e]);
-      sum += seen ? ex2(s[e] - st.x) * st.y : 0.f;
+          for (int e = 0; e < 8; ++e) piece[e] = c + e <= c1 ? from[e * hop] : make_float2(-INFINITY, 0.f);
+          f = join8(f, piece);
+          from += 8 * hop;
+        }
+        f = query_row(a, r, b, col / g, x < cc && tile == t0) < 0 ? make_float2(0.f, 0.f) : finish(f);
+      }
+      stat[x] = f;                              // (no weights: 1 / l is 0)
+      row_of[x] = static_cast<uint8_t>(col / g);
     }
-    src += kSumThreads / KEYS * kEarly * KEYS;
+    __syncthreads();
+    const int behind = t - (r.kv - r.look);     // > 0: only columns from that row on see it
+    float sum = 0.f;
+#pragma unroll 1
+    for (int x0 = part * kEarly; x0 < all; x0 += kSumThreads / KEYS * kEarly) {
 #pragma unroll
-    for (int e = 0; e < kEarly; ++e) s[e] = x0 + kSumThreads / KEYS * kEarly + e < all ? src[e * KEYS] : 0.f;
+      for (int e = 0; e < kEarly; ++e) {
+        const float2 st = stat[x0 + e];
+        const bool seen = st.y != 0.f && (behind <= 0 || behind <= row_of[x0 + e]);
+        sum += seen ? ex2(s[e] - st.x) * st.y : 0.f;
+      }
+      load_from(x0 + kSumThreads / KEYS * kEarly);
+    }
+    sums[tid] = sum;
+    __syncthreads();
+    if (tid < KEYS && t < r.kv) store_mass(a, r, b, t, sums[tid] + sums[KEYS + tid], old);
+    tile += gridDim.x;
+    if (tile < total) load_from(part * kEarly);
   }
-  sums[tid] = sum;
-  __syncthreads();
-  if (tid < KEYS && t < r.kv) store_mass(a, r, b, t, sums[tid] + sums[KEYS + tid], old);
 }
 
 int score_runs(bool f32, int num_sms) { return (f32 ? 4 : 2) * num_sms; }
@@ -524,6 +530,7 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
   const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(a.pages.head_dim));
   const int line = (a.B + 1) * static_cast<int>(sizeof(int)), most_line = (kPageTableMaxB + 1) * static_cast<int>(sizeof(int));
   const int most_tiles = tile_capacity(a), sums_smem = 9 * (columns(a) + kEarly);
+  const dim3 sums(most_tiles < 16 * num_sms ? most_tiles : 16 * num_sms);
   a.runs = score_runs(f32, num_sms);
   cudaError_t e = cudaErrorInvalidValue;
   if (f32) {
@@ -533,7 +540,7 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
     e = set_smem_limit_once(mass_scores_f32_kernel, static_cast<int>(sizeof(TileShared)) + most_line, set0);
     if (e == cudaSuccess) e = set_smem_limit_once(mass_sums_kernel<true>, 9 * (kMassColumns + kEarly), set1);
     if (e == cudaSuccess) e = launch_kernel(mass_scores_f32_kernel, grid, dim3(kThreads), sizeof(TileShared) + line, st, a, scale);
-    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel<true>, dim3(most_tiles), dim3(kSumThreads), sums_smem, st, a);
+    if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel<true>, sums, dim3(kSumThreads), sums_smem, st, a);
     return e;
   }
   const dim3 grid(most_tiles < a.runs ? most_tiles : a.runs);
@@ -554,7 +561,7 @@ cudaError_t launch_mass(int type, const MassArgs& args, int num_sms, cudaStream_
   SEER_FEW(true, 128, 1)
   SEER_FEW(true, 128, 2)
 #undef SEER_FEW
-  if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel<false>, dim3(most_tiles), dim3(kSumThreads), sums_smem, st, a);
+  if (e == cudaSuccess) e = launch_kernel(mass_sums_kernel<false>, sums, dim3(kSumThreads), sums_smem, st, a);
   return e;
 }
 

@@ -517,35 +517,42 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 // A key's sums of all units, in order, and what came in.  A tile a block; latency: the sums of the
-// first 16 are loaded before it is known whose they are (any tile's memory is there).
+// first 16 are loaded before it is known whose they are (any tile's memory is there; of a capacity
+// far above the keys that there are, only a GPU's worth of tiles is).
 constexpr int FINAL_THREADS = 128;
 __global__ void __launch_bounds__(FINAL_THREADS) mass_final_kernel(const MassArgs a) {
   pdl_enter();
   const Sizes z = sizes_of(a.n_heads, a.pages.n_kv, a.window);
   const Work w = work_of(a, z);
   const size_t step = work_tiles(a.T_kv_cap, a.B) * KEYS;
-  const int x = blockIdx.x;
-  const float* src = w.sums + static_cast<size_t>(x) * KEYS + threadIdx.x;
+  int x = blockIdx.x;
   float s[16];
+  const auto load_from = [&](int i) {
+    const float* src = w.sums + i * step + static_cast<size_t>(x) * KEYS + threadIdx.x;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) s[e] = e < 2 * z.slices ? src[e * step] : 0.f;
-  if (x >= w.tiles[a.B]) return;
-  const int b = request_at(w.tiles, a.B, x);
-  const MassRequest r = read_request(a, b);
-  const int t = (x - w.tiles[b]) * KEYS + threadIdx.x;
-  if (t >= r.kv) return;
-  const float old = old_mass(a, r, b, t);
-  const int blocks = (r.look + 2 * z.tpt - 1) / (2 * z.tpt);      // column blocks that the request has
-  float sum = 0.f;
+    for (int e = 0; e < 16; ++e) s[e] = i + e < 2 * z.slices ? src[e * step] : 0.f;
+  };
+  load_from(0);
+  const int total = w.tiles[a.B];
 #pragma unroll 1
-  for (int i0 = 0; i0 < 2 * z.slices; i0 += 16) {
+  while (x < total) {
+    const int b = request_at(w.tiles, a.B, x);
+    const MassRequest r = read_request(a, b);
+    const int t = (x - w.tiles[b]) * KEYS + threadIdx.x;
+    const float old = t < r.kv ? old_mass(a, r, b, t) : 0.f;
+    const int blocks = (r.look + 2 * z.tpt - 1) / (2 * z.tpt);    // column blocks that the request has
+    float sum = 0.f;
+#pragma unroll 1
+    for (int i0 = 0; i0 < 2 * z.slices; i0 += 16) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (i0 + e < 2 * z.slices && (z.blocks == 1 ? blocks > 0 : (i0 + e) / 2 % z.blocks < blocks)) sum += s[e];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = i0 + 16 + e < 2 * z.slices ? src[(i0 + 16 + e) * step] : 0.f;
+      for (int e = 0; e < 16; ++e)
+        if (i0 + e < 2 * z.slices && (z.blocks == 1 ? blocks > 0 : (i0 + e) / 2 % z.blocks < blocks)) sum += s[e];
+      load_from(i0 + 16);
+    }
+    if (t < r.kv) store_mass(a, r, b, t, sum, old);
+    x += gridDim.x;
+    if (x < total) load_from(0);
   }
-  store_mass(a, r, b, t, sum, old);
 }
 
 template <bool F16, int DH>
@@ -581,7 +588,8 @@ cudaError_t launch_tc_mass(const CUtensorMap& mQ, const CUtensorMap& mK, const M
   if (a.pages.head_dim == 64) e = f16 ? launch_typed<true, 64>(mQ, mK, a, scale, st) : launch_typed<false, 64>(mQ, mK, a, scale, st);
   else e = f16 ? launch_typed<true, 128>(mQ, mK, a, scale, st) : launch_typed<false, 128>(mQ, mK, a, scale, st);
   if (e != cudaSuccess) return e;
-  return launch_kernel(mass_final_kernel, dim3(static_cast<unsigned>(work_tiles(a.T_kv_cap, a.B))), dim3(FINAL_THREADS), 0, st, a);
+  const size_t tiles = work_tiles(a.T_kv_cap, a.B);
+  return launch_kernel(mass_final_kernel, dim3(static_cast<unsigned>(tiles < 16ul * num_sms ? tiles : 16ul * num_sms)), dim3(FINAL_THREADS), 0, st, a);
 }
 
 }  // namespace seer

@@ -59,6 +59,55 @@ def test_mass_of_a_step_without_rows_fades(window):
     assert torch.equal(mass, want) and S.seer_check_device() == 0
 
 
+@pytest.mark.parametrize("dt,hq,window", [("f32", 2, 1), ("bf16", 2, 1), ("bf16", 24, 1)])
+def test_mass_of_more_tiles_than_blocks(dt, hq, window):
+    """A capacity far above the keys, and more tiles of keys than the second kernel has blocks."""
+    rng = np.random.default_rng(3)
+    B = 3000
+    cached = [int(v) for v in rng.integers(0, 130, B)]
+    s = setup_mass(rng, dt, hq, 1, 64, 16, cached, [1] * B)
+    mass_in = torch.from_numpy(rng.random((B, s["ld"])).astype(np.float32)).to(cuda())
+    want, birth = run_mass(s, dt, hq, 1, 64, 16, window, 1.0, mass_in, None)
+    got, _ = run_mass(s, dt, hq, 1, 64, 16, window, 1.0, mass_in, None, T_kv_cap=600000)
+    if dt == "f32" or hq * window <= 16:           # (the runs follow from the keys alone)
+        assert torch.equal(got, want)
+    check_mass(s, got, birth, dt, hq, 1, 64, 16, window, 1.0, mass_in, None)
+
+
+@pytest.mark.parametrize("dt,hq,window", [("f32", 1, 1), ("f16", 1, 1), ("f16", 17, 1)])
+def test_the_most_requests(dt, hq, window):
+    """16384 requests of one to three rows: mass, choice and moves."""
+    rng = np.random.default_rng(4)
+    B, page = S.MAX_REQUESTS, 8
+    cached = rng.integers(0, 3, B)
+    kv_len = cached + 1
+    kv = rnd(rng, (B * page, 2 * 64), dt)
+    table = i32(rng.permutation(B)[:, None])
+    pages = S.make_pages(kv, table, B, page, 1, 1, 64)
+    q = rnd(rng, (B, hq * 64), dt)
+    need = S.seer_attention_mass_workspace_size(dt, B, int(kv_len.sum()), hq, 1, 64, window)
+    ws = torch.empty(need, dtype=torch.uint8, device=cuda())
+    mass, birth = torch.zeros(B, 4, device=cuda()), torch.zeros(B, 4, dtype=torch.int32, device=cuda())
+    birth[:] = torch.arange(4, dtype=torch.int32, device=cuda())
+    lens = i32(kv_len)
+    S.seer_attention_mass(q, hq * 64, dt, i32(np.arange(B + 1)), lens, None, None, 0, window, B, B, int(kv_len.sum()), hq, pages, 1.0, None, mass, mass,
+                          birth, 4, ws, need)
+    total = mass.double().sum(1)
+    assert float((total - hq).abs().max()) < 1e-4 * hq
+    out = [i32([0] * B) for _ in range(3)] + [torch.zeros(B, 1, dtype=torch.int32, device=cuda()) for _ in range(2)]
+    S.seer_evict_select(mass, birth, 4, lens, None, i32([2] * B), B, 0, 1, *out, 1)
+    host_mass, before = host(mass), kv.clone()
+    S.seer_kv_evict(dt, lens, out[2], out[3], out[4], 1, B, pages, mass, birth, 4)
+    three = np.nonzero(kv_len == 3)[0]                # the last row stays, and the heavier of the others: it moves to row 0 or 1
+    weaker = np.where(host_mass[three, 0] >= host_mass[three, 1], 1, 0)
+    assert (out[2].cpu().numpy() == (kv_len == 3)).all() and (out[0].cpu().numpy() == np.minimum(kv_len, 2)).all()
+    assert (out[3].cpu().numpy()[three, 0] == 2).all() and (out[4].cpu().numpy()[three, 0] == weaker).all()
+    at = table[:, 0].long()[torch.from_numpy(three).to(cuda())] * page
+    weaker = torch.from_numpy(weaker).to(cuda())
+    before[at + weaker] = before[at + 2]
+    assert torch.equal(kv, before) and S.seer_check_device() == 0
+
+
 def test_far_pages():
     """A pool of more than 2^31 values and 2^32 bytes, its last pages in use."""
     rng = np.random.default_rng(0)
