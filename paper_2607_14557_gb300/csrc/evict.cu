@@ -22,7 +22,7 @@ constexpr int kSelKeys = 16384;             // keys of a CTA in shared memory
 constexpr int kBins = 2048;
 constexpr long kRankRows = 8192;            // of a request per CTA, while the GPU has room for more CTAs
 constexpr int kMostRanks = 16;
-constexpr int kAhead = 4;                   // rows of a thread whose loads are under way
+constexpr int kAhead = 8;                   // rows of a thread whose loads are under way
 constexpr uint32_t kKeyRecent = 0xffffffffu, kKeySink = 0xfffffffeu, kKeyNan = 0xfffffffdu;
 
 struct SelShared {
@@ -30,7 +30,7 @@ struct SelShared {
   uint4 totals[kMostRanks];                 // per CTA: rows above / at the key before K, above / at it behind
   uint4 counts[kSelWarps];                  // the same per warp of this CTA
   unsigned warp_sum[kSelWarps];
-  unsigned found_bin, found_above;
+  unsigned found_bin, found_above, found_all;   // found_all: every row of the bin stays
   uint32_t keys[kSelKeys];
 };
 
@@ -151,13 +151,16 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
       if (before < need && need <= before + sum) {         // one thread's bins
         const bool upper = need <= before + own.y;
         const unsigned bin = low + upper, over = upper ? before : before + own.y;
+        const unsigned whole = need - over == (upper ? own.y : own.x);
         if (RANKS == 1) {
           sh.found_bin = bin;
           sh.found_above = over;
+          sh.found_all = whole;
         } else {
           for (int r = 0; r < RANKS; ++r) {
             st_cluster(cluster_addr(&sh.found_bin, r), bin);
             st_cluster(cluster_addr(&sh.found_above, r), over);
+            st_cluster(cluster_addr(&sh.found_all, r), whole);
           }
         }
       }
@@ -165,6 +168,11 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     sync_ranks<RANKS>();
     prefix |= sh.found_bin << shift;
     need -= sh.found_above;
+    if (sh.found_all != 0) {                // often after two passes: the keys from the bin's first on stay
+      prefix -= 1;                          // (not 0, or all rows would)
+      need = 0;
+      break;
+    }
     // (the next found is written behind a barrier that every thread reaches after this)
   }
 
