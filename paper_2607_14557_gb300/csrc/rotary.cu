@@ -197,14 +197,18 @@ __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const RotateArgs a,
               w = fmaf(w0, cs, p0 * sn);
             }
           }
-          const Words<W> a0 = lo[u], b0 = hi[u];
           lo[u] = pack<T, W>(x);
           hi[u] = pack<T, W>(y);
-          if (INTER && (c + 1) * N > a.half) {     // what does not turn keeps its bits, a NaN's too
+          if (INTER && (c + 1) * N > a.half) {
+            // what does not turn keeps its bits, a NaN's too: read again, as few items end so and holding
+            // every item's words cost a quarter of the speed
+            long xo, yo;
+            offsets(head[u], c, xo, yo);
+            const uint8_t* src = a.x + static_cast<size_t>(row0 + r) * a.ld;
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-              if (c * N + i * 4 / (2 * es) >= a.half) lo[u].w[i] = a0.w[i];
-              if (c * N + (W + i) * 4 / (2 * es) >= a.half) hi[u].w[i] = b0.w[i];
+              if (c * N + i * 4 / (2 * es) >= a.half) lo[u].w[i] = *reinterpret_cast<const uint32_t*>(src + xo + 4 * i);
+              if (c * N + (W + i) * 4 / (2 * es) >= a.half) hi[u].w[i] = *reinterpret_cast<const uint32_t*>(src + yo + 4 * i);
             }
           }
         }
