@@ -85,7 +85,11 @@ __device__ __forceinline__ int request_of(const int* cu, int B, int row, int lan
 // cache row); where out is x itself only the turned part moves.  Bound by HBM for many rows.
 // A thread's item is 2 W words of one head: the two sides of W words' pairs, or 2 W words
 // that stay as they are.  UNROLL items' loads are under way before the angles are made; the
-// rows' sines lie in groups of four, neighbouring lanes' groups side by side.
+// rows' sines lie in groups of four, neighbouring lanes' groups side by side.  17.9k rows of 32
+// heads of 128, half of each turned in interleaved pairs, 293 MB, 51 us (5.8 TB/s; two items a
+// thread 66, four 57); 24k rows of 32 + 8 + 8 heads into the cache, 479 MB, 77 us (6.2 TB/s); a step
+// of 64 rows 3.8 and 4.9.  The registers of three items leave four blocks on an SM; held to five or
+// six blocks they spill (68, 98 us).
 template <int T, int W, bool INTER>
 __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const RotateArgs a, const __grid_constant__ TurnRates rates) {
   pdl_enter();
@@ -238,7 +242,7 @@ cudaError_t launch_rotate(int type, bool interleaved, const RotateArgs& args, co
   // the widest words that both sides of a pair are aligned to
   const int es = type == kF32 ? 4 : 2, side = a.half * es;
   const int words = interleaved || side % 16 == 0 ? 4 : (side % 8 == 0 ? 2 : 1);
-  // rows of a block: those whose items fill its threads' loads best (32 heads of 128: three rows 47
+  // rows of a block: those whose items fill its threads' loads best (32 heads of 128: three rows 51
   // us, four 53)
   a.rows_per_block = 1;
   if (a.T_cap >= 2 * kRotRows * num_sms) {
