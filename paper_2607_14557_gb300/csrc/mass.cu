@@ -242,6 +242,20 @@ constexpr int kStages = 3, kLoaders = 2, kScoreThreads = kThreads + 32 * kLoader
 __host__ __device__ constexpr int stage_bytes(int heads, int dh) { return kWarps / heads * GROUP * (heads * dh * 2 + 64); }
 __host__ __device__ constexpr int ring_bytes(int n_kv, int dh) { return kStages * stage_bytes(n_kv < kWarps ? n_kv : kWarps, dh); }
 
+// A barrier of the multiplying warps; whether any of their threads says so.
+__device__ __forceinline__ bool any_of_multipliers(bool mine) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, 1, %2, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"(static_cast<uint32_t>(mine)), "n"(kThreads)
+      : "memory");
+  return any != 0;
+}
+
 __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
   asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
@@ -424,7 +438,10 @@ __global__ void __launch_bounds__(kScoreThreads, 2) mass_scores_kernel(const Mas
             x = join(x, make_float2(__shfl_xor_sync(0xffffffffu, x.x, off), __shfl_xor_sync(0xffffffffu, x.y, off)));
           if (row == 0) shares[warp][nt * 8 + 2 * quad + e] = x;
         }
-      asm volatile("bar.sync 1, %0;" ::"r"(kThreads) : "memory");
+      if (any_of_multipliers(!ok)) {                         // all of them give up together, or a barrier would miss some
+        ok = false;
+        continue;
+      }
       float2* out = w.stats + (static_cast<size_t>(run) + b) * hk * cc;
 #pragma unroll 1
       for (int x = tid; x < here * cols; x += kThreads) {
