@@ -99,20 +99,20 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     unsigned* hist = sh.hist[pass];
     if (pass == 0) {
 #pragma unroll 1
-      for (int t0 = r0 + tid; t0 < r1; t0 += kAhead * kSelThreads) {
+      for (unsigned t0 = r0 + tid; t0 < static_cast<unsigned>(r1); t0 += kAhead * kSelThreads) {   // (may pass 2^31)
         int born[kAhead];
         float m[kAhead];
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {  // all loads first
-          const int t = min(t0 + e * kSelThreads, r1 - 1);
+          const unsigned t = min(t0 + e * kSelThreads, r1 - 1u);
           born[e] = birth[t];
           m[e] = mass[t];
         }
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
-          const int t = t0 + e * kSelThreads;
+          const unsigned t = t0 + e * kSelThreads;
           const uint32_t k = row_key(born[e], m[e]);
-          if (t < r1) {
+          if (t < static_cast<unsigned>(r1)) {
             if (held) sh.keys[t - r0] = k;
             atomicAdd(&hist[k >> 21], 1u);
           }
@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
 
   // ---- counts per warp: rows above the key and at it, before row K and behind
   const int wshare = (share / 32 + kSelWarps - 1) / kSelWarps * 32;
-  const int w0 = min(r1, r0 + warp * wshare), w1 = min(r1, w0 + wshare);
+  const int w0 = static_cast<int>(min(static_cast<long long>(r1), r0 + static_cast<long long>(warp) * wshare));
+  const int w1 = static_cast<int>(min(static_cast<long long>(r1), static_cast<long long>(w0) + wshare));
   uint4 n = make_uint4(0, 0, 0, 0);
 #pragma unroll 2
   for (int t = w0 + lane; t - lane < w1; t += 32) {

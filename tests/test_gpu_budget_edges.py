@@ -211,6 +211,19 @@ def test_select_of_many_long_requests():
         assert out[3][b, :len(src)].tolist() == src and out[4][b, :len(to)].tolist() == to
 
 
+def test_select_of_the_longest_request():
+    """2^31 - 1025 rows, all but five of one weight: indexes next to the end of 32 bits."""
+    L = 2 ** 31 - 1025
+    mass = torch.ones(1, L, device=cuda())
+    gaps = [7, 10 ** 9, 2 ** 31 - 2000, L - 2, L - 1]
+    mass[0, gaps] = 0.25
+    birth = torch.arange(L, dtype=torch.int32, device=cuda())
+    out = [i32([0]) for _ in range(3)] + [torch.full((1, 5), -7, dtype=torch.int32, device=cuda()) for _ in range(2)]
+    S.seer_evict_select(mass, birth, L, i32([L]), None, i32([L - 5]), 1, 0, 0, *out, 5)
+    assert (int(out[0]), int(out[1]), int(out[2])) == (L - 5, 5, 3) and S.seer_check_device() == 0
+    assert out[3][0].tolist() == [L - 5, L - 4, L - 3, -7, -7] and out[4][0].tolist() == gaps[:3] + [-7, -7]
+
+
 @pytest.mark.parametrize("scaling", ["linear", "turns", "pairs"])
 def test_scaled_rates_to_the_last_position(scaling):
     """Far positions of every scaling, in fp32, against angles reduced in integers."""
