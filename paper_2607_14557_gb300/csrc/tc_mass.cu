@@ -27,7 +27,9 @@
 // tiles a CTA; a pass's first scores are there after 5 to 8 us (the run's requests, then the first
 // 150 KB of every SM), and four launches.  Tried: four warps a quarter (no change), 32 columns on
 // their way out of tensor memory while 32 are computed (1.1 and 1.4 us a tile), every CTA summing
-// the line itself (2 us longer each pass, 4 saved), the walk out of line (74 us).
+// the line itself (2 us longer each pass, 4 saved), the walk out of line (74 us), both passes in one
+// cooperative kernel with a count of the CTAs that have ended the first (50 us: it starts without launch
+// overlap).
 #include "mass_common.cuh"
 
 namespace seer {
@@ -316,7 +318,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int qb = i & 1;
       const int ntok = p.r.look - p.tok0, rows1 = min(max(ntok - tpt, 0), tpt) * G;
       const bool two = rows1 > 0;
-      // columns of the second pass: whole 16s (rows of Q behind the block's are zeros)
+      // columns of the second pass: whole 16s (nobody looks at those of rows behind the block's)
       const uint32_t n = two ? 128 + (rows1 + 15) / 16 * 16 : (ntok * G + 15) / 16 * 16;
       const uint32_t idesc = WEIGHTS ? make_idesc(KEYS, n, 0, F16) : make_idesc(128, KEYS, 0, F16);
       if (!warp_wait(&q_full[qb], (i / 2) & 1, abort_flag, a.err)) break;
