@@ -88,7 +88,7 @@ __device__ __forceinline__ int request_of(const int* cu, int B, int row, int lan
 // rows' sines lie in groups of four, neighbouring lanes' groups side by side.  17.9k rows of 32
 // heads of 128, half of each turned in interleaved pairs, 293 MB, 51 us (5.8 TB/s; two items a
 // thread 66, four 57); 24k rows of 32 + 8 + 8 heads into the cache, 479 MB, 77 us (6.2 TB/s); a step
-// of 64 rows 3.8 and 4.9.  The registers of three items leave four blocks on an SM; held to five or
+// of 64 rows 2.8 and 3.6 (a call's host part is more).  The registers of three items leave four blocks on an SM; held to five or
 // six blocks they spill (68, 98 us).
 template <int T, int W, bool INTER>
 __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const RotateArgs a, const __grid_constant__ TurnRates rates) {
