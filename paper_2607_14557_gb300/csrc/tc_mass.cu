@@ -58,7 +58,7 @@ struct Layout {
 // Workspace: prefix sums over the requests, the pieces' (m, l), the keys' sums per unit.
 struct Work {
   int* tiles;             // [B + 1] key tiles of the requests before b
-  int* places;            // [B + 1] places on the line
+  int4* records;          // [B + 1][2] places and tiles before a request, its q0 and rows; n, look, kv
   float2* stats;          // [runs + B * slices][256]
   float* sums;            // [2 * slices][capacity tiles][128]
 };
@@ -73,12 +73,12 @@ __host__ __device__ inline Sizes sizes_of(int n_heads, int n_kv, int window) {
   return z;
 }
 __host__ __device__ inline size_t work_tiles(int T_kv_cap, int B) { return static_cast<size_t>(T_kv_cap) / KEYS + B; }
-__host__ __device__ inline size_t prefix_bytes(int B) { return (8 * (static_cast<size_t>(B) + 1) + 15) / 16 * 16; }
+__host__ __device__ inline size_t prefix_bytes(int B) { return 32 * (static_cast<size_t>(B) + 1) + (4 * (static_cast<size_t>(B) + 1) + 15) / 16 * 16; }
 __device__ __forceinline__ Work work_of(const MassArgs& a, const Sizes& z) {
   Work w;
   uint8_t* p = static_cast<uint8_t*>(a.ws);
-  w.places = reinterpret_cast<int*>(p);
-  w.tiles = w.places + a.B + 1;
+  w.records = reinterpret_cast<int4*>(p);
+  w.tiles = reinterpret_cast<int*>(w.records + 2 * (static_cast<size_t>(a.B) + 1));
   w.stats = reinterpret_cast<float2*>(p + prefix_bytes(a.B));
   w.sums = reinterpret_cast<float*>(w.stats + (a.runs + static_cast<size_t>(a.B) * z.slices) * COLS);
   return w;
@@ -96,8 +96,9 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
   for (int b0 = 0; b0 < a.B; b0 += 1024) {
     const int b = b0 + tid;
     long long v[2] = {0, 0};
+    MassRequest r{};
     if (b < a.B) {
-      const MassRequest r = read_request(a, b);
+      r = read_request(a, b);
       if (!r.good) record_error(a.err, kErrLayout);
       v[0] = (r.kv + KEYS - 1) / KEYS;
       v[1] = v[0] * a.pages.n_kv * ((r.look + 2 * z.tpt - 1) / (2 * z.tpt));
@@ -130,27 +131,28 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
       const bool fits = before[0] + inc[0] <= cap;
       if (!fits && v[0] > 0) record_error(a.err, kErrCapacity);
       w.tiles[b + 1] = fits ? static_cast<int>(before[0] + inc[0]) : -1;
-      w.places[b + 1] = static_cast<int>(before[1] + inc[1]);   // below 2^31 where it fits
+      // (below 2^31 where it fits)
+      w.records[2 * b] = make_int4(static_cast<int>(before[1] + inc[1] - v[1]), static_cast<int>(before[0] + inc[0] - v[0]), r.q0, r.rows);
+      w.records[2 * b + 1] = make_int4(r.n, r.look, r.kv, 0);
     }
     __syncthreads();
   }
-  if (tid == 0) {
-    w.tiles[0] = 0;
-    w.places[0] = 0;
-  }
+  if (tid == 0) w.tiles[0] = 0;
   __syncthreads();
-  if (w.tiles[a.B] >= 0) return;
+  if (w.tiles[a.B] >= 0) {
+    if (tid == 0) w.records[2 * a.B] = make_int4(static_cast<int>(places), static_cast<int>(tiles), 0, 0);
+    return;
+  }
   int lo = 0, hi = a.B;                     // tiles[lo] >= 0, tiles[hi] < 0
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (w.tiles[mid] >= 0) lo = mid; else hi = mid;
   }
-  const int end = w.tiles[lo];
-  const int last = w.places[lo];
+  const int end = w.tiles[lo], last = w.records[2 * lo].x;
   __syncthreads();
   for (int b = lo + 1 + tid; b <= a.B; b += 1024) {
     w.tiles[b] = end;
-    w.places[b] = last;
+    w.records[2 * b] = make_int4(last, end, 0, 0);
   }
 }
 
@@ -158,34 +160,65 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
 struct Piece {
   int b, kvh, tok0;       // tok0: the block's first token among the rows that look
   int tile0, tile1, tiles;
-  int slice, first;       // first: the unit's first place
+  int slice, first, row0; // first: the unit's first place; row0: the request's first tile
   MassRequest r;
 };
-// The pieces of run blockIdx.x, the same for every role of the CTA.
+// The pieces of run blockIdx.x, the same for every role of the CTA, by a whole warp.  32 requests'
+// records are in its lanes: one load tells a batch of 31 all that a run's first piece needs (a chain
+// of three took 1.3 us more a pass).
 struct Walk {
   const MassArgs& a;
   const Sizes z;
   const Work w;
   int at, end, length;                      // of a run: places
-  int b = 0;
-  bool fresh = true;
+  int window;                               // requests window .. window + 31
+  int4 first, second;                       // this lane's of them
 
-  __device__ __forceinline__ Walk(const MassArgs& a_) : a(a_), z(sizes_of(a_.n_heads, a_.pages.n_kv, a_.window)), w(work_of(a_, z)) {
-    const int total = w.places[a.B];
+  __device__ __forceinline__ void load_window() {
+    const int b = min(window + static_cast<int>(threadIdx.x & 31), a.B);
+    first = w.records[2 * b];
+    second = w.records[2 * b + 1];
+  }
+  __device__ __forceinline__ Walk(const MassArgs& a_)
+      : a(a_), z(sizes_of(a_.n_heads, a_.pages.n_kv, a_.window)), w(work_of(a_, z)), window(0) {
+    load_window();
+    const int total = a.B < 32 ? __shfl_sync(0xffffffffu, first.x, a.B & 31) : w.records[2 * a.B].x;
     length = run_length(total, a.runs);
     at = min(static_cast<int>(blockIdx.x) * length, total);
     end = min(at + length, total);
+    if (a.B >= 32 && at < end) {            // the window that holds `at`: narrowed 32-fold a step
+      const int lane = threadIdx.x & 31;
+      int left = a.B;
+#pragma unroll 1
+      while (left > 32) {
+        const int hop = (left + 31) / 32, k = lane * hop;
+        const unsigned below = __ballot_sync(0xffffffffu, k < left && w.records[2 * (window + k)].x <= at);
+        const int last = 31 - __clz(below);
+        window += last * hop;
+        left = min(hop, left - last * hop);
+      }
+      load_window();
+    }
   }
   __device__ __forceinline__ bool next(Piece& p) {
     if (at >= end) return false;
-    if (fresh || w.places[b + 1] <= at) {
-      fresh = false;
-      b = request_at(w.places, a.B, at);
-      p.r = read_request(a, b);
+    int lane;                               // of the last request that begins at or before `at`
+#pragma unroll 1
+    for (;;) {
+      lane = 31 - __clz(__ballot_sync(0xffffffffu, first.x <= at));
+      if (lane < 31 || window + 31 >= a.B) break;
+      window += 31;                         // (a run of requests without places moves on, too)
+      load_window();
     }
-    p.b = b;
-    p.tiles = w.tiles[b + 1] - w.tiles[b];
-    const int off = at - w.places[b], unit = off / p.tiles, blocks = (p.r.look + 2 * z.tpt - 1) / (2 * z.tpt);
+    p.b = window + lane;
+    p.row0 = __shfl_sync(0xffffffffu, first.y, lane);
+    p.tiles = __shfl_sync(0xffffffffu, first.y, lane + 1) - p.row0;
+    p.r.q0 = __shfl_sync(0xffffffffu, first.z, lane);
+    p.r.rows = __shfl_sync(0xffffffffu, first.w, lane);
+    p.r.n = __shfl_sync(0xffffffffu, second.x, lane);
+    p.r.look = __shfl_sync(0xffffffffu, second.y, lane);
+    p.r.kv = __shfl_sync(0xffffffffu, second.z, lane);
+    const int off = at - __shfl_sync(0xffffffffu, first.x, lane), unit = off / p.tiles, blocks = (p.r.look + 2 * z.tpt - 1) / (2 * z.tpt);
     p.first = at - (off - unit * p.tiles);
     p.tile0 = off - unit * p.tiles;
     p.tile1 = min(p.tiles, p.tile0 + (end - at));
@@ -446,7 +479,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&s_empty[buf]);
-          walk.w.sums[((2 * static_cast<size_t>(p.slice) + half) * work_tiles(a.T_kv_cap, a.B) + walk.w.tiles[p.b] + j) * KEYS + r] =
+          walk.w.sums[((2 * static_cast<size_t>(p.slice) + half) * work_tiles(a.T_kv_cap, a.B) + p.row0 + j) * KEYS + r] =
               (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
         __syncwarp();
