@@ -250,3 +250,70 @@ def test_a_turn_and_its_inverse():
         S.seer_rotate(y, 128, "f32", 1, 128, 50, None, i32(-pos), rot, z, 128)
         size = float(x.abs().max()) * 2
         assert float((z - x).abs().max()) <= size * (16 * 2.0 ** -24 + 2 * math.pi * 2.0 ** -23)
+
+
+def test_evict_without_lengths_takes_the_rows_that_the_table_holds():
+    rng = np.random.default_rng(2)
+    s = setup_mass(rng, "bf16", 1, 1, 64, 8, [30, 9], [0, 0])
+    table = i32(s["table"])
+    pages = S.make_pages(s["kv"], table, s["n_pages"], 8, s["max_pages"], 1, 64)
+    kv = s["kv"].clone()
+    S.seer_kv_evict("bf16", None, i32([2, 1]), i32([[29, 31], [15, 0]]), i32([[0, 8], [3, 0]]), 2, 2, pages, None, None, 0)
+
+    def row(b, t):
+        return int(s["table"][b][t // 8]) * 8 + t % 8
+    for b, f, t in ((0, 29, 0), (0, 31, 8), (1, 15, 3)):   # rows 30 to 31 of a last page are its rows, too
+        kv[row(b, t)] = kv[row(b, f)]
+    assert torch.equal(s["kv"], kv) and S.seer_check_device() == 0
+    S.seer_kv_evict("bf16", None, i32([1, 0]), i32([[32, 0], [0, 0]]), i32([[0, 0], [0, 0]]), 2, 2, pages, None, None, 0)   # past the last page
+    assert torch.equal(s["kv"], kv) and S.seer_check_device() == 2
+
+
+def test_append_rotary_of_keys_alone():
+    """No query heads, no rotated output; and queries and keys in place without a cache slot."""
+    rng = np.random.default_rng(3)
+    rot, rate = rotary(10000.0, 64, True, "linear")
+    x = rnd(rng, (9, 4 * 64), "f16")
+    kv, table = torch.zeros(16, 4 * 64, dtype=torch.float16, device=cuda()), i32([[0]])
+    pages = S.make_pages(kv, table, 2, 8, 1, 2, 64)
+    before = x.clone()
+    S.seer_kv_append_rotary(x, 256, "f16", 0, 9, None, i32(range(9)), i32(range(100, 109)), i32([0, 9]), i32([50]), 1, rot, None, 0, pages)
+    heads = host(before).reshape(9, 4, 64)
+    ref = R.turn(heads[:, :2], range(150, 159), rate, True)
+    close(kv[:9, :128].reshape(9, 2, 64), ref, R.turn_bound(heads[:, :2], ref, range(150, 159), 64, True, "f16"), "keys")
+    assert torch.equal(kv[:9, 128:], before[:, 128:]) and torch.equal(x, before) and (kv[9:] == 0).all()
+
+
+def test_requests_may_share_pages_that_are_only_read():
+    rng = np.random.default_rng(4)
+    for dt, hq, window in (("f32", 4, 1), ("bf16", 4, 1), ("bf16", 24, 2)):
+        s = setup_mass(rng, dt, hq, 2, 64, 16, [100, 100], [2, 2])
+        s["table"][1][:6] = s["table"][0][:6]             # 96 rows of a common prompt
+        mass_in = torch.rand(2, s["ld"], device=cuda())
+        out, birth = run_mass(s, dt, hq, 2, 64, 16, window, 1.0, mass_in, None)
+        check_mass(s, out, birth, dt, hq, 2, 64, 16, window, 1.0, mass_in, None)
+
+
+def test_results_do_not_depend_on_launch_overlap():
+    rng = np.random.default_rng(5)
+    for dt, hq, window in (("f32", 4, 2), ("bf16", 4, 2), ("bf16", 24, 2)):
+        s = setup_mass(rng, dt, hq, 2, 64, 16, [500, 33, 0], [2, 1, 2])
+        mass_in = torch.rand(3, s["ld"], device=cuda())
+        results = []
+        for overlap in (True, False):
+            was = S.seer_set_launch_overlap(overlap)
+            try:
+                for _ in range(3):                        # calls behind one another share the workspace's memory
+                    out, birth = run_mass(s, dt, hq, 2, 64, 16, window, 1.0, mass_in, [1, 2, 3])
+                kv, table = s["kv"].clone(), i32(s["table"])
+                pages = S.make_pages(kv, table, s["n_pages"], 16, s["max_pages"], 2, 64)
+                t = [i32([0] * 3) for _ in range(3)] + [torch.zeros(3, 60, dtype=torch.int32, device=cuda()) for _ in range(2)]
+                lens = i32(s["kv_len"])
+                S.seer_evict_select(out, birth, s["ld"], lens, i32([1, 2, 3]), i32([450, 20, 2]), 3, 1, 2, *t, 60)
+                S.seer_kv_evict(dt, lens, t[2], t[3], t[4], 60, 3, pages, out, birth, s["ld"])
+                torch.cuda.synchronize()
+            finally:
+                S.seer_set_launch_overlap(was)
+            results.append([out, birth, kv, *t])
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert S.seer_check_device() == 0
