@@ -255,7 +255,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* stat_empty = stat_full + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(stat_empty + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert(8 * (2 * RING + 10) + 8 <= 256, "barrier block");
+  int* gaps = const_cast<int*>(abort_flag) + 1;        // [4] of a second pass's block: columns that do not look
+  static_assert(8 * (2 * RING + 10) + 24 <= 256, "barrier block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -442,6 +443,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       } else {
         // a lane a key: every second 32 columns
         if (!warp_wait(stat_full, i & 1, abort_flag, a.err)) break;
+        // keys up to it are summed without a look at the columns: nothing times a NaN score is not nothing, so
+        // a block with a column that does not look is looked through
+        const int plain_to = (gaps[0] | gaps[1] | gaps[2] | gaps[3]) != 0 ? -1 : free_to;
         for (int j = p.tile0; j < p.tile1; ++j, ++g) {
           const int buf = g & 1;
           if (!warp_wait(&s_full[buf], (g / 2) & 1, abort_flag, a.err)) {
@@ -457,11 +461,11 @@ __global__ void __launch_bounds__(THREADS, 1)
             uint32_t v[32];
             tmem_ld32(tmem + lane_off + buf * COLS + c, v);
             tmem_ld_wait();
-            if (j * KEYS + KEYS - 1 > free_to || left < 32) {
+            if (j * KEYS + KEYS - 1 > plain_to || left < 32) {
 #pragma unroll
               for (int x = 0; x < 32; ++x) {
                 const float w = ex2(fmaf(__uint_as_float(v[x]), scale, neg_m[c + x])) * inv_l[c + x];
-                if (x < left && t <= free_to + token[c + x]) sum[x & 3] += w;
+                if (x < left && inv_l[c + x] != 0.f && t <= free_to + token[c + x]) sum[x & 3] += w;
               }
             } else {
 #pragma unroll
@@ -524,6 +528,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       if constexpr (WEIGHTS) {
         // columns tid and tid + 128: their pieces in order of the keys
         float2 s[2];
+        bool gap = false;
         const int c0 = p.first / walk.length, c1 = (p.first + p.tiles - 1) / walk.length;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -535,6 +540,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           const bool looks = row_of(t, tid, p.kvh == 0 && p.tile0 == 0) >= 0;
           s[t] = looks ? finish(s[t]) : make_float2(INFINITY, 0.f);
+          gap |= !looks && tid < (t == 0 ? rows0 : rows1);
         }
         if (i >= 1 && !warp_wait(stat_empty, (i - 1) & 1, abort_flag, a.err)) break;
 #pragma unroll
@@ -543,6 +549,8 @@ __global__ void __launch_bounds__(THREADS, 1)
           inv_l[t * 128 + tid] = s[t].y;
           token[t * 128 + tid] = static_cast<uint8_t>(min(255, t * tpt + tid / G));
         }
+        gap = __any_sync(0xffffffffu, gap);
+        if (lane == 0) gaps[w] = gap;
         __syncwarp();
         if (lane == 0) mbar_arrive(stat_full);
       }
