@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
   float* neg_m = reinterpret_cast<float*>(smem + L::OFF_STAT);
   float* inv_l = neg_m + COLS;
-  uint8_t* token = reinterpret_cast<uint8_t*>(inv_l + COLS);
+  int8_t* token = reinterpret_cast<int8_t*>(inv_l + COLS);         // a column's row among the block's, -1: it does not look
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
   uint64_t* k_full = bars;                  // [RING]
   uint64_t* k_empty = k_full + RING;        // [RING]
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!warp_wait(stat_full, i & 1, abort_flag, a.err)) break;
         // keys up to it are summed without a look at the columns: nothing times a NaN score is not nothing, so
         // a block with a column that does not look is looked through
-        const int plain_to = (gaps[0] | gaps[1] | gaps[2] | gaps[3]) != 0 ? -1 : free_to;
+        const int plain_to = a.accepted && (gaps[0] | gaps[1] | gaps[2] | gaps[3]) != 0 ? -1 : free_to;
         for (int j = p.tile0; j < p.tile1; ++j, ++g) {
           const int buf = g & 1;
           if (!warp_wait(&s_full[buf], (g / 2) & 1, abort_flag, a.err)) {
@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             break;
           }
           tc_fence_after();
-          const int t = j * KEYS + r;
+          const int from = max(j * KEYS + r - free_to, 0);            // the first row that sees the key
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
           for (int c = half * 32; c < COLS; c += 64) {
             const int left = c < 128 ? rows0 - c : rows1 - (c - 128);   // columns from c on in this tile of Q
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
               for (int x = 0; x < 32; ++x) {
                 const float w = ex2(fmaf(__uint_as_float(v[x]), scale, neg_m[c + x])) * inv_l[c + x];
-                if (x < left && inv_l[c + x] != 0.f && t <= free_to + token[c + x]) sum[x & 3] += w;
+                if (token[c + x] >= from) sum[x & 3] += w;
               }
             } else {
 #pragma unroll
@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int t = 0; t < 2; ++t) {
           neg_m[t * 128 + tid] = -s[t].x;
           inv_l[t * 128 + tid] = s[t].y;
-          token[t * 128 + tid] = static_cast<uint8_t>(min(255, t * tpt + tid / G));
+          token[t * 128 + tid] = static_cast<int8_t>(s[t].y == 0.f ? -1 : t * tpt + tid / G);
         }
         gap = __any_sync(0xffffffffu, gap);
         if (lane == 0) gaps[w] = gap;
