@@ -19,24 +19,23 @@ __device__ __forceinline__ int tiles_of(const MassRequest& r) { return (r.kv + K
 __host__ __device__ inline int tile_capacity(const MassArgs& a) { return a.T_kv_cap / KEYS + a.B; }
 
 // first[b] = key tiles of the requests before b, first[B] all; by the whole block.  Requests
-// past the call's key capacity have no tiles, nor has any behind them.
+// past the call's key capacity, counted in keys, have no tiles, nor has any behind them.
 __device__ __forceinline__ void tile_line(const MassArgs& a, int* first, long long* warp_sum, bool report) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  const long long cap = tile_capacity(a);
   long long sum = 0;
 #pragma unroll 1
   for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
     const int b = b0 + tid;
-    int v = 0;                                  // at most 2^25, so a warp's sum has 32 bits
+    long long v = 0;
     if (b < a.B) {
       const MassRequest r = read_request(a, b);
       if (!r.good && report) record_error(a.err, kErrLayout);
-      v = tiles_of(r);
+      v = pack_keys<KEYS>(r.kv);
     }
-    int inc = v;
+    long long inc = v;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, inc, off);
+      const long long x = __shfl_up_sync(0xffffffffu, inc, off);
       if (lane >= off) inc += x;
     }
     if (lane == 31) warp_sum[warp] = inc;
@@ -48,9 +47,11 @@ __device__ __forceinline__ void tile_line(const MassArgs& a, int* first, long lo
       sum += warp_sum[w];
     }
     if (b < a.B) {
-      if (before > cap && v > 0 && report) record_error(a.err, kErrCapacity);
-      first[b + 1] = static_cast<int>(before > cap ? -1 : before);
+      const bool fits = within(before, a.T_kv_cap);
+      if (!fits && v > 0 && report) record_error(a.err, kErrCapacity);
+      first[b + 1] = fits ? static_cast<int>(tiles_in<KEYS>(before)) : -1;
     }
+    sum = cut_sum(sum, a.T_kv_cap);
     __syncthreads();
   }
   if (tid == 0) first[0] = 0;

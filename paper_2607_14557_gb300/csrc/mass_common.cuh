@@ -32,6 +32,22 @@ __device__ __forceinline__ MassRequest read_request(const MassArgs& a, int b) {
   return r;
 }
 
+// A request's keys in one 64-bit sum with what its last tile lacks of TILE keys (at most 127 of each
+// of 16384 requests: 21 bits), from which both the keys of all requests and their tiles follow.  The keys
+// of 1024 requests, each at most kMaxKeys, and a sum that was cut stay below 2^63.
+constexpr int kLackBits = 21;
+template <int TILE>
+__device__ __forceinline__ long long pack_keys(int kv) {
+  return static_cast<long long>(kv) << kLackBits | (-kv & (TILE - 1));
+}
+template <int TILE>
+__device__ __forceinline__ long long tiles_in(long long sum) {
+  return static_cast<unsigned long long>((sum >> kLackBits) + (sum & ((1 << kLackBits) - 1))) / TILE;
+}
+__device__ __forceinline__ bool within(long long sum, int T_kv_cap) { return (sum >> kLackBits) <= T_kv_cap; }
+// A sum past the capacity stays past it, and is let grow no further.
+__device__ __forceinline__ long long cut_sum(long long sum, int T_kv_cap) { return min(sum, (T_kv_cap + 1ll) << kLackBits); }
+
 // The request of place x on a line, first[b] the places before request b: by a whole warp, the
 // prefix sums narrowed 128-fold a step (four loads a lane, one after the other's heels).
 __device__ __forceinline__ int request_at(const int* first, int B, int x) {

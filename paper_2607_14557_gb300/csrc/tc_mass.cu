@@ -90,8 +90,7 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
   const Sizes z = sizes_of(a.n_heads, a.pages.n_kv, a.window);
   const Work w = work_of(a, z);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long cap = static_cast<long long>(work_tiles(a.T_kv_cap, a.B));
-  long long tiles = 0, places = 0;          // of the requests before
+  long long keys = 0, places = 0;           // of the requests before
   for (int b0 = 0; b0 < a.B; b0 += 1024) {
     const int b = b0 + tid;
     long long v[2] = {0, 0};
@@ -99,8 +98,8 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
     if (b < a.B) {
       r = read_request(a, b);
       if (!r.good) record_error(a.err, kErrLayout);
-      v[0] = (r.kv + KEYS - 1) / KEYS;
-      v[1] = v[0] * a.pages.n_kv * ((r.look + 2 * z.tpt - 1) / (2 * z.tpt));
+      v[0] = pack_keys<KEYS>(r.kv);
+      v[1] = static_cast<long long>((r.kv + KEYS - 1) / KEYS) * a.pages.n_kv * ((r.look + 2 * z.tpt - 1) / (2 * z.tpt));
     }
     long long inc[2] = {v[0], v[1]};
 #pragma unroll
@@ -116,30 +115,31 @@ __global__ void __launch_bounds__(1024) mass_line_kernel(const MassArgs a) {
       warp_sum[1][warp] = inc[1];
     }
     __syncthreads();
-    long long before[2] = {tiles, places};
+    long long before[2] = {keys, places};
     for (int x = 0; x < 32; ++x) {
       if (x < warp) {
         before[0] += warp_sum[0][x];
         before[1] += warp_sum[1][x];
       }
-      tiles += warp_sum[0][x];
+      keys += warp_sum[0][x];
       places += warp_sum[1][x];
     }
     if (b < a.B) {
       // past the key capacity nobody has tiles: such a request begins and ends where the last good one did
-      const bool fits = before[0] + inc[0] <= cap;
+      const bool fits = within(before[0] + inc[0], a.T_kv_cap);
       if (!fits && v[0] > 0) record_error(a.err, kErrCapacity);
-      w.tiles[b + 1] = fits ? static_cast<int>(before[0] + inc[0]) : -1;
+      w.tiles[b + 1] = fits ? static_cast<int>(tiles_in<KEYS>(before[0] + inc[0])) : -1;
       // (below 2^31 where it fits)
-      w.records[2 * b] = make_int4(static_cast<int>(before[1] + inc[1] - v[1]), static_cast<int>(before[0] + inc[0] - v[0]), r.q0, r.rows);
+      w.records[2 * b] = make_int4(static_cast<int>(before[1] + inc[1] - v[1]), static_cast<int>(tiles_in<KEYS>(before[0] + inc[0] - v[0])), r.q0, r.rows);
       w.records[2 * b + 1] = make_int4(r.n, r.look, r.kv, 0);
     }
+    keys = cut_sum(keys, a.T_kv_cap);
     __syncthreads();
   }
   if (tid == 0) w.tiles[0] = 0;
   __syncthreads();
   if (w.tiles[a.B] >= 0) {
-    if (tid == 0) w.records[2 * a.B] = make_int4(static_cast<int>(places), static_cast<int>(tiles), 0, 0);
+    if (tid == 0) w.records[2 * a.B] = make_int4(static_cast<int>(places), w.tiles[a.B], 0, 0);
     return;
   }
   int lo = 0, hi = a.B;                     // tiles[lo] >= 0, tiles[hi] < 0

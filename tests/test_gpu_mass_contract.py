@@ -89,3 +89,46 @@ def test_rows_outside_the_draft_do_not_look_at_odd_keys(dt, hq, hk, window, valu
         w, err = expected(s, b, looking, hq, hk, dh, page, odd)
         close(out[b, :s["kv_len"][b]], w, err, f"request {b}")
         assert (out[b, odd] == 0).all()
+
+# ------------------------------------------------------------------ the key capacity
+@pytest.mark.parametrize("dt,hq,hk,window", PATHS)
+def test_the_key_capacity_is_counted_in_keys(dt, hq, hk, window):
+    rng = np.random.default_rng(3)
+    s = setup_mass(rng, dt, hq, hk, 64, 16, [63, 63, 0, 62, 0, 9], [1, 1, 0, 2, 0, 1])
+    mass_in = torch.rand(6, s["ld"], device=cuda())
+    want, _ = run_mass(s, dt, hq, hk, 64, 16, window, 1.0, mass_in, None)
+    assert S.seer_check_device() == 0 and sum(s["kv_len"]) == 202
+    for cap, served in ((202, 6), (201, 5), (192, 5), (191, 3), (128, 3), (127, 1), (64, 1), (63, 0), (0, 0)):
+        got, birth = run_mass(s, dt, hq, hk, 64, 16, window, 1.0, mass_in, None, T_kv_cap=cap)
+        assert torch.equal(got[:served], want[:served]), cap
+        assert (got[served:] == -3).all() and (birth[served:] == -9).all(), cap
+        assert S.seer_check_device() == (0 if cap == 202 else 5), cap
+
+
+@pytest.mark.parametrize("dt,hq,hk,window", PATHS)
+def test_requests_that_do_not_fit_their_matrix_take_no_capacity(dt, hq, hk, window):
+    rng = np.random.default_rng(4)
+    s = setup_mass(rng, dt, hq, hk, 64, 16, [100, 40, 30], [1, 1, 1])
+    mass_in = torch.rand(3, s["ld"], device=cuda())
+    want, _ = run_mass(s, dt, hq, hk, 64, 16, window, 1.0, mass_in, None)
+    cap = s["kv_len"][0] + s["kv_len"][2]
+    s["kv_len"][1] = 2 ** 31 - 1
+    got, _ = run_mass(s, dt, hq, hk, 64, 16, window, 1.0, mass_in, None, T_kv_cap=cap)
+    assert torch.equal(got[[0, 2]], want[[0, 2]]) and (got[1] == -3).all() and S.seer_check_device() == 2
+
+
+@pytest.mark.parametrize("dt,hq,hk,window,B", [("f32", 2, 1, 3, 700), ("bf16", 2, 1, 3, 2000), ("f16", 2, 1, 30, 1500)])
+def test_the_key_capacity_ends_inside_a_large_batch(dt, hq, hk, window, B):
+    rng = np.random.default_rng(B)
+    cached, new = [int(v) for v in rng.integers(0, 40, B)], [int(v) for v in rng.integers(0, 3, B)]
+    s = setup_mass(rng, dt, hq, hk, 64, 8, cached, new)
+    mass_in = torch.rand(B, s["ld"], device=cuda())
+    want, _ = run_mass(s, dt, hq, hk, 64, 8, window, 1.0, mass_in, None)
+    ends = np.cumsum(s["kv_len"])
+    for served in (B // 3, B - 2):
+        while s["kv_len"][served] == 0:          # (the first that is left out has keys)
+            served += 1
+        for cap in (int(ends[served - 1]), int(ends[served]) - 1):
+            got, _ = run_mass(s, dt, hq, hk, 64, 8, window, 1.0, mass_in, None, T_kv_cap=cap)
+            assert torch.equal(got[:served], want[:served]) and (got[served:] == -3).all()
+            assert S.seer_check_device() == 5
