@@ -504,7 +504,7 @@ typedef struct {
   double theta;             /* pair i turns by theta^(-2i / rotary_dim) per position; >= 1 */
   double factor;            /* scalings: >= 1 */
   double low, high;         /* TURNS, PAIRS: 0 < low < high */
-  double magnitude;         /* cosines and sines are multiplied by it (1: a rotation) */
+  double magnitude;         /* cosines and sines are multiplied by it (1: a rotation); finite in fp32 */
   int original_len;         /* TURNS, PAIRS: > 0 */
   int rotary_dim;           /* the head's first values that turn: even, from 2 to head_dim */
   int interleaved;          /* 0: pairs (i, i + rotary_dim / 2); 1: pairs (2i, 2i + 1) */

@@ -1,6 +1,7 @@
 // C ABI of the paged K/V cache (declared in include/seer.h): argument checks and
 // launches; the arithmetic runs in paged.cu, rotary.cu, mass.cu, evict.cu and the
 // grouped-head attention kernels.
+#include <cfloat>
 #include <cmath>
 
 #include "api.h"
@@ -112,7 +113,7 @@ seer_status rotary_rates(const char* what, const seer_rotary* r, int head_dim, s
   if (!(r->theta >= 1.0) || !std::isfinite(r->theta)) return fail(SEER_ERR_INVALID_ARG, "%s: theta must be a finite base from 1 on", what);
   if (r->scaling < SEER_ROTARY_PLAIN || r->scaling > SEER_ROTARY_PAIRS) return fail(SEER_ERR_INVALID_ARG, "%s: unknown rotary scaling %d", what, r->scaling);
   if (r->interleaved != 0 && r->interleaved != 1) return fail(SEER_ERR_INVALID_ARG, "%s: interleaved must be 0 or 1", what);
-  if (!std::isfinite(r->magnitude)) return fail(SEER_ERR_INVALID_ARG, "%s: magnitude must be finite", what);
+  if (!(std::fabs(r->magnitude) <= FLT_MAX)) return fail(SEER_ERR_INVALID_ARG, "%s: magnitude must be finite in fp32", what);
   const int rd = r->rotary_dim;
   if (rd < 2 || rd > head_dim || rd % 2 != 0)
     return fail(SEER_ERR_INVALID_ARG, "%s: rotary_dim must be even, from 2 to head_dim (got %d of %d)", what, rd, head_dim);
