@@ -547,17 +547,24 @@ seer_status seer_kv_append_rotary(const void* qkv, int ld_qkv, seer_dtype dt, in
  *                 same lists: n = n_accepted[b], and new row i's query is row cu_new[b] +
  *                 accepted[b * max_draft + i]; kv_len is then seer_kv_accept's len_out.  A
  *                 row whose entry is outside its draft is recorded and does not look
- * window          rows that look at most, 1 .. SEER_MAX_DRAFT
+ * window          rows that look at most, 1 .. SEER_MAX_DRAFT.  For the weight from all rows
+ *                 of a prompt make a call per window of them with keep 1, their numbers as
+ *                 accepted and kv_len up to the last of them; each goes through the keys up
+ *                 to there once (scores kept, see ws) or twice
  * T_kv_cap        the requests' kv_len add up to at most this; requests past it are left
  *                 out and recorded
  * mass_in         may be mass_out itself (not overlap it otherwise); NULL where keep is 0
  * Entries from kv_len[b] to ld_mass are untouched.  A request without new rows keeps
- * keep * mass_in.  A row's infinite or NaN scores make its weights NaN for the rows that
- * it sees.  Pages outside the pool read as zeros and are recorded.  Types, heads and
+ * keep * mass_in.  A score of minus infinity weighs nothing; one of plus infinity or NaN, or
+ * nothing but minus infinity, makes a row's weights NaN for all rows that it sees.  Pages outside the pool read as zeros and are recorded.  Types, heads and
  * head_dim as for seer_attention_tree (fp32: n_heads * window at most 16384); weights and
  * sums are fp32.
  * ws: seer_attention_mass_workspace_size() bytes, 16-byte aligned; calls that share one
- * must not overlap on the GPU; nothing in it needs to start at zero. */
+ * must not overlap on the GPU; nothing in it needs to start at zero.  In fp32, and in 16 bits
+ * where a key/value head has at most 16 query heads times rows of the window (n_heads * window
+ * at most 1024), it holds all scores: 4 * n_heads * window bytes per key of T_kv_cap and per
+ * request 64 keys more (fp32, 32 heads, 64 rows, 2^20 keys: 8.6 GB; a smaller window or
+ * fewer requests a call take less). */
 seer_status seer_attention_mass(const void* q, int ld_q, seer_dtype dt, const int32_t* cu_new, const int32_t* kv_len,
                                 const int32_t* accepted, const int32_t* n_accepted, int max_draft, int window, int B,
                                 int T_cap, int T_kv_cap, int n_heads, const seer_pages* pages, float keep,

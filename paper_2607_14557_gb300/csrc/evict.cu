@@ -17,7 +17,7 @@ namespace {
 // others (all reading all: 5 us a pass of 16 CTAs).  Sums of integers: the order of the atomics
 // leaves no trace.  Bound by latency: two loads, three passes of a barrier or two each, the two
 // counts, and 20 KB of instructions.  64 requests of 200 to 8000 rows 7.7 to 8.8 us, one of 120000
-// 11.3 to 13.
+// 12.4 to 13.5.
 constexpr int kSelThreads = 1024;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelKeys = 16384;             // keys of a CTA in shared memory
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
 // Row move_from of a request becomes its row move_to; sources and places are apart, so all
 // moves go at once.  Bound by HBM behind a chain of loads (counts, lists, pages, rows): each moved
 // row is read once and written once.  All requests' moves form one line; a warp takes 2 KB of a row
-// at a time, its loads ahead of its stores.  6.7k rows of 4 KB, 55 MB, 13 us; 64 rows 3.4.  (1 or 4 KB
+// at a time, its loads ahead of its stores.  6.7k rows of 4 KB, 55 MB, 13 us; 64 rows 3.6.  (1 or 4 KB
 // a warp and 32 registers: the same; two pieces a warp at once 18 us, the next piece's places
 // looked up meanwhile 15: both cost warps.)
 constexpr int kEvictThreads = 256;

@@ -101,8 +101,10 @@ __device__ __forceinline__ ScoreWork score_work(const MassArgs& a, bool f32) {
 // Scores of a 64-key tile and 16 columns at a time on the CUDA cores: keys and queries of a head in
 // shared memory, a thread 4 columns of one key.  Units (request, key/value head, 16 columns) times
 // tiles form the line, so that a small call spreads over the GPU; a run's tiles of a unit leave one
-// (m, l) per column.  Bound by the latency of a step for small calls, by shared memory for large.
-// 2 to 24 accepted rows of 5 requests over 1 to 900 rows, 4 / 2 heads of 64: 14 us with the sums.
+// (m, l) per column.  Bound by the latency of a step for small calls, by shared memory for large: 16
+// columns are multiplied where a head has four, and no key is on its way meanwhile.  2 to 24 accepted
+// rows of 5 requests over 1 to 900 rows, 4 / 2 heads of 64: 14 to 15 us with the sums; one token for
+// each of 64 requests over 200 to 8000 rows (32 / 8 heads of 128) 250 us for 497 MB.
 struct TileShared {
   float k[KEYS][132];
   float q[COLS][128];
@@ -215,7 +217,9 @@ __global__ void __launch_bounds__(kThreads) mass_scores_f32_kernel(const MassArg
 // of 64 requests over 200 to 8000 rows (32 / 8 heads of 128), 249 MB, 57 us of which the sums' kernel
 // takes 8 behind this one (4.4 TB/s; 5.6 while the keys stream); two requests over 700 and 433
 // 11.4 us.  Against the tensor cores' path (tc_mass.cu), four and 16 columns a head: 64 requests 69
-// and 105 us against 140, eight 25 and 39.5 against 39.5, two 17 and 29 against 26.
+// and 105 us against 140, eight 25 and 39.5 against 39.5, two 17 and 29 against 26.  (With caches cold;
+// 16 columns a head of 64 requests 95 us in a row of calls: at head_dim 128 two column blocks' queries beside
+// the keys spill 68 bytes at the 96 registers of two CTAs an SM.)
 // A warp multiplies 16 keys of a head at a time by m16n8k16: the order of a product's terms is
 // free, so a lane's 16 bytes of a row serve as the k-indices that the fragment wants from it, and Q
 // is cut alike.  A lane keeps the maxima and sums of its two columns over its keys.
@@ -238,7 +242,9 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
 // A CTA: eight warps that multiply and two that load.  A stage is what the eight take at once, 16
 // keys of eight heads, or of fewer heads more keys; a key's heads lie side by side in the pool and
 // come as one bulk copy, rows of a stage 64 bytes further apart than they are long, so that the
-// fragments' 16-byte reads meet in no bank.  Two CTAs per SM, three stages each.
+// fragments' 16-byte reads meet in no bank.  Two CTAs per SM, three stages each.  One key/value
+// head of 128 takes 120 KB of them, which leaves one CTA per SM (as many thousands of requests do, whose
+// sums lie beside the stages), and the runs come in two waves: 64 requests, 16 / 1 heads, 32 MB, 41 us.
 constexpr int kStages = 3, kLoaders = 2, kScoreThreads = kThreads + 32 * kLoaders, kWarps = kThreads / 32;
 __host__ __device__ constexpr int stage_bytes(int heads, int dh) { return kWarps / heads * GROUP * (heads * dh * 2 + 64); }
 __host__ __device__ constexpr int ring_bytes(int n_kv, int dh) { return kStages * stage_bytes(n_kv < kWarps ? n_kv : kWarps, dh); }

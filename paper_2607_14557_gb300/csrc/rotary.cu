@@ -89,7 +89,10 @@ __device__ __forceinline__ int request_of(const int* cu, int B, int row, int lan
 // heads of 128, half of each turned in interleaved pairs, 293 MB, 51 us (5.8 TB/s; two items a
 // thread 66, four 57); 24k rows of 32 + 8 + 8 heads into the cache, 479 MB, 77 us (6.2 TB/s); a step
 // of 64 rows 2.8 and 3.6 (a call's host part is more).  The registers of three items leave four blocks on an SM; held to five or
-// six blocks they spill (68, 98 us).
+// six blocks they spill (68, 98 us).  A pair's width is the whole head's: 17.9k rows of 32 heads of 80, ten
+// pairs of each turned in halves (4-byte words), 183 MB, 87 us; 32 heads of 128 in fp32, 587 MB, 90.
+// seer_kv_append keeps its own kernel (whole heads, half layout, no shift): of 1000 rows into the cache
+// 6.4 us where this one takes 7.0 (64 rows 4.1 and 3.7, 17.9k rows 73.2 and 73.8).
 template <int T, int W, bool INTER>
 __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const RotateArgs a, const __grid_constant__ TurnRates rates) {
   pdl_enter();

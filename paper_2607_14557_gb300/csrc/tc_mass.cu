@@ -22,13 +22,13 @@
 //   warps 10-13  the joined statistics of the next piece, and of accepted drafts its queries, whose
 //                rows lie anywhere
 // 16 prompts of 300 to 4000 rows under 64-row windows (32 / 8 heads of 128, 17.6k keys, 18 GFLOP in
-// both passes) 48 us: a tile of 128 keys and 256 columns takes 0.9 us in the first pass (the keys'
-// way from HBM) and 1.0 in the second (exponentials), eight tiles a CTA; a pass's first scores are
-// there after 4 to 7 us (the run's requests, then the first 150 KB of every SM), and four launches.  Tried: four warps a quarter (no change), 32 columns on
-// their way out of tensor memory while 32 are computed (1.1 and 1.4 us a tile), every CTA summing
-// the line itself (2 us longer each pass, 4 saved), the walk out of line (74 us), both passes in one
-// cooperative kernel with a count of the CTAs that have ended the first (50 us: it starts without launch
-// overlap).
+// both passes) 45 us: a tile of 128 keys and 256 columns takes 0.9 to 1.1 us in either pass (the keys'
+// way from HBM in the first, exponentials in the second), eight tiles a CTA; a pass's first scores are
+// there after 4 to 7 us (the run's requests, then the first 150 KB of every SM), and four launches.
+// Tried, when it took 48: four warps a quarter (no change), 32 columns on their way out of tensor
+// memory while 32 are computed (1.1 and 1.4 us a tile), every CTA summing the line itself (2 us longer
+// each pass, 4 saved), the walk out of line (74 us), both passes in one cooperative kernel with a count
+// of the CTAs that have ended the first (50 us: it starts without launch overlap).
 #include "mass_common.cuh"
 
 namespace seer {
